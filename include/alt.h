@@ -56,7 +56,8 @@ typedef enum {
     ALT_NOT_TUNED = 7             /* cache lookup found no entry */
 } alt_status_t;
 
-typedef enum { ALT_F32 = 0, ALT_BF16 = 1 } alt_dtype_t;
+/* ALT_I8 (two's complement bytes): only the calls that name it take it. */
+typedef enum { ALT_F32 = 0, ALT_BF16 = 1, ALT_I8 = 2 } alt_dtype_t;
 
 typedef struct alt_context *alt_handle_t;
 
@@ -494,6 +495,70 @@ alt_status_t alt_gemm_variant_count(alt_handle_t h, const alt_gemm_desc_t *d, in
 /* (variant = -1 names the variant alt_gemm picks for the descriptor, as alt_conv2d_variant_name does) */
 alt_status_t alt_gemm_variant_name(alt_handle_t h, const alt_gemm_desc_t *d, int variant,
                                    char *buf, size_t buflen);
+
+/* ---- products of 8-bit layers and of expert layers ------------------------- */
+
+/* Rows to 8 bits: for every row m of x (rows x cols, dtype ALT_F32 or ALT_BF16)
+ *   scale[m] = max_k |x[m,k]| / 127, rounded up to 16 significant bits and at least 2^-126,
+ *   q[m,k]   = x[m,k] / scale[m] to the nearest whole number, ties to even (-127 .. 127).
+ * A scale of 16 bits makes q * scale exact in fp32, so that every q is the one the formula names.  A row that holds an infinity or a
+ * NaN gets scale NaN and q = 0: products with it are NaN.  x_stride, q_stride: elements between rows, 0 = cols.  The buffers need the
+ * alignment of their elements only, and must not overlap.  Asynchronous on `stream`. */
+alt_status_t alt_quantize_rows(alt_handle_t h, alt_dtype_t dtype, int64_t rows, int64_t cols, const void *x, int64_t x_stride,
+                               void *q, int64_t q_stride, float *scale, void *stream);
+
+#define ALT_I8_MAX_K 131072       /* products of two numbers in -128 .. 127 that a 32-bit sum holds */
+
+typedef struct {
+    int64_t M, N, K;
+    int64_t lda, ldb, ldc;        /* elements between rows of a, b and y; 0 = dense (K, K, N) */
+    int32_t out_dtype;            /* ALT_F32 or ALT_BF16 (one rounding of the fp32 value, to nearest even) */
+    int32_t epilogue;             /* ALT_EPI_* flags */
+} alt_gemm_i8_desc_t;
+
+/* y[m,n] = (sum_k a[m,k] * b[n,k]) * a_scale[m] * b_scale[n] (+ bias[n], then max(., 0) by `epilogue`): 8-bit a (M x K, a row per
+ * token) and b (N x K, a row per output channel), fp32 scales and bias.  The sum is exact (32-bit integers, K <= ALT_I8_MAX_K); it is
+ * scaled in fp32.  NaN stays NaN through the ReLU.  Any alignment of a and b; rows of 16-byte chunks at 16-byte addresses are
+ * fastest.  `workspace` (ws_bytes) is optional, as for alt_gemm.  Asynchronous on `stream`. */
+alt_status_t alt_gemm_i8(alt_handle_t h, const alt_gemm_i8_desc_t *d, const void *a, const float *a_scale, const void *b,
+                         const float *b_scale, const float *bias, void *y, void *workspace, size_t ws_bytes, void *stream);
+alt_status_t alt_gemm_i8_workspace_size(alt_handle_t h, const alt_gemm_i8_desc_t *d, size_t *bytes);
+
+/* A layer of experts: `rows` tokens in the order of their experts, expert e owning the rows [offsets[e], offsets[e+1]).  `offsets` is an
+ * int32 array of groups + 1 on the device, not decreasing, read when the kernels run; an expert may own no row.  Rows before offsets[0]
+ * and from offsets[groups] on belong to no expert.  (Offsets outside 0 .. rows are clamped; with offsets out of order results are
+ * unspecified, but nothing outside the buffers is read or written.) */
+typedef struct {
+    int64_t rows, N, K;           /* rows may be 0 */
+    int64_t lda, ldb, ldc;        /* elements between rows of a and dx; of b and dw (an expert's matrix is N * ldb elements); of y and dy; 0 = dense */
+    int32_t groups;               /* experts */
+    int32_t in_dtype;             /* of a, b, dy: ALT_BF16, ALT_F32, or (forward only) ALT_I8 */
+    int32_t out_dtype;            /* of the result: ALT_F32, or (not for ALT_F32 operands) ALT_BF16 */
+    int32_t epilogue;             /* ALT_EPI_* flags; what they mean in each call stands there */
+} alt_grouped_desc_t;
+
+/* y[m,n] = sum_k a[m,k] * b[e,n,k] for the expert e of row m, + bias[e,n] with ALT_EPI_BIAS (fp32), then max(., 0) with ALT_EPI_RELU
+ * (NaN stays NaN).  8-bit operands are scaled as in alt_gemm_i8: a_scale[rows], b_scale[groups][N]; otherwise the scales may be NULL.
+ * Rows of no expert get zeros.  Buffers need the alignment of their elements and must not overlap; operand rows of whole 16-byte chunks at
+ * 16-byte addresses are fastest.  Asynchronous on `stream`. */
+alt_status_t alt_gemm_grouped(alt_handle_t h, const alt_grouped_desc_t *d, const void *a, const float *a_scale, const void *b,
+                              const float *b_scale, const float *bias, const int32_t *offsets, void *y, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Gradient by the rows: dx[m,k] = sum_n dy[m,n] * b[e,n,k].  With ALT_EPI_RELU, a having come out of a ReLU, `relu_of` is a (or any tensor
+ * of its type and strides) and dx is zero where it is not positive.  Rows of no expert get zeros.  dy has in_dtype, dx out_dtype. */
+alt_status_t alt_gemm_grouped_dx(alt_handle_t h, const alt_grouped_desc_t *d, const void *dy, const void *b, const void *relu_of,
+                                 const int32_t *offsets, void *dx, void *workspace, size_t ws_bytes, void *stream);
+
+/* Gradients by the weights: dw[e,n,k] = sum over the rows m of expert e of dy[m,n] * a[m,k], and with ALT_EPI_BIAS dbias[e,n] = sum of
+ * dy[m,n] (fp32).  Experts without rows get zeros.  dy is the gradient by the value before any ReLU of the forward call. */
+alt_status_t alt_gemm_grouped_dw(alt_handle_t h, const alt_grouped_desc_t *d, const void *a, const void *dy, const int32_t *offsets,
+                                 void *dw, float *dbias, void *workspace, size_t ws_bytes, void *stream);
+
+/* Bytes of workspace each call would like (NULL / 0 always works; the sums of a long reduction cut into slices go there). */
+alt_status_t alt_gemm_grouped_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);
+alt_status_t alt_gemm_grouped_dx_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);
+alt_status_t alt_gemm_grouped_dw_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);
 
 /* ---- joint tuning (Section 5.2: cross exploration — pick a layout, tune the
  *      loops under it, feed the best latency back; budget counted in on-device

@@ -11,7 +11,7 @@ except ImportError:                       # built where Python's headers are (bu
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIBPATH = os.environ.get("ALT_LIBRARY", os.path.join(_HERE, "libalt.so"))   # ALT_LIBRARY: developer builds
 
-F32, BF16 = 0, 1
+F32, BF16, I8 = 0, 1, 2
 EPI_BIAS, EPI_RELU = 1, 2
 MAX_RANK, MAX_PRIMS, MAX_CAND, MAX_CHAIN = 8, 8, 16, 8
 
@@ -75,6 +75,16 @@ class GemmDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("batch", "M", "N", "K")] + \
                [(n, ctypes.c_int32) for n in ("in_dtype", "out_dtype", "variant", "reserved")] + \
                [("a_layout", Layout), ("b_layout", Layout), ("c_layout", Layout)]
+
+
+class GemmI8Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "K", "lda", "ldb", "ldc")] + \
+               [(n, ctypes.c_int32) for n in ("out_dtype", "epilogue")]
+
+
+class GroupedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "N", "K", "lda", "ldb", "ldc")] + \
+               [(n, ctypes.c_int32) for n in ("groups", "in_dtype", "out_dtype", "epilogue")]
 
 
 class TuneOpts(ctypes.Structure):
@@ -177,7 +187,10 @@ _V, _I, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
 _OPERATOR = (_V, _V, _V, _V, _V, _V, _V, ctypes.c_size_t, _V)
 _PROTOTYPES = {"alt_layout_transform": (_V, _I, _I, _V, _V, _V, _V, _V, _V), "alt_eltwise_add": (_V, _I, _L, _V, _V, _V, _I, _V),
                "alt_gemm": (_V, _V, _V, _V, _V, _V, ctypes.c_size_t, _V), "alt_conv2d": _OPERATOR, "alt_conv3d": _OPERATOR,
-               "alt_conv2d_transpose": _OPERATOR, "alt_conv3d_transpose": _OPERATOR}
+               "alt_conv2d_transpose": _OPERATOR, "alt_conv3d_transpose": _OPERATOR,
+               "alt_quantize_rows": (_V, _I, _L, _L, _V, _L, _V, _L, _V, _V), "alt_gemm_i8": (_V,) * 9 + (ctypes.c_size_t, _V),
+               "alt_gemm_grouped": (_V,) * 10 + (ctypes.c_size_t, _V), "alt_gemm_grouped_dx": (_V,) * 8 + (ctypes.c_size_t, _V),
+               "alt_gemm_grouped_dw": (_V,) * 8 + (ctypes.c_size_t, _V)}
 _calls = {}
 
 # The same calls by the native module (native/altcall.c), for arguments of plain types; it answers None to others, and without the module
@@ -220,7 +233,9 @@ def exported_symbols():
             "alt_tune_conv2d_arena_size", "alt_tune_gemm_arena_size", "alt_tune_conv2d", "alt_tune_gemm",
             "alt_tune_conv2d_variants", "alt_tune_conv2d_multi", "alt_tune_chain", "alt_plan_chain",
             "alt_eltwise_add", "alt_tune_graph", "alt_plan_graph", "alt_unfold", "alt_unfold_shape",
-            "alt_cache_save", "alt_cache_load", "alt_cache_clear", "alt_get_peak", "alt_layout_transform_plan", "alt_splitk_status", "alt_conv2d_static", "alt_layout_transform_pad"]
+            "alt_cache_save", "alt_cache_load", "alt_cache_clear", "alt_get_peak", "alt_layout_transform_plan", "alt_splitk_status", "alt_conv2d_static", "alt_layout_transform_pad",
+            "alt_quantize_rows", "alt_gemm_i8", "alt_gemm_i8_workspace_size", "alt_gemm_grouped", "alt_gemm_grouped_dx", "alt_gemm_grouped_dw",
+            "alt_gemm_grouped_workspace_size", "alt_gemm_grouped_dx_workspace_size", "alt_gemm_grouped_dw_workspace_size"]
 
 
 def version():
@@ -413,6 +428,15 @@ def gemm_desc(M, N, K, batch=1, in_dtype=BF16, out_dtype=F32, variant=-1,
     d = GemmDesc(batch, M, N, K, in_dtype, out_dtype, variant, 0)
     d.a_layout, d.b_layout, d.c_layout = _as_layout(a_layout), _as_layout(b_layout), _as_layout(c_layout)
     return d
+
+
+def gemm_i8_desc(M, N, K, out_dtype=BF16, epilogue=0, lda=0, ldb=0, ldc=0):
+    return GemmI8Desc(M, N, K, lda, ldb, ldc, out_dtype, epilogue)
+
+
+def grouped_desc(rows, groups, N, K, in_dtype=BF16, out_dtype=BF16, epilogue=0, lda=0, ldb=0, ldc=0):
+    """A layer of experts: lda, ldb, ldc are the row strides of a (and dx), b (and dw), y (and dy) in elements, 0 where dense."""
+    return GroupedDesc(rows, N, K, lda, ldb, ldc, groups, in_dtype, out_dtype, epilogue)
 
 
 # ----------------------------------------------------------------------- handle ----
@@ -685,6 +709,53 @@ class Handle:
         buf = ctypes.create_string_buffer(96)
         _ck(lib().alt_gemm_variant_name(self._h, ctypes.byref(d), variant, buf, ctypes.c_size_t(96)), self._h)
         return buf.value.decode()
+
+    # 8-bit layers and layers of experts
+    def quantize_rows(self, dtype, rows, cols, x, q, scale, x_stride=0, q_stride=0, stream=None):
+        status = _call("alt_quantize_rows")(self._h, dtype, rows, cols, _address(x), x_stride, _address(q), q_stride, _address(scale), _stream_address(stream))
+        if status != 0:
+            _ck(status, self._h)
+
+    def gemm_i8(self, d, a, a_scale, b, b_scale, y, bias=None, workspace=None, ws_bytes=0, stream=None):
+        status = _call("alt_gemm_i8")(self._h, ctypes.byref(d), _address(a), _address(a_scale), _address(b), _address(b_scale), _address(bias), _address(y),
+                                      _address(workspace), ws_bytes, _stream_address(stream))
+        if status != 0:
+            _ck(status, self._h)
+
+    def gemm_grouped(self, d, a, b, offsets, y, a_scale=None, b_scale=None, bias=None, workspace=None, ws_bytes=0, stream=None):
+        status = _call("alt_gemm_grouped")(self._h, ctypes.byref(d), _address(a), _address(a_scale), _address(b), _address(b_scale), _address(bias),
+                                           _address(offsets), _address(y), _address(workspace), ws_bytes, _stream_address(stream))
+        if status != 0:
+            _ck(status, self._h)
+
+    def gemm_grouped_dx(self, d, dy, b, offsets, dx, relu_of=None, workspace=None, ws_bytes=0, stream=None):
+        status = _call("alt_gemm_grouped_dx")(self._h, ctypes.byref(d), _address(dy), _address(b), _address(relu_of), _address(offsets), _address(dx),
+                                              _address(workspace), ws_bytes, _stream_address(stream))
+        if status != 0:
+            _ck(status, self._h)
+
+    def gemm_grouped_dw(self, d, a, dy, offsets, dw, dbias=None, workspace=None, ws_bytes=0, stream=None):
+        status = _call("alt_gemm_grouped_dw")(self._h, ctypes.byref(d), _address(a), _address(dy), _address(offsets), _address(dw), _address(dbias),
+                                              _address(workspace), ws_bytes, _stream_address(stream))
+        if status != 0:
+            _ck(status, self._h)
+
+    def _workspace_size(self, name, d):
+        n = ctypes.c_size_t()
+        _ck(getattr(lib(), name)(self._h, ctypes.byref(d), ctypes.byref(n)), self._h)
+        return n.value
+
+    def gemm_i8_workspace_size(self, d):
+        return self._workspace_size("alt_gemm_i8_workspace_size", d)
+
+    def gemm_grouped_workspace_size(self, d):
+        return self._workspace_size("alt_gemm_grouped_workspace_size", d)
+
+    def gemm_grouped_dx_workspace_size(self, d):
+        return self._workspace_size("alt_gemm_grouped_dx_workspace_size", d)
+
+    def gemm_grouped_dw_workspace_size(self, d):
+        return self._workspace_size("alt_gemm_grouped_dw_workspace_size", d)
 
     # tuning
     def _opts(self, arena, arena_bytes, max_trials, warmup, reps, layout_mask, stream):

@@ -1,0 +1,452 @@
+"""Products of expert layers and of 8-bit layers, and the quantizer of rows, against plain sums in 64 bits.
+
+Tolerances.  fp32 sums of n products, in any order: n * 2^-24 * sum |a||b| (the textbook bound), for the fused bias one rounding more;
+sums of 8-bit products are exact and take three roundings (to fp32, and two scales), the bias a fourth: 4 * 2^-24 of the largest
+intermediate value; a bf16 result one rounding more, 2^-8 of the value.  Quantized rows have one right answer."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2210_12415_amd as alt
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {alt.F32: torch.float32, alt.BF16: torch.bfloat16, alt.I8: torch.int8}
+EPS = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def h():
+    return alt.Handle()
+
+
+class Canary:
+    """A device matrix with unused columns and guard rows, all holding a pattern."""
+
+    def __init__(self, rows, cols, dtype, stride=0, lead=()):
+        self.rows, self.cols = rows, cols
+        self.stride = stride or cols
+        n = int(np.prod(lead, dtype=np.int64)) if lead else 1
+        self.whole = torch.full((n * rows * self.stride + 256,), 77, dtype=dtype, device="cuda")
+        self.at = self.whole[128:128 + n * rows * self.stride]
+        self.t = self.at.view(*lead, rows, self.stride)[..., :cols]
+
+    def data_ptr(self):
+        return self.at.data_ptr()
+
+    def untouched(self):
+        edge = bool((self.whole[:128] == 77).all()) and bool((self.whole[-128:] == 77).all())
+        pad = self.at.view(-1, self.stride)[:, self.cols:]
+        return edge and bool((pad == 77).all())
+
+
+def matrix(values, dtype, stride=0, offset=0):
+    """A device matrix with `values` in rows `stride` apart (what lies between them is NaN, or 99 in 8 bits), `offset` elements into its buffer."""
+    values = torch.as_tensor(values)
+    rows, cols = values.shape[-2:]
+    stride = stride or cols
+    fill = 99 if dtype == torch.int8 else float("nan")
+    buf = torch.full((int(np.prod(values.shape[:-1], dtype=np.int64)) * stride + offset,), fill, dtype=dtype, device="cuda")
+    view = buf[offset:].view(*values.shape[:-1], stride)[..., :cols]
+    view.copy_(values.to(dtype))
+    return view
+
+
+def f64(t):
+    return t.cpu().double().numpy()
+
+
+def normal(seed, *shape, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(*shape, generator=g) * std
+
+
+def close(got, want, tol, what=""):
+    got, want = f64(got), np.asarray(want)
+    bad = ~(np.abs(got - want) <= tol)
+    bad &= ~(np.isnan(got) & np.isnan(want))
+    assert not bad.any(), "%s: %d of %d off, first at %s: %r for %r" % (what, bad.sum(), bad.size, np.argwhere(bad)[0], got[bad][0], want[bad][0])
+
+
+# ---- quantizer -------------------------------------------------------------------------------------------------------------
+
+def exact_rows(x):
+    """The definition in 64 bits (x / s of a 24-bit by a 16-bit number is exact enough there to tell every tie)."""
+    x = f64(x)
+    top = np.abs(x).max(axis=1)
+    with np.errstate(over="ignore"):
+        m, e = np.frexp((top / 127.0).astype(np.float32).astype(np.float64))
+    s = np.maximum(np.ldexp(np.ceil(m * 65536.0) / 65536.0, e), 2.0 ** -126)
+    return np.rint(x / s[:, None]).astype(np.int8), s
+
+
+def quantize(h, x, dtype, ldq=0):
+    rows, cols = x.shape
+    q, s = Canary(rows, cols, torch.int8, ldq), Canary(1, rows, torch.float32)
+    h.quantize_rows(dtype, rows, cols, x, q, s, x_stride=x.stride(0) if rows > 1 else 0, q_stride=ldq)
+    torch.cuda.synchronize()
+    assert q.untouched() and s.untouched()
+    return q.t, s.t[0]
+
+
+@pytest.mark.parametrize("dtype", [alt.F32, alt.BF16])
+@pytest.mark.parametrize("rows,cols,ldx,ldq", [(1, 1, 0, 0), (1, 7, 0, 0), (3, 8, 0, 0), (5, 63, 65, 71), (2, 768, 0, 0), (128, 768, 0, 0), (7, 2048, 0, 0),
+                                               (9, 2049, 0, 0), (4, 4099, 4101, 4107), (1, 8192, 0, 0), (3, 8200, 8208, 0), (2, 20011, 0, 0), (3, 70000, 0, 0),
+                                               (1000, 33, 0, 40)])
+def test_quantize_rows(h, dtype, rows, cols, ldx, ldq):
+    x = normal(rows * 7 + cols, rows, cols) * torch.exp(2 * normal(cols, rows, 1))
+    x = matrix(x, TORCH[dtype], ldx, offset=1)
+    q, s = quantize(h, x, dtype, ldq)
+    want_q, want_s = exact_rows(x)
+    assert np.array_equal(f64(s), want_s)
+    assert np.array_equal(q.cpu().numpy(), want_q)
+
+
+def test_quantize_rows_ties_extremes_and_specials(h):
+    cols = 300
+    half = torch.arange(cols) % 255 - 127.0
+    rows = [torch.zeros(cols), torch.full((cols,), 3.0), half, half - 0.5 * (half > -127), (half + 0.5) * 2.0 ** -20, half * 2.0 ** -133, half * 2.0 ** -149,
+            half * 2.0 ** 120, torch.cat([half[:-1], torch.tensor([127.5])])]
+    rows.append(torch.full((cols,), 2.0 ** -149))
+    rows.append(torch.full((cols,), torch.finfo(torch.float32).max))
+    x = matrix(torch.stack(rows), torch.float32)
+    q, s = quantize(h, x, alt.F32)
+    want_q, want_s = exact_rows(x)
+    assert np.array_equal(f64(s), want_s) and np.array_equal(q.cpu().numpy(), want_q)
+    # rows with an infinity or a NaN: scale NaN, q zero, and their neighbours as ever
+    bad = x.clone()
+    for r, v in ((1, float("inf")), (3, float("-inf")), (5, float("nan"))):
+        bad[r, (r * 97) % cols] = v
+    q2, s2 = quantize(h, bad, alt.F32)
+    lost = torch.tensor([r in (1, 3, 5) for r in range(len(rows))])
+    assert torch.isnan(s2.cpu()[lost]).all() and (q2.cpu()[lost] == 0).all()
+    assert torch.equal(q2.cpu()[~lost], q.cpu()[~lost]) and torch.equal(s2.cpu()[~lost], s.cpu()[~lost])
+
+
+# ---- 8-bit product ---------------------------------------------------------------------------------------------------------
+
+def scaled_reference(q, s, w, t, bias, relu):
+    """(value, largest intermediate value) in 64 bits."""
+    y = (f64(q) @ f64(w).T) * f64(s)[:, None] * f64(t)
+    size = np.abs(y)
+    if bias is not None:
+        y = y + f64(bias)
+        size = size + np.abs(f64(bias))
+    return (np.maximum(y, 0) if relu else y), size
+
+
+I8_SHAPES = [(1, 1, 1), (1, 64, 64), (1, 3072, 768), (2, 65, 16), (3, 17, 130), (16, 256, 1024), (17, 100, 333), (31, 129, 127), (33, 512, 48), (64, 64, 128),
+             (65, 200, 2049), (100, 1000, 15), (128, 768, 3072), (200, 192, 256), (257, 513, 640), (513, 300, 1031)]
+
+
+@pytest.mark.parametrize("M,N,K", I8_SHAPES)
+@pytest.mark.parametrize("out,bias,relu,pad", [(alt.BF16, False, False, 0), (alt.F32, True, True, 0), (alt.F32, True, False, 16), (alt.BF16, True, True, 3)])
+def test_gemm_i8(h, M, N, K, out, bias, relu, pad):
+    g = torch.Generator().manual_seed(M * 31 + N * 7 + K)
+    q = matrix(torch.randint(-128, 128, (M, K), generator=g), torch.int8, K + pad, offset=pad)
+    w = matrix(torch.randint(-128, 128, (N, K), generator=g), torch.int8, K + pad, offset=pad)
+    s, t = normal(1, M).abs().cuda() * 0.01, normal(2, N).abs().cuda() * 0.01
+    b = normal(3, N).cuda() if bias else None
+    y = Canary(M, N, TORCH[out], N + pad)
+    d = alt.gemm_i8_desc(M, N, K, out_dtype=out, epilogue=(alt.EPI_BIAS if bias else 0) | (alt.EPI_RELU if relu else 0), lda=K + pad, ldb=K + pad, ldc=N + pad)
+    need = h.gemm_i8_workspace_size(d)
+    for ws in ([0, need] if need else [0]):
+        y.t.fill_(55)
+        h.gemm_i8(d, q, s, w, t, y, bias=b, workspace=torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None, ws_bytes=ws)
+        torch.cuda.synchronize()
+        assert y.untouched()
+        want, size = scaled_reference(q, s, w, t, b, relu)
+        close(y.t, want, 4 * EPS * size + (2.0 ** -8 * np.abs(want) if out == alt.BF16 else 0), "ws %d" % ws)
+
+
+@pytest.mark.parametrize("M", [1, 16, 40, 200])
+def test_gemm_i8_sums_are_exact(h, M):
+    """Scales of powers of two and sums below 2^24: every output has one right value, also at the ends of the 8-bit range."""
+    N, K = 96, 1000
+    g = torch.Generator().manual_seed(M)
+    q = torch.randint(-128, 128, (M, K), generator=g, dtype=torch.int32)
+    w = torch.randint(-128, 128, (N, K), generator=g, dtype=torch.int32)
+    q[0], w[0], w[1] = -128, -128, 127
+    y = torch.empty(M, N, device="cuda")
+    one = torch.full((M,), 0.5, device="cuda"), torch.full((N,), 4.0, device="cuda")
+    h.gemm_i8(alt.gemm_i8_desc(M, N, K, out_dtype=alt.F32), matrix(q, torch.int8), one[0], matrix(w, torch.int8), one[1], y)
+    assert torch.equal(y.cpu().double(), 2.0 * (q.double() @ w.double().T))
+
+
+def test_gemm_i8_rows_without_a_scale_are_nan(h):
+    q, w = torch.ones(20, 64, dtype=torch.int8, device="cuda"), torch.ones(32, 64, dtype=torch.int8, device="cuda")
+    s, t = torch.ones(20, device="cuda"), torch.ones(32, device="cuda")
+    s[3] = float("nan")
+    y = torch.empty(20, 32, device="cuda")
+    h.gemm_i8(alt.gemm_i8_desc(20, 32, 64, out_dtype=alt.F32, epilogue=alt.EPI_RELU), q, s, w, t, y)
+    want = torch.full((20, 32), 64.0)
+    want[3] = float("nan")
+    assert torch.equal(torch.nan_to_num(y.cpu(), nan=-1.0), torch.nan_to_num(want, nan=-1.0))
+
+
+# ---- products of groups ----------------------------------------------------------------------------------------------------
+
+# (offsets, rows of the tensors): empty experts, rows of no expert before, behind and alone, single tokens, tiles that end inside
+SPANS = [([0, 1], 1), ([0, 0, 0, 1, 1], 1), ([0, 3, 3, 20, 37, 37], 37), ([0, 64, 128, 192], 192), ([0, 65, 65, 66, 300], 300), ([5, 9, 100], 120), ([0, 0, 0], 13),
+         ([13, 13], 13), ([0] + [i for i in range(1, 71)], 70), ([0] + [2 * i for i in range(1, 131)] + [300], 310), ([0, 500], 500), ([0, 16, 200, 217, 700], 700)]
+SIZES = [(64, 64), (96, 200), (33, 17), (129, 1030), (515, 72), (256, 320), (1, 1), (8, 2049)]
+
+
+def make_offsets(off):
+    return torch.tensor(off, dtype=torch.int32, device="cuda")
+
+
+def spans_of(off):
+    return [(e, off[e], off[e + 1]) for e in range(len(off) - 1) if off[e + 1] > off[e]]
+
+
+def cases():
+    """Every span list with a size, every size with a span list, and all types and paddings among them."""
+    out = []
+    for i in range(24):
+        off, rows = SPANS[i % len(SPANS)]
+        n, k = SIZES[(i * 5 + i // 8) % len(SIZES)]
+        out.append((off, rows, n, k, [alt.BF16, alt.F32][(i + i // 12) % 2], [0, 8, 3][i % 3]))
+    return out
+
+
+@pytest.mark.parametrize("off,rows,N,K,dtype,pad", cases())
+def test_grouped_forward(h, off, rows, N, K, dtype, pad):
+    E, td = len(off) - 1, TORCH[dtype]
+    x = matrix(normal(1, rows, K), td, K + pad, offset=pad)
+    w = matrix(normal(2, E, N, K, std=K ** -0.5), td, K + pad, offset=pad)
+    bias = normal(3, E, N).cuda()
+    offsets = make_offsets(off)
+    for out, epi in ((alt.F32, 0), (alt.F32, alt.EPI_BIAS | alt.EPI_RELU)) + (((alt.BF16, alt.EPI_BIAS),) if dtype == alt.BF16 else ()):
+        y = Canary(rows, N, TORCH[out], N + pad)
+        d = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=out, epilogue=epi, lda=K + pad, ldb=K + pad, ldc=N + pad)
+        need = h.gemm_grouped_workspace_size(d)
+        want, tol = np.zeros((rows, N)), np.zeros((rows, N))
+        for e, lo, hi in spans_of(off):
+            a, b = f64(x[lo:hi]), f64(w[e])
+            want[lo:hi], tol[lo:hi] = a @ b.T, K * EPS * (np.abs(a) @ np.abs(b).T)
+            if epi & alt.EPI_BIAS:
+                want[lo:hi] += f64(bias[e])
+                tol[lo:hi] += 2 * EPS * np.abs(want[lo:hi])
+        if epi & alt.EPI_RELU:
+            want = np.maximum(want, 0)
+        if out == alt.BF16:
+            tol += 2.0 ** -8 * np.abs(want)
+        for ws in ([0, need] if need else [0]):
+            y.t.fill_(55)
+            h.gemm_grouped(d, x, w, offsets, y, bias=bias if epi & alt.EPI_BIAS else None,
+                           workspace=torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None, ws_bytes=ws)
+            torch.cuda.synchronize()
+            assert y.untouched()
+            close(y.t, want, tol, "out %d epilogue %d ws %d" % (out, epi, ws))
+
+
+@pytest.mark.parametrize("off,rows,N,K", [(o, r) + SIZES[(i * 3) % len(SIZES)] for i, (o, r) in enumerate(SPANS)])
+def test_grouped_forward_i8(h, off, rows, N, K):
+    E, pad = len(off) - 1, [0, 16, 5][rows % 3]
+    g = torch.Generator().manual_seed(rows)
+    q = matrix(torch.randint(-127, 128, (rows, K), generator=g), torch.int8, K + pad)
+    w = matrix(torch.randint(-127, 128, (E, N, K), generator=g), torch.int8, K + pad)
+    s, t, bias = normal(1, rows).abs().cuda() * 0.01, normal(2, E, N).abs().cuda() * 0.01, normal(3, E, N).cuda()
+    offsets = make_offsets(off)
+    for out, relu in ((alt.F32, False), (alt.BF16, True)):
+        y = Canary(rows, N, TORCH[out])
+        d = alt.grouped_desc(rows, E, N, K, in_dtype=alt.I8, out_dtype=out, epilogue=alt.EPI_BIAS | (alt.EPI_RELU if relu else 0), lda=K + pad, ldb=K + pad)
+        need = h.gemm_grouped_workspace_size(d)
+        h.gemm_grouped(d, q, w, offsets, y, a_scale=s, b_scale=t, bias=bias, workspace=torch.empty(need, dtype=torch.uint8, device="cuda") if need else None, ws_bytes=need)
+        torch.cuda.synchronize()
+        assert y.untouched()
+        want, tol = np.zeros((rows, N)), np.zeros((rows, N))
+        for e, lo, hi in spans_of(off):
+            want[lo:hi], size = scaled_reference(q[lo:hi], s[lo:hi], w[e], t[e], bias[e], relu)
+            tol[lo:hi] = 4 * EPS * size + (2.0 ** -8 * np.abs(want[lo:hi]) if out == alt.BF16 else 0)
+        close(y.t, want, tol, "out %d" % out)
+
+
+@pytest.mark.parametrize("off,rows,N,K,dtype,pad", cases())
+def test_grouped_gradients(h, off, rows, N, K, dtype, pad):
+    E, td = len(off) - 1, TORCH[dtype]
+    x = matrix(normal(1, rows, K).clamp_(min=0), td, K + pad, offset=pad)
+    w = matrix(normal(2, E, N, K, std=K ** -0.5), td, K + pad, offset=pad)
+    dy = matrix(normal(3, rows, N), td, N + pad, offset=pad)
+    offsets = make_offsets(off)
+    for out in (alt.F32, alt.BF16) if dtype == alt.BF16 else (alt.F32,):
+        for mask in (False, True):
+            dx = Canary(rows, K, TORCH[out], K + pad)
+            d = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=out, epilogue=alt.EPI_RELU if mask else 0, lda=K + pad, ldb=K + pad, ldc=N + pad)
+            need = h.gemm_grouped_dx_workspace_size(d)
+            h.gemm_grouped_dx(d, dy, w, offsets, dx, relu_of=x if mask else None, workspace=torch.empty(need, dtype=torch.uint8, device="cuda") if need else None,
+                              ws_bytes=need)
+            torch.cuda.synchronize()
+            assert dx.untouched()
+            want, tol = np.zeros((rows, K)), np.zeros((rows, K))
+            for e, lo, hi in spans_of(off):
+                g, b = f64(dy[lo:hi]), f64(w[e])
+                want[lo:hi], tol[lo:hi] = g @ b, N * EPS * (np.abs(g) @ np.abs(b))
+            if mask:
+                want *= f64(x) > 0
+            close(dx.t, want, tol + (2.0 ** -8 * np.abs(want) if out == alt.BF16 else 0), "dx out %d mask %d" % (out, mask))
+        for with_bias in (True, False):
+            dw, db = Canary(N, K, TORCH[out], K + pad, lead=(E,)), Canary(E, N, torch.float32)
+            d = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=out, epilogue=alt.EPI_BIAS if with_bias else 0, lda=K + pad, ldb=K + pad, ldc=N + pad)
+            need = h.gemm_grouped_dw_workspace_size(d)
+            want, tol = np.zeros((E, N, K)), np.zeros((E, N, K))
+            want_b, tol_b = np.zeros((E, N)), np.zeros((E, N))
+            for e, lo, hi in spans_of(off):
+                g, a = f64(dy[lo:hi]), f64(x[lo:hi])
+                want[e], tol[e] = g.T @ a, (hi - lo) * EPS * (np.abs(g).T @ np.abs(a))
+                want_b[e], tol_b[e] = g.sum(axis=0), (hi - lo) * EPS * np.abs(g).sum(axis=0)
+            for ws in ([0, need] if need else [0]):
+                dw.t.fill_(55)
+                db.t.fill_(77)
+                h.gemm_grouped_dw(d, x, dy, offsets, dw, dbias=db if with_bias else None,
+                                  workspace=torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None, ws_bytes=ws)
+                torch.cuda.synchronize()
+                assert dw.untouched() and db.untouched()
+                close(dw.t, want, tol + (2.0 ** -8 * np.abs(want) if out == alt.BF16 else 0), "dw out %d ws %d" % (out, ws))
+                if with_bias:
+                    close(db.t, want_b, tol_b, "db")
+
+
+@pytest.mark.parametrize("rows", [24, 500])
+def test_gradients_against_differences(h, rows):
+    """L = sum y * g is linear in x, w and bias, so a difference over any step is the derivative: along a random direction of each operand the
+    differences of forward products equal the products with the gradients, but for the roundings of their fp32 sums (n * 2^-24 each)."""
+    off, E, N, K = [0, 7, 7, rows], 3, 70, 90
+    x, w, b, g = normal(1, rows, K).cuda(), normal(2, E, N, K).cuda(), normal(3, E, N).cuda(), normal(4, rows, N).cuda()
+    ox, ow, ob = normal(5, rows, K).cuda(), normal(6, E, N, K).cuda(), normal(7, E, N).cuda()
+    offsets = make_offsets(off)
+    d = alt.grouped_desc(rows, E, N, K, in_dtype=alt.F32, out_dtype=alt.F32, epilogue=alt.EPI_BIAS)
+    plain = alt.grouped_desc(rows, E, N, K, in_dtype=alt.F32, out_dtype=alt.F32)
+
+    def loss(x, w, b):
+        y = torch.empty(rows, N, device="cuda")
+        h.gemm_grouped(d, x, w, offsets, y, bias=b)
+        return float((y.double() * g.double()).sum()), float((y.double() * g.double()).abs().sum())
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    h.gemm_grouped_dx(plain, g, w, offsets, dx)
+    h.gemm_grouped_dw(d, x, g, offsets, dw, dbias=db)
+    for got, (up, down) in (((dx.double() * ox.double()).sum(), ((x + ox, w, b), (x - ox, w, b))), ((dw.double() * ow.double()).sum(), ((x, w + ow, b), (x, w - ow, b))),
+                            ((db.double() * ob.double()).sum(), ((x, w, b + ob), (x, w, b - ob)))):
+        (hi, size_hi), (lo, size_lo) = loss(*up), loss(*down)
+        # each y is off by K * 2^-24 of sums that are K^0.5 times larger than itself at most here, and so is the gradient by its own
+        assert abs(float(got) - (hi - lo) / 2) <= (rows + K + N) * EPS * 10 * (size_hi + size_lo)
+
+
+@pytest.mark.parametrize("dtype", [alt.F32, alt.BF16, alt.I8])
+def test_values_of_one_expert_stay_there(h, dtype):
+    """Infinities and NaN in an expert's rows or weights reach that expert's results alone."""
+    off, E, N, K = [0, 5, 40, 45, 80], 4, 72, 96
+    rows, offsets = off[-1], make_offsets([0, 5, 40, 45, 80])
+    if dtype == alt.I8:
+        s = torch.ones(rows, device="cuda")
+        s[5:40] = float("nan")
+        t = torch.ones(E, N, device="cuda")
+        t[3] = float("inf")
+        x, w = torch.ones(rows, K, dtype=torch.int8, device="cuda"), torch.ones(E, N, K, dtype=torch.int8, device="cuda")
+        y = torch.empty(rows, N, device="cuda")
+        h.gemm_grouped(alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=alt.F32), x, w, offsets, y, a_scale=s, b_scale=t)
+        y = y.cpu()
+        assert torch.isnan(y[5:40]).all() and torch.isinf(y[45:]).all() and (y[:5] == K).all() and (y[40:45] == K).all()
+        return
+    x, w = normal(1, rows, K), normal(2, E, N, K)
+    x[5:40, 3] = float("nan")
+    w[3] = float("inf")
+    x, w = matrix(x, TORCH[dtype]), matrix(w, TORCH[dtype])
+    dy = matrix(normal(3, rows, N), TORCH[dtype])
+    y, dx, dw = torch.empty(rows, N, device="cuda"), torch.empty(rows, K, device="cuda"), torch.empty(E, N, K, device="cuda")
+    d = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=alt.F32)
+    h.gemm_grouped(d, x, w, offsets, y)
+    h.gemm_grouped_dx(d, dy, w, offsets, dx)
+    h.gemm_grouped_dw(d, x, dy, offsets, dw)
+    y, dx, dw = y.cpu(), dx.cpu(), dw.cpu()
+    ok = torch.isfinite
+    assert torch.isnan(y[5:40]).all() and not ok(y[45:]).any() and ok(y[:5]).all() and ok(y[40:45]).all()
+    assert ok(dx[:45]).all() and not ok(dx[45:]).any()
+    assert torch.isnan(dw[1, :, 3]).all() and ok(dw[[0, 2, 3]]).all() and ok(dw[1, :, [0, 95]]).all()
+
+
+@pytest.mark.parametrize("off", [[-5, 20, 10 ** 9], [40, 10, 30], [2 ** 31 - 1, -2 ** 31, 7]])
+def test_offsets_out_of_range_stay_in_the_buffers(h, off):
+    rows, E, N, K = 40, 2, 70, 64
+    x, w, dy = normal(1, rows, K).bfloat16().cuda(), normal(2, E, N, K).bfloat16().cuda(), normal(3, rows, N).bfloat16().cuda()
+    y, dx, dw = Canary(rows, N, torch.float32), Canary(rows, K, torch.float32), Canary(N, K, torch.float32, lead=(E,))
+    d, o = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32), make_offsets(off)
+    h.gemm_grouped(d, x, w, o, y)
+    h.gemm_grouped_dx(d, dy, w, o, dx)
+    h.gemm_grouped_dw(d, x, dy, o, dw)
+    torch.cuda.synchronize()
+    assert y.untouched() and dx.untouched() and dw.untouched()
+    assert torch.isfinite(dw.t).all()
+
+
+def test_no_rows(h):
+    E, N, K = 3, 64, 64
+    o = make_offsets([0, 0, 0, 0])
+    d = alt.grouped_desc(0, E, N, K, out_dtype=alt.F32, epilogue=alt.EPI_BIAS)
+    h.gemm_grouped(d, None, None, o, None)
+    dw, db = torch.ones(E, N, K, device="cuda"), torch.ones(E, N, device="cuda")
+    h.gemm_grouped_dw(d, None, None, o, dw, dbias=db)
+    assert not dw.any() and not db.any()
+    h.quantize_rows(alt.F32, 0, 8, None, None, None)
+    h.gemm_i8(alt.gemm_i8_desc(0, 8, 8), None, None, None, None, None)
+
+
+def test_streams_and_graphs(h):
+    """A layer on a stream of its own, and captured: every replay equals the eager pass, with other inputs and offsets each time."""
+    rows, E, N, K = 48, 4, 192, 128
+    x, w = normal(1, rows, K).bfloat16().cuda(), normal(2, E, N, K).bfloat16().cuda()
+    o = make_offsets([0, 10, 11, 40, 48])
+    y, dx, dw = torch.empty(rows, N, device="cuda"), torch.empty(rows, K, device="cuda"), torch.empty(E, N, K, device="cuda")
+    q, s, wq = torch.empty(rows, K, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(E, N, K, dtype=torch.int8, device="cuda")
+    t = torch.empty(E, N, device="cuda")
+    y8 = torch.empty(rows, N, device="cuda")
+    h.quantize_rows(alt.BF16, E * N, K, w, wq, t)
+    d = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32)
+    d8 = alt.grouped_desc(rows, E, N, K, in_dtype=alt.I8, out_dtype=alt.F32)
+    dy = normal(3, rows, N).bfloat16().cuda()
+    ws = {}
+    for name, size in (("y", h.gemm_grouped_workspace_size(d)), ("dx", h.gemm_grouped_dx_workspace_size(d)), ("dw", h.gemm_grouped_dw_workspace_size(d))):
+        ws[name] = dict(workspace=torch.empty(size, dtype=torch.uint8, device="cuda") if size else None, ws_bytes=size)
+
+    def step():
+        h.gemm_grouped(d, x, w, o, y, **ws["y"])
+        h.gemm_grouped_dx(d, dy, w, o, dx, **ws["dx"])
+        h.gemm_grouped_dw(d, x, dy, o, dw, **ws["dw"])
+        h.quantize_rows(alt.BF16, rows, K, x, q, s)
+        h.gemm_grouped(d8, q, wq, o, y8, a_scale=s, b_scale=t)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i, off in enumerate(([0, 10, 11, 40, 48], [0, 0, 0, 0, 0], [0, 48, 48, 48, 48], [3, 4, 5, 6, 7])):
+        x.copy_(normal(10 + i, rows, K))
+        o.copy_(make_offsets(off))
+        step()
+        eager = [v.clone() for v in (y, dx, dw, y8)]
+        for v in (y, dx, dw, y8):
+            v.fill_(-3)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager, (y, dx, dw, y8)):
+            assert torch.equal(a, b), i
+
+
+def test_results_repeat(h):
+    """The same call gives the same bits."""
+    off, E, N, K = [0, 300, 301, 2000], 3, 200, 264
+    x, w, dy = normal(1, 2000, K).bfloat16().cuda(), normal(2, E, N, K).bfloat16().cuda(), normal(3, 2000, N).bfloat16().cuda()
+    o, d = make_offsets(off), alt.grouped_desc(2000, E, N, K, out_dtype=alt.F32, epilogue=alt.EPI_BIAS)
+    need = h.gemm_grouped_dw_workspace_size(d)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    first = None
+    for _ in range(4):
+        dw, db = torch.empty(E, N, K, device="cuda"), torch.empty(E, N, device="cuda")
+        h.gemm_grouped_dw(d, x, dy, o, dw, dbias=db, workspace=ws, ws_bytes=need)
+        torch.cuda.synchronize()
+        first = first or (dw, db)
+        assert torch.equal(dw, first[0]) and torch.equal(db, first[1])
