@@ -14,6 +14,9 @@
 // 16; fp32: four instructions of one float each), so tiles are laid out in bytes and one body serves all three.
 #pragma once
 
+#include <algorithm>
+#include <cmath>
+
 #include "dconv.h"
 
 namespace alt {
@@ -37,9 +40,11 @@ struct GroupedParams {
     int32_t rows, cols, red;   // of one problem (kWeights: red = all rows of the tensors, of which a group takes its own)
     int32_t groups;
     int32_t tiles_n;           // column tiles
+    int32_t places;            // compute units
+    FastDiv d_panel;           // of kPanel * tiles_n
     int32_t flags;
 };
-enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpVecOut = 4, kGrpMask = 8 };
+enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpMask = 4, kGrpWhole = 8 };   // kGrpWhole: the columns are whole 16-byte chunks of the output, and whole fours
 
 template <typename T> struct GrpTraits;
 template <> struct GrpTraits<bf16_tag> { static constexpr int ES = 2; typedef floatx16_t acc_t; };
@@ -71,13 +76,15 @@ struct GrpTile {
     int col_tile;
 };
 
-__device__ __forceinline__ int grp_scan(int v, int lane)        // inclusive prefix sum over the wave
+__device__ __forceinline__ int grp_scan(int v)                  // inclusive prefix sum over the wave
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(v, d);
-        v += lane >= d ? o : 0;
-    }
+    // (shifts inside rows of 16 lanes, then the rows' last lanes handed on)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
     return v;
 }
 
@@ -97,6 +104,14 @@ __device__ __forceinline__ void grp_span(const GroupedParams &p, int s, int &beg
 // operands in their XCD's L2), and each XCD gets a block of consecutive tiles: workgroups go to the XCDs in turn.
 constexpr int kPanel = 8;
 
+__device__ __forceinline__ void grp_order(const GroupedParams &p, int q, int tiles_m, int &row_tile, int &col_tile)
+{
+    const int panel = (int)fast_div((uint32_t)q, p.d_panel), rest = q - panel * (kPanel * p.tiles_n);
+    const int pm = min(kPanel, tiles_m - panel * kPanel);
+    col_tile = pm == kPanel ? rest / kPanel : rest / pm;
+    row_tile = panel * kPanel + rest - col_tile * pm;
+}
+
 template <int BM>
 __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint32_t wg, GrpTile &t)
 {
@@ -105,7 +120,7 @@ __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint3
     for (int s0 = 0; s0 < spans; s0 += 64) {
         if (p.offsets) grp_span(p, s0 + lane, beg, end);
         else { beg = 0; end = lane == 0 ? p.rows : 0; }
-        upto = grp_scan((end - beg + BM - 1) / BM, lane);
+        upto = grp_scan((end - beg + BM - 1) / BM);
         total += __builtin_amdgcn_readlane(upto, 63);
     }
     const uint32_t tiles = (uint32_t)total * (uint32_t)p.tiles_n, per = (tiles + 7) / 8;
@@ -116,21 +131,19 @@ __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint3
     for (int s0 = 0; s0 < spans; s0 += 64) {
         if (spans > 64) {
             grp_span(p, s0 + lane, beg, end);
-            upto = grp_scan((end - beg + BM - 1) / BM, lane);
+            upto = grp_scan((end - beg + BM - 1) / BM);
         }
         const uint64_t past = __ballot((uint32_t)(before + upto) * (uint32_t)p.tiles_n > logical);
         if (past) {
             const int l = __builtin_ctzll(past);
             const int mt = (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(beg, l) + BM - 1) / BM;
             const int first = before + __builtin_amdgcn_readlane(upto, l) - mt;
-            const int q = (int)(logical - (uint32_t)first * (uint32_t)p.tiles_n);
-            const int panel = q / (kPanel * p.tiles_n), rest = q - panel * (kPanel * p.tiles_n);
-            const int pm = min(kPanel, mt - panel * kPanel);
+            int row_tile;
+            grp_order(p, (int)(logical - (uint32_t)first * (uint32_t)p.tiles_n), mt, row_tile, t.col_tile);
             t.group = min(s0 + l, p.groups);
-            t.col_tile = rest / pm;
             t.row_end = __builtin_amdgcn_readlane(end, l);
-            t.row0 = __builtin_amdgcn_readlane(beg, l) + (panel * kPanel + rest % pm) * BM;
-            return true;
+            t.row0 = __builtin_amdgcn_readlane(beg, l) + row_tile * BM;
+            return (unsigned)row_tile < (unsigned)mt && (unsigned)t.col_tile < (unsigned)p.tiles_n;    // (sums of offsets out of order may wrap)
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
@@ -146,6 +159,7 @@ __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint3
 //        together (four consecutive ones; fp32: four apart) swap places
 template <int ES, bool RED, int OUTER, int BKB>
 struct GrpOperand {
+    static constexpr bool kRed = RED;
     static constexpr int EPC = 16 / ES;                     // elements per chunk
     static constexpr int BK = BKB / ES;                     // reduction steps per stage
     static constexpr int BYTES = OUTER * BKB;
@@ -182,6 +196,8 @@ struct GrpOperand {
             return (uint32_t)(k * PITCH + (((o >> 2) ^ swz(k)) * 16) + (o & 3) * 4);
         }
     }
+    // From this lane's address of (RED) tile 0, chunk kc or (!RED) tile i, chunk 0 to that of tile i, chunk kc.
+    static __device__ __forceinline__ constexpr int apart(int i, int kc) { return RED ? i * 32 * PITCH : kc * (32 / ES) * PITCH; }
     static __device__ __forceinline__ u32x4_t read(const char *lds, uint32_t at)
     {
         if constexpr (RED) {
@@ -240,132 +256,530 @@ __device__ __forceinline__ float grp_sum(const u32x4_t &v)
 
 // ---- epilogue ----------------------------------------------------------------------------------------------------------------
 
-// Four consecutive columns of one output row.
-template <typename T>
-__device__ __forceinline__ void grp_store4(const GroupedParams &p, char *y_row, const char *mask_row, int col, const float *v)
+// W consecutive floats of a row, `count` of which exist (the others are zero).  Any alignment of whole elements.
+template <int W>
+__device__ __forceinline__ void grp_load_f(const float *p, int count, float (&v)[W])
 {
-    float o[4] = {v[0], v[1], v[2], v[3]};
-    const bool whole = (p.flags & kGrpVecOut) && col + 4 <= p.cols;
-    if (p.flags & kGrpMask) {
-        constexpr int ES = GrpTraits<T>::ES;
+    if (count >= W) {
+        __builtin_memcpy(v, p, 4 * W);
+    } else {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (col + q >= p.cols) break;
-            float m;
-            if constexpr (ES == 4) m = ((const float *)mask_row)[col + q];
-            else m = __builtin_bit_cast(float, (uint32_t)((const uint16_t *)mask_row)[col + q] << 16);
-            o[q] = m > 0.f ? o[q] : 0.f;
-        }
+        for (int q = 0; q < W; ++q) v[q] = q < count ? p[q] : 0.f;
     }
+}
+
+// W elements (16 bytes of output, of type T) of the tensor that says which outputs stay, as far as `count` of them exist.
+template <int ES, int W> struct GrpMask { uint32_t w[ES * W / 4]; };
+
+// All bits where the element is positive (its sign and magnitude as a number of ES bytes; NaN is not).
+template <int ES>
+__device__ __forceinline__ bool grp_positive(uint32_t bits)
+{
+    const uint32_t f = ES == 4 ? bits : bits << 16;
+    return f - 1u < 0x7f800000u;
+}
+
+// W (4 or 8) consecutive columns of one output row: ReLU, rounding.
+template <int W>
+__device__ __forceinline__ void grp_store(const GroupedParams &p, char *y_row, int col, float (&v)[W])
+{
+    const int count = p.cols - col;
     if (p.flags & kGrpRelu) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] = o[q] < 0.f ? 0.f : o[q];           // (keeps NaN)
+        for (int q = 0; q < W; ++q) v[q] = v[q] < 0.f ? 0.f : v[q];           // (keeps NaN)
     }
     if (p.flags & kGrpOutBf16) {
-        const uint32_t lo = f32x2_to_bf16x2(o[0], o[1]), hi = f32x2_to_bf16x2(o[2], o[3]);
+        uint32_t w[W / 2];
+#pragma unroll
+        for (int q = 0; q < W / 2; ++q) w[q] = f32x2_to_bf16x2(v[2 * q], v[2 * q + 1]);
         uint16_t *d = (uint16_t *)y_row + col;
-        if (whole) {
-            *(u32x2_t *)d = (u32x2_t){lo, hi};
+        if (count >= W) {
+            __builtin_memcpy(d, w, 2 * W);
         } else {
-            if (col < p.cols) d[0] = (uint16_t)lo;
-            if (col + 1 < p.cols) d[1] = (uint16_t)(lo >> 16);
-            if (col + 2 < p.cols) d[2] = (uint16_t)hi;
-            if (col + 3 < p.cols) d[3] = (uint16_t)(hi >> 16);
+#pragma unroll
+            for (int q = 0; q < W; ++q)
+                if (q < count) d[q] = (uint16_t)(w[q / 2] >> (q % 2 * 16));
         }
     } else {
         float *d = (float *)y_row + col;
-        if (whole) {
-            *(f32x4_t *)d = (f32x4_t){o[0], o[1], o[2], o[3]};
+        if (count >= W) {
+            __builtin_memcpy(d, v, 4 * W);
         } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (col + q < p.cols) d[q] = o[q];
+            for (int q = 0; q < W; ++q)
+                if (q < count) d[q] = v[q];
         }
     }
 }
 
-// ---- the tile kernel ---------------------------------------------------------------------------------------------------------
+// ---- what the tile kernels share ---------------------------------------------------------------------------------------------
 
-template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB>
-__global__ __launch_bounds__(64 * WGM * WGN) void grouped_kernel(const GroupedParams p)
+// One workgroup's tile: rows [row0, row_end) of the output (at most BM of them), columns from col0, reduced over `red` steps from a0 and b0.
+struct GrpProblem {
+    int row0, row_end, col0, red, group;
+    const char *a0, *b0;
+    char *y;
+};
+
+// kForward, kInput: the tile at row0 and col0 of a group's rows.
+template <typename T, int FORM>
+__device__ __forceinline__ void grp_at(const GroupedParams &p, int group, int row0, int row_end, int col0, GrpProblem &g)
+{
+    const bool owned = group < p.groups;
+    g.group = group;
+    g.row0 = row0;
+    g.row_end = row_end;
+    g.col0 = col0;
+    g.red = owned ? p.red : 0;
+    g.a0 = (const char *)p.a + (int64_t)row0 * p.lda;
+    g.b0 = (const char *)p.b + (int64_t)(owned ? group : 0) * p.b_group + (FORM == kForward ? (int64_t)col0 * p.ldb : (int64_t)col0 * GrpTraits<T>::ES);
+    g.y = (char *)p.y;
+}
+
+// Workgroups of one group of a kWeights launch: blocks of tiles for each XCD, where there are tiles enough for that.
+__host__ __device__ inline int grp_weight_tiles(int tiles) { return tiles >= 64 ? (tiles + 7) / 8 * 8 : tiles; }
+
+template <typename T, int FORM, int BM, int BN>
+__device__ __forceinline__ bool grp_problem(const GroupedParams &p, int lane, GrpProblem &g)
 {
     constexpr int ES = GrpTraits<T>::ES;
-    constexpr int THREADS = 64 * WGM * WGN;
+    if constexpr (FORM == kWeights) {
+        const int tiles_m = (p.rows + BM - 1) / BM, tiles = tiles_m * p.tiles_n, per = grp_weight_tiles(tiles);
+        g.group = (int)(blockIdx.x / (unsigned)per);
+        int q = (int)(blockIdx.x % (unsigned)per), mt, nt;
+        if (tiles >= 64) q = (q & 7) * (per / 8) + (q >> 3);
+        if (q >= tiles) return false;
+        grp_order(p, q, tiles_m, mt, nt);
+        g.row0 = mt * BM;
+        g.row_end = p.rows;
+        g.col0 = nt * BN;
+        const int beg = min(max(p.offsets[g.group], 0), p.red), end = min(max(p.offsets[g.group + 1], beg), p.red);
+        g.red = end - beg;
+        g.a0 = (const char *)p.a + (int64_t)beg * p.lda + (int64_t)g.row0 * ES;
+        g.b0 = (const char *)p.b + (int64_t)beg * p.ldb + (int64_t)g.col0 * ES;
+        g.y = (char *)p.y + (int64_t)g.group * p.y_group;
+    } else {
+        GrpTile tile;
+        if (!grp_find<BM>(p, lane, blockIdx.x, tile)) return false;
+        grp_at<T, FORM>(p, tile.group, tile.row0, tile.row_end, tile.col_tile * BN, g);
+    }
+    return true;
+}
+
+// Stores a wave's tile, whose first row and column inside the workgroup's are wrow and wcol.  The matrix instructions leave lane = output row,
+// registers = columns (the right operand is their first); 32 rows by 128 bytes at a time go through 4 KB of LDS of the wave's own and out as whole
+// lines, 16 bytes per lane.  (Stored as they lie, a 256x256 tile took 13000 instructions, most of them branches at the edges.)  What the sums are
+// combined with is asked for first.  The wave's earlier memory operations are complete when the first store goes out.
+constexpr int kStageBytes = 4096;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t grp_buffer(const void *base, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000);
+}
+
+// WHOLE: every chunk of an output row, and every four columns, exist or do not (no path for parts of them).  Rows and columns that do not exist
+// lie outside the buffer descriptors: what is asked for there is zero, and what is stored there is dropped, without a branch.
+template <typename T, int FORM, int TM, int TN, bool BF16, bool WHOLE>
+__device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProblem &g, typename GrpTraits<T>::acc_t (&acc)[TM][TN], char *stage, int wrow, int wcol, int lane)
+{
+    constexpr int ES = GrpTraits<T>::ES, OS = BF16 ? 2 : 4;
+    constexpr int JB = BF16 && TN > 1 ? 2 : 1, CPB = BF16 ? 4 * JB : 8;      // column tiles and 16-byte chunks of a band's rows
+    constexpr int W = 16 / OS, RPP = 64 / CPB, PASSES = 32 / RPP;             // columns of a chunk; rows per pass, passes per band
+    constexpr int BANDS = TM * (TN / JB);
+    const bool owned = g.group < p.groups, masked = FORM == kInput && (p.flags & kGrpMask), relu = FORM == kForward && (p.flags & kGrpRelu);
+    const int col_in = g.col0 + wcol + (lane >> 5) * 4, col_out = g.col0 + wcol + lane % CPB * W;  // of the sums and of the chunks
+    const int row_out = wrow + lane / CPB, last = g.row_end - g.row0 - 1;                           // from the tile's first row on
+    float sa[TM];
+    f32x4_t scale[TN][4], bias[TN][4];
+    auto columns = [&](f32x4_t (&v)[TN][4], const float *row, bool exist) {
+        const __amdgpu_buffer_rsrc_t r = grp_buffer(row, exist ? (uint32_t)p.cols * 4u : 0u);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const int at = (col_in + j * 32 + q4 * 8) * 4;
+                if constexpr (WHOLE) {
+                    v[j][q4] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[j][q4][q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at + q * 4, 0, 0));
+                }
+            }
+    };
+    if constexpr (FORM == kForward) {
+        const int64_t at = (int64_t)(owned ? g.group : 0) * p.cols;
+        if constexpr (ES == 1) {
+            // (rows of no group: scales of zero columns, so that their zeros stay zeros)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) sa[i] = owned ? p.a_scale[g.row0 + min(wrow + (lane & 31) + i * 32, last)] : 0.f;
+            columns(scale, p.b_scale + at, owned);
+        }
+        columns(bias, p.bias ? p.bias + at : nullptr, p.bias && owned);
+    }
+    // A lane's chunk of row r lies at `at` + r * ld, outside everything where its columns do not exist.
+    const __amdgpu_buffer_rsrc_t y_rsrc = grp_buffer(g.y + (int64_t)g.row0 * p.ldy, (uint32_t)last * (uint32_t)p.ldy + (uint32_t)(p.cols * OS));
+    const __amdgpu_buffer_rsrc_t m_rsrc = grp_buffer((const char *)p.mask + (int64_t)g.row0 * p.ldmask, masked ? (uint32_t)last * (uint32_t)p.ldmask + (uint32_t)(p.cols * ES) : 0u);
+    // (of two bands: the one that is stored and the one behind it)
+    GrpMask<ES, W> mask[2][PASSES];
+    auto load_mask = [&](int band) {
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+            const int col = col_out + band % (TN / JB) * JB * 32, at = (row_out + band / (TN / JB) * 32 + q * RPP) * (int)p.ldmask + col * ES;
+            GrpMask<ES, W> &m = mask[band & 1][q];
+            if constexpr (WHOLE && ES * W == 16) {
+                const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(m_rsrc, col < p.cols ? at : (int)kOutOfRange, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m.w[e % (ES * W / 4)] = v[e];
+            } else if constexpr (WHOLE && ES * W == 8) {
+                const u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(m_rsrc, col < p.cols ? at : (int)kOutOfRange, 0, 0);
+                m.w[0] = v.x;
+                m.w[1] = v.y;
+            } else {
+#pragma unroll
+                for (int e = 0; e < ES * W / 4; ++e) m.w[e] = 0;
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const int o = col + e < p.cols ? at + e * ES : (int)kOutOfRange;
+                    if constexpr (ES == 4) m.w[e % (ES * W / 4)] = __builtin_amdgcn_raw_buffer_load_b32(m_rsrc, o, 0, 0);
+                    else if constexpr (ES == 2) m.w[e / 2] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(m_rsrc, o, 0, 0) << (e % 2 * 16);
+                }
+            }
+        }
+    };
+    if constexpr (FORM == kInput) {
+        if (masked) load_mask(0);
+    }
+    wait_vmcnt<0>();
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; j += JB) {
+            const int r_in = lane & 31, band = i * (TN / JB) + j / JB;
+            if constexpr (FORM == kInput) {
+                if (masked && band + 1 < BANDS) load_mask(band + 1);
+            }
+#pragma unroll
+            for (int jj = 0; jj < JB; ++jj)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    f32x4_t f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        f[q] = (float)acc[i][j + jj][q4 * 4 + q];
+                        if constexpr (ES == 1) f[q] = f[q] * sa[i] * scale[j + jj][q4][q];
+                        if constexpr (FORM == kForward) f[q] += bias[j + jj][q4][q];
+                    }
+                    if (relu) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) f[q] = f[q] < 0.f ? 0.f : f[q];                            // (keeps NaN)
+                    }
+                    if constexpr (BF16) {
+                        const u32x2_t w = {f32x2_to_bf16x2(f.x, f.y), f32x2_to_bf16x2(f.z, f.w)};
+                        *(u32x2_t *)(stage + r_in * (CPB * 16) + (((jj * 4 + q4) ^ (r_in & (CPB - 1))) * 16) + (lane >> 5) * 8) = w;
+                    } else {
+                        *(f32x4_t *)(stage + r_in * (CPB * 16) + (((q4 * 2 + (lane >> 5)) ^ (r_in & (CPB - 1))) * 16)) = f;
+                    }
+                }
+            const int col = col_out + j * 32;
+#pragma unroll
+            for (int q = 0; q < PASSES; ++q) {
+                const int r = lane / CPB + q * RPP;
+                u32x4_t w = *(const u32x4_t *)(stage + r * (CPB * 16) + (((lane % CPB) ^ (r & (CPB - 1))) * 16));
+                if constexpr (FORM == kInput) {
+                    if (masked) {
+                        const GrpMask<ES, W> &m = mask[band & 1][q];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if constexpr (!BF16) w[e] = grp_positive<ES>(ES == 4 ? m.w[e % (ES * W / 4)] : m.w[e / 2 % (ES * W / 4)] >> (e % 2 * 16)) ? w[e] : 0u;
+                            else w[e] &= (grp_positive<2>(m.w[e] & 0xffffu) ? 0xffffu : 0u) | (grp_positive<2>(m.w[e] >> 16) ? 0xffff0000u : 0u);
+                        }
+                    }
+                }
+                const int at = (row_out + i * 32 + q * RPP) * (int)p.ldy + col * OS;
+                if constexpr (WHOLE) {
+                    __builtin_amdgcn_raw_buffer_store_b128(w, y_rsrc, col < p.cols ? at : (int)kOutOfRange, 0, 0);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        const int o = col + e < p.cols ? at + e * OS : (int)kOutOfRange;
+                        if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16((short)(w[e / 2] >> (e % 2 * 16)), y_rsrc, o, 0, 0);
+                        else __builtin_amdgcn_raw_buffer_store_b32(w[e], y_rsrc, o, 0, 0);
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int FORM, int TM, int TN>
+__device__ __forceinline__ void grp_epilogue(const GroupedParams &p, const GrpProblem &g, typename GrpTraits<T>::acc_t (&acc)[TM][TN], char *stage, int wrow, int wcol,
+                                             int lane)
+{
+    const bool bf16 = GrpTraits<T>::ES < 4 && (p.flags & kGrpOutBf16);
+    if (p.flags & kGrpWhole) {
+        if (bf16) grp_emit<T, FORM, TM, TN, (GrpTraits<T>::ES < 4), true>(p, g, acc, stage, wrow, wcol, lane);
+        else grp_emit<T, FORM, TM, TN, false, true>(p, g, acc, stage, wrow, wcol, lane);
+    } else {
+        if (bf16) grp_emit<T, FORM, TM, TN, (GrpTraits<T>::ES < 4), false>(p, g, acc, stage, wrow, wcol, lane);
+        else grp_emit<T, FORM, TM, TN, false, false>(p, g, acc, stage, wrow, wcol, lane);
+    }
+}
+
+// kWeights: the sums of the left operand's rows, which lane and lane + 32 hold halves of.
+template <int TM>
+__device__ __forceinline__ void grp_store_sums(const GroupedParams &p, const GrpProblem &g, const float (&sums)[TM], int wrow, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int row = g.row0 + wrow + i * 32 + (lane & 31);
+        const float s = sums[i] + __shfl_xor(sums[i], 32);
+        if (lane < 32 && row < g.row_end) p.colsum[(int64_t)g.group * p.rows + row] = s;
+    }
+}
+
+// ---- the kernel for few rows per group: the weights stream through registers, once ---------------------------------------------
+//
+// Bound by the weights' bytes.  A tile is 16 * MT rows by 16 * NT columns; the NW waves of a workgroup share its reduction, wave w taking units
+// of 128 bytes w, w + NW, ... of every row, so that each line is read whole by one wave and the workgroup walks along the rows.  Fragments of the
+// 16-row matrix instructions are 16 bytes of a row per lane (row lane % 16, quarter lane / 16 of 64 bytes) and come straight from memory at any
+// alignment; two batches of loads are in flight per wave.  The waves' sums meet in LDS and are added in the waves' order.
+template <typename T> struct GrpFew;
+template <> struct GrpFew<bf16_tag> { typedef f32x4_t acc_t; };
+template <> struct GrpFew<float> { typedef f32x4_t acc_t; };
+typedef int i32x4s_t __attribute__((ext_vector_type(4)));
+template <> struct GrpFew<i8_tag> { typedef i32x4s_t acc_t; };
+
+template <typename T>
+__device__ __forceinline__ void grp_mma16(typename GrpFew<T>::acc_t &c, const u32x4_t &first, const u32x4_t &second)
+{
+    if constexpr (std::is_same<T, bf16_tag>::value) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, first), __builtin_bit_cast(bf16x8_t, second), c, 0, 0, 0);
+    } else if constexpr (std::is_same<T, i8_tag>::value) {
+        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4s_t, first), __builtin_bit_cast(i32x4s_t, second), c, 0, 0, 0);
+    } else {
+        const f32x4_t f = __builtin_bit_cast(f32x4_t, first), s = __builtin_bit_cast(f32x4_t, second);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(f[j], s[j], c, 0, 0, 0);
+    }
+}
+
+template <typename T, int MT, int NT, int NW, int BATCH>
+__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParams p)
+{
+    constexpr int ES = GrpTraits<T>::ES, UNIT = 128;
+    __shared__ u32x4_t part[NW * MT * NT * 64];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    GrpProblem g;
+    if (!grp_problem<T, kForward, 16 * MT, 16 * NT>(p, lane, g)) return;
+    const int rows_left = g.row_end - g.row0, cols_left = p.cols - g.col0;
+
+    // (rows and columns outside the tile's repeat its last one: their sums are never stored)
+    const char *ap[MT], *bp[NT];
+    const int at = lane / 16 * 16;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) ap[i] = g.a0 + (int64_t)min(i * 16 + lane % 16, rows_left - 1) * p.lda + at;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) bp[j] = g.b0 + (int64_t)min(j * 16 + lane % 16, cols_left - 1) * p.ldb + at;
+
+    typename GrpFew<T>::acc_t acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+
+    struct Batch { u32x4_t a[BATCH][2][MT], b[BATCH][2][NT]; };
+    const int bytes = g.red * ES, units = bytes / UNIT;    // whole units
+    auto load = [&](Batch &f, int u) {                     // units u, u + NW, ... (past the last one the first again, which mma leaves out)
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+            const int64_t off = (int64_t)(u + q * NW < units ? u + q * NW : 0) * UNIT;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) __builtin_memcpy(&f.b[q][h][j], bp[j] + off + h * 64, 16);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) __builtin_memcpy(&f.a[q][h][i], ap[i] + off + h * 64, 16);
+            }
+        }
+    };
+    auto mma = [&](const Batch &f, int u) {
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+            if (u + q * NW >= units) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[i][j], f.b[q][h][j], f.a[q][h][i]);
+        }
+    };
+    constexpr int STEP = NW * BATCH;
+    if (wave < units) {
+        Batch x, y;
+        load(x, wave);
+        for (int u = wave; u < units; u += 2 * STEP) {
+            if (u + STEP < units) load(y, u + STEP);
+            mma(x, u);
+            if (u + 2 * STEP < units) load(x, u + 2 * STEP);
+            if (u + STEP < units) mma(y, u + STEP);
+        }
+    }
+    // what the reduction ends with: less than a unit
+    if (bytes % UNIT && wave == units % NW) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = units * UNIT + h * 64, count = (bytes - k - at) / ES;
+            u32x4_t a[MT], b[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[i] = grp_load_chunk<ES>(ap[i] + k, count);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j] = grp_load_chunk<ES>(bp[j] + k, count);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[i][j], b[j], a[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) part[(wave * MT * NT + i * NT + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[i][j]);
+    __syncthreads();
+    // each thread: four columns (lane / 16 of a tile's) of one row (lane % 16)
+    const bool owned = g.group < p.groups;
+    for (int s = t; s < MT * NT * 64; s += NW * 64) {
+        typename GrpFew<T>::acc_t sum = __builtin_bit_cast(typename GrpFew<T>::acc_t, part[s]);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) sum += __builtin_bit_cast(typename GrpFew<T>::acc_t, part[w * MT * NT * 64 + s]);
+        const int tile = s / 64, l = s % 64;
+        const int row = g.row0 + tile / NT * 16 + l % 16, col = g.col0 + tile % NT * 16 + l / 16 * 4;
+        if (row >= g.row_end || col >= p.cols) continue;
+        float v[4], scale[4] = {1.f, 1.f, 1.f, 1.f}, bias[4] = {0.f, 0.f, 0.f, 0.f}, sa = 1.f;
+        if (owned) {
+            const int64_t c = (int64_t)g.group * p.cols + col;
+            if constexpr (ES == 1) {
+                sa = p.a_scale[row];
+                grp_load_f<4>(p.b_scale + c, p.cols - col, scale);
+            }
+            if (p.bias) grp_load_f<4>(p.bias + c, p.cols - col, bias);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            v[q] = (float)sum[q];
+            if constexpr (ES == 1) v[q] = v[q] * sa * scale[q];
+            v[q] += bias[q];
+        }
+        grp_store<4>(p, g.y + (int64_t)row * p.ldy, col, v);
+    }
+}
+
+// ---- the kernel for any size, stride and alignment: operands go through registers --------------------------------------------
+//
+// Chunks of 16 bytes are loaded at whatever address they start at.  Rows and columns that do not exist repeat the tile's last ones (their sums are
+// never stored), or, where the outer index is contiguous, the last tile is moved back to end with the matrix (what two tiles both compute they
+// compute alike); so only the reduction's last step has chunks of which a part exists.  Loads are two steps ahead: those of step s + 2 go out
+// before step s is computed, and reach LDS behind it a step later.
+template <int ES, bool RED, int OUTER, int BKB, int THREADS>
+struct GrpLoader {
+    using Op = GrpOperand<ES, RED, OUTER, BKB>;
+    static constexpr int NL = Op::BYTES / 16 / THREADS;
+    static_assert(NL * THREADS * 16 == Op::BYTES, "whole chunks per thread");
+    uint32_t voff[NL];
+    int row[NL], elem[NL];
+    const char *base;                      // of the step that is loaded next
+    int64_t ld;
+    int left, outer_left;                  // steps of the reduction from base on; outer indices from the tile's first on
+
+    __device__ __forceinline__ void start(const char *p0, int64_t ld_, int outer, int red, int t)
+    {
+        base = p0;
+        ld = ld_;
+        left = red;
+        outer_left = outer;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            Op::slot(i * THREADS + t, row[i], elem[i]);
+            voff[i] = (uint32_t)(RED ? min(row[i], outer - 1) : row[i]) * (uint32_t)ld + (uint32_t)(elem[i] * ES);
+        }
+    }
+    __device__ __forceinline__ void load(u32x4_t (&v)[NL])
+    {
+        if (left >= Op::BK && (RED || outer_left >= OUTER)) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) __builtin_memcpy(&v[i], base + voff[i], 16);
+        } else if (left <= 0) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) v[i] = (u32x4_t){0, 0, 0, 0};
+        } else if (!RED && outer_left >= OUTER) {
+            // (rows behind the last: the last one's, cleared)
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                __builtin_memcpy(&v[i], base + (row[i] < left ? voff[i] : (uint32_t)(left - 1) * (uint32_t)ld + (uint32_t)(elem[i] * ES)), 16);
+                if (row[i] >= left) v[i] = (u32x4_t){0, 0, 0, 0};
+            }
+        } else if (RED && left >= Op::EPC) {
+            // (a chunk that ends behind the row is loaded to end with it, and shifted)
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int over = elem[i] + Op::EPC - left;                     // elements behind the end
+                __builtin_memcpy(&v[i], base + voff[i] - (uint32_t)(max(over, 0) * ES), 16);
+            }
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int over = min(max(elem[i] + Op::EPC - left, 0), Op::EPC) * ES;
+                unsigned __int128 w = __builtin_bit_cast(unsigned __int128, v[i]);
+                w = over >= 16 ? 0 : w >> (over * 8);
+                v[i] = __builtin_bit_cast(u32x4_t, w);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NL; ++i)
+                v[i] = grp_load_chunk<ES>(base + voff[i], RED ? left - elem[i] : row[i] < left ? outer_left - elem[i] : 0);
+        }
+        base += RED ? (int64_t)BKB : ld * Op::BK;
+        left -= Op::BK;
+    }
+};
+
+template <typename T, int FORM, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const GroupedParams p)
+{
+    constexpr int ES = GrpTraits<T>::ES, BKB = 128, THREADS = 64 * WGM * WGN;
     constexpr int WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32, NKC = BKB / 32;
-    using A = GrpOperand<ES, FORM != kWeights, BM, BKB>;
-    using B = GrpOperand<ES, FORM == kForward, BN, BKB>;
-    constexpr int BK = A::BK, STAGE = A::BYTES + B::BYTES;
-    constexpr int NLA = A::BYTES / 16 / THREADS, NLB = B::BYTES / 16 / THREADS;
-    static_assert(NLA * THREADS * 16 == A::BYTES && NLB * THREADS * 16 == B::BYTES, "whole chunks per thread");
+    using LA = GrpLoader<ES, FORM != kWeights, BM, BKB, THREADS>;
+    using LB = GrpLoader<ES, FORM == kForward, BN, BKB, THREADS>;
+    using A = typename LA::Op;
+    using B = typename LB::Op;
+    constexpr int STAGE = A::BYTES + B::BYTES;
+    static_assert(WGM * WGN * kStageBytes <= 2 * STAGE, "staging");
 
     extern __shared__ uint4 smem_u4[];
     char *lds = (char *)smem_u4;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave / WGN, wn = wave % WGN;
-
-    // ---- the tile: rows [row0, row_end) of the output, columns from col0, reduction over `red` steps from the operands' bases
-    int row0, row_end, col0, red, group;
-    const char *a0, *b0;
-    char *y = (char *)p.y;
-    if constexpr (FORM == kWeights) {
-        const int per = ((p.rows + BM - 1) / BM) * p.tiles_n;
-        group = (int)(blockIdx.x / (unsigned)per);
-        const int q = (int)(blockIdx.x % (unsigned)per);
-        row0 = q / p.tiles_n * BM;
-        row_end = p.rows;
-        col0 = q % p.tiles_n * BN;
-        const int beg = min(max(p.offsets[group], 0), p.red), end = min(max(p.offsets[group + 1], beg), p.red);
-        red = end - beg;
-        a0 = (const char *)p.a + (int64_t)beg * p.lda + (int64_t)row0 * ES;
-        b0 = (const char *)p.b + (int64_t)beg * p.ldb + (int64_t)col0 * ES;
-        y += (int64_t)group * p.y_group;
-    } else {
-        GrpTile tile;
-        if (!grp_find<BM>(p, lane, blockIdx.x, tile)) return;
-        group = tile.group;
-        row0 = tile.row0;
-        row_end = tile.row_end;
-        col0 = tile.col_tile * BN;
-        red = group < p.groups ? p.red : 0;
-        a0 = (const char *)p.a + (int64_t)row0 * p.lda;
-        b0 = (const char *)p.b + (int64_t)(group < p.groups ? group : 0) * p.b_group + (FORM == kForward ? (int64_t)col0 * p.ldb : (int64_t)col0 * ES);
+    GrpProblem g;
+    if (!grp_problem<T, FORM, BM, BN>(p, lane, g)) return;
+    if (FORM != kForward && g.col0 + BN > p.cols && p.cols >= BN) {
+        g.b0 -= (int64_t)(g.col0 + BN - p.cols) * ES;
+        g.col0 = p.cols - BN;
     }
-    const int rows_left = row_end - row0, cols_left = p.cols - col0;
+    if (FORM == kWeights && g.row0 + BM > p.rows && p.rows >= BM) {
+        g.a0 -= (int64_t)(g.row0 + BM - p.rows) * ES;
+        g.row0 = p.rows - BM;
+    }
 
-    // ---- operand chunks through registers
-    u32x4_t ra[NLA], rb[NLB];
-    auto load = [&](int step) {
-#pragma unroll
-        for (int i = 0; i < NLA; ++i) {
-            int r, e;
-            A::slot(i * THREADS + t, r, e);
-            if constexpr (FORM != kWeights) {
-                const int k = step * BK + e;
-                ra[i] = grp_load_chunk<ES>(a0 + (int64_t)r * p.lda + (int64_t)k * ES, r < rows_left ? red - k : 0);
-            } else {
-                const int k = step * BK + r;
-                ra[i] = grp_load_chunk<ES>(a0 + (int64_t)k * p.lda + (int64_t)e * ES, k < red ? rows_left - e : 0);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < NLB; ++i) {
-            int r, e;
-            B::slot(i * THREADS + t, r, e);
-            if constexpr (FORM == kForward) {
-                const int k = step * BK + e;
-                rb[i] = grp_load_chunk<ES>(b0 + (int64_t)r * p.ldb + (int64_t)k * ES, r < cols_left ? red - k : 0);
-            } else {
-                const int k = step * BK + r;
-                rb[i] = grp_load_chunk<ES>(b0 + (int64_t)k * p.ldb + (int64_t)e * ES, k < red ? cols_left - e : 0);
-            }
-        }
-    };
-    auto store = [&](int stage) {
+    LA la;
+    LB lb;
+    la.start(g.a0, p.lda, g.row_end - g.row0, g.red, t);
+    lb.start(g.b0, p.ldb, p.cols - g.col0, g.red, t);
+    u32x4_t ra[2][LA::NL], rb[2][LB::NL];
+    auto store = [&](int stage, const u32x4_t (&va)[LA::NL], const u32x4_t (&vb)[LB::NL]) {
         char *d = lds + stage * STAGE;
 #pragma unroll
-        for (int i = 0; i < NLA; ++i) *(u32x4_t *)(d + (i * THREADS + t) * 16) = ra[i];
+        for (int i = 0; i < LA::NL; ++i) *(u32x4_t *)(d + (i * THREADS + t) * 16) = va[i];
 #pragma unroll
-        for (int i = 0; i < NLB; ++i) *(u32x4_t *)(d + A::BYTES + (i * THREADS + t) * 16) = rb[i];
+        for (int i = 0; i < LB::NL; ++i) *(u32x4_t *)(d + A::BYTES + (i * THREADS + t) * 16) = vb[i];
     };
 
     typename GrpTraits<T>::acc_t acc[TM][TN];
@@ -378,17 +792,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_kernel(const GroupedPa
     float sums[TM];                                        // kWeights: of this lane's row of the left operand
 #pragma unroll
     for (int i = 0; i < TM; ++i) sums[i] = 0.f;
-    const bool take_sums = FORM == kWeights && p.colsum && col0 == 0 && wn == 0;
+    const bool take_sums = FORM == kWeights && p.colsum && g.col0 == 0 && wn == 0;
 
-    const int steps = (red + BK - 1) / BK;
-    if (steps > 0) {
-        load(0);
-        store(0);
-    }
-    for (int s = 0; s < steps; ++s) {
-        __syncthreads();                                   // stage s is written, stage s + 1's last readers are through
-        if (s + 1 < steps) load(s + 1);
-        const char *d = lds + (s & 1) * STAGE;
+    const int steps = (g.red + A::BK - 1) / A::BK;
+    auto compute = [&](int stage) {
+        const char *d = lds + stage * STAGE;
 #pragma unroll
         for (int kc = 0; kc < NKC; ++kc) {
             u32x4_t fa[TM], fb[TN];
@@ -403,65 +811,372 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_kernel(const GroupedPa
             if constexpr (FORM == kWeights) {
                 if (take_sums) {
 #pragma unroll
-                    for (int i = 0; i < TM; ++i)
-                        sums[i] += grp_sum<ES>(fa[i]);
+                    for (int i = 0; i < TM; ++i) sums[i] += grp_sum<ES>(fa[i]);
                 }
             }
         }
-        if (s + 1 < steps) store((s + 1) & 1);
+    };
+    // step s in stage s & 1, its successor's operands in registers of parity (s + 1) & 1
+    auto step = [&](int s, auto PARITY) {
+        constexpr int q = decltype(PARITY)::value;
+        __syncthreads();                                   // stage q is written, stage q ^ 1's last readers are through
+        la.load(ra[q]);                                    // of step s + 2
+        lb.load(rb[q]);
+        compute(q);
+        if (s + 1 < steps) store(q ^ 1, ra[q ^ 1], rb[q ^ 1]);
+    };
+    if (steps > 0) {
+        la.load(ra[0]);
+        lb.load(rb[0]);
+        la.load(ra[1]);
+        lb.load(rb[1]);
+        store(0, ra[0], rb[0]);
     }
+    for (int s = 0; s < steps; s += 2) {
+        step(s, std::integral_constant<int, 0>{});
+        if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{});
+    }
+    __syncthreads();                                       // the last stage's readers are through
+    if (take_sums) grp_store_sums(p, g, sums, wm * WTM, lane);
+    grp_epilogue<T, FORM, TM, TN>(p, g, acc, lds + wave * kStageBytes, wm * WTM, wn * WTN, lane);
+}
 
-    // ---- epilogue: lane = output row, registers = columns (the right operand is the instructions' first)
+// ---- the kernel for operands of whole 16-byte chunks: global memory straight into LDS -------------------------------------------
+
+// An operand's loads: every lane's byte offset from the tile's base of step 0 is fixed; the base moves on from step to step, and the descriptor
+// ends where the operand does, so that what lies behind the reduction or outside the tile reads zeros.
+template <int ES, bool RED, int OUTER, int BKB, int NW>
+struct GrpStream {
+    using Op = GrpOperand<ES, RED, OUTER, BKB>;
+    static constexpr int NL = Op::BYTES / 1024 / NW;       // wave loads per wave and step
+    static_assert(NL * NW * 1024 == Op::BYTES && NL >= 1, "whole wave loads");
+    static_assert(!RED || NW * 64 / Op::CPR % (256 / BKB * Op::CPR) == 0, "a lane's loads lie in one chunk column");
+    uint32_t voff[NL];
+    int chunk;                             // RED: this lane's chunk, as a byte offset inside a step
+    uint64_t base;
+    int left;                              // of the reduction from base on: bytes of a row (RED) or rows
+    int ld, tail;                          // bytes between rows; RED: span of the rows before the last
+
+    __device__ __forceinline__ void start(const char *p0, int64_t ld_, int outer_left, int red, int wave, int lane)
+    {
+        const uint64_t at = (uint64_t)p0;
+        base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+        ld = (int)ld_;
+        left = __builtin_amdgcn_readfirstlane(RED ? red * ES : red);
+        tail = __builtin_amdgcn_readfirstlane((min(max(outer_left, 1), OUTER) - 1) * ld);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int r = wm * WTM + i * 32 + (lane & 31);
-        const bool row_ok = r < rows_left;
-        if constexpr (FORM == kWeights) {
-            if (take_sums) {
-                const float s = sums[i] + __shfl_xor(sums[i], 32);
-                if (lane < 32 && row_ok) p.colsum[(int64_t)group * p.rows + row0 + r] = s;
-            }
+        for (int i = 0; i < NL; ++i) {
+            int r, e;
+            Op::slot((i * NW + wave) * 64 + lane, r, e);
+            const bool in = RED ? r < outer_left : e < outer_left;
+            voff[i] = in ? (uint32_t)(r * ld + e * ES) : kOutOfRange;
+            if (i == 0) chunk = e * ES;
         }
-        if (!row_ok) continue;
-        char *y_row = y + (int64_t)(row0 + r) * p.ldy;
-        const char *mask_row = (const char *)p.mask + (int64_t)(row0 + r) * p.ldmask;
-        float sa = 1.f;
-        if constexpr (ES == 1) sa = group < p.groups ? p.a_scale[row0 + r] : 1.f;
+    }
+    // (a step behind the operand's end has nothing left)
+    __device__ __forceinline__ i32x4_t rsrc() const
+    {
+        const int bytes = RED ? left + tail : min(left, Op::BK) * ld;
+        return make_rsrc((const void *)base, left > 0 ? (uint32_t)bytes : 0u);
+    }
+    // RED: this lane's chunk lies behind the reduction's end, which is not the descriptor's but in the last row
+    __device__ __forceinline__ uint32_t past() const { return RED && chunk >= left ? kOutOfRange : 0u; }
+    __device__ __forceinline__ void none() { left = 0; }
+    __device__ __forceinline__ void next()
+    {
+        base += RED ? (uint64_t)BKB : (uint64_t)((int64_t)ld * Op::BK);
+        left -= RED ? BKB : Op::BK;
+    }
+};
+
+// A workgroup's operands run through a ring of NS stages in LDS.  At the barrier of step s the stages of steps s and s + 1 have landed and
+// every wave has read stage s - 1 for the last time; then the loads of step s + NS - 1 go out into that stage, and each chunk's fragments are
+// read some chunks before they are used, across the barrier too: one chunk where a wave's tile has eight matrix instructions for each, three
+// where it has fewer (a read takes about as long as four).  A wave issues in order, and a matrix instruction hides eight other instructions
+// at most: behind each stands one operand read or one load where they are that many, and the order is pinned.
+template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB, int NS>
+struct GrpKernel {
+    static constexpr int ES = GrpTraits<T>::ES;
+    static constexpr int NW = WGM * WGN, THREADS = 64 * NW;
+    static constexpr int WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32, NKC = BKB / 32;
+    using SA = GrpStream<ES, FORM != kWeights, BM, BKB, NW>;
+    using SB = GrpStream<ES, FORM == kForward, BN, BKB, NW>;
+    using A = typename SA::Op;
+    using B = typename SB::Op;
+    using acc_t = typename GrpTraits<T>::acc_t;
+    static constexpr int BK = A::BK, STAGE = A::BYTES + B::BYTES, LPS = SA::NL + SB::NL;
+    static constexpr int AHEAD = TM * TN >= 8 || NKC < 4 ? 1 : 3, NBUF = AHEAD + 1;
+    static_assert(NS == 4 && NS * LPS < 60 && NKC % NBUF == 0, "ring");
+    static constexpr int kLds = NS * STAGE;
+    static_assert(NW * kStageBytes <= kLds, "staging");
+    static_assert(kLds <= 160 * 1024, "LDS");
+
+    static __device__ __forceinline__ void tile(const GroupedParams &p, const GrpProblem &g, char *lds)
+    {
+        const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = wave / WGN, wn = wave % WGN;
+        SA sa;
+        SB sb;
+        sa.start(g.a0, p.lda, g.row_end - g.row0, g.red, wave, lane);
+        sb.start(g.b0, p.ldb, p.cols - g.col0, g.red, wave, lane);
+        i32x4_t rsa, rsb;
+        uint32_t pasta, pastb, ldst = lds0 + wave * 1024;
+        int lstage = 0;
+        auto open_stage = [&]() { rsa = sa.rsrc(); rsb = sb.rsrc(); pasta = sa.past(); pastb = sb.past(); };
+        auto issue_one = [&](int i) {
+            if (i < SA::NL) dma_load16_s(rsa, sa.voff[i] | pasta, 0u, ldst + i * (NW * 1024));
+            else dma_load16_s(rsb, sb.voff[i - SA::NL] | pastb, 0u, ldst + A::BYTES + (i - SA::NL) * (NW * 1024));
+        };
+        auto close_stage = [&]() {
+            sa.next();
+            sb.next();
+            ++lstage;
+            ldst += STAGE;
+            if (lstage == NS) { lstage = 0; ldst -= NS * STAGE; }
+        };
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+        for (int s = 0; s < NS - 1; ++s) {
+            open_stage();
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = col0 + wn * WTN + j * 32 + g * 8 + (lane >> 5) * 4;
-                if (col >= p.cols) continue;
-                float v[4];
+            for (int i = 0; i < LPS; ++i) issue_one(i);
+            close_stage();
+        }
+
+        // This lane's fragments in stage 0.  Where the reduction is contiguous, the wave's tiles are a fixed distance apart (whole swizzle periods)
+        // and every chunk has an address of its own; otherwise the chunks are, and every tile has one.
+        constexpr int NA = A::kRed ? NKC : TM, NB = B::kRed ? NKC : TN;
+        uint32_t a_at[NA], b_at[NB];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] = (float)acc[i][j][g * 4 + q];
-                    if constexpr (FORM == kForward) {
-                        if (group < p.groups && col + q < p.cols) {
-                            const int64_t c = (int64_t)group * p.cols + col + q;
-                            if constexpr (ES == 1) v[q] = v[q] * sa * p.b_scale[c];
-                            if (p.bias) v[q] += p.bias[c];
+        for (int i = 0; i < NA; ++i) a_at[i] = A::kRed ? A::frag(wm * WTM, i, lane) : A::frag(wm * WTM + i * 32, 0, lane);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) b_at[i] = A::BYTES + (B::kRed ? B::frag(wn * WTN, i, lane) : B::frag(wn * WTN + i * 32, 0, lane));
+
+        acc_t acc[TM][TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+        float sums[TM];                                    // kWeights: of this lane's row of the left operand
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sums[i] = 0.f;
+        const bool take_sums = FORM == kWeights && p.colsum && g.col0 == 0 && wn == 0;
+
+        u32x4_t fa[NBUF][TM], fb[NBUF][TN];
+        auto read_one = [&](int buf, int r, uint32_t stage, int kc) {
+            // (in the order in which the matrix instructions want them: the first row, all columns, the other rows)
+            if (r == 0 || r > TN) {
+                const int i = r == 0 ? 0 : r - TN;
+                fa[buf][i] = A::read(lds, stage + a_at[A::kRed ? kc : i] + A::apart(i, kc));
+            } else {
+                fb[buf][r - 1] = B::read(lds, stage + b_at[B::kRed ? kc : r - 1] + B::apart(r - 1, kc));
+            }
+        };
+
+        const int steps = (g.red + BK - 1) / BK;
+        wait_vmcnt<(NS - 3) * LPS>();
+        lds_barrier();
+        uint32_t stage = 0;
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c)
+#pragma unroll
+            for (int r = 0; r < TM + TN; ++r) read_one(c, r, 0, c);
+        for (int s = 0; s < steps; ++s) {
+            if (s > 0) {
+                wait_vmcnt<(NS - 3) * LPS>();
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_barrier" ::: "memory");
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const uint32_t next_stage = stage + STAGE == NS * STAGE ? 0 : stage + STAGE;
+            open_stage();
+            constexpr int READS = TM + TN, LOADS = (LPS + NKC - 1) / NKC, SLOTS = TM * TN;    // of a chunk
+            constexpr int PER = (READS + LOADS + SLOTS - 1) / SLOTS;
+#pragma unroll
+            for (int kc = 0; kc < NKC; ++kc) {
+                const int buf = kc % NBUF, ahead = (kc + AHEAD) % NKC;
+                const bool wraps = kc + AHEAD >= NKC;
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        grp_mma<T>(acc[i][j], fb[buf][j], fa[buf][i]);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int q = (i * TN + j) * PER; q < (i * TN + j + 1) * PER; ++q) {
+                            if (q < READS) read_one((kc + AHEAD) % NBUF, q, wraps ? next_stage : stage, ahead);
+                            else if (q < READS + LOADS && kc * LOADS + q - READS < LPS) issue_one(kc * LOADS + q - READS);
                         }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if constexpr (FORM == kWeights) {
+                        if (take_sums) sums[i] += grp_sum<ES>(fa[buf][i]);
                     }
                 }
-                grp_store4<T>(p, y_row, mask_row, col, v);
             }
+            close_stage();
+            stage = next_stage;
+        }
+        wait_vmcnt<0>();                                   // (the stages behind the last step's)
+        __syncthreads();                                   // the last stage's readers are through
+        if (take_sums) grp_store_sums(p, g, sums, wm * WTM, lane);
+        grp_epilogue<T, FORM, TM, TN>(p, g, acc, lds + wave * kStageBytes, wm * WTM, wn * WTN, lane);
+    }
+};
+
+template <typename K, typename T, int FORM, int BM, int BN>
+__global__ __launch_bounds__(K::THREADS, K::kLds > 80 * 1024 ? (K::NW + 3) / 4 : 1) void grouped_kernel(const GroupedParams p)
+{
+    extern __shared__ uint4 smem_u4[];
+    GrpProblem only;
+    if (!grp_problem<T, FORM, BM, BN>(p, threadIdx.x & 63, only)) return;
+    K::tile(p, only, (char *)smem_u4);
+}
+
+// ---- large tiles, and small ones where they end ------------------------------------------------------------------------------------
+//
+// Tiles of 256x256 need the fewest bytes per product, but they are coarse: of 16384 rows in eight groups and 2048 columns they make 2.1 rounds of
+// the chip, which take as long as three, and a group that ends one row into a tile pays for the whole.  So a launch has tiles of two sizes, first
+// all large ones, then small ones of 128x128 (a round of them counts 0.36 of a round of large ones): where a group's last tile would be half empty, and in
+// place of the large tiles of the last round where those would leave most of the chip idle.  As many workgroups as compute units walk over them.
+constexpr int kSmallCost = 36;                             // percent
+
+struct GrpSchedule {
+    int beg, end, upto_large, upto_small;                  // of this lane's span (spans 0 .. 63): rows; row tiles up to and with it
+    int spans, large, cut, units;                          // tiles that stay large; tiles cut into four; small tiles in all
+};
+
+__device__ __forceinline__ void grp_rows(int len, int &large, int &small)
+{
+    const int rest = len & 255;
+    large = (len >> 8) + (rest > 128);
+    small = rest > 0 && rest <= 128;
+}
+
+__device__ __forceinline__ void grp_span_rows(const GroupedParams &p, int s, int &beg, int &end)
+{
+    if (p.offsets) grp_span(p, s, beg, end);
+    else { beg = 0; end = s == 0 ? p.rows : 0; }
+}
+
+__device__ __forceinline__ void grp_schedule(const GroupedParams &p, int lane, GrpSchedule &h)
+{
+    int large = 0, small = 0;
+    h.spans = p.offsets ? p.groups + 2 : 1;
+    for (int s0 = 0; s0 < h.spans; s0 += 64) {
+        int beg, end, l, m;
+        grp_span_rows(p, s0 + lane, beg, end);
+        grp_rows(end - beg, l, m);
+        l = grp_scan(l);
+        m = grp_scan(m);
+        if (s0 == 0) { h.beg = beg; h.end = end; h.upto_large = l; h.upto_small = m; }
+        large += __builtin_amdgcn_readlane(l, 63);
+        small += __builtin_amdgcn_readlane(m, 63);
+    }
+    const int tiles = large * p.tiles_n, rest = small * ((p.cols + 127) / 128), over = tiles % p.places;
+    const int idle = over ? (p.places - over) * 2 : 0;     // small tiles that fit beside the last round's large ones
+    const int whole = 100 + max(0, rest - idle + p.places - 1) / p.places * kSmallCost, cut = (4 * over + rest + p.places - 1) / p.places * kSmallCost;
+    h.cut = over > 0 && cut < whole ? over : 0;
+    h.large = tiles - h.cut;
+    h.units = 4 * h.cut + rest;
+}
+
+// Row tile `q` of one size, counted over all spans: its span's rows and its place among the span's tiles of that size.
+__device__ __forceinline__ bool grp_row_tile(const GroupedParams &p, const GrpSchedule &h, int lane, bool is_small, uint32_t q, uint32_t per_row, int &span, int &beg, int &end,
+                                             int &first, int &count)
+{
+    int before = 0;
+    for (int s0 = 0; s0 < h.spans; s0 += 64) {
+        int b = h.beg, e = h.end, upto = is_small ? h.upto_small : h.upto_large;
+        if (h.spans > 64) {
+            int l, m;
+            grp_span_rows(p, s0 + lane, b, e);
+            grp_rows(e - b, l, m);
+            upto = grp_scan(is_small ? m : l);
+        }
+        const uint64_t past = __ballot((uint32_t)(before + upto) * per_row > q);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            span = s0 + at;
+            beg = __builtin_amdgcn_readlane(b, at);
+            end = __builtin_amdgcn_readlane(e, at);
+            int l, m;
+            grp_rows(end - beg, l, m);
+            count = is_small ? m : l;
+            first = before + __builtin_amdgcn_readlane(upto, at) - count;
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// Large (or small) tile i of XCD x.  False: there is none.
+template <typename T, int FORM, bool SMALL>
+__device__ __forceinline__ bool grp_unit(const GroupedParams &p, const GrpSchedule &h, int lane, int x, int i, GrpProblem &g)
+{
+    const int all = SMALL ? h.units : h.large, per = (all + 7) / 8;
+    int span, beg, end, first, count, q = x * per + i, sub = 0;
+    if (i >= per || q >= all) return false;
+    if (SMALL && q >= 4 * h.cut) {                         // the small tiles behind a group's large ones
+        q -= 4 * h.cut;
+        const int cols = (p.cols + 127) / 128;
+        if (!grp_row_tile(p, h, lane, true, q, cols, span, beg, end, first, count)) return false;
+        grp_at<T, FORM>(p, min(span, p.groups), beg + ((end - beg) & ~255), end, (q - first * cols) % cols * 128, g);
+        return true;
+    }
+    if (SMALL) { sub = q & 3; q = h.large + (q >> 2); }
+    if (!grp_row_tile(p, h, lane, false, q, p.tiles_n, span, beg, end, first, count)) return false;
+    int mt, nt;
+    grp_order(p, q - first * p.tiles_n, count, mt, nt);
+    if ((unsigned)mt >= (unsigned)count || (unsigned)nt >= (unsigned)p.tiles_n) return false;             // (sums of offsets out of order may wrap)
+    grp_at<T, FORM>(p, min(span, p.groups), beg + mt * 256 + (sub >> 1) * 128, end, nt * 256 + (sub & 1) * 128, g);
+    if (g.col0 >= p.cols) g.red = 0;                       // (nothing is left of the large tile there)
+    return true;
+}
+
+constexpr int kLargeThreads = 512;
+
+template <typename T, int FORM> struct GrpLarge {
+    using Large = GrpKernel<T, FORM, 256, 256, 2, 4, 64, 4>;
+    using Small = GrpKernel<T, FORM, 128, 128, 2, 4, 128, 4>;
+    static_assert(Large::THREADS == kLargeThreads && Small::THREADS == kLargeThreads, "threads");
+    static constexpr int kLds = Large::kLds > Small::kLds ? Large::kLds : Small::kLds;
+};
+
+template <typename T, int FORM>
+__global__ __launch_bounds__(kLargeThreads, 2) void grouped_large_kernel(const GroupedParams p)
+{
+    extern __shared__ uint4 smem_u4[];
+    const int lane = threadIdx.x & 63;
+    GrpSchedule h;
+    grp_schedule(p, lane, h);
+    const int x = blockIdx.x & 7, step = gridDim.x >> 3;
+    for (int i = blockIdx.x >> 3;; i += step) {
+        GrpProblem g;
+        if (!grp_unit<T, FORM, false>(p, h, lane, x, i, g)) break;
+        GrpLarge<T, FORM>::Large::tile(p, g, (char *)smem_u4);
+        __syncthreads();                                   // the staging is read before the next tile's loads land there
+    }
+    // (two small tiles each for the workgroups that have no large one in the last round, then one for each in turn)
+    const int slot = blockIdx.x >> 3, busy = (h.large + 7) / 8 % step, idle = busy ? step - busy : 0;
+    for (int k = slot >= busy && idle ? 0 : 2;; ++k) {
+        GrpProblem g;
+        const int i = k < 2 ? slot - busy + k * idle : 2 * idle + slot + (k - 2) * step;
+        if (!grp_unit<T, FORM, true>(p, h, lane, x, i, g)) break;
+        GrpLarge<T, FORM>::Small::tile(p, g, (char *)smem_u4);
+        __syncthreads();
     }
 }
 
-template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB>
-hipError_t grouped_launch(const GroupedParams &p, unsigned grid, hipStream_t st)
-{
-    constexpr size_t lds = (size_t)2 * (BM + BN) * BKB;
-    hipLaunchKernelGGL((grouped_kernel<T, FORM, BM, BN, WGM, WGN, BKB>), dim3(grid), dim3(64 * WGM * WGN), lds, st, p);
-    return hipGetLastError();
-}
+// ---- launches ------------------------------------------------------------------------------------------------------------------
 
 // One product of `form` on the kernel that suits it (grouped_bf16.hip, grouped_f32.hip, grouped_i8.hip).
-hipError_t grouped_run_bf16(int form, GroupedParams p, hipStream_t st);
-hipError_t grouped_run_f32(int form, GroupedParams p, hipStream_t st);
-hipError_t grouped_run_i8(GroupedParams p, hipStream_t st);
+hipError_t grouped_run_bf16(int form, const GroupedParams &p, hipStream_t st);
+hipError_t grouped_run_f32(int form, const GroupedParams &p, hipStream_t st);
+hipError_t grouped_run_i8(const GroupedParams &p, hipStream_t st);
 
 // Most tiles of BM rows that any offsets in order can make of p.rows rows: each span ends in one part tile at most.
 inline int64_t grp_row_tiles(const GroupedParams &p, int BM)
@@ -471,16 +1186,146 @@ inline int64_t grp_row_tiles(const GroupedParams &p, int BM)
     return p.rows / BM + (spans < p.rows ? spans : p.rows);
 }
 
-template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB>
-hipError_t grouped_tiles(GroupedParams p, hipStream_t st)
+// Sets the column tiles and works out the workgroups of a launch (0: nothing to do).
+template <int FORM, int BM, int BN>
+hipError_t grp_grid(GroupedParams &p, int threads, unsigned *grid)
 {
     p.tiles_n = (p.cols + BN - 1) / BN;
-    int64_t grid;
-    if (FORM == kWeights) grid = (int64_t)((p.rows + BM - 1) / BM) * p.tiles_n * p.groups;
-    else grid = (grp_row_tiles(p, BM) * p.tiles_n + 7) / 8 * 8;            // (a block of tiles for each XCD)
-    if (grid <= 0) return hipSuccess;
-    if (grid * (64 * WGM * WGN) > 0xffffffffll) return hipErrorInvalidConfiguration;   // (threads of a launch)
-    return grouped_launch<T, FORM, BM, BN, WGM, WGN, BKB>(p, (unsigned)grid, st);
+    p.d_panel = make_fastdiv((uint32_t)(kPanel * p.tiles_n));
+    int64_t n;
+    if (FORM == kWeights) n = (int64_t)grp_weight_tiles((p.rows + BM - 1) / BM * p.tiles_n) * p.groups;
+    else n = (grp_row_tiles(p, BM) * p.tiles_n + 7) / 8 * 8;               // (a block of tiles for each XCD)
+    if (n * threads > 0xffffffffll) return hipErrorInvalidConfiguration;   // (threads of a launch)
+    *grid = (unsigned)n;
+    return hipSuccess;
+}
+
+template <typename T, int FORM, int BM, int BN, int WGM, int WGN>
+hipError_t grouped_any(GroupedParams p, hipStream_t st)
+{
+    unsigned grid;
+    const hipError_t e = grp_grid<FORM, BM, BN>(p, 64 * WGM * WGN, &grid);
+    if (e != hipSuccess || !grid) return e;
+    hipLaunchKernelGGL((grouped_any_kernel<T, FORM, BM, BN, WGM, WGN>), dim3(grid), dim3(64 * WGM * WGN), 2 * (BM + BN) * 128, st, p);
+    return hipGetLastError();
+}
+
+template <typename T, int MT, int NT, int NW, int BATCH>
+hipError_t grouped_few(GroupedParams p, hipStream_t st)
+{
+    unsigned grid;
+    const hipError_t e = grp_grid<kForward, 16 * MT, 16 * NT>(p, 64 * NW, &grid);
+    if (e != hipSuccess || !grid) return e;
+    hipLaunchKernelGGL((grouped_few_kernel<T, MT, NT, NW, BATCH>), dim3(grid), dim3(64 * NW), 0, st, p);
+    return hipGetLastError();
+}
+
+// Whether the direct loads take a product: whole chunks at whole addresses, and a tile's rows (or steps) within a descriptor.
+template <typename T, int FORM>
+bool grp_streams(const GroupedParams &p)
+{
+    constexpr int ES = GrpTraits<T>::ES;
+    const uint64_t bits = (uint64_t)p.a | (uint64_t)p.b | (uint64_t)p.lda | (uint64_t)p.ldb | (uint64_t)p.b_group |
+                          (FORM != kWeights ? (uint64_t)p.red * ES : (uint64_t)p.rows * ES) | (FORM == kForward ? 0 : (uint64_t)p.cols * ES);
+    return bits % 16 == 0 && p.lda <= (1 << 22) && p.ldb <= (1 << 22) && p.ldy <= (1 << 22) && p.ldmask <= (1 << 22);
+}
+
+template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB, int NS>
+hipError_t grouped_tiles(GroupedParams p, hipStream_t st)
+{
+    using K = GrpKernel<T, FORM, BM, BN, WGM, WGN, BKB, NS>;
+    unsigned grid;
+    hipError_t e = grp_grid<FORM, BM, BN>(p, K::THREADS, &grid);
+    if (e != hipSuccess || !grid) return e;
+    auto kern = grouped_kernel<K, T, FORM, BM, BN>;
+    static bool attr_set = false;
+    if (!attr_set) {
+        e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (e != hipSuccess) return e;
+        attr_set = true;
+    }
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(K::THREADS), K::kLds, st, p);
+    return hipGetLastError();
+}
+
+template <typename T, int FORM>
+hipError_t grouped_large(GroupedParams p, hipStream_t st)
+{
+    p.tiles_n = (p.cols + 255) / 256;
+    p.d_panel = make_fastdiv((uint32_t)(kPanel * p.tiles_n));
+    if (grp_row_tiles(p, 256) * p.tiles_n * 4 > 0x7fffffff) return hipErrorInvalidConfiguration;
+    auto kern = grouped_large_kernel<T, FORM>;
+    static bool attr_set = false;
+    if (!attr_set) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (e != hipSuccess) return e;
+        attr_set = true;
+    }
+    constexpr int lds = GrpLarge<T, FORM>::kLds;
+    hipLaunchKernelGGL(kern, dim3((p.places + 7) / 8 * 8), dim3(kLargeThreads), lds, st, p);
+    return hipGetLastError();
+}
+
+// ---- which kernel a call runs ------------------------------------------------------------------------------------------------------
+//
+// Rows of each group: the offsets lie on the device, so the rule takes them as even.
+
+// Tiles of BM x BN.
+template <int FORM>
+inline double grp_tiles(const GroupedParams &p, int BM, int BN)
+{
+    const int64_t cols = (p.cols + BN - 1) / BN;
+    if (FORM == kWeights) return (double)((p.rows + BM - 1) / BM) * cols * p.groups;
+    const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows, each = (p.rows + spans - 1) / spans;
+    return (double)spans * ((each + BM - 1) / BM) * cols;
+}
+
+// Time of a launch in us without what every launch costs: rounds of the chip's `places`, each a fixed part and a part for every 128 bytes of the
+// reduction; a round that leaves places idle runs faster, the others having more of the caches and the clock to themselves.
+inline double grp_rounds(double tiles, double places, double units, double fixed, double per_unit)
+{
+    const double rounds = std::ceil(tiles / places);
+    return rounds * (fixed + per_unit * units * (0.5 + 0.5 * tiles / (rounds * places)));
+}
+
+template <typename T, int FORM>
+hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
+{
+    constexpr int ES = GrpTraits<T>::ES;
+    const double places = p.places;
+    if constexpr (FORM == kForward) {
+        // Up to 32 rows each, the weights are what there is to read: 16 x 8192 x 8192 in 8 bits 14.8 us so, 39 us in tiles of 64 rows; at 33 to 64 rows
+        // 64 x 4096 x 4096 takes 10.6 us so, 9.6 in tiles.  Columns in twos (four waves) where that fills the chip, else one by one and eight waves
+        // to a reduction: 16 x 4096 x 4096 6.6 against 8.5 us, 32 x 4096 x 4096 10.4 against 8.6.
+        const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows;
+        if (p.rows <= 32 * spans)
+            return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 1, 8, 2>(p, st) : grouped_few<T, 1, 2, 4, 2>(p, st);
+    }
+    if (!grp_streams<T, FORM>(p)) {
+        // Tiles of 128x128 once they fill three quarters of the chip: 1000 x 3884 x 1115 in 8 bits 24.5 us, in tiles of 64x64 31.1; 2048 x 770 x 3073
+        // (112 tiles) 37.4 and 26.8.  In fp32 the matrix cores are the bound, and small tiles leave none idle: 1001 rows of 13 groups, 515 x 1030, 29 against 73 us.
+        return grp_tiles<FORM>(p, 128, 128) >= (ES == 4 ? 4 : 0.75) * places ? grouped_any<T, FORM, 128, 128, 2, 4>(p, st) : grouped_any<T, FORM, 64, 64, 2, 2>(p, st);
+    }
+    if constexpr (ES == 4) {
+        // (as above; 5000 rows of 5 groups, 2048 x 4096: forward 695 us in tiles of 64x64, 762 of 128x128, by the weights 682 and 657)
+        return FORM == kWeights && grp_tiles<FORM>(p, 128, 128) >= 4 * places ? grouped_tiles<T, FORM, 128, 128, 2, 4, 128, 4>(p, st)
+                                                                               : grouped_tiles<T, FORM, 64, 64, 2, 2, 128, 4>(p, st);
+    } else {
+        // Tiles of 64x64 with a deep ring (one to a compute unit) or a shallow one (two), of 128x128, of 256x256; the constants are those of 8-bit
+        // products of 32 .. 8192 rows, 768 .. 8192 columns and reductions of 512 .. 8192, which they give to 10 %; bf16 has the same tiles in bytes.
+        const double units = FORM == kWeights ? std::ceil((double)p.red * ES / 128.0 / p.groups) : std::ceil(p.red * ES / 128.0);
+        const double n64 = grp_tiles<FORM>(p, 64, 64);
+        const double deep = n64 <= places ? 2.0 + 0.21 * units : 1e30;
+        const double small = grp_rounds(n64, 2 * places, units, 3.0, 0.43);
+        const double middle = grp_rounds(grp_tiles<FORM>(p, 128, 128), places, units, 3.3, 0.54);
+        const double large = grp_rounds(grp_tiles<FORM>(p, 256, 256), places, units, 8.0, 1.73);
+        const double best = std::min(std::min(deep, small), std::min(middle, large));
+        if (best == deep) return grouped_tiles<T, FORM, 64, 64, 2, 2, 256, 4>(p, st);
+        if (best == small) return grouped_tiles<T, FORM, 64, 64, 2, 2, 128, 4>(p, st);
+        if (best == middle) return grouped_tiles<T, FORM, 128, 128, 2, 4, 128, 4>(p, st);
+        if constexpr (FORM == kWeights) return grouped_tiles<T, FORM, 256, 256, 2, 4, 64, 4>(p, st);
+        else return grouped_large<T, FORM>(p, st);
+    }
 }
 
 }  // namespace alt

@@ -28,8 +28,8 @@ alt_status_t check_layer(alt_handle_t h, const char *call, const alt_grouped_des
     if (out->lda < d->K || out->ldb < d->K || out->ldc < d->N) return fail(h, ALT_SHAPE_MISMATCH, "%s: a row stride is shorter than a row", call);
     if (gradient && d->in_dtype == ALT_I8) return fail(h, ALT_UNSUPPORTED, "%s: 8-bit products have no gradients", call);
     if (d->in_dtype == ALT_F32 && d->out_dtype != ALT_F32) return fail(h, ALT_UNSUPPORTED, "%s: fp32 operands give fp32 results", call);
-    if (d->rows > (1 << 30) || d->N > (1 << 24) || d->K > (1 << 24) || d->groups > (1 << 20) || out->lda > 0x7fffffff || out->ldb > 0x7fffffff || out->ldc > 0x7fffffff)
-        return fail(h, ALT_UNSUPPORTED, "%s: more than 2^30 rows, 2^24 columns, 2^20 groups or a stride over 2^31", call);
+    if (d->rows > (1 << 30) || d->groups > (1 << 20) || out->lda > (1 << 22) || out->ldb > (1 << 22) || out->ldc > (1 << 22))
+        return fail(h, ALT_UNSUPPORTED, "%s: more than 2^30 rows, 2^20 groups or 2^22 elements between rows", call);
     if (d->in_dtype == ALT_I8 && d->K > ALT_I8_MAX_K) return fail(h, ALT_UNSUPPORTED, "%s: 32-bit sums hold %d products of 8-bit numbers at most", call, ALT_I8_MAX_K);
     return ALT_OK;
 }
@@ -52,7 +52,8 @@ alt_status_t run(alt_handle_t h, const char *call, int dtype, int form, GroupedP
     const size_t os = p.flags & kGrpOutBf16 ? 2 : 4;
     p.ldy = ldy_elems * (int64_t)os;
     p.y_group *= (int64_t)os;
-    if ((uintptr_t)p.y % (4 * os) == 0 && ldy_elems % 4 == 0) p.flags |= kGrpVecOut;
+    p.places = h->compute_units;
+    if (p.cols % (os == 2 ? 8 : 4) == 0) p.flags |= kGrpWhole;
     const hipError_t e = dtype == ALT_I8 ? grouped_run_i8(p, st) : dtype == ALT_BF16 ? grouped_run_bf16(form, p, st) : grouped_run_f32(form, p, st);
     if (e == hipErrorInvalidConfiguration) return fail(h, ALT_UNSUPPORTED, "%s: more output tiles than a launch holds", call);
     ALT_CHECK_HIP(h, e);

@@ -1,16 +1,11 @@
-// Grouped products in bf16: which kernel a call runs.
+// Grouped products in bf16.
 #include "grouped.h"
 
 namespace alt {
 
-hipError_t grouped_run_bf16(int form, GroupedParams p, hipStream_t st)
+hipError_t grouped_run_bf16(int form, const GroupedParams &p, hipStream_t st)
 {
-    switch (form) {
-        case kForward: return grouped_tiles<bf16_tag, kForward, 64, 64, 2, 2, 128>(p, st);
-        case kInput: return grouped_tiles<bf16_tag, kInput, 64, 64, 2, 2, 128>(p, st);
-        case kWeights: return grouped_tiles<bf16_tag, kWeights, 64, 64, 2, 2, 128>(p, st);
-    }
-    return hipErrorInvalidValue;
+    return form == kForward ? grouped_run<bf16_tag, kForward>(p, st) : form == kInput ? grouped_run<bf16_tag, kInput>(p, st) : grouped_run<bf16_tag, kWeights>(p, st);
 }
 
 }  // namespace alt

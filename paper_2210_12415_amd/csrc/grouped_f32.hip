@@ -1,16 +1,11 @@
-// Grouped products in f32: which kernel a call runs.
+// Grouped products in fp32.
 #include "grouped.h"
 
 namespace alt {
 
-hipError_t grouped_run_f32(int form, GroupedParams p, hipStream_t st)
+hipError_t grouped_run_f32(int form, const GroupedParams &p, hipStream_t st)
 {
-    switch (form) {
-        case kForward: return grouped_tiles<float, kForward, 64, 64, 2, 2, 128>(p, st);
-        case kInput: return grouped_tiles<float, kInput, 64, 64, 2, 2, 128>(p, st);
-        case kWeights: return grouped_tiles<float, kWeights, 64, 64, 2, 2, 128>(p, st);
-    }
-    return hipErrorInvalidValue;
+    return form == kForward ? grouped_run<float, kForward>(p, st) : form == kInput ? grouped_run<float, kInput>(p, st) : grouped_run<float, kWeights>(p, st);
 }
 
 }  // namespace alt

@@ -1,11 +1,8 @@
-// Grouped products in i8: which kernel a call runs.
+// Grouped products in 8-bit integers.
 #include "grouped.h"
 
 namespace alt {
 
-hipError_t grouped_run_i8(GroupedParams p, hipStream_t st)
-{
-    return grouped_tiles<i8_tag, kForward, 64, 64, 2, 2, 128>(p, st);
-}
+hipError_t grouped_run_i8(const GroupedParams &p, hipStream_t st) { return grouped_run<i8_tag, kForward>(p, st); }
 
 }  // namespace alt

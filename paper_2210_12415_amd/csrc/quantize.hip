@@ -11,123 +11,137 @@ namespace {
 typedef uint32_t w4_t __attribute__((ext_vector_type(4)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 
-// Eight elements as floats; `count` of them exist (the others are zero).  Any alignment of whole elements.
 template <int ELSZ>
-__device__ __forceinline__ void load8(const char *p, int count, float (&v)[8])
+__device__ __forceinline__ float element(const char *p)
 {
-    if (count >= 8) {
-        if constexpr (ELSZ == 4) {
-            float w[8];
-            __builtin_memcpy(w, p, 32);
+    if constexpr (ELSZ == 4) return *(const float *)p;
+    else return __builtin_bit_cast(float, (uint32_t)*(const uint16_t *)p << 16);
+}
+
+// A chunk of eight elements as it lies in memory, at any alignment of whole elements, and as floats.
+template <int ELSZ> struct Chunk { w4_t w[ELSZ / 2]; };
+
+template <int ELSZ>
+__device__ __forceinline__ Chunk<ELSZ> load_chunk(const char *p)
+{
+    Chunk<ELSZ> c;
+    __builtin_memcpy(&c, p, 8 * ELSZ);
+    return c;
+}
+
+template <int ELSZ>
+__device__ __forceinline__ void floats(const Chunk<ELSZ> &c, float (&v)[8])
+{
+    if constexpr (ELSZ == 4) {
+        const f4_t a = __builtin_bit_cast(f4_t, c.w[0]), b = __builtin_bit_cast(f4_t, c.w[1]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = w[i];
-        } else {
-            w4_t w;
-            __builtin_memcpy(&w, p, 16);
-            const f4_t lo = __builtin_bit_cast(f4_t, w << 16), hi = __builtin_bit_cast(f4_t, w & 0xffff0000u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = lo[i];
-                v[2 * i + 1] = hi[i];
-            }
-        }
+        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     } else {
+        const f4_t lo = __builtin_bit_cast(f4_t, c.w[0] << 16), hi = __builtin_bit_cast(f4_t, c.w[0] & 0xffff0000u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = 0.f;
-            if (i < count) {
-                if constexpr (ELSZ == 4) v[i] = ((const float *)p)[i];
-                else v[i] = __builtin_bit_cast(float, (uint32_t)((const uint16_t *)p)[i] << 16);
-            }
-        }
+        for (int i = 0; i < 4; ++i) { v[2 * i] = lo[i]; v[2 * i + 1] = hi[i]; }
     }
 }
 
 // The largest |v| so far, as bits: they order like the numbers, infinity and NaN above all.
-__device__ __forceinline__ uint32_t top8(uint32_t top, const float (&v)[8])
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+
+template <int ELSZ>
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const Chunk<ELSZ> &c)
 {
+    float v[8];
+    floats<ELSZ>(c, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
     return top;
 }
 
-// v / s to the nearest whole number: the product with 1 / s is off by less than one part in 2^22, so it is rounded to a neighbour of
-// the quotient at most, and v - r * s, which is exact (s has 16 significant bits, r seven), tells which side of the tie v lies on.
-__device__ __forceinline__ uint32_t quantize1(float v, float s, float half, float inv)
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
-    float r = __builtin_rintf(v * inv);
-    const float rest = __builtin_fmaf(-r, s, v), far = __builtin_fabsf(rest);
-    if (far > half || (far == half && ((int)r & 1))) r += __builtin_copysignf(1.f, rest);
-    return (uint32_t)(int)r & 0xffu;
+    // (shifts inside rows of 16 lanes, then the rows' last lanes handed on: lane 63 holds the largest)
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, true));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-__device__ __forceinline__ void store8(char *q, int count, const float (&v)[8], float s, float half, float inv, bool finite)
+struct Scale {
+    float s, inv, half, below;             // below: the number before half
+};
+
+// v / s to the nearest whole number, as a byte 128 above it at byte `at` of `w`: the product with 1 / s is off by less than one part in 2^22,
+// so it is rounded to a neighbour of the quotient at most, and v - r * s, which is exact (s has 16 significant bits, r seven), tells which side
+// of the tie v lies on; on the tie itself odd numbers give way.
+__device__ __forceinline__ uint32_t quantize1(float v, const Scale &k, uint32_t at, uint32_t w)
 {
+    const float r = __builtin_rintf(v * k.inv), rest = __builtin_fmaf(-r, k.s, v);
+    const float most = (int)r & 1 ? k.below : k.half;
+    const float step = __builtin_fabsf(rest) > most ? __builtin_copysignf(1.f, rest) : 0.f;
+    return __builtin_amdgcn_cvt_pk_u8_f32(r + step + 128.f, at, w);
+}
+
+template <int ELSZ>
+__device__ __forceinline__ void store_chunk(char *q, const Chunk<ELSZ> &c, const Scale &k, uint32_t finite)
+{
+    float v[8];
+    floats<ELSZ>(c, v);
     uint32_t w[2] = {0, 0};
-    if (finite) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i / 4] |= quantize1(v[i], s, half, inv) << (i % 4 * 8);
-    }
-    if (count >= 8) {
-        __builtin_memcpy(q, w, 8);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) q[i] = (char)(w[i / 4] >> (i % 4 * 8));
-    }
+    for (int i = 0; i < 8; ++i) w[i / 4] = quantize1(v[i], k, i % 4, w[i / 4]);
+    w[0] = (w[0] ^ 0x80808080u) & finite;
+    w[1] = (w[1] ^ 0x80808080u) & finite;
+    __builtin_memcpy(q, w, 8);
 }
 
 constexpr int kQuantThreads = 256;
-constexpr int kQuantKeep = 4;              // chunks of eight elements that a thread keeps
+constexpr int kQuantKeep = 4;              // chunks that a thread keeps
 
 // TPR threads (a wave or the workgroup) per row.
 template <int ELSZ, int TPR>
 __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const char *x, int64_t ldx, char *q, int64_t ldq, float *scale, int64_t rows, int cols)
 {
-    constexpr int RPW = kQuantThreads / TPR;               // rows per workgroup
     __shared__ uint32_t part[kQuantThreads / 64];
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / TPR;
-    if (TPR == 64 && row >= rows) return;
+    const int64_t row = (int64_t)blockIdx.x * (kQuantThreads / TPR) + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    if (row >= rows) return;
     x += row * ldx;
     q += row * ldq;
-    float v[kQuantKeep][8];
+    const int chunks = cols / 8, rest = cols % 8;
+    Chunk<ELSZ> keep[kQuantKeep];
     uint32_t top = 0;
+    float last = 0.f;                                      // of the elements behind the last whole chunk, one per thread
+    if (t < rest) last = element<ELSZ>(x + (int64_t)(chunks * 8 + t) * ELSZ);
+    // (a thread without a chunk of its own takes the row's first again: it changes no maximum, and no load waits for a branch)
 #pragma unroll
-    for (int i = 0; i < kQuantKeep; ++i) {
-        const int c = (i * TPR + t) * 8;
-        load8<ELSZ>(x + (int64_t)c * ELSZ, cols - c, v[i]);
-    }
+    for (int i = 0; i < kQuantKeep; ++i)
+        if (i * TPR < chunks) keep[i] = load_chunk<ELSZ>(x + (int64_t)(i * TPR + t < chunks ? i * TPR + t : 0) * (8 * ELSZ));
 #pragma unroll
-    for (int i = 0; i < kQuantKeep; ++i) top = top8(top, v[i]);
-    for (int c = (kQuantKeep * TPR + t) * 8; c < cols; c += TPR * 8) {
-        float w[8];
-        load8<ELSZ>(x + (int64_t)c * ELSZ, cols - c, w);
-        top = top8(top, w);
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    for (int i = 0; i < kQuantKeep; ++i)
+        if (i * TPR < chunks) top = top_of<ELSZ>(top, keep[i]);
+    for (int c = kQuantKeep * TPR + t; c < chunks; c += TPR) top = top_of<ELSZ>(top, load_chunk<ELSZ>(x + (int64_t)c * (8 * ELSZ)));
+    top = wave_max(max(top, magnitude(last)));
     if constexpr (TPR > 64) {
         if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kQuantThreads / 64; ++i) top = max(top, part[i]);
     }
-    const bool finite = top < 0x7f800000u;
-    float s = __builtin_bit_cast(float, top) / 127.f;
-    s = fmaxf(__builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, s) + 0xffu) & ~0xffu), 0x1p-126f);
-    if (t == 0) scale[row] = finite ? s : __builtin_nanf("");
-    const float half = 0.5f * s, inv = 1.f / s;
+    const uint32_t finite = top < 0x7f800000u ? 0xffffffffu : 0u;
+    const float s = __builtin_bit_cast(float, top) / 127.f;
+    Scale k;
+    k.s = fmaxf(__builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, s) + 0xffu) & ~0xffu), 0x1p-126f);
+    k.inv = 1.f / k.s;
+    k.half = 0.5f * k.s;
+    k.below = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, k.half) - 1u);
+    if (t == 0) scale[row] = finite ? k.s : __builtin_nanf("");
 #pragma unroll
-    for (int i = 0; i < kQuantKeep; ++i) {
-        const int c = (i * TPR + t) * 8;
-        store8(q + c, cols - c, v[i], s, half, inv, finite);
-    }
-    for (int c = (kQuantKeep * TPR + t) * 8; c < cols; c += TPR * 8) {
-        float w[8];
-        load8<ELSZ>(x + (int64_t)c * ELSZ, cols - c, w);
-        store8(q + c, cols - c, w, s, half, inv, finite);
-    }
+    for (int i = 0; i < kQuantKeep; ++i)
+        if (i * TPR + t < chunks) store_chunk<ELSZ>(q + (int64_t)(i * TPR + t) * 8, keep[i], k, finite);
+    for (int c = kQuantKeep * TPR + t; c < chunks; c += TPR) store_chunk<ELSZ>(q + (int64_t)c * 8, load_chunk<ELSZ>(x + (int64_t)c * (8 * ELSZ)), k, finite);
+    if (t < rest) q[chunks * 8 + t] = (char)((quantize1(last, k, 0, 0) ^ 0x80u) & finite);
 }
 
 template <int ELSZ>
