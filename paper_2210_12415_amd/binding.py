@@ -1,11 +1,14 @@
 """ctypes marshalling for libalt.so, with a native module for the calls that programs repeat.  Function names follow include/alt.h."""
 import ctypes
+import operator
 import os
 import struct
 
 try:
     from . import _altcall as _native
 except ImportError:                       # built where Python's headers are (build.py)
+    _native = None
+if not hasattr(_native, "gemm_grouped_dw"):   # (nor is one that an older source was built to)
     _native = None
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -175,7 +178,7 @@ def lib():
         L.alt_version.restype = ctypes.c_char_p
         if _native is not None:
             _native.setup(*[ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _REPEATED],
-                          ctypes.c_void_p, ConvDesc, Conv3dDesc, GemmDesc, Layout)
+                          ctypes.c_void_p, ConvDesc, Conv3dDesc, GemmDesc, Layout, GemmI8Desc, GroupedDesc)
         _lib = L
     return _lib
 
@@ -195,7 +198,8 @@ _calls = {}
 
 # The same calls by the native module (native/altcall.c), for arguments of plain types; it answers None to others, and without the module
 # everything is another.  (A conversion's arguments took 1.8 us through ctypes, beside 3.5 for the launch.)
-_REPEATED = ("alt_conv2d", "alt_conv3d", "alt_conv2d_transpose", "alt_conv3d_transpose", "alt_gemm", "alt_layout_transform", "alt_eltwise_add")
+_REPEATED = ("alt_conv2d", "alt_conv3d", "alt_conv2d_transpose", "alt_conv3d_transpose", "alt_gemm", "alt_layout_transform", "alt_eltwise_add",
+             "alt_quantize_rows", "alt_gemm_i8", "alt_gemm_grouped", "alt_gemm_grouped_dx", "alt_gemm_grouped_dw")
 
 
 def _not_taken(*_):
@@ -208,6 +212,8 @@ def _quick(name):
 
 _quick_conv2d, _quick_conv3d = _quick("conv2d"), _quick("conv3d")
 _quick_conv2d_transpose, _quick_conv3d_transpose = _quick("conv2d_transpose"), _quick("conv3d_transpose")
+_quick_quantize, _quick_gemm_i8 = _quick("quantize_rows"), _quick("gemm_i8")
+_quick_grouped, _quick_grouped_dx, _quick_grouped_dw = _quick("gemm_grouped"), _quick("gemm_grouped_dx"), _quick("gemm_grouped_dw")
 _quick_gemm, _quick_transform, _quick_add, _quick_prepare = _quick("gemm"), _quick("layout_transform"), _quick("eltwise_add"), _quick("prepare_conv2d")
 
 
@@ -712,33 +718,34 @@ class Handle:
 
     # 8-bit layers and layers of experts
     def quantize_rows(self, dtype, rows, cols, x, q, scale, x_stride=0, q_stride=0, stream=None):
-        status = _call("alt_quantize_rows")(self._h, dtype, rows, cols, _address(x), x_stride, _address(q), q_stride, _address(scale), _stream_address(stream))
+        status = _quick_quantize(self._h, dtype, rows, cols, x, x_stride, q, q_stride, scale, stream)
+        if status is None:
+            i = operator.index
+            status = _call("alt_quantize_rows")(self._h, i(dtype), i(rows), i(cols), _address(x), i(x_stride), _address(q), i(q_stride), _address(scale),
+                                                _stream_address(stream))
+        if status != 0:
+            _ck(status, self._h)
+
+    def _buffers(self, quick, name, d, buffers, workspace, ws_bytes, stream):
+        """A call of a handle, a descriptor, buffers and a workspace."""
+        status = quick(self._h, d, *buffers, workspace, ws_bytes, stream)
+        if status is None:
+            status = _call(name)(self._h, ctypes.byref(d), *[_address(b) for b in buffers], _address(workspace), ctypes.c_size_t(ws_bytes).value,
+                                 _stream_address(stream))
         if status != 0:
             _ck(status, self._h)
 
     def gemm_i8(self, d, a, a_scale, b, b_scale, y, bias=None, workspace=None, ws_bytes=0, stream=None):
-        status = _call("alt_gemm_i8")(self._h, ctypes.byref(d), _address(a), _address(a_scale), _address(b), _address(b_scale), _address(bias), _address(y),
-                                      _address(workspace), ws_bytes, _stream_address(stream))
-        if status != 0:
-            _ck(status, self._h)
+        self._buffers(_quick_gemm_i8, "alt_gemm_i8", d, (a, a_scale, b, b_scale, bias, y), workspace, ws_bytes, stream)
 
     def gemm_grouped(self, d, a, b, offsets, y, a_scale=None, b_scale=None, bias=None, workspace=None, ws_bytes=0, stream=None):
-        status = _call("alt_gemm_grouped")(self._h, ctypes.byref(d), _address(a), _address(a_scale), _address(b), _address(b_scale), _address(bias),
-                                           _address(offsets), _address(y), _address(workspace), ws_bytes, _stream_address(stream))
-        if status != 0:
-            _ck(status, self._h)
+        self._buffers(_quick_grouped, "alt_gemm_grouped", d, (a, a_scale, b, b_scale, bias, offsets, y), workspace, ws_bytes, stream)
 
     def gemm_grouped_dx(self, d, dy, b, offsets, dx, relu_of=None, workspace=None, ws_bytes=0, stream=None):
-        status = _call("alt_gemm_grouped_dx")(self._h, ctypes.byref(d), _address(dy), _address(b), _address(relu_of), _address(offsets), _address(dx),
-                                              _address(workspace), ws_bytes, _stream_address(stream))
-        if status != 0:
-            _ck(status, self._h)
+        self._buffers(_quick_grouped_dx, "alt_gemm_grouped_dx", d, (dy, b, relu_of, offsets, dx), workspace, ws_bytes, stream)
 
     def gemm_grouped_dw(self, d, a, dy, offsets, dw, dbias=None, workspace=None, ws_bytes=0, stream=None):
-        status = _call("alt_gemm_grouped_dw")(self._h, ctypes.byref(d), _address(a), _address(dy), _address(offsets), _address(dw), _address(dbias),
-                                              _address(workspace), ws_bytes, _stream_address(stream))
-        if status != 0:
-            _ck(status, self._h)
+        self._buffers(_quick_grouped_dw, "alt_gemm_grouped_dw", d, (a, dy, offsets, dw, dbias), workspace, ws_bytes, stream)
 
     def _workspace_size(self, name, d):
         n = ctypes.c_size_t()

@@ -47,26 +47,58 @@ struct GroupedParams {
 enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpMask = 4, kGrpWhole = 8 };   // kGrpWhole: the columns are whole 16-byte chunks of the output, and whole fours
 
 template <typename T> struct GrpTraits;
-template <> struct GrpTraits<bf16_tag> { static constexpr int ES = 2; typedef floatx16_t acc_t; };
-template <> struct GrpTraits<float> { static constexpr int ES = 4; typedef floatx16_t acc_t; };
+// (SUMS: sums per output.  fp32 keeps four, each over every fourth product, added at the end: that halves their rounding error, 5e-7 to 2.5e-7 of the
+// result in the 2-norm at reductions of 1000.)
+template <> struct GrpTraits<bf16_tag> { static constexpr int ES = 2, SUMS = 1; typedef floatx16_t acc_t; };
+template <> struct GrpTraits<float> { static constexpr int ES = 4, SUMS = 4; typedef floatx16_t acc_t; };
 typedef int intx16_t __attribute__((ext_vector_type(16)));
-template <> struct GrpTraits<i8_tag> { static constexpr int ES = 1; typedef intx16_t acc_t; };
+template <> struct GrpTraits<i8_tag> { static constexpr int ES = 1, SUMS = 1; typedef intx16_t acc_t; };
 
-template <typename T>
-__device__ __forceinline__ void grp_mma(typename GrpTraits<T>::acc_t &c, const u32x4_t &first, const u32x4_t &second)
+template <typename T, int SUMS>
+__device__ __forceinline__ void grp_mma(typename GrpTraits<T>::acc_t (&c)[SUMS], const u32x4_t &first, const u32x4_t &second)
 {
     if constexpr (std::is_same<T, bf16_tag>::value) {
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, first), __builtin_bit_cast(bf16x8_t, second), c, 0, 0, 0);
+        c[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, first), __builtin_bit_cast(bf16x8_t, second), c[0], 0, 0, 0);
     } else if constexpr (std::is_same<T, i8_tag>::value) {
         typedef int i32x4v_t __attribute__((ext_vector_type(4)));
-        c = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4v_t, first), __builtin_bit_cast(i32x4v_t, second), c, 0, 0, 0);
+        c[0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4v_t, first), __builtin_bit_cast(i32x4v_t, second), c[0], 0, 0, 0);
     } else {
         // (each instruction takes one float of each lane half, the same of both operands: any order of the reduction will do)
         const f32x4_t f = __builtin_bit_cast(f32x4_t, first), s = __builtin_bit_cast(f32x4_t, second);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(f[j], s[j], c, 0, 0, 0);
+        for (int j = 0; j < 4; ++j) c[j % SUMS] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[j], s[j], c[j % SUMS], 0, 0, 0);
     }
 }
+
+// A wave's sums, TM x TN matrix tiles.
+template <typename T, int TM, int TN, int SUMS = GrpTraits<T>::SUMS>
+struct GrpSums {
+    typename GrpTraits<T>::acc_t c[TM][TN][SUMS];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int s = 0; s < SUMS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) c[i][j][s][e] = 0;
+    }
+    __device__ __forceinline__ void join()                 // into c[i][j][0]
+    {
+#pragma unroll
+        for (int h = SUMS / 2; h > 0; h /= 2)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int s = 0; s < h; ++s)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) c[i][j][s][e] += c[i][j][s + h][e];
+    }
+};
 
 // ---- which tile a workgroup computes ---------------------------------------------------------------------------------------
 
@@ -379,8 +411,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t grp_buffer(const void *base, u
 
 // WHOLE: every chunk of an output row, and every four columns, exist or do not (no path for parts of them).  Rows and columns that do not exist
 // lie outside the buffer descriptors: what is asked for there is zero, and what is stored there is dropped, without a branch.
-template <typename T, int FORM, int TM, int TN, bool BF16, bool WHOLE>
-__device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProblem &g, typename GrpTraits<T>::acc_t (&acc)[TM][TN], char *stage, int wrow, int wcol, int lane)
+template <typename T, int FORM, int TM, int TN, bool BF16, bool WHOLE, int SUMS>
+__device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProblem &g, const GrpSums<T, TM, TN, SUMS> &acc, char *stage, int wrow, int wcol, int lane)
 {
     constexpr int ES = GrpTraits<T>::ES, OS = BF16 ? 2 : 4;
     constexpr int JB = BF16 && TN > 1 ? 2 : 1, CPB = BF16 ? 4 * JB : 8;      // column tiles and 16-byte chunks of a band's rows
@@ -465,7 +497,7 @@ __device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProble
                     f32x4_t f;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        f[q] = (float)acc[i][j + jj][q4 * 4 + q];
+                        f[q] = (float)acc.c[i][j + jj][0][q4 * 4 + q];
                         if constexpr (ES == 1) f[q] = f[q] * sa[i] * scale[j + jj][q4][q];
                         if constexpr (FORM == kForward) f[q] += bias[j + jj][q4][q];
                     }
@@ -511,8 +543,8 @@ __device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProble
     }
 }
 
-template <typename T, int FORM, int TM, int TN>
-__device__ __forceinline__ void grp_epilogue(const GroupedParams &p, const GrpProblem &g, typename GrpTraits<T>::acc_t (&acc)[TM][TN], char *stage, int wrow, int wcol,
+template <typename T, int FORM, int TM, int TN, int SUMS>
+__device__ __forceinline__ void grp_epilogue(const GroupedParams &p, const GrpProblem &g, const GrpSums<T, TM, TN, SUMS> &acc, char *stage, int wrow, int wcol,
                                              int lane)
 {
     const bool bf16 = GrpTraits<T>::ES < 4 && (p.flags & kGrpOutBf16);
@@ -550,16 +582,16 @@ typedef int i32x4s_t __attribute__((ext_vector_type(4)));
 template <> struct GrpFew<i8_tag> { typedef i32x4s_t acc_t; };
 
 template <typename T>
-__device__ __forceinline__ void grp_mma16(typename GrpFew<T>::acc_t &c, const u32x4_t &first, const u32x4_t &second)
+__device__ __forceinline__ void grp_mma16(typename GrpFew<T>::acc_t (&c)[GrpTraits<T>::SUMS], const u32x4_t &first, const u32x4_t &second)
 {
     if constexpr (std::is_same<T, bf16_tag>::value) {
-        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, first), __builtin_bit_cast(bf16x8_t, second), c, 0, 0, 0);
+        c[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, first), __builtin_bit_cast(bf16x8_t, second), c[0], 0, 0, 0);
     } else if constexpr (std::is_same<T, i8_tag>::value) {
-        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4s_t, first), __builtin_bit_cast(i32x4s_t, second), c, 0, 0, 0);
+        c[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4s_t, first), __builtin_bit_cast(i32x4s_t, second), c[0], 0, 0, 0);
     } else {
         const f32x4_t f = __builtin_bit_cast(f32x4_t, first), s = __builtin_bit_cast(f32x4_t, second);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(f[j], s[j], c, 0, 0, 0);
+        for (int j = 0; j < 4; ++j) c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[j], s[j], c[j], 0, 0, 0);
     }
 }
 
@@ -581,11 +613,14 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
 #pragma unroll
     for (int j = 0; j < NT; ++j) bp[j] = g.b0 + (int64_t)min(j * 16 + lane % 16, cols_left - 1) * p.ldb + at;
 
-    typename GrpFew<T>::acc_t acc[MT][NT];
+    constexpr int SUMS = GrpTraits<T>::SUMS;
+    typename GrpFew<T>::acc_t acc[MT][NT][SUMS];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int s = 0; s < SUMS; ++s) acc[i][j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
 
     struct Batch { u32x4_t a[BATCH][2][MT], b[BATCH][2][NT]; };
     const int bytes = g.red * ES, units = bytes / UNIT;    // whole units
@@ -644,7 +679,10 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) part[(wave * MT * NT + i * NT + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[i][j]);
+        for (int j = 0; j < NT; ++j) {
+            if constexpr (SUMS == 4) acc[i][j][0] = (acc[i][j][0] + acc[i][j][1]) + (acc[i][j][2] + acc[i][j][3]);
+            part[(wave * MT * NT + i * NT + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[i][j][0]);
+        }
     __syncthreads();
     // each thread: four columns (lane / 16 of a tile's) of one row (lane % 16)
     const bool owned = g.group < p.groups;
@@ -782,13 +820,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const Group
         for (int i = 0; i < LB::NL; ++i) *(u32x4_t *)(d + A::BYTES + (i * THREADS + t) * 16) = vb[i];
     };
 
-    typename GrpTraits<T>::acc_t acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+    // (two sums for fp32: four take the registers of a third wave, and 1001 rows of 13 groups, 515 x 1030, 34 us forward for 30)
+    GrpSums<T, TM, TN, (ES == 4 ? 2 : 1)> acc;
+    acc.clear();
     float sums[TM];                                        // kWeights: of this lane's row of the left operand
 #pragma unroll
     for (int i = 0; i < TM; ++i) sums[i] = 0.f;
@@ -807,7 +841,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const Group
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) grp_mma<T>(acc[i][j], fb[j], fa[i]);
+                for (int j = 0; j < TN; ++j) grp_mma<T>(acc.c[i][j], fb[j], fa[i]);
             if constexpr (FORM == kWeights) {
                 if (take_sums) {
 #pragma unroll
@@ -836,6 +870,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const Group
         step(s, std::integral_constant<int, 0>{});
         if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{});
     }
+    acc.join();
     __syncthreads();                                       // the last stage's readers are through
     if (take_sums) grp_store_sums(p, g, sums, wm * WTM, lane);
     grp_epilogue<T, FORM, TM, TN>(p, g, acc, lds + wave * kStageBytes, wm * WTM, wn * WTN, lane);
@@ -952,13 +987,8 @@ struct GrpKernel {
 #pragma unroll
         for (int i = 0; i < NB; ++i) b_at[i] = A::BYTES + (B::kRed ? B::frag(wn * WTN, i, lane) : B::frag(wn * WTN + i * 32, 0, lane));
 
-        acc_t acc[TM][TN];
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+        GrpSums<T, TM, TN> acc;
+        acc.clear();
         float sums[TM];                                    // kWeights: of this lane's row of the left operand
 #pragma unroll
         for (int i = 0; i < TM; ++i) sums[i] = 0.f;
@@ -1002,7 +1032,7 @@ struct GrpKernel {
                 for (int i = 0; i < TM; ++i) {
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
-                        grp_mma<T>(acc[i][j], fb[buf][j], fa[buf][i]);
+                        grp_mma<T>(acc.c[i][j], fb[buf][j], fa[buf][i]);
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int q = (i * TN + j) * PER; q < (i * TN + j + 1) * PER; ++q) {
@@ -1019,6 +1049,7 @@ struct GrpKernel {
             close_stage();
             stage = next_stage;
         }
+        acc.join();
         wait_vmcnt<0>();                                   // (the stages behind the last step's)
         __syncthreads();                                   // the last stage's readers are through
         if (take_sums) grp_store_sums(p, g, sums, wm * WTM, lane);
@@ -1303,8 +1334,12 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
     }
     if (!grp_streams<T, FORM>(p)) {
         // Tiles of 128x128 once they fill three quarters of the chip: 1000 x 3884 x 1115 in 8 bits 24.5 us, in tiles of 64x64 31.1; 2048 x 770 x 3073
-        // (112 tiles) 37.4 and 26.8.  In fp32 the matrix cores are the bound, and small tiles leave none idle: 1001 rows of 13 groups, 515 x 1030, 29 against 73 us.
-        return grp_tiles<FORM>(p, 128, 128) >= (ES == 4 ? 4 : 0.75) * places ? grouped_any<T, FORM, 128, 128, 2, 4>(p, st) : grouped_any<T, FORM, 64, 64, 2, 2>(p, st);
+        // (112 tiles) 37.4 and 26.8.  In fp32 the matrix cores are the bound, and small tiles leave none idle: 1001 rows of 13 groups, 515 x 1030, 29
+        // against 73 us, 5000 rows of 5 groups, 2047 x 4095, by the rows 720 against 827.
+        if constexpr (ES < 4) {
+            if (grp_tiles<FORM>(p, 128, 128) >= 0.75 * places) return grouped_any<T, FORM, 128, 128, 2, 4>(p, st);
+        }
+        return grouped_any<T, FORM, 64, 64, 2, 2>(p, st);
     }
     if constexpr (ES == 4) {
         // (as above; 5000 rows of 5 groups, 2048 x 4096: forward 695 us in tiles of 64x64, 762 of 128x128, by the weights 682 and 657)

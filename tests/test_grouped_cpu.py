@@ -101,3 +101,47 @@ def test_calls_without_a_gpu_fail_loudly(h):
         assert refused(lambda: getattr(h, name)(d, stream=0, **CALLS[name])) == 6
     assert refused(lambda: h.quantize_rows(alt.BF16, 4, 64, 4096, 8192, 16384, stream=0)) == 6
     assert refused(lambda: h.gemm_i8(alt.gemm_i8_desc(4, 32, 64), 4096, 4096, 4096, 4096, 4096, stream=0)) == 6
+
+
+class Tensor:
+    def __init__(self, at):
+        self.at = at
+
+    def data_ptr(self):
+        return self.at
+
+
+@pytest.mark.parametrize("name", ["quantize_rows", "gemm_i8"] + sorted(CALLS))
+def test_native_and_ctypes_calls_agree(h, name, monkeypatch):
+    """Every argument that the native marshalling takes, and some that it leaves to ctypes, end alike (here, without a GPU, in the library's status)."""
+    import os
+
+    import numpy as np
+
+    from paper_2210_12415_amd import binding
+    if binding._native is None or os.path.exists("/dev/kfd"):
+        pytest.skip("needs the native module, and no GPU: the addresses are of no buffer")
+    quick = {"quantize_rows": "_quick_quantize", "gemm_i8": "_quick_gemm_i8"}.get(name, name.replace("gemm", "_quick"))
+    if name == "quantize_rows":
+        base = dict(dtype=alt.BF16, rows=4, cols=64, x=4096, q=8192, scale=16384, stream=0)
+        forms = [dict(rows=np.int64(4)), dict(rows=4.0), dict(rows=-1), dict(dtype=np.int32(1)), dict(dtype="1"), dict(x=Tensor(4096)), dict(x=None), dict(q="text"), dict(x_stride=1 << 63)]
+    else:
+        d = alt.gemm_i8_desc(4, 32, 64) if name == "gemm_i8" else alt.grouped_desc(4, 2, 32, 64, epilogue=EPILOGUE[name])
+        base = dict(dict(a=4096, a_scale=4096, b=4096, b_scale=4096, y=4096) if name == "gemm_i8" else CALLS[name], d=d, stream=0)
+        first = next(k for k in base)
+        forms = [dict(d=None), {first: Tensor(4096)}, {first: None}, {first: "text"}, {first: np.int64(4096)}, dict(workspace=Tensor(4096), ws_bytes=64),
+                 dict(ws_bytes=np.int64(8)), dict(ws_bytes=None), dict(stream="text")]
+
+    def outcome(kw):
+        try:
+            return getattr(h, name)(**kw)
+        except Exception as e:
+            return type(e), str(e)
+    native, taken = getattr(binding, quick), []
+    for form in [{}] + forms:
+        kw = dict(base, **form)
+        monkeypatch.setattr(binding, quick, lambda *a: taken.append(native(*a)) or taken[-1])
+        one = outcome(kw)
+        monkeypatch.setattr(binding, quick, binding._not_taken)
+        assert one == outcome(kw), form
+    assert any(t is not None for t in taken) and any(t is None for t in taken)
