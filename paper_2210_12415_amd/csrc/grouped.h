@@ -311,6 +311,8 @@ __device__ __forceinline__ bool grp_positive(uint32_t bits)
     return f - 1u < 0x7f800000u;
 }
 
+__device__ __forceinline__ float grp_relu(float v) { return __builtin_elementwise_maximum(v, 0.f); }      // (keeps NaN)
+
 // W (4 or 8) consecutive columns of one output row: ReLU, rounding.
 template <int W>
 __device__ __forceinline__ void grp_store(const GroupedParams &p, char *y_row, int col, float (&v)[W])
@@ -318,7 +320,7 @@ __device__ __forceinline__ void grp_store(const GroupedParams &p, char *y_row, i
     const int count = p.cols - col;
     if (p.flags & kGrpRelu) {
 #pragma unroll
-        for (int q = 0; q < W; ++q) v[q] = v[q] < 0.f ? 0.f : v[q];           // (keeps NaN)
+        for (int q = 0; q < W; ++q) v[q] = grp_relu(v[q]);
     }
     if (p.flags & kGrpOutBf16) {
         uint32_t w[W / 2];
@@ -498,12 +500,12 @@ __device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProble
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         f[q] = (float)acc.c[i][j + jj][0][q4 * 4 + q];
-                        if constexpr (ES == 1) f[q] = f[q] * sa[i] * scale[j + jj][q4][q];
-                        if constexpr (FORM == kForward) f[q] += bias[j + jj][q4][q];
+                        if constexpr (ES == 1) f[q] = __builtin_fmaf(f[q] * sa[i], scale[j + jj][q4][q], bias[j + jj][q4][q]);
+                        else if constexpr (FORM == kForward) f[q] += bias[j + jj][q4][q];
                     }
                     if (relu) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) f[q] = f[q] < 0.f ? 0.f : f[q];                            // (keeps NaN)
+                        for (int q = 0; q < 4; ++q) f[q] = grp_relu(f[q]);
                     }
                     if constexpr (BF16) {
                         const u32x2_t w = {f32x2_to_bf16x2(f.x, f.y), f32x2_to_bf16x2(f.z, f.w)};
@@ -548,7 +550,7 @@ __device__ __forceinline__ void grp_epilogue(const GroupedParams &p, const GrpPr
                                              int lane)
 {
     const bool bf16 = GrpTraits<T>::ES < 4 && (p.flags & kGrpOutBf16);
-    if (p.flags & kGrpWhole) {
+    if ((p.flags & kGrpWhole) || g.col0 + wcol + TN * 32 <= p.cols) {
         if (bf16) grp_emit<T, FORM, TM, TN, (GrpTraits<T>::ES < 4), true>(p, g, acc, stage, wrow, wcol, lane);
         else grp_emit<T, FORM, TM, TN, false, true>(p, g, acc, stage, wrow, wcol, lane);
     } else {
@@ -571,10 +573,10 @@ __device__ __forceinline__ void grp_store_sums(const GroupedParams &p, const Grp
 
 // ---- the kernel for few rows per group: the weights stream through registers, once ---------------------------------------------
 //
-// Bound by the weights' bytes.  A tile is 16 * MT rows by 16 * NT columns; the NW waves of a workgroup share its reduction, wave w taking units
+// Bound by the weights' bytes.  A tile is 16 rows by 16 * NT columns; the NW waves of a workgroup share its reduction, wave w taking units
 // of 128 bytes w, w + NW, ... of every row, so that each line is read whole by one wave and the workgroup walks along the rows.  Fragments of the
-// 16-row matrix instructions are 16 bytes of a row per lane (row lane % 16, quarter lane / 16 of 64 bytes) and come straight from memory at any
-// alignment; two batches of loads are in flight per wave.  The waves' sums meet in LDS and are added in the waves' order.
+// 16-row matrix instructions are 16 bytes of a row per lane; a lane takes both halves of 32 bytes (row lane % 16, quarter lane / 16 of the unit: both
+// operands in the same order, so any order will do), straight from memory at any alignment; two batches of loads are in flight per wave.  The waves' sums meet in LDS and are added in the waves' order.
 template <typename T> struct GrpFew;
 template <> struct GrpFew<bf16_tag> { typedef f32x4_t acc_t; };
 template <> struct GrpFew<float> { typedef f32x4_t acc_t; };
@@ -595,46 +597,64 @@ __device__ __forceinline__ void grp_mma16(typename GrpFew<T>::acc_t (&c)[GrpTrai
     }
 }
 
-template <typename T, int MT, int NT, int NW, int BATCH>
+// 32 bytes at p.  Memory takes more than twice as long over addresses inside a dword (16 x 6005 x 8192 in 8 bits 27.4 us, 14.3 at whole dwords), so
+// where there are such (!DW) they are the eight dwords they start in and, if they start inside one, the dword they end in, shifted together.
+template <bool DW>
+struct GrpPair {
+    u32x4_t lo, hi;
+    uint32_t more;
+    __device__ __forceinline__ void load(const char *p)
+    {
+        const char *first = DW ? p : (const char *)((uintptr_t)p & ~(uintptr_t)3);
+        __builtin_memcpy(&lo, __builtin_assume_aligned(first, 4), 16);
+        __builtin_memcpy(&hi, __builtin_assume_aligned(first + 16, 4), 16);
+        if constexpr (!DW) more = *(const uint32_t *)(first + ((uintptr_t)p & 3 ? 32 : 28));
+    }
+    __device__ __forceinline__ u32x4_t chunk(int h, uint32_t address) const
+    {
+        const u32x4_t &v = h ? hi : lo;
+        if constexpr (DW) {
+            return v;
+        } else {
+            const uint32_t next = h ? more : hi.x;
+            return (u32x4_t){__builtin_amdgcn_alignbyte(v.y, v.x, address), __builtin_amdgcn_alignbyte(v.z, v.y, address),
+                             __builtin_amdgcn_alignbyte(v.w, v.z, address), __builtin_amdgcn_alignbyte(next, v.w, address)};
+        }
+    }
+};
+
+template <typename T, int NT, int NW, int BATCH, bool DW>
 __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParams p)
 {
     constexpr int ES = GrpTraits<T>::ES, UNIT = 128;
-    __shared__ u32x4_t part[NW * MT * NT * 64];
+    __shared__ u32x4_t part[NW * NT * 64];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     GrpProblem g;
-    if (!grp_problem<T, kForward, 16 * MT, 16 * NT>(p, lane, g)) return;
+    if (!grp_problem<T, kForward, 16, 16 * NT>(p, lane, g)) return;
     const int rows_left = g.row_end - g.row0, cols_left = p.cols - g.col0;
 
     // (rows and columns outside the tile's repeat its last one: their sums are never stored)
-    const char *ap[MT], *bp[NT];
-    const int at = lane / 16 * 16;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) ap[i] = g.a0 + (int64_t)min(i * 16 + lane % 16, rows_left - 1) * p.lda + at;
+    const int at = lane / 16 * 32;
+    const char *ap = g.a0 + (int64_t)min(lane % 16, rows_left - 1) * p.lda + at, *bp[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) bp[j] = g.b0 + (int64_t)min(j * 16 + lane % 16, cols_left - 1) * p.ldb + at;
 
     constexpr int SUMS = GrpTraits<T>::SUMS;
-    typename GrpFew<T>::acc_t acc[MT][NT][SUMS];
+    typename GrpFew<T>::acc_t acc[NT][SUMS];
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int s = 0; s < SUMS; ++s) acc[i][j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+        for (int s = 0; s < SUMS; ++s) acc[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
 
-    struct Batch { u32x4_t a[BATCH][2][MT], b[BATCH][2][NT]; };
+    struct Batch { GrpPair<DW> a[BATCH], b[BATCH][NT]; };
     const int bytes = g.red * ES, units = bytes / UNIT;    // whole units
     auto load = [&](Batch &f, int u) {                     // units u, u + NW, ... (past the last one the first again, which mma leaves out)
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
             const int64_t off = (int64_t)(u + q * NW < units ? u + q * NW : 0) * UNIT;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int j = 0; j < NT; ++j) __builtin_memcpy(&f.b[q][h][j], bp[j] + off + h * 64, 16);
-#pragma unroll
-                for (int i = 0; i < MT; ++i) __builtin_memcpy(&f.a[q][h][i], ap[i] + off + h * 64, 16);
-            }
+            for (int j = 0; j < NT; ++j) f.b[q][j].load(bp[j] + off);
+            f.a[q].load(ap + off);
         }
     };
     auto mma = [&](const Batch &f, int u) {
@@ -642,11 +662,11 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
         for (int q = 0; q < BATCH; ++q) {
             if (u + q * NW >= units) break;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+                const u32x4_t a = f.a[q].chunk(h, (uint32_t)(uintptr_t)ap);
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[i][j], f.b[q][h][j], f.a[q][h][i]);
+                for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[j], f.b[q][j].chunk(h, (uint32_t)(uintptr_t)bp[j]), a);
+            }
         }
     };
     constexpr int STEP = NW * BATCH;
@@ -664,34 +684,25 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
     if (bytes % UNIT && wave == units % NW) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int k = units * UNIT + h * 64, count = (bytes - k - at) / ES;
-            u32x4_t a[MT], b[NT];
+            const int k = units * UNIT + h * 16, count = (bytes - k - at) / ES;
+            const u32x4_t a = grp_load_chunk<ES>(ap + k, count);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) a[i] = grp_load_chunk<ES>(ap[i] + k, count);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) b[j] = grp_load_chunk<ES>(bp[j] + k, count);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[i][j], b[j], a[i]);
+            for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[j], grp_load_chunk<ES>(bp[j] + k, count), a);
         }
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            if constexpr (SUMS == 4) acc[i][j][0] = (acc[i][j][0] + acc[i][j][1]) + (acc[i][j][2] + acc[i][j][3]);
-            part[(wave * MT * NT + i * NT + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[i][j][0]);
-        }
+    for (int j = 0; j < NT; ++j) {
+        if constexpr (SUMS == 4) acc[j][0] = (acc[j][0] + acc[j][1]) + (acc[j][2] + acc[j][3]);
+        part[(wave * NT + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[j][0]);
+    }
     __syncthreads();
     // each thread: four columns (lane / 16 of a tile's) of one row (lane % 16)
     const bool owned = g.group < p.groups;
-    for (int s = t; s < MT * NT * 64; s += NW * 64) {
+    for (int s = t; s < NT * 64; s += NW * 64) {
         typename GrpFew<T>::acc_t sum = __builtin_bit_cast(typename GrpFew<T>::acc_t, part[s]);
 #pragma unroll
-        for (int w = 1; w < NW; ++w) sum += __builtin_bit_cast(typename GrpFew<T>::acc_t, part[w * MT * NT * 64 + s]);
-        const int tile = s / 64, l = s % 64;
-        const int row = g.row0 + tile / NT * 16 + l % 16, col = g.col0 + tile % NT * 16 + l / 16 * 4;
+        for (int w = 1; w < NW; ++w) sum += __builtin_bit_cast(typename GrpFew<T>::acc_t, part[w * NT * 64 + s]);
+        const int tile = s / 64, l = s % 64, row = g.row0 + l % 16, col = g.col0 + tile * 16 + l / 16 * 4;
         if (row >= g.row_end || col >= p.cols) continue;
         float v[4], scale[4] = {1.f, 1.f, 1.f, 1.f}, bias[4] = {0.f, 0.f, 0.f, 0.f}, sa = 1.f;
         if (owned) {
@@ -705,8 +716,8 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             v[q] = (float)sum[q];
-            if constexpr (ES == 1) v[q] = v[q] * sa * scale[q];
-            v[q] += bias[q];
+            if constexpr (ES == 1) v[q] = __builtin_fmaf(v[q] * sa, scale[q], bias[q]);
+            else v[q] += bias[q];
         }
         grp_store<4>(p, g.y + (int64_t)row * p.ldy, col, v);
     }
@@ -759,15 +770,12 @@ struct GrpLoader {
         } else if (RED && left >= Op::EPC) {
             // (a chunk that ends behind the row is loaded to end with it, and shifted)
 #pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                const int over = elem[i] + Op::EPC - left;                     // elements behind the end
-                __builtin_memcpy(&v[i], base + voff[i] - (uint32_t)(max(over, 0) * ES), 16);
-            }
+            for (int i = 0; i < NL; ++i) __builtin_memcpy(&v[i], base + voff[i] - (uint32_t)(max(elem[i] + Op::EPC - left, 0) * ES), 16);
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                const int over = min(max(elem[i] + Op::EPC - left, 0), Op::EPC) * ES;
+                const int over = max(elem[i] + Op::EPC - left, 0);             // elements behind the end
                 unsigned __int128 w = __builtin_bit_cast(unsigned __int128, v[i]);
-                w = over >= 16 ? 0 : w >> (over * 8);
+                w = over >= Op::EPC ? 0 : w >> (over * ES * 8);
                 v[i] = __builtin_bit_cast(u32x4_t, w);
             }
         } else {
@@ -1241,13 +1249,19 @@ hipError_t grouped_any(GroupedParams p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <typename T, int MT, int NT, int NW, int BATCH>
+template <typename T, int NT, int NW, int BATCH>
 hipError_t grouped_few(GroupedParams p, hipStream_t st)
 {
     unsigned grid;
-    const hipError_t e = grp_grid<kForward, 16 * MT, 16 * NT>(p, 64 * NW, &grid);
+    const hipError_t e = grp_grid<kForward, 16, 16 * NT>(p, 64 * NW, &grid);
     if (e != hipSuccess || !grid) return e;
-    hipLaunchKernelGGL((grouped_few_kernel<T, MT, NT, NW, BATCH>), dim3(grid), dim3(64 * NW), 0, st, p);
+    if constexpr (GrpTraits<T>::ES < 4) {
+        if (((uint64_t)p.a | (uint64_t)p.b | (uint64_t)p.lda | (uint64_t)p.ldb | (uint64_t)p.b_group) % 4) {
+            hipLaunchKernelGGL((grouped_few_kernel<T, NT, NW, BATCH, false>), dim3(grid), dim3(64 * NW), 0, st, p);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((grouped_few_kernel<T, NT, NW, BATCH, true>), dim3(grid), dim3(64 * NW), 0, st, p);
     return hipGetLastError();
 }
 
@@ -1330,7 +1344,7 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
         // to a reduction: 16 x 4096 x 4096 6.6 against 8.5 us, 32 x 4096 x 4096 10.4 against 8.6.
         const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows;
         if (p.rows <= 32 * spans)
-            return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 1, 8, 2>(p, st) : grouped_few<T, 1, 2, 4, 2>(p, st);
+            return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 8, 2>(p, st) : grouped_few<T, 2, 4, 2>(p, st);
     }
     if (!grp_streams<T, FORM>(p)) {
         // Tiles of 128x128 once they fill three quarters of the chip: 1000 x 3884 x 1115 in 8 bits 24.5 us, in tiles of 64x64 31.1; 2048 x 770 x 3073

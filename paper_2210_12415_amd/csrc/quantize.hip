@@ -97,10 +97,9 @@ __device__ __forceinline__ void store_chunk(char *q, const Chunk<ELSZ> &c, const
 }
 
 constexpr int kQuantThreads = 256;
-constexpr int kQuantKeep = 4;              // chunks that a thread keeps
 
-// TPR threads (a wave or the workgroup) per row.
-template <int ELSZ, int TPR>
+// TPR threads (a wave or the workgroup) per row, each of which keeps KEEP chunks.
+template <int ELSZ, int TPR, int KEEP>
 __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const char *x, int64_t ldx, char *q, int64_t ldq, float *scale, int64_t rows, int cols)
 {
     __shared__ uint32_t part[kQuantThreads / 64];
@@ -110,18 +109,18 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const char
     x += row * ldx;
     q += row * ldq;
     const int chunks = cols / 8, rest = cols % 8;
-    Chunk<ELSZ> keep[kQuantKeep];
+    Chunk<ELSZ> keep[KEEP];
     uint32_t top = 0;
     float last = 0.f;                                      // of the elements behind the last whole chunk, one per thread
     if (t < rest) last = element<ELSZ>(x + (int64_t)(chunks * 8 + t) * ELSZ);
     // (a thread without a chunk of its own takes the row's first again: it changes no maximum, and no load waits for a branch)
 #pragma unroll
-    for (int i = 0; i < kQuantKeep; ++i)
+    for (int i = 0; i < KEEP; ++i)
         if (i * TPR < chunks) keep[i] = load_chunk<ELSZ>(x + (int64_t)(i * TPR + t < chunks ? i * TPR + t : 0) * (8 * ELSZ));
 #pragma unroll
-    for (int i = 0; i < kQuantKeep; ++i)
+    for (int i = 0; i < KEEP; ++i)
         if (i * TPR < chunks) top = top_of<ELSZ>(top, keep[i]);
-    for (int c = kQuantKeep * TPR + t; c < chunks; c += TPR) top = top_of<ELSZ>(top, load_chunk<ELSZ>(x + (int64_t)c * (8 * ELSZ)));
+    for (int c = KEEP * TPR + t; c < chunks; c += TPR) top = top_of<ELSZ>(top, load_chunk<ELSZ>(x + (int64_t)c * (8 * ELSZ)));
     top = wave_max(max(top, magnitude(last)));
     if constexpr (TPR > 64) {
         if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
@@ -138,21 +137,29 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const char
     k.below = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, k.half) - 1u);
     if (t == 0) scale[row] = finite ? k.s : __builtin_nanf("");
 #pragma unroll
-    for (int i = 0; i < kQuantKeep; ++i)
+    for (int i = 0; i < KEEP; ++i)
         if (i * TPR + t < chunks) store_chunk<ELSZ>(q + (int64_t)(i * TPR + t) * 8, keep[i], k, finite);
-    for (int c = kQuantKeep * TPR + t; c < chunks; c += TPR) store_chunk<ELSZ>(q + (int64_t)c * 8, load_chunk<ELSZ>(x + (int64_t)c * (8 * ELSZ)), k, finite);
+    for (int c = KEEP * TPR + t; c < chunks; c += TPR) store_chunk<ELSZ>(q + (int64_t)c * 8, load_chunk<ELSZ>(x + (int64_t)c * (8 * ELSZ)), k, finite);
     if (t < rest) q[chunks * 8 + t] = (char)((quantize1(last, k, 0, 0) ^ 0x80u) & finite);
 }
 
-template <int ELSZ>
+template <int ELSZ, int TPR, int KEEP>
 void quantize_launch(const void *x, int64_t ldx, void *q, int64_t ldq, float *scale, int64_t rows, int cols, hipStream_t st)
 {
-    if (cols <= 64 * 8 * kQuantKeep)
-        hipLaunchKernelGGL((quantize_rows_kernel<ELSZ, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(kQuantThreads), 0, st, (const char *)x, ldx * ELSZ, (char *)q,
-                           ldq, scale, rows, cols);
-    else
-        hipLaunchKernelGGL((quantize_rows_kernel<ELSZ, 256>), dim3((unsigned)rows), dim3(kQuantThreads), 0, st, (const char *)x, ldx * ELSZ, (char *)q, ldq, scale,
-                           rows, cols);
+    constexpr int64_t RPW = kQuantThreads / TPR;
+    hipLaunchKernelGGL((quantize_rows_kernel<ELSZ, TPR, KEEP>), dim3((unsigned)((rows + RPW - 1) / RPW)), dim3(kQuantThreads), 0, st, (const char *)x, ldx * ELSZ, (char *)q,
+                       ldq, scale, rows, cols);
+}
+
+template <int ELSZ>
+void quantize_run(const void *x, int64_t ldx, void *q, int64_t ldq, float *scale, int64_t rows, int cols, hipStream_t st)
+{
+    // A wave for each of many short rows (16384 x 1000 10.9 us, 16.4 with a workgroup each), a workgroup for the others (1 x 4096 2.6 us, 5.2 with a
+    // wave; 16384 x 4096 31.8 us, 6.3 TB/s, and 43.1), which keeps as many chunks as it needs up to 8192 columns (4096 x 8192 19.1 us with four
+    // to a thread, 22.2 with two, the rest read again; 16384 x 4096 31.8 with two, 33.4 with four).
+    if (cols <= 1024 && rows >= 512) quantize_launch<ELSZ, 64, 2>(x, ldx, q, ldq, scale, rows, cols, st);
+    else if (cols <= 4096) quantize_launch<ELSZ, 256, 2>(x, ldx, q, ldq, scale, rows, cols, st);
+    else quantize_launch<ELSZ, 256, 4>(x, ldx, q, ldq, scale, rows, cols, st);
 }
 
 }  // namespace
@@ -174,8 +181,8 @@ extern "C" alt_status_t alt_quantize_rows(alt_handle_t h, alt_dtype_t dtype, int
     if (!x || !q || !scale) return fail(h, ALT_INVALID_ARG, "alt_quantize_rows: null buffer");
     if ((uintptr_t)x % dtype_size(dtype) || (uintptr_t)scale % 4) return fail(h, ALT_INVALID_ARG, "alt_quantize_rows: a buffer is not aligned to its elements");
     if (!h->has_gpu) return fail(h, ALT_HIP_ERROR, "no GPU device available");
-    if (dtype == ALT_F32) quantize_launch<4>(x, ldx, q, ldq, scale, rows, (int)cols, (hipStream_t)stream);
-    else quantize_launch<2>(x, ldx, q, ldq, scale, rows, (int)cols, (hipStream_t)stream);
+    if (dtype == ALT_F32) quantize_run<4>(x, ldx, q, ldq, scale, rows, (int)cols, (hipStream_t)stream);
+    else quantize_run<2>(x, ldx, q, ldq, scale, rows, (int)cols, (hipStream_t)stream);
     ALT_CHECK_HIP(h, hipGetLastError());
     return ALT_OK;
 }
