@@ -555,7 +555,8 @@ alt_status_t alt_gemm_grouped_dx(alt_handle_t h, const alt_grouped_desc_t *d, co
 alt_status_t alt_gemm_grouped_dw(alt_handle_t h, const alt_grouped_desc_t *d, const void *a, const void *dy, const int32_t *offsets,
                                  void *dw, float *dbias, void *workspace, size_t ws_bytes, void *stream);
 
-/* Bytes of workspace each call would like (NULL / 0 always works; the sums of a long reduction cut into slices go there). */
+/* Bytes of workspace each call would like (NULL / 0 always works).  Operands whose rows are not whole 16-byte chunks (K, N or a stride) are laid out
+ * anew there, in that call, where the product is large enough to pay for it. */
 alt_status_t alt_gemm_grouped_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);
 alt_status_t alt_gemm_grouped_dx_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);
 alt_status_t alt_gemm_grouped_dw_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);

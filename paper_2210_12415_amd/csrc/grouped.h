@@ -44,7 +44,8 @@ struct GroupedParams {
     FastDiv d_panel;           // of kPanel * tiles_n
     int32_t flags;
 };
-enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpMask = 4, kGrpWhole = 8 };   // kGrpWhole: the columns are whole 16-byte chunks of the output, and whole fours
+enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpMask = 4, kGrpWhole = 8, kGrpPacked = 16 };
+// (kGrpWhole: the columns are whole 16-byte chunks of the output, and whole fours; kGrpPacked: operand rows are filled up with zeros to whole chunks)
 
 template <typename T> struct GrpTraits;
 // (SUMS: sums per output.  fp32 keeps four, each over every fourth product, added at the end: that halves their rounding error, 5e-7 to 2.5e-7 of the
@@ -260,11 +261,12 @@ __device__ __forceinline__ u32x4_t grp_load_chunk(const char *p, int count)
         uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 16 / ES; ++i) {
-            if (i >= count) break;
-            uint32_t e;
-            if constexpr (ES == 4) e = *(const uint32_t *)(p + i * 4);
-            else if constexpr (ES == 2) e = *(const uint16_t *)(p + i * 2);
-            else e = *(const uint8_t *)(p + i);
+            uint32_t e = 0;
+            if (i < count) {
+                if constexpr (ES == 4) e = *(const uint32_t *)(p + i * 4);
+                else if constexpr (ES == 2) e = *(const uint16_t *)(p + i * 2);
+                else e = *(const uint8_t *)(p + i);
+            }
             w[i * ES / 4] |= e << (i * ES % 4 * 8);
         }
         v = (u32x4_t){w[0], w[1], w[2], w[3]};
@@ -905,7 +907,7 @@ struct GrpStream {
         const uint64_t at = (uint64_t)p0;
         base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
         ld = (int)ld_;
-        left = __builtin_amdgcn_readfirstlane(RED ? red * ES : red);
+        left = __builtin_amdgcn_readfirstlane(RED ? (red * ES + 15) & ~15 : red);       // (rows are whole chunks)
         tail = __builtin_amdgcn_readfirstlane((min(max(outer_left, 1), OUTER) - 1) * ld);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
@@ -1272,7 +1274,7 @@ bool grp_streams(const GroupedParams &p)
     constexpr int ES = GrpTraits<T>::ES;
     const uint64_t bits = (uint64_t)p.a | (uint64_t)p.b | (uint64_t)p.lda | (uint64_t)p.ldb | (uint64_t)p.b_group |
                           (FORM != kWeights ? (uint64_t)p.red * ES : (uint64_t)p.rows * ES) | (FORM == kForward ? 0 : (uint64_t)p.cols * ES);
-    return bits % 16 == 0 && p.lda <= (1 << 22) && p.ldb <= (1 << 22) && p.ldy <= (1 << 22) && p.ldmask <= (1 << 22);
+    return (bits % 16 == 0 || (p.flags & kGrpPacked)) && p.lda <= (1 << 22) && p.ldb <= (1 << 22) && p.ldy <= (1 << 22) && p.ldmask <= (1 << 22);
 }
 
 template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB, int NS>
@@ -1327,10 +1329,36 @@ inline double grp_tiles(const GroupedParams &p, int BM, int BN)
 
 // Time of a launch in us without what every launch costs: rounds of the chip's `places`, each a fixed part and a part for every 128 bytes of the
 // reduction; a round that leaves places idle runs faster, the others having more of the caches and the clock to themselves.
-inline double grp_rounds(double tiles, double places, double units, double fixed, double per_unit)
+struct GrpTime { double fixed, reduction; };
+inline GrpTime grp_rounds(double tiles, double places, double units, double fixed, double per_unit)
 {
     const double rounds = std::ceil(tiles / places);
-    return rounds * (fixed + per_unit * units * (0.5 + 0.5 * tiles / (rounds * places)));
+    return {rounds * fixed, rounds * per_unit * units * (0.5 + 0.5 * tiles / (rounds * places))};
+}
+
+// Up to 32 rows each, the weights are what there is to read: 16 x 8192 x 8192 in 8 bits 14.8 us so, 39 us in tiles of 64 rows; at 33 to 64 rows
+// 64 x 4096 x 4096 takes 10.6 us so, 9.6 in tiles.
+inline bool grp_is_few(const GroupedParams &p)
+{
+    const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows;
+    return p.rows <= 32 * spans;
+}
+
+// Tiles of 64x64 with a deep ring (one to a compute unit) or a shallow one (two), of 128x128, of 256x256, for operands of 8 or 16 bits; the constants
+// are those of 8-bit products of 32 .. 8192 rows, 768 .. 8192 columns and reductions of 512 .. 8192, which they give to 10 %; bf16 has the same
+// tiles in bytes.
+enum { kDeep, kShallow, kMiddle, kLarge };
+template <int FORM>
+inline int grp_choose(const GroupedParams &p, int ES, GrpTime *time)
+{
+    const double places = p.places, units = std::ceil((double)p.red * ES / 128.0 / (FORM == kWeights ? p.groups : 1)), n64 = grp_tiles<FORM>(p, 64, 64);
+    const GrpTime t[4] = {n64 <= places ? GrpTime{2.0, 0.21 * units} : GrpTime{1e30, 0.0}, grp_rounds(n64, 2 * places, units, 3.0, 0.43),
+                          grp_rounds(grp_tiles<FORM>(p, 128, 128), places, units, 3.3, 0.54), grp_rounds(grp_tiles<FORM>(p, 256, 256), places, units, 8.0, 1.73)};
+    int best = 0;
+    for (int i = 1; i < 4; ++i)
+        if (t[i].fixed + t[i].reduction < t[best].fixed + t[best].reduction) best = i;
+    *time = t[best];
+    return best;
 }
 
 template <typename T, int FORM>
@@ -1339,12 +1367,9 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
     constexpr int ES = GrpTraits<T>::ES;
     const double places = p.places;
     if constexpr (FORM == kForward) {
-        // Up to 32 rows each, the weights are what there is to read: 16 x 8192 x 8192 in 8 bits 14.8 us so, 39 us in tiles of 64 rows; at 33 to 64 rows
-        // 64 x 4096 x 4096 takes 10.6 us so, 9.6 in tiles.  Columns in twos (four waves) where that fills the chip, else one by one and eight waves
-        // to a reduction: 16 x 4096 x 4096 6.6 against 8.5 us, 32 x 4096 x 4096 10.4 against 8.6.
-        const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows;
-        if (p.rows <= 32 * spans)
-            return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 8, 2>(p, st) : grouped_few<T, 2, 4, 2>(p, st);
+        // (columns in twos, four waves, where that fills the chip, else one by one and eight waves to a reduction: 16 x 4096 x 4096 6.6 against 8.5 us,
+        // 32 x 4096 x 4096 10.4 against 8.6)
+        if (grp_is_few(p)) return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 8, 2>(p, st) : grouped_few<T, 2, 4, 2>(p, st);
     }
     if (!grp_streams<T, FORM>(p)) {
         // Tiles of 128x128 once they fill three quarters of the chip: 1000 x 3884 x 1115 in 8 bits 24.5 us, in tiles of 64x64 31.1; 2048 x 770 x 3073
@@ -1360,18 +1385,12 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
         return FORM == kWeights && grp_tiles<FORM>(p, 128, 128) >= 4 * places ? grouped_tiles<T, FORM, 128, 128, 2, 4, 128, 4>(p, st)
                                                                                : grouped_tiles<T, FORM, 64, 64, 2, 2, 128, 4>(p, st);
     } else {
-        // Tiles of 64x64 with a deep ring (one to a compute unit) or a shallow one (two), of 128x128, of 256x256; the constants are those of 8-bit
-        // products of 32 .. 8192 rows, 768 .. 8192 columns and reductions of 512 .. 8192, which they give to 10 %; bf16 has the same tiles in bytes.
-        const double units = FORM == kWeights ? std::ceil((double)p.red * ES / 128.0 / p.groups) : std::ceil(p.red * ES / 128.0);
-        const double n64 = grp_tiles<FORM>(p, 64, 64);
-        const double deep = n64 <= places ? 2.0 + 0.21 * units : 1e30;
-        const double small = grp_rounds(n64, 2 * places, units, 3.0, 0.43);
-        const double middle = grp_rounds(grp_tiles<FORM>(p, 128, 128), places, units, 3.3, 0.54);
-        const double large = grp_rounds(grp_tiles<FORM>(p, 256, 256), places, units, 8.0, 1.73);
-        const double best = std::min(std::min(deep, small), std::min(middle, large));
-        if (best == deep) return grouped_tiles<T, FORM, 64, 64, 2, 2, 256, 4>(p, st);
-        if (best == small) return grouped_tiles<T, FORM, 64, 64, 2, 2, 128, 4>(p, st);
-        if (best == middle) return grouped_tiles<T, FORM, 128, 128, 2, 4, 128, 4>(p, st);
+        GrpTime time;
+        switch (grp_choose<FORM>(p, ES, &time)) {
+            case kDeep: return grouped_tiles<T, FORM, 64, 64, 2, 2, 256, 4>(p, st);
+            case kShallow: return grouped_tiles<T, FORM, 64, 64, 2, 2, 128, 4>(p, st);
+            case kMiddle: return grouped_tiles<T, FORM, 128, 128, 2, 4, 128, 4>(p, st);
+        }
         if constexpr (FORM == kWeights) return grouped_tiles<T, FORM, 256, 256, 2, 4, 64, 4>(p, st);
         else return grouped_large<T, FORM>(p, st);
     }

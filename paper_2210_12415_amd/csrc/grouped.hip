@@ -47,43 +47,161 @@ alt_status_t check_buffers(alt_handle_t h, const char *call, std::initializer_li
 
 size_t in_size(int dt) { return dt == ALT_I8 ? 1 : dtype_size(dt); }
 
-alt_status_t run(alt_handle_t h, const char *call, int dtype, int form, GroupedParams &p, int64_t ldy_elems, hipStream_t st)
+// ---- operands whose rows are not whole 16-byte chunks, laid out anew -------------------------------------------------------------
+
+// dst[r] = src[r] filled up with zeros to `dst_bytes` a row (a multiple of 16).  A thread moves 32 bytes: the eight dwords they start in and the one
+// they end in, shifted together.  Bound by memory: 33 MB of 4099-byte rows in 15 us.
+__global__ __launch_bounds__(256) void grp_pack_kernel(const char *src, int64_t src_ld, int bytes, char *dst, int dst_bytes, uint32_t pieces, FastDiv per_row, uint32_t row0)
 {
-    const size_t os = p.flags & kGrpOutBf16 ? 2 : 4;
-    p.ldy = ldy_elems * (int64_t)os;
-    p.y_group *= (int64_t)os;
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+    if (i >= pieces) return;
+    const uint32_t r = fast_div(i, per_row), at = (i - r * per_row.d) * 32u;
+    const char *p = src + (int64_t)(row0 + r) * src_ld + at;
+    char *d = dst + (int64_t)(row0 + r) * dst_bytes + at;
+    const int exist = bytes - (int)at;
+    u32x4_t v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (exist >= 32) {
+        GrpPair<false> w;
+        w.load(p);
+        v[0] = w.chunk(0, (uint32_t)(uintptr_t)p);
+        v[1] = w.chunk(1, (uint32_t)(uintptr_t)p);
+    } else {
+        v[0] = grp_load_chunk<1>(p, exist);
+        v[1] = grp_load_chunk<1>(p + 16, exist - 16);
+    }
+    *(u32x4_t *)d = v[0];
+    if ((int)at + 16 < dst_bytes) *(u32x4_t *)(d + 16) = v[1];
+}
+
+struct Matrix {
+    const void **p;                        // where the problem keeps it
+    int64_t *ld;
+    int64_t rows, bytes;                   // rows, and bytes of each that exist
+    int64_t packed() const { return (bytes + 15) / 16 * 16; }
+    int64_t size() const { return rows * packed(); }
+    bool whole() const { return ((uint64_t)*p | (uint64_t)*ld | (uint64_t)bytes) % 16 == 0; }
+};
+
+// The operands as matrices of `form`.
+void matrices(int form, int es, GroupedParams &p, Matrix &a, Matrix &b)
+{
+    a = {&p.a, &p.lda, form == kWeights ? p.red : p.rows, (int64_t)(form == kWeights ? p.rows : p.red) * es};
+    b = {&p.b, &p.ldb, form == kWeights ? p.red : (int64_t)p.groups * (form == kForward ? p.cols : p.red), (int64_t)(form == kForward ? p.red : p.cols) * es};
+}
+
+// Bytes for operands laid out anew, 0 where that does not pay.  The kernel for any alignment takes 1.6 times as long as those for whole chunks at
+// least, but for what a tile costs whatever its reduction is, and that has to outweigh a copy (8191^3 in 8 bits 911 us, 536 laid out anew; 5000 rows of 5
+// experts, 2047 x 4095 bf16, by the weights 155 and 130; 1001 rows of 13, 515 x 1030, 16 and 26).
+size_t pack_bytes(int form, int dtype, GroupedParams &p)
+{
+    if (dtype == ALT_F32 || p.rows == 0 || p.red == 0) return 0;
+    if (form == kForward && grp_is_few(p)) return 0;
+    const int es = dtype == ALT_I8 ? 1 : 2;
+    Matrix a, b;
+    matrices(form, es, p, a, b);
+    size_t need = 0;
+    double cost = 0;
+    for (const Matrix *m : {&a, &b})
+        if (!m->whole()) {
+            if (m->packed() > (1 << 22) || m->rows > 0x7fffffff) return 0;
+            need += (size_t)m->size();
+            cost += 2.0 + 2.0 * (double)m->size() / 4.5e6;
+        }
+    GrpTime t;
+    if (form == kForward) grp_choose<kForward>(p, es, &t);
+    else if (form == kInput) grp_choose<kInput>(p, es, &t);
+    else grp_choose<kWeights>(p, es, &t);
+    return cost < 0.7 * t.reduction ? need : 0;
+}
+
+hipError_t pack(Matrix &m, char *to, hipStream_t st)
+{
+    const int64_t per_row = (m.packed() + 31) / 32;
+    // (a launch's index has 31 bits)
+    const int64_t most = (1ll << 30) / per_row;
+    for (int64_t r = 0; r < m.rows; r += most) {
+        const int64_t n = std::min(most, m.rows - r);
+        hipLaunchKernelGGL(grp_pack_kernel, dim3((unsigned)((n * per_row + 255) / 256)), dim3(256), 0, st, (const char *)*m.p, *m.ld, (int)m.bytes, to, (int)m.packed(),
+                           (uint32_t)(n * per_row), make_fastdiv((uint32_t)per_row), (uint32_t)r);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    *m.p = to;
+    *m.ld = m.packed();
+    return hipSuccess;
+}
+
+// What the problem takes of its operands' and outputs' extents, strides in bytes.
+GroupedParams problem(alt_handle_t h, const alt_grouped_desc_t &l, int form, const void *a, const void *b, void *y)
+{
+    const int64_t es = (int64_t)in_size(l.in_dtype), os = (int64_t)dtype_size(l.out_dtype), lda = l.lda * es, ldb = l.ldb * es, ldc = l.ldc * es;
+    GroupedParams p{};
+    p.a = a; p.b = b; p.y = y;
+    p.groups = l.groups;
     p.places = h->compute_units;
+    p.flags = l.out_dtype == ALT_BF16 ? kGrpOutBf16 : 0;
+    p.rows = (int32_t)(form == kWeights ? l.N : l.rows);
+    p.cols = (int32_t)(form == kForward ? l.N : l.K);
+    p.red = (int32_t)(form == kForward ? l.K : form == kInput ? l.N : l.rows);
+    p.lda = form == kForward ? lda : ldc;
+    p.ldb = form == kWeights ? lda : ldb;
+    p.ldy = (form == kForward ? l.ldc : form == kInput ? l.lda : l.ldb) * os;
+    p.ldmask = form == kInput ? lda : 0;
+    p.y_group = form == kWeights ? l.N * l.ldb * os : 0;
     if (p.cols % (os == 2 ? 8 : 4) == 0) p.flags |= kGrpWhole;
+    return p;
+}
+
+alt_status_t run(alt_handle_t h, const char *call, int dtype, int form, GroupedParams &p, void *workspace, size_t ws_bytes, hipStream_t st)
+{
+    if (workspace && ws_bytes) {
+        const uintptr_t ws = ((uintptr_t)workspace + 15) / 16 * 16;
+        const size_t need = pack_bytes(form, dtype, p);
+        if (need && need + (ws - (uintptr_t)workspace) <= ws_bytes) {
+            Matrix a, b;
+            matrices(form, dtype == ALT_I8 ? 1 : 2, p, a, b);
+            char *to = (char *)ws;
+            for (Matrix *m : {&a, &b})
+                if (!m->whole()) {
+                    const int64_t size = m->size();
+                    ALT_CHECK_HIP(h, pack(*m, to, st));
+                    to += size;
+                }
+            p.flags |= kGrpPacked;
+        }
+    }
+    p.b_group = form == kWeights ? 0 : (int64_t)(form == kForward ? p.cols : p.red) * p.ldb;
     const hipError_t e = dtype == ALT_I8 ? grouped_run_i8(p, st) : dtype == ALT_BF16 ? grouped_run_bf16(form, p, st) : grouped_run_f32(form, p, st);
     if (e == hipErrorInvalidConfiguration) return fail(h, ALT_UNSUPPORTED, "%s: more output tiles than a launch holds", call);
     ALT_CHECK_HIP(h, e);
     return ALT_OK;
 }
 
-alt_status_t forward(alt_handle_t h, const char *call, const alt_grouped_desc_t &d, const void *a, const float *a_scale, const void *b, const float *b_scale,
-                     const float *bias, const int32_t *offsets, void *y, void *stream)
-{
-    const size_t es = in_size(d.in_dtype);
-    GroupedParams p{};
-    p.a = a; p.b = b; p.y = y;
-    p.a_scale = a_scale; p.b_scale = b_scale;
-    p.bias = d.epilogue & ALT_EPI_BIAS ? bias : nullptr;
-    p.offsets = offsets;
-    p.lda = d.lda * (int64_t)es; p.ldb = d.ldb * (int64_t)es;
-    p.b_group = d.N * p.ldb;
-    p.rows = (int32_t)d.rows; p.cols = (int32_t)d.N; p.red = (int32_t)d.K; p.groups = d.groups;
-    p.flags = (d.epilogue & ALT_EPI_RELU ? kGrpRelu : 0) | (d.out_dtype == ALT_BF16 ? kGrpOutBf16 : 0);
-    return run(h, call, d.in_dtype, kForward, p, d.ldc, (hipStream_t)stream);
-}
-
-alt_status_t no_workspace(alt_handle_t h, const alt_grouped_desc_t *d, bool gradient, const char *call, size_t *bytes)
+alt_status_t workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, int form, bool one_group, const char *call, size_t *bytes)
 {
     alt_grouped_desc_t l;
-    const alt_status_t s = check_layer(h, call, d, gradient, &l);
+    const alt_status_t s = check_layer(h, call, d, form != kForward, &l);
     if (s != ALT_OK) return s;
     if (!bytes) return fail(h, ALT_INVALID_ARG, "%s: null result", call);
-    *bytes = 0;
+    // (buffers that start at whole chunks: what their rows do is known here)
+    GroupedParams p = problem(h, l, form, nullptr, nullptr, nullptr);
+    p.offsets = one_group ? nullptr : (const int32_t *)16;                  // (asked for, not read)
+    if (p.places == 0) p.places = 256;
+    const size_t need = pack_bytes(form, l.in_dtype, p);
+    *bytes = need ? need + 16 : 0;                         // (a workspace may start anywhere)
     return ALT_OK;
+}
+
+alt_status_t forward(alt_handle_t h, const char *call, const alt_grouped_desc_t &l, const void *a, const float *a_scale, const void *b, const float *b_scale,
+                     const float *bias, const int32_t *offsets, void *y, void *workspace, size_t ws_bytes, void *stream)
+{
+    GroupedParams p = problem(h, l, kForward, a, b, y);
+    p.a_scale = a_scale;
+    p.b_scale = b_scale;
+    p.bias = l.epilogue & ALT_EPI_BIAS ? bias : nullptr;
+    p.offsets = offsets;
+    if (l.epilogue & ALT_EPI_RELU) p.flags |= kGrpRelu;
+    return run(h, call, l.in_dtype, kForward, p, workspace, ws_bytes, (hipStream_t)stream);
 }
 
 // The 8-bit product as a layer of one group.
@@ -108,14 +226,13 @@ extern "C" alt_status_t alt_gemm_grouped(alt_handle_t h, const alt_grouped_desc_
     alt_grouped_desc_t l;
     alt_status_t s = check_layer(h, "alt_gemm_grouped", d, false, &l);
     if (s != ALT_OK) return s;
-    (void)workspace; (void)ws_bytes;
     if (l.rows == 0) return ALT_OK;
     const size_t es = in_size(l.in_dtype);
     const bool scaled = l.in_dtype == ALT_I8;
     s = check_buffers(h, "alt_gemm_grouped", {{"a", a, es}, {"b", b, es}, {"offsets", offsets, 4}, {"y", y, dtype_size(l.out_dtype)}, {"a_scale", a_scale, 4, scaled},
                                               {"b_scale", b_scale, 4, scaled}, {"bias", bias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}});
     if (s != ALT_OK) return s;
-    return forward(h, "alt_gemm_grouped", l, a, a_scale, b, b_scale, bias, offsets, y, stream);
+    return forward(h, "alt_gemm_grouped", l, a, a_scale, b, b_scale, bias, offsets, y, workspace, ws_bytes, stream);
 }
 
 extern "C" alt_status_t alt_gemm_grouped_dx(alt_handle_t h, const alt_grouped_desc_t *d, const void *dy, const void *b, const void *relu_of, const int32_t *offsets,
@@ -124,22 +241,17 @@ extern "C" alt_status_t alt_gemm_grouped_dx(alt_handle_t h, const alt_grouped_de
     alt_grouped_desc_t l;
     alt_status_t s = check_layer(h, "alt_gemm_grouped_dx", d, true, &l);
     if (s != ALT_OK) return s;
-    (void)workspace; (void)ws_bytes;
     if (l.epilogue & ALT_EPI_BIAS) return fail(h, ALT_INVALID_ARG, "alt_gemm_grouped_dx: a bias has no part in the gradient of x");
     if (l.rows == 0) return ALT_OK;
     const size_t es = in_size(l.in_dtype);
     s = check_buffers(h, "alt_gemm_grouped_dx", {{"dy", dy, es}, {"b", b, es}, {"offsets", offsets, 4}, {"dx", dx, dtype_size(l.out_dtype)},
                                                  {"relu_of", relu_of, es, (l.epilogue & ALT_EPI_RELU) != 0}});
     if (s != ALT_OK) return s;
-    GroupedParams p{};
-    p.a = dy; p.b = b; p.y = dx;
-    p.mask = relu_of;
+    GroupedParams p = problem(h, l, kInput, dy, b, dx);
     p.offsets = offsets;
-    p.lda = l.ldc * (int64_t)es; p.ldb = l.ldb * (int64_t)es; p.ldmask = l.lda * (int64_t)es;
-    p.b_group = l.N * p.ldb;
-    p.rows = (int32_t)l.rows; p.cols = (int32_t)l.K; p.red = (int32_t)l.N; p.groups = l.groups;
-    p.flags = (l.epilogue & ALT_EPI_RELU ? kGrpMask : 0) | (l.out_dtype == ALT_BF16 ? kGrpOutBf16 : 0);
-    return run(h, "alt_gemm_grouped_dx", l.in_dtype, kInput, p, l.lda, (hipStream_t)stream);
+    p.mask = relu_of;
+    if (l.epilogue & ALT_EPI_RELU) p.flags |= kGrpMask;
+    return run(h, "alt_gemm_grouped_dx", l.in_dtype, kInput, p, workspace, ws_bytes, (hipStream_t)stream);
 }
 
 extern "C" alt_status_t alt_gemm_grouped_dw(alt_handle_t h, const alt_grouped_desc_t *d, const void *a, const void *dy, const int32_t *offsets, void *dw, float *dbias,
@@ -148,37 +260,31 @@ extern "C" alt_status_t alt_gemm_grouped_dw(alt_handle_t h, const alt_grouped_de
     alt_grouped_desc_t l;
     alt_status_t s = check_layer(h, "alt_gemm_grouped_dw", d, true, &l);
     if (s != ALT_OK) return s;
-    (void)workspace; (void)ws_bytes;
     if (l.epilogue & ALT_EPI_RELU) return fail(h, ALT_INVALID_ARG, "alt_gemm_grouped_dw: dy is the gradient before the ReLU");
     const size_t es = in_size(l.in_dtype);
     // (without rows the gradients are zeros, and a and dy need not exist)
     s = check_buffers(h, "alt_gemm_grouped_dw", {{"a", a, es, l.rows > 0}, {"dy", dy, es, l.rows > 0}, {"offsets", offsets, 4},
                                                  {"dw", dw, dtype_size(l.out_dtype)}, {"dbias", dbias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}});
     if (s != ALT_OK) return s;
-    GroupedParams p{};
-    p.a = dy; p.b = a; p.y = dw;
-    p.colsum = l.epilogue & ALT_EPI_BIAS ? dbias : nullptr;
+    GroupedParams p = problem(h, l, kWeights, dy, a, dw);
     p.offsets = offsets;
-    p.lda = l.ldc * (int64_t)es; p.ldb = l.lda * (int64_t)es;
-    p.y_group = l.N * l.ldb;
-    p.rows = (int32_t)l.N; p.cols = (int32_t)l.K; p.red = (int32_t)l.rows; p.groups = l.groups;
-    p.flags = l.out_dtype == ALT_BF16 ? kGrpOutBf16 : 0;
-    return run(h, "alt_gemm_grouped_dw", l.in_dtype, kWeights, p, l.ldb, (hipStream_t)stream);
+    p.colsum = l.epilogue & ALT_EPI_BIAS ? dbias : nullptr;
+    return run(h, "alt_gemm_grouped_dw", l.in_dtype, kWeights, p, workspace, ws_bytes, (hipStream_t)stream);
 }
 
 extern "C" alt_status_t alt_gemm_grouped_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes)
 {
-    return no_workspace(h, d, false, "alt_gemm_grouped_workspace_size", bytes);
+    return workspace_size(h, d, kForward, false, "alt_gemm_grouped_workspace_size", bytes);
 }
 
 extern "C" alt_status_t alt_gemm_grouped_dx_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes)
 {
-    return no_workspace(h, d, true, "alt_gemm_grouped_dx_workspace_size", bytes);
+    return workspace_size(h, d, kInput, false, "alt_gemm_grouped_dx_workspace_size", bytes);
 }
 
 extern "C" alt_status_t alt_gemm_grouped_dw_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes)
 {
-    return no_workspace(h, d, true, "alt_gemm_grouped_dw_workspace_size", bytes);
+    return workspace_size(h, d, kWeights, false, "alt_gemm_grouped_dw_workspace_size", bytes);
 }
 
 extern "C" alt_status_t alt_gemm_i8(alt_handle_t h, const alt_gemm_i8_desc_t *d, const void *a, const float *a_scale, const void *b, const float *b_scale,
@@ -190,12 +296,11 @@ extern "C" alt_status_t alt_gemm_i8(alt_handle_t h, const alt_gemm_i8_desc_t *d,
     alt_grouped_desc_t l;
     alt_status_t s = check_layer(h, "alt_gemm_i8", &g, false, &l);
     if (s != ALT_OK) return s;
-    (void)workspace; (void)ws_bytes;
     if (l.rows == 0) return ALT_OK;
     s = check_buffers(h, "alt_gemm_i8", {{"a", a, 1}, {"b", b, 1}, {"a_scale", a_scale, 4}, {"b_scale", b_scale, 4}, {"y", y, dtype_size(l.out_dtype)},
                                          {"bias", bias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}});
     if (s != ALT_OK) return s;
-    return forward(h, "alt_gemm_i8", l, a, a_scale, b, b_scale, bias, nullptr, y, stream);
+    return forward(h, "alt_gemm_i8", l, a, a_scale, b, b_scale, bias, nullptr, y, workspace, ws_bytes, stream);
 }
 
 extern "C" alt_status_t alt_gemm_i8_workspace_size(alt_handle_t h, const alt_gemm_i8_desc_t *d, size_t *bytes)
@@ -203,5 +308,5 @@ extern "C" alt_status_t alt_gemm_i8_workspace_size(alt_handle_t h, const alt_gem
     if (!h) return ALT_INVALID_ARG;
     if (!d) return fail(h, ALT_INVALID_ARG, "alt_gemm_i8_workspace_size: null descriptor");
     const alt_grouped_desc_t g = one_group(d);
-    return no_workspace(h, &g, false, "alt_gemm_i8_workspace_size", bytes);
+    return workspace_size(h, &g, kForward, true, "alt_gemm_i8_workspace_size", bytes);
 }

@@ -308,6 +308,105 @@ def test_grouped_gradients(h, off, rows, N, K, dtype, pad):
                     close(db.t, want_b, tol_b, "db")
 
 
+def filled(shape, dtype, seed, offset=0):
+    """A large operand of random values, `offset` elements into its buffer."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = int(np.prod(shape))
+    buf = torch.empty(n + offset, dtype=dtype, device="cuda")
+    if dtype == torch.int8:
+        buf.copy_(torch.randint(-127, 128, (n + offset,), generator=g, device="cuda"))
+    else:
+        buf.copy_(torch.randn(n + offset, generator=g, device="cuda"))
+    return buf[offset:].view(shape)
+
+
+def worst(got, want, size, n):
+    """The largest error in units of n * 2^-24 of the sums of magnitudes."""
+    return float(((got.double() - want).abs() / (n * EPS * size).clamp(min=1e-30)).max())
+
+
+@pytest.mark.parametrize("M,N,K,offset", [(2049, 2051, 4099, 0), (2500, 2048, 4100, 3), (3000, 3001, 4096, 0)])
+def test_large_8_bit_products_at_any_alignment(h, M, N, K, offset):
+    """Without a workspace, with one in which the operands are laid out anew where that pays, and with one that starts anywhere: the same sums."""
+    q, w = filled((M, K), torch.int8, 1, offset), filled((N, K), torch.int8, 2, offset)
+    s, t = torch.ones(M, device="cuda"), torch.ones(N, device="cuda")
+    want = q.double() @ w.double().T
+    d = alt.gemm_i8_desc(M, N, K, out_dtype=alt.F32)
+    need = h.gemm_i8_workspace_size(d)
+    assert (need > 0) == (K % 16 != 0)
+    ws = torch.empty(need + 64, dtype=torch.uint8, device="cuda")
+    y = Canary(M, N, torch.float32)
+    for at, nbytes in ((None, 0), (ws, need), (ws[5:], need), (ws, need // 2)):
+        y.t.fill_(55)
+        h.gemm_i8(d, q, s, w, t, y, workspace=at, ws_bytes=nbytes)
+        torch.cuda.synchronize()
+        assert y.untouched() and torch.equal(y.t.double(), want.float().double())
+
+
+@pytest.mark.parametrize("off,N,K,offset", [([0, 700, 700, 2100, 3001], 1027, 2051, 0), ([0, 1500, 3000], 2047, 2050, 1), ([0, 2048, 4096], 2048, 2052, 0)])
+def test_large_layers_at_any_alignment(h, off, N, K, offset):
+    """Products and gradients with and without a workspace in which the operands are laid out anew."""
+    rows, E = off[-1], len(off) - 1
+    x, w, dy = filled((rows, K), torch.bfloat16, 1, offset), filled((E, N, K), torch.bfloat16, 2, offset), filled((rows, N), torch.bfloat16, 3, offset)
+    o = make_offsets(off)
+    d = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32)
+    db = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32, epilogue=alt.EPI_BIAS)
+    dm = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32, epilogue=alt.EPI_RELU)
+    needs = h.gemm_grouped_workspace_size(d), h.gemm_grouped_dx_workspace_size(dm), h.gemm_grouped_dw_workspace_size(db)
+    assert any(needs)
+    ws = torch.empty(max(needs), dtype=torch.uint8, device="cuda")
+    for use in (False, True):
+        arg = [dict(workspace=ws, ws_bytes=n) if use and n else {} for n in needs]
+        y, dx, dw, bias = Canary(rows, N, torch.float32), Canary(rows, K, torch.float32), Canary(N, K, torch.float32, lead=(E,)), torch.empty(E, N, device="cuda")
+        h.gemm_grouped(d, x, w, o, y, **arg[0])
+        h.gemm_grouped_dx(dm, dy, w, o, dx, relu_of=x, **arg[1])
+        h.gemm_grouped_dw(db, x, dy, o, dw, dbias=bias, **arg[2])
+        torch.cuda.synchronize()
+        assert y.untouched() and dx.untouched() and dw.untouched()
+        for e in range(E):
+            lo, hi = off[e], off[e + 1]
+            xd, wd, gd = x[lo:hi].double(), w[e].double(), dy[lo:hi].double()
+            if hi == lo:
+                assert not dw.t[e].any() and not bias[e].any()
+                continue
+            assert worst(y.t[lo:hi], xd @ wd.T, xd.abs() @ wd.abs().T, K) <= 1
+            assert worst(dx.t[lo:hi], (gd @ wd) * (xd > 0), gd.abs() @ wd.abs(), N) <= 1
+            assert worst(dw.t[e], gd.T @ xd, gd.abs().T @ xd.abs(), hi - lo) <= 1
+            assert worst(bias[e], gd.sum(0), gd.abs().sum(0), hi - lo) <= 1
+
+
+@pytest.mark.parametrize("off,N,K", [([0, 2304, 2305, 4700, 8192], 1024, 512), ([0, 300, 5000, 5100], 2304, 1024)])
+@pytest.mark.parametrize("dtype", [alt.BF16, alt.I8])
+def test_large_layers(h, off, N, K, dtype):
+    """Tiles of both sizes, groups that end inside one."""
+    rows, E, td = off[-1], len(off) - 1, TORCH[dtype]
+    x, w = filled((rows, K), td, 1), filled((E, N, K), td, 2)
+    o, y = make_offsets(off), Canary(rows, N, torch.float32)
+    one = dict(a_scale=torch.ones(rows, device="cuda"), b_scale=torch.ones(E, N, device="cuda")) if dtype == alt.I8 else {}
+    h.gemm_grouped(alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=alt.F32), x, w, o, y, **one)
+    torch.cuda.synchronize()
+    assert y.untouched()
+    for e in range(E):
+        lo, hi = off[e], off[e + 1]
+        xd, wd = x[lo:hi].double(), w[e].double()
+        assert worst(y.t[lo:hi], xd @ wd.T, xd.abs() @ wd.abs().T, K) <= 1
+    if dtype == alt.I8:
+        return
+    dy = filled((rows, N), td, 3)
+    d = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32, epilogue=alt.EPI_BIAS)
+    dx, dw, bias = Canary(rows, K, torch.float32), Canary(N, K, torch.float32, lead=(E,)), torch.empty(E, N, device="cuda")
+    h.gemm_grouped_dx(alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32), dy, w, o, dx)
+    h.gemm_grouped_dw(d, x, dy, o, dw, dbias=bias)
+    torch.cuda.synchronize()
+    assert dx.untouched() and dw.untouched()
+    for e in range(E):
+        lo, hi = off[e], off[e + 1]
+        xd, wd, gd = x[lo:hi].double(), w[e].double(), dy[lo:hi].double()
+        assert worst(dx.t[lo:hi], gd @ wd, gd.abs() @ wd.abs(), N) <= 1
+        assert worst(dw.t[e], gd.T @ xd, gd.abs().T @ xd.abs(), hi - lo) <= 1
+        assert worst(bias[e], gd.sum(0), gd.abs().sum(0), hi - lo) <= 1
+
+
 @pytest.mark.parametrize("rows", [24, 500])
 def test_gradients_against_differences(h, rows):
     """L = sum y * g is linear in x, w and bias, so a difference over any step is the derivative: along a random direction of each operand the
