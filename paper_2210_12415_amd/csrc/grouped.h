@@ -424,7 +424,9 @@ __device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProble
     constexpr int BANDS = TM * (TN / JB);
     const bool owned = g.group < p.groups, masked = FORM == kInput && (p.flags & kGrpMask), relu = FORM == kForward && (p.flags & kGrpRelu);
     const int col_in = g.col0 + wcol + (lane >> 5) * 4, col_out = g.col0 + wcol + lane % CPB * W;  // of the sums and of the chunks
-    const int row_out = wrow + lane / CPB, last = g.row_end - g.row0 - 1;                           // from the tile's first row on
+    // From the tile's first row on; the last row is the last that is this wave's, so that a descriptor's size stays below kOutOfRange (rows are 16 MB
+    // apart at most, 4 MB in tiles of more than 128).
+    const int row_out = wrow + lane / CPB, last = min(g.row_end - g.row0, wrow + TM * 32) - 1;
     float sa[TM];
     f32x4_t scale[TN][4], bias[TN][4];
     auto columns = [&](f32x4_t (&v)[TN][4], const float *row, bool exist) {

@@ -549,3 +549,85 @@ def test_results_repeat(h):
         torch.cuda.synchronize()
         first = first or (dw, db)
         assert torch.equal(dw, first[0]) and torch.equal(db, first[1])
+
+
+def small_integers(shape, dtype, seed):
+    """Values of -3 .. 3: sums of a few thousand products of them are exact in 32 bits, in any order."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randint(-3, 4, shape, generator=g, device="cuda").to(dtype)
+
+
+def far_apart(rows, cols, stride, dtype, seed, offset=0):
+    """Rows `stride` elements apart in a buffer of more than 4 GiB, of which only they are written."""
+    buf = torch.empty(rows * stride + offset, dtype=dtype, device="cuda")
+    assert buf.numel() * buf.element_size() > 1 << 32
+    view = buf[offset:].view(rows, stride)[:, :cols]
+    view.copy_(small_integers((rows, cols), dtype, seed))
+    return view
+
+
+@pytest.mark.parametrize("rows,stride,offset", [(1030, 1 << 22, 0), (1030, (1 << 22) - 5, 3), (17, 1 << 22, 0)])
+def test_operands_beyond_32_bits(h, rows, stride, offset):
+    """Rows of every operand in buffers of more than 4 GiB (the few rows' weights are what is far apart there)."""
+    N, K = (40, 72) if rows > 32 else (1030, 72)
+    x8 = far_apart(rows, K, stride, torch.int8, 1, offset) if rows > 32 else small_integers((rows, K), torch.int8, 1)
+    w8 = far_apart(N, K, stride, torch.int8, 2, offset) if N > 1024 else small_integers((N, K), torch.int8, 2)
+    y = torch.empty(rows, N, device="cuda")
+    d = alt.gemm_i8_desc(rows, N, K, out_dtype=alt.F32, lda=x8.stride(0), ldb=w8.stride(0))
+    h.gemm_i8(d, x8, torch.ones(rows, device="cuda"), w8, torch.ones(N, device="cuda"), y)
+    torch.cuda.synchronize()
+    assert torch.equal(y, x8.float() @ w8.float().T)
+    del x8, w8
+    if rows <= 32:
+        return
+    rows, x, w = 600, small_integers((600, K), torch.bfloat16, 3), small_integers((2, N, K), torch.bfloat16, 4)
+    o, far = make_offsets([0, 250, 600]), far_apart(600, N, stride, torch.bfloat16, 5, offset)
+    want = torch.cat([x[:250].float() @ w[0].float().T, x[250:].float() @ w[1].float().T])
+    h.gemm_grouped(alt.grouped_desc(rows, 2, N, K, ldc=stride), x, w, o, far)
+    torch.cuda.synchronize()
+    assert torch.equal(far.float(), want.bfloat16().float())
+    far.copy_(small_integers((rows, N), torch.bfloat16, 6))
+    dx, dw = torch.empty(rows, K, device="cuda"), torch.empty(2, N, K, device="cuda")
+    d = alt.grouped_desc(rows, 2, N, K, out_dtype=alt.F32, ldc=stride)
+    h.gemm_grouped_dx(d, far, w, o, dx)
+    h.gemm_grouped_dw(d, x, far, o, dw)
+    torch.cuda.synchronize()
+    for e, (lo, hi) in enumerate(((0, 250), (250, 600))):
+        assert torch.equal(dx[lo:hi], far[lo:hi].float() @ w[e].float()) and torch.equal(dw[e], far[lo:hi].float().T @ x[lo:hi].float())
+
+
+def test_weights_beyond_32_bits(h):
+    """An expert whose weights begin behind 4 GiB, with all three products of its layer."""
+    E, N, K, rows = 34, 8192, 8192, 300
+    w = torch.empty(E, N, K, dtype=torch.bfloat16, device="cuda")
+    assert w.numel() * 2 > 1 << 32
+    off = [0] * (E - 1) + [100, 300]
+    for e in (E - 2, E - 1):
+        w[e] = small_integers((N, K), torch.bfloat16, e)
+    x, dy, o = small_integers((rows, K), torch.bfloat16, 1), small_integers((rows, N), torch.bfloat16, 2), make_offsets(off)
+    y, dx = torch.empty(rows, N, device="cuda"), torch.empty(rows, K, device="cuda")
+    d = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32)
+    h.gemm_grouped(d, x, w, o, y)
+    h.gemm_grouped_dx(d, dy, w, o, dx)
+    torch.cuda.synchronize()
+    for e, lo, hi in ((E - 2, 0, 100), (E - 1, 100, 300)):
+        assert torch.equal(y[lo:hi], x[lo:hi].float() @ w[e].float().T) and torch.equal(dx[lo:hi], dy[lo:hi].float() @ w[e].float())
+    del w
+    dw = torch.full((E, N, K), 3, dtype=torch.bfloat16, device="cuda")
+    h.gemm_grouped_dw(alt.grouped_desc(rows, E, N, K), x, dy, o, dw)
+    torch.cuda.synchronize()
+    assert not dw[:E - 2].any()
+    for e, lo, hi in ((E - 2, 0, 100), (E - 1, 100, 300)):
+        assert torch.equal(dw[e].float(), (dy[lo:hi].float().T @ x[lo:hi].float()).bfloat16().float())
+
+
+def test_quantize_rows_beyond_32_bits(h):
+    rows, cols, stride = 1030, 70, 1 << 22
+    x = far_apart(rows, cols, stride, torch.bfloat16, 7)
+    x[:, 1] = 3
+    q = torch.empty(rows * stride, dtype=torch.int8, device="cuda").view(rows, stride)[:, :cols]
+    s = torch.empty(rows, device="cuda")
+    h.quantize_rows(alt.BF16, rows, cols, x, q, s, x_stride=stride, q_stride=stride)
+    torch.cuda.synchronize()
+    want, scale = exact_rows(x)
+    assert np.array_equal(q.cpu().numpy(), want) and np.array_equal(f64(s), scale)
