@@ -936,23 +936,24 @@ struct GrpStream {
     }
 };
 
-// A workgroup's operands run through a ring of NS stages in LDS.  At the barrier of step s the stages of steps s and s + 1 have landed and
-// every wave has read stage s - 1 for the last time; then the loads of step s + NS - 1 go out into that stage, and each chunk's fragments are
-// read some chunks before they are used, across the barrier too: one chunk where a wave's tile has eight matrix instructions for each, three
-// where it has fewer (a read takes about as long as four).  A wave issues in order, and a matrix instruction hides eight other instructions
-// at most: behind each stands one operand read or one load where they are that many, and the order is pinned.
+// Tiles of 64x64 and 128x128: a workgroup's operands run through a ring of NS stages in LDS.  At the barrier of step s the stages of steps s and
+// s + 1 have landed and every wave has read stage s - 1 for the last time; then the loads of step s + NS - 1 go out into that stage, and each
+// chunk's fragments are read three chunks before they are used, across the barrier too (a read takes about as long as four matrix instructions).
+// A wave issues in order, and a matrix instruction hides eight other instructions at most: behind each stand a few operand reads and loads, and
+// the order is pinned.  Bound by latency on small calls (the loads of three steps in flight are what hides it: 64 x 4096 x 4096 in 8 bits 9.6 us,
+// 1.8 TB/s), by the matrix instructions and the loads' issue above (2048 x 768 x 3072 in 8 bits 13.8 us, 0.7 POP/s).
 template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB, int NS>
-struct GrpKernel {
-    static constexpr int ES = GrpTraits<T>::ES;
+struct GrpRing {
+    using type = T;
+    static constexpr int kForm = FORM, kBM = BM, kBN = BN, ES = GrpTraits<T>::ES;
     static constexpr int NW = WGM * WGN, THREADS = 64 * NW;
     static constexpr int WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32, NKC = BKB / 32;
     using SA = GrpStream<ES, FORM != kWeights, BM, BKB, NW>;
     using SB = GrpStream<ES, FORM == kForward, BN, BKB, NW>;
     using A = typename SA::Op;
     using B = typename SB::Op;
-    using acc_t = typename GrpTraits<T>::acc_t;
     static constexpr int BK = A::BK, STAGE = A::BYTES + B::BYTES, LPS = SA::NL + SB::NL;
-    static constexpr int AHEAD = TM * TN >= 8 || NKC < 4 ? 1 : 3, NBUF = AHEAD + 1;
+    static constexpr int AHEAD = 3, NBUF = AHEAD + 1;
     static_assert(NS == 4 && NS * LPS < 60 && NKC % NBUF == 0, "ring");
     static constexpr int kLds = NS * STAGE;
     static_assert(NW * kStageBytes <= kLds, "staging");
@@ -1034,8 +1035,7 @@ struct GrpKernel {
             }
             const uint32_t next_stage = stage + STAGE == NS * STAGE ? 0 : stage + STAGE;
             open_stage();
-            constexpr int READS = TM + TN, LOADS = (LPS + NKC - 1) / NKC, SLOTS = TM * TN;    // of a chunk
-            constexpr int PER = (READS + LOADS + SLOTS - 1) / SLOTS;
+            constexpr int READS = TM + TN, LOADS = (LPS + NKC - 1) / NKC, PER = (READS + LOADS + TM * TN - 1) / (TM * TN);    // of a chunk
 #pragma unroll
             for (int kc = 0; kc < NKC; ++kc) {
                 const int buf = kc % NBUF, ahead = (kc + AHEAD) % NKC;
@@ -1069,12 +1069,147 @@ struct GrpKernel {
     }
 };
 
-template <typename K, typename T, int FORM, int BM, int BN>
+// Tiles of 256x256, eight waves of 128x64 each: 64 KB of operands for 128 bytes of the reduction.  A step takes whole cache lines (with steps of
+// 64 bytes each line comes to the L1 twice, and these requests are the bound: 8192 x 8192 x 8192 in bf16 870 us, so 785 us, 1.40 PFLOP/s; in 8
+// bits 470 and 433 us, 2.54 POP/s, where the chip's power is the bound: it runs at two thirds of its clock).  Two stages fit and a half, so the
+// ring has five units of one operand each, A and B in turn.  One barrier a step stands before its last chunk, whose fragments every wave has read
+// by then: the step's two units are free, the next step's have landed, and its first fragments are read behind the last chunk's matrix
+// instructions.  Into the freed units go B of the step after next (which has one step to land) and A of the one behind it (which has two), the
+// loads evenly behind the matrix instructions of this chunk and the next.
+template <typename T, int FORM>
+struct GrpWide {
+    using type = T;
+    static constexpr int kForm = FORM, kBM = 256, kBN = 256, ES = GrpTraits<T>::ES, BM = kBM, BN = kBN, BKB = 128;
+    static constexpr int WGM = 2, WGN = 4, NW = WGM * WGN, THREADS = 64 * NW;
+    static constexpr int WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32, NKC = BKB / 32;
+    using SA = GrpStream<ES, FORM != kWeights, BM, BKB, NW>;
+    using SB = GrpStream<ES, FORM == kForward, BN, BKB, NW>;
+    using A = typename SA::Op;
+    using B = typename SB::Op;
+    static constexpr int BK = A::BK, UNIT = A::BYTES, UNITS = 5, NL = SA::NL;
+    static_assert(A::BYTES == B::BYTES && SB::NL == NL && NKC == 4, "units");
+    static constexpr int kLds = UNITS * UNIT;
+    static_assert(kLds <= 160 * 1024 && NW * kStageBytes <= kLds, "LDS");
+
+    static __device__ __forceinline__ void tile(const GroupedParams &p, const GrpProblem &g, char *lds)
+    {
+        const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = wave / WGN, wn = wave % WGN;
+        SA sa;
+        SB sb;
+        sa.start(g.a0, p.lda, g.row_end - g.row0, g.red, wave, lane);
+        sb.start(g.b0, p.ldb, p.cols - g.col0, g.red, wave, lane);
+        i32x4_t rs;
+        uint32_t past, fill = 0;                           // fill: the unit that is loaded next, as an offset
+        auto after = [&](uint32_t unit) { return unit + UNIT == UNITS * UNIT ? 0u : unit + UNIT; };
+        auto open_a = [&]() { rs = sa.rsrc(); past = sa.past(); };
+        auto open_b = [&]() { rs = sb.rsrc(); past = sb.past(); };
+        auto load_a = [&](int i) { dma_load16_s(rs, sa.voff[i] | past, 0u, lds0 + fill + wave * 1024 + i * (NW * 1024)); };
+        auto load_b = [&](int i) { dma_load16_s(rs, sb.voff[i] | past, 0u, lds0 + fill + wave * 1024 + i * (NW * 1024)); };
+        auto close_a = [&]() { sa.next(); fill = after(fill); };
+        auto close_b = [&]() { sb.next(); fill = after(fill); };
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            if (u % 2 == 0) open_a(); else open_b();
+#pragma unroll
+            for (int i = 0; i < NL; ++i) { if (u % 2 == 0) load_a(i); else load_b(i); }
+            if (u % 2 == 0) close_a(); else close_b();
+        }
+
+        constexpr int NA = A::kRed ? NKC : TM, NB = B::kRed ? NKC : TN;
+        uint32_t a_at[NA], b_at[NB];
+#pragma unroll
+        for (int i = 0; i < NA; ++i) a_at[i] = A::kRed ? A::frag(wm * WTM, i, lane) : A::frag(wm * WTM + i * 32, 0, lane);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) b_at[i] = B::kRed ? B::frag(wn * WTN, i, lane) : B::frag(wn * WTN + i * 32, 0, lane);
+
+        GrpSums<T, TM, TN> acc;
+        acc.clear();
+        float sums[TM];                                    // kWeights: of this lane's row of the left operand
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sums[i] = 0.f;
+        const bool take_sums = FORM == kWeights && p.colsum && g.col0 == 0 && wn == 0;
+
+        u32x4_t fa[2][TM], fb[2][TN];
+        auto read_one = [&](int buf, int r, uint32_t unit_a, uint32_t unit_b, int kc) {
+            // (in the order in which the matrix instructions want them: the first row, all columns, the other rows)
+            if (r == 0 || r > TN) {
+                const int i = r == 0 ? 0 : r - TN;
+                fa[buf][i] = A::read(lds, unit_a + a_at[A::kRed ? kc : i] + A::apart(i, kc));
+            } else {
+                fb[buf][r - 1] = B::read(lds, unit_b + b_at[B::kRed ? kc : r - 1] + B::apart(r - 1, kc));
+            }
+        };
+
+        const int steps = (g.red + BK - 1) / BK;
+        wait_vmcnt<(UNITS - 2) * NL>();
+        lds_barrier();
+        uint32_t ua = 0, ub = UNIT;
+#pragma unroll
+        for (int r = 0; r < TM + TN; ++r) read_one(0, r, ua, ub, 0);
+        constexpr int READS = TM + TN, SLOTS = TM * TN, PER = (READS + SLOTS - 1) / SLOTS;
+        open_a();                                          // (nothing is loaded in the first step's first chunk: its units are the prologue's)
+        for (int s = 0; s < steps; ++s) {
+            const uint32_t na = after(ub), nb = after(na);
+#pragma unroll
+            for (int kc = 0; kc < NKC; ++kc) {
+                const int buf = kc & 1;
+                if (kc == NKC - 1) {
+                    // this wave has read the step's last fragments, and the next step's units have landed but for A of the step behind
+                    wait_vmcnt<NL>();
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);
+                    asm volatile("s_barrier" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);
+                    open_b();
+                }
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        const int slot = i * TN + j;
+                        grp_mma<T>(acc.c[i][j], fb[buf][j], fa[buf][i]);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int q = slot * PER; q < (slot + 1) * PER && q < READS; ++q)
+                            read_one(buf ^ 1, q, kc + 1 < NKC ? ua : na, kc + 1 < NKC ? ub : nb, (kc + 1) % NKC);
+                        if (kc == NKC - 1 || (kc == 0 && s > 0)) {
+#pragma unroll
+                            for (int l = 0; l < NL; ++l)
+                                if ((l * SLOTS + SLOTS / 2) / NL == slot) {
+                                    if (kc == 0) load_a(l); else load_b(l);
+                                }
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if constexpr (FORM == kWeights) {
+                        if (take_sums) sums[i] += grp_sum<ES>(fa[buf][i]);
+                    }
+                }
+                if (kc == NKC - 1) {
+                    close_b();
+                    open_a();
+                }
+                if (kc == 0 && s > 0) close_a();
+            }
+            ua = na;
+            ub = nb;
+        }
+        acc.join();
+        wait_vmcnt<0>();                                   // (the units behind the last step's)
+        __syncthreads();                                   // the last units' readers are through
+        if (take_sums) grp_store_sums(p, g, sums, wm * WTM, lane);
+        grp_epilogue<T, FORM, TM, TN>(p, g, acc, lds + wave * kStageBytes, wm * WTM, wn * WTN, lane);
+    }
+};
+
+template <typename K>
 __global__ __launch_bounds__(K::THREADS, K::kLds > 80 * 1024 ? (K::NW + 3) / 4 : 1) void grouped_kernel(const GroupedParams p)
 {
     extern __shared__ uint4 smem_u4[];
     GrpProblem only;
-    if (!grp_problem<T, FORM, BM, BN>(p, threadIdx.x & 63, only)) return;
+    if (!grp_problem<typename K::type, K::kForm, K::kBM, K::kBN>(p, threadIdx.x & 63, only)) return;
     K::tile(p, only, (char *)smem_u4);
 }
 
@@ -1183,8 +1318,8 @@ __device__ __forceinline__ bool grp_unit(const GroupedParams &p, const GrpSchedu
 constexpr int kLargeThreads = 512;
 
 template <typename T, int FORM> struct GrpLarge {
-    using Large = GrpKernel<T, FORM, 256, 256, 2, 4, 64, 4>;
-    using Small = GrpKernel<T, FORM, 128, 128, 2, 4, 128, 4>;
+    using Large = GrpWide<T, FORM>;
+    using Small = GrpRing<T, FORM, 128, 128, 2, 4, 128, 4>;
     static_assert(Large::THREADS == kLargeThreads && Small::THREADS == kLargeThreads, "threads");
     static constexpr int kLds = Large::kLds > Small::kLds ? Large::kLds : Small::kLds;
 };
@@ -1279,14 +1414,13 @@ bool grp_streams(const GroupedParams &p)
     return (bits % 16 == 0 || (p.flags & kGrpPacked)) && p.lda <= (1 << 22) && p.ldb <= (1 << 22) && p.ldy <= (1 << 22) && p.ldmask <= (1 << 22);
 }
 
-template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB, int NS>
+template <typename K>
 hipError_t grouped_tiles(GroupedParams p, hipStream_t st)
 {
-    using K = GrpKernel<T, FORM, BM, BN, WGM, WGN, BKB, NS>;
     unsigned grid;
-    hipError_t e = grp_grid<FORM, BM, BN>(p, K::THREADS, &grid);
+    hipError_t e = grp_grid<K::kForm, K::kBM, K::kBN>(p, K::THREADS, &grid);
     if (e != hipSuccess || !grid) return e;
-    auto kern = grouped_kernel<K, T, FORM, BM, BN>;
+    auto kern = grouped_kernel<K>;
     static bool attr_set = false;
     if (!attr_set) {
         e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
@@ -1355,7 +1489,7 @@ inline int grp_choose(const GroupedParams &p, int ES, GrpTime *time)
 {
     const double places = p.places, units = std::ceil((double)p.red * ES / 128.0 / (FORM == kWeights ? p.groups : 1)), n64 = grp_tiles<FORM>(p, 64, 64);
     const GrpTime t[4] = {n64 <= places ? GrpTime{2.0, 0.21 * units} : GrpTime{1e30, 0.0}, grp_rounds(n64, 2 * places, units, 3.0, 0.43),
-                          grp_rounds(grp_tiles<FORM>(p, 128, 128), places, units, 3.3, 0.54), grp_rounds(grp_tiles<FORM>(p, 256, 256), places, units, 8.0, 1.73)};
+                          grp_rounds(grp_tiles<FORM>(p, 128, 128), places, units, 3.3, 0.54), grp_rounds(grp_tiles<FORM>(p, 256, 256), places, units, 8.6, 1.57)};
     int best = 0;
     for (int i = 1; i < 4; ++i)
         if (t[i].fixed + t[i].reduction < t[best].fixed + t[best].reduction) best = i;
@@ -1384,16 +1518,16 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
     }
     if constexpr (ES == 4) {
         // (as above; 5000 rows of 5 groups, 2048 x 4096: forward 695 us in tiles of 64x64, 762 of 128x128, by the weights 682 and 657)
-        return FORM == kWeights && grp_tiles<FORM>(p, 128, 128) >= 4 * places ? grouped_tiles<T, FORM, 128, 128, 2, 4, 128, 4>(p, st)
-                                                                               : grouped_tiles<T, FORM, 64, 64, 2, 2, 128, 4>(p, st);
+        return FORM == kWeights && grp_tiles<FORM>(p, 128, 128) >= 4 * places ? grouped_tiles<GrpRing<T, FORM, 128, 128, 2, 4, 128, 4>>(p, st)
+                                                                               : grouped_tiles<GrpRing<T, FORM, 64, 64, 2, 2, 128, 4>>(p, st);
     } else {
         GrpTime time;
         switch (grp_choose<FORM>(p, ES, &time)) {
-            case kDeep: return grouped_tiles<T, FORM, 64, 64, 2, 2, 256, 4>(p, st);
-            case kShallow: return grouped_tiles<T, FORM, 64, 64, 2, 2, 128, 4>(p, st);
-            case kMiddle: return grouped_tiles<T, FORM, 128, 128, 2, 4, 128, 4>(p, st);
+            case kDeep: return grouped_tiles<GrpRing<T, FORM, 64, 64, 2, 2, 256, 4>>(p, st);
+            case kShallow: return grouped_tiles<GrpRing<T, FORM, 64, 64, 2, 2, 128, 4>>(p, st);
+            case kMiddle: return grouped_tiles<GrpRing<T, FORM, 128, 128, 2, 4, 128, 4>>(p, st);
         }
-        if constexpr (FORM == kWeights) return grouped_tiles<T, FORM, 256, 256, 2, 4, 64, 4>(p, st);
+        if constexpr (FORM == kWeights) return grouped_tiles<GrpWide<T, FORM>>(p, st);
         else return grouped_large<T, FORM>(p, st);
     }
 }

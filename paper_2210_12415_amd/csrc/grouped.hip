@@ -89,8 +89,8 @@ void matrices(int form, int es, GroupedParams &p, Matrix &a, Matrix &b)
     b = {&p.b, &p.ldb, form == kWeights ? p.red : (int64_t)p.groups * (form == kForward ? p.cols : p.red), (int64_t)(form == kForward ? p.red : p.cols) * es};
 }
 
-// Bytes for operands laid out anew, 0 where that does not pay.  The kernel for any alignment takes 1.6 times as long as those for whole chunks at
-// least, but for what a tile costs whatever its reduction is, and that has to outweigh a copy (8191^3 in 8 bits 911 us, 536 laid out anew; 5000 rows of 5
+// Bytes for operands laid out anew, 0 where that does not pay.  The kernel for any alignment takes 1.8 times as long as those for whole chunks at
+// least, but for what a tile costs whatever its reduction is, and that has to outweigh a copy (8191^3 in 8 bits 911 us, 500 laid out anew; 5000 rows of 5
 // experts, 2047 x 4095 bf16, by the weights 155 and 130; 1001 rows of 13, 515 x 1030, 16 and 26).
 size_t pack_bytes(int form, int dtype, GroupedParams &p)
 {
@@ -111,7 +111,7 @@ size_t pack_bytes(int form, int dtype, GroupedParams &p)
     if (form == kForward) grp_choose<kForward>(p, es, &t);
     else if (form == kInput) grp_choose<kInput>(p, es, &t);
     else grp_choose<kWeights>(p, es, &t);
-    return cost < 0.7 * t.reduction ? need : 0;
+    return cost < 0.8 * t.reduction ? need : 0;
 }
 
 hipError_t pack(Matrix &m, char *to, hipStream_t st)

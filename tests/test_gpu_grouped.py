@@ -557,6 +557,30 @@ def small_integers(shape, dtype, seed):
     return torch.randint(-3, 4, shape, generator=g, device="cuda").to(dtype)
 
 
+@pytest.mark.parametrize("red", [8, 64, 72, 136, 192, 264, 320, 400])
+@pytest.mark.parametrize("dtype", [alt.BF16, alt.I8])
+def test_large_tiles_with_any_number_of_steps(h, dtype, red):
+    """Fewer steps of the reduction than the loads run ahead, as many, and some more; all sums exact."""
+    M, N, td = 4093, 4096, TORCH[dtype]
+    red *= 2 if dtype == alt.I8 else 1
+    o = make_offsets([0, M])
+    x, w, y = small_integers((M, red), td, 1), small_integers((1, N, red), td, 2), Canary(M, N, torch.float32)
+    one = dict(a_scale=torch.ones(M, device="cuda"), b_scale=torch.ones(N, device="cuda")) if dtype == alt.I8 else {}
+    h.gemm_grouped(alt.grouped_desc(M, 1, N, red, in_dtype=dtype, out_dtype=alt.F32), x, w, o, y, **one)
+    torch.cuda.synchronize()
+    assert y.untouched() and torch.equal(y.t, x.float() @ w[0].float().T)
+    if dtype == alt.I8:
+        return
+    dy, w, dx = small_integers((M, red), td, 3), small_integers((1, red, N), td, 4), Canary(M, N, torch.float32)
+    h.gemm_grouped_dx(alt.grouped_desc(M, 1, red, N, out_dtype=alt.F32), dy, w, o, dx)
+    torch.cuda.synchronize()
+    assert dx.untouched() and torch.equal(dx.t, dy.float() @ w[0].float())
+    x, dy, dw, db = small_integers((red, 4088), td, 5), small_integers((red, N), td, 6), Canary(N, 4088, torch.float32), torch.empty(N, device="cuda")
+    h.gemm_grouped_dw(alt.grouped_desc(red, 1, N, 4088, out_dtype=alt.F32, epilogue=alt.EPI_BIAS), x, dy, make_offsets([0, red]), dw, dbias=db)
+    torch.cuda.synchronize()
+    assert dw.untouched() and torch.equal(dw.t, dy.float().T @ x.float()) and torch.equal(db, dy.float().sum(0))
+
+
 def far_apart(rows, cols, stride, dtype, seed, offset=0):
     """Rows `stride` elements apart in a buffer of more than 4 GiB, of which only they are written."""
     buf = torch.empty(rows * stride + offset, dtype=dtype, device="cuda")
