@@ -503,7 +503,7 @@ alt_status_t alt_gemm_variant_name(alt_handle_t h, const alt_gemm_desc_t *d, int
  *   q[m,k]   = x[m,k] / scale[m] to the nearest whole number, ties to even (-127 .. 127).
  * A scale of 16 bits makes q * scale exact in fp32, so that every q is the one the formula names.  A row that holds an infinity or a
  * NaN gets scale NaN and q = 0: products with it are NaN.  x_stride, q_stride: elements between rows, 0 = cols.  The buffers need the
- * alignment of their elements only, and must not overlap.  Asynchronous on `stream`. */
+ * alignment of their elements only, and must not overlap.  2^23 rows at most.  Asynchronous on `stream`. */
 alt_status_t alt_quantize_rows(alt_handle_t h, alt_dtype_t dtype, int64_t rows, int64_t cols, const void *x, int64_t x_stride,
                                void *q, int64_t q_stride, float *scale, void *stream);
 
@@ -527,7 +527,8 @@ alt_status_t alt_gemm_i8_workspace_size(alt_handle_t h, const alt_gemm_i8_desc_t
 /* A layer of experts: `rows` tokens in the order of their experts, expert e owning the rows [offsets[e], offsets[e+1]).  `offsets` is an
  * int32 array of groups + 1 on the device, not decreasing, read when the kernels run; an expert may own no row.  Rows before offsets[0]
  * and from offsets[groups] on belong to no expert.  (Offsets outside 0 .. rows are clamped; with offsets out of order results are
- * unspecified, but nothing outside the buffers is read or written.) */
+ * unspecified, but nothing outside the buffers is read or written.)  2^30 rows, 2^20 experts and 2^22 elements between rows at most, here and
+ * in alt_gemm_i8. */
 typedef struct {
     int64_t rows, N, K;           /* rows may be 0 */
     int64_t lda, ldb, ldc;        /* elements between rows of a and dx; of b and dw (an expert's matrix is N * ldb elements); of y and dy; 0 = dense */
