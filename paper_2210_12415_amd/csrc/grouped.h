@@ -732,7 +732,9 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
 // Chunks of 16 bytes are loaded at whatever address they start at.  Rows and columns that do not exist repeat the tile's last ones (their sums are
 // never stored), or, where the outer index is contiguous, the last tile is moved back to end with the matrix (what two tiles both compute they
 // compute alike); so only the reduction's last step has chunks of which a part exists.  Loads are two steps ahead: those of step s + 2 go out
-// before step s is computed, and reach LDS behind it a step later.
+// before step s is computed, and reach LDS behind it a step later (four steps ahead: 12.8 us for 12.0 at 64 x 1001 x 2049 in 8 bits).  WGK = 2: twice
+// the waves, halves of every step's chunks to each half of them, whose sums meet in LDS.  Bound in 8 and 16 bits by the issue of loads, LDS
+// writes and reads (5000 rows of 5 groups, 2047 x 4095, bf16 147 us, 0.57 PFLOP/s), in fp32 by the matrix instructions (690 us, 122 TFLOP/s).
 template <int ES, bool RED, int OUTER, int BKB, int THREADS>
 struct GrpLoader {
     using Op = GrpOperand<ES, RED, OUTER, BKB>;
@@ -755,6 +757,19 @@ struct GrpLoader {
             Op::slot(i * THREADS + t, row[i], elem[i]);
             voff[i] = (uint32_t)(RED ? min(row[i], outer - 1) : row[i]) * (uint32_t)ld + (uint32_t)(elem[i] * ES);
         }
+    }
+    // Steps from `base` on that are whole.
+    __device__ __forceinline__ int whole() const { return RED || outer_left >= OUTER ? max(left, 0) / Op::BK : 0; }
+    __device__ __forceinline__ void next()
+    {
+        base += RED ? (int64_t)BKB : ld * Op::BK;
+        left -= Op::BK;
+    }
+    __device__ __forceinline__ void load_whole(u32x4_t (&v)[NL])
+    {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) __builtin_memcpy(&v[i], base + voff[i], 16);
+        next();
     }
     __device__ __forceinline__ void load(u32x4_t (&v)[NL])
     {
@@ -787,27 +802,42 @@ struct GrpLoader {
             for (int i = 0; i < NL; ++i)
                 v[i] = grp_load_chunk<ES>(base + voff[i], RED ? left - elem[i] : row[i] < left ? outer_left - elem[i] : 0);
         }
-        base += RED ? (int64_t)BKB : ld * Op::BK;
-        left -= Op::BK;
+        next();
     }
 };
 
-template <typename T, int FORM, int BM, int BN, int WGM, int WGN>
-__global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const GroupedParams p)
+// Registers 4 q to 4 q + 3 of a matrix tile's sums.
+template <typename ACC>
+__device__ __forceinline__ u32x4_t grp_quarter(const ACC &c, int q)
 {
-    constexpr int ES = GrpTraits<T>::ES, BKB = 128, THREADS = 64 * WGM * WGN;
-    constexpr int WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32, NKC = BKB / 32;
+    const auto v = __builtin_shufflevector(c, c, 0, 1, 2, 3), w = __builtin_shufflevector(c, c, 4, 5, 6, 7), x = __builtin_shufflevector(c, c, 8, 9, 10, 11),
+               y = __builtin_shufflevector(c, c, 12, 13, 14, 15);
+    return __builtin_bit_cast(u32x4_t, q == 0 ? v : q == 1 ? w : q == 2 ? x : y);
+}
+template <typename ACC>
+__device__ __forceinline__ void grp_add_quarter(ACC &c, int q, const u32x4_t &v)
+{
+    const auto w = __builtin_bit_cast(decltype(__builtin_shufflevector(c, c, 0, 1, 2, 3)), v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[q * 4 + e] += w[e];
+}
+
+template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int WGK>
+__global__ __launch_bounds__(64 * WGM * WGN * WGK) void grouped_any_kernel(const GroupedParams p)
+{
+    constexpr int ES = GrpTraits<T>::ES, BKB = 128, THREADS = 64 * WGM * WGN * WGK;
+    constexpr int WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32, NKC = BKB / 32, TILES = WGM * WGN;
     using LA = GrpLoader<ES, FORM != kWeights, BM, BKB, THREADS>;
     using LB = GrpLoader<ES, FORM == kForward, BN, BKB, THREADS>;
     using A = typename LA::Op;
     using B = typename LB::Op;
     constexpr int STAGE = A::BYTES + B::BYTES;
-    static_assert(WGM * WGN * kStageBytes <= 2 * STAGE, "staging");
+    static_assert(TILES * kStageBytes <= 2 * STAGE && (WGK == 1 || (WGK == 2 && TM * TN == 1 && FORM != kWeights && TILES * 4096 <= 2 * STAGE)), "staging");
 
     extern __shared__ uint4 smem_u4[];
     char *lds = (char *)smem_u4;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int wm = wave / WGN, wn = wave % WGN;
+    const int wk = wave / TILES, tile = wave % TILES, wm = tile / WGN, wn = tile % WGN;
     GrpProblem g;
     if (!grp_problem<T, FORM, BM, BN>(p, lane, g)) return;
     if (FORM != kForward && g.col0 + BN > p.cols && p.cols >= BN) {
@@ -823,7 +853,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const Group
     LB lb;
     la.start(g.a0, p.lda, g.row_end - g.row0, g.red, t);
     lb.start(g.b0, p.ldb, p.cols - g.col0, g.red, t);
-    u32x4_t ra[2][LA::NL], rb[2][LB::NL];
+    constexpr int PF = 2;
+    u32x4_t ra[PF][LA::NL], rb[PF][LB::NL];
     auto store = [&](int stage, const u32x4_t (&va)[LA::NL], const u32x4_t (&vb)[LB::NL]) {
         char *d = lds + stage * STAGE;
 #pragma unroll
@@ -844,7 +875,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const Group
     auto compute = [&](int stage) {
         const char *d = lds + stage * STAGE;
 #pragma unroll
-        for (int kc = 0; kc < NKC; ++kc) {
+        for (int c = 0; c < NKC / WGK; ++c) {
+            const int kc = wk * (NKC / WGK) + c;
             u32x4_t fa[TM], fb[TN];
 #pragma unroll
             for (int i = 0; i < TM; ++i) fa[i] = A::read(d, A::frag(wm * WTM + i * 32, kc, lane));
@@ -862,30 +894,61 @@ __global__ __launch_bounds__(64 * WGM * WGN) void grouped_any_kernel(const Group
             }
         }
     };
-    // step s in stage s & 1, its successor's operands in registers of parity (s + 1) & 1
-    auto step = [&](int s, auto PARITY) {
+    // Step s in stage s & 1, its operands having come through registers s % PF.  WHOLE: steps s + PF and s + 1 exist, and s + PF is whole.
+    auto step = [&](int s, auto PARITY, auto WHOLE) {
         constexpr int q = decltype(PARITY)::value;
-        __syncthreads();                                   // stage q is written, stage q ^ 1's last readers are through
-        la.load(ra[q]);                                    // of step s + 2
-        lb.load(rb[q]);
-        compute(q);
-        if (s + 1 < steps) store(q ^ 1, ra[q ^ 1], rb[q ^ 1]);
+        __syncthreads();                                   // stage s & 1 is written, the other stage's last readers are through
+        if constexpr (decltype(WHOLE)::value) {
+            la.load_whole(ra[q]);
+            lb.load_whole(rb[q]);
+        } else {
+            la.load(ra[q]);
+            lb.load(rb[q]);
+        }
+        compute(q & 1);
+        if (decltype(WHOLE)::value || s + 1 < steps) store((q & 1) ^ 1, ra[(q + 1) % PF], rb[(q + 1) % PF]);
     };
     if (steps > 0) {
-        la.load(ra[0]);
-        lb.load(rb[0]);
-        la.load(ra[1]);
-        lb.load(rb[1]);
+#pragma unroll
+        for (int i = 0; i < PF; ++i) {
+            la.load(ra[i]);
+            lb.load(rb[i]);
+        }
         store(0, ra[0], rb[0]);
     }
-    for (int s = 0; s < steps; s += 2) {
-        step(s, std::integral_constant<int, 0>{});
-        if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{});
-    }
+    const int whole = min(la.whole(), lb.whole());
+    int s = 0;
+    auto round = [&](auto WHOLE) {
+        step(s, std::integral_constant<int, 0>{}, WHOLE);
+        if (decltype(WHOLE)::value || s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{}, WHOLE);
+        s += PF;
+    };
+    // (without branches around the loads, so that no step waits for more of them than it needs)
+    while (s + PF <= whole) round(std::true_type{});
+    while (s < steps) round(std::false_type{});
     acc.join();
     __syncthreads();                                       // the last stage's readers are through
+    if constexpr (WGK > 1) {
+        char *mine = lds + tile * TM * TN * 4096;
+        if (wk > 0) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) *(u32x4_t *)(mine + ((i * TN + j) * 4 + q) * 1024 + lane * 16) = grp_quarter(acc.c[i][j][0], q);
+        }
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) grp_add_quarter(acc.c[i][j][0], q, *(const u32x4_t *)(mine + ((i * TN + j) * 4 + q) * 1024 + lane * 16));
+    }
     if (take_sums) grp_store_sums(p, g, sums, wm * WTM, lane);
-    grp_epilogue<T, FORM, TM, TN>(p, g, acc, lds + wave * kStageBytes, wm * WTM, wn * WTN, lane);
+    grp_epilogue<T, FORM, TM, TN>(p, g, acc, lds + tile * kStageBytes, wm * WTM, wn * WTN, lane);
 }
 
 // ---- the kernel for operands of whole 16-byte chunks: global memory straight into LDS -------------------------------------------
@@ -1378,13 +1441,13 @@ hipError_t grp_grid(GroupedParams &p, int threads, unsigned *grid)
     return hipSuccess;
 }
 
-template <typename T, int FORM, int BM, int BN, int WGM, int WGN>
+template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int WGK>
 hipError_t grouped_any(GroupedParams p, hipStream_t st)
 {
     unsigned grid;
-    const hipError_t e = grp_grid<FORM, BM, BN>(p, 64 * WGM * WGN, &grid);
+    const hipError_t e = grp_grid<FORM, BM, BN>(p, 64 * WGM * WGN * WGK, &grid);
     if (e != hipSuccess || !grid) return e;
-    hipLaunchKernelGGL((grouped_any_kernel<T, FORM, BM, BN, WGM, WGN>), dim3(grid), dim3(64 * WGM * WGN), 2 * (BM + BN) * 128, st, p);
+    hipLaunchKernelGGL((grouped_any_kernel<T, FORM, BM, BN, WGM, WGN, WGK>), dim3(grid), dim3(64 * WGM * WGN * WGK), 2 * (BM + BN) * 128, st, p);
     return hipGetLastError();
 }
 
@@ -1505,16 +1568,24 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
     if constexpr (FORM == kForward) {
         // (columns in twos, four waves, where that fills the chip, else one by one and eight waves to a reduction: 16 x 4096 x 4096 6.6 against 8.5 us,
         // 32 x 4096 x 4096 10.4 against 8.6)
-        if (grp_is_few(p)) return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 8, 2>(p, st) : grouped_few<T, 2, 4, 2>(p, st);
+        // Operands of any alignment go that way too while its tiles are few: 128 x 1001 x 2049 in 8 bits (504 tiles) 7.8 us for 11.0, 64 fp32 rows,
+        // 2047 x 2049 (512), 15.4 for 38.8; 40 x 4095 x 4097 in 8 bits (768) 18.2 for 17.4.
+        if (grp_is_few(p) || (!grp_streams<T, FORM>(p) && grp_tiles<FORM>(p, 16, 16) <= 2 * places))
+            return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 8, 2>(p, st) : grouped_few<T, 2, 4, 2>(p, st);
     }
     if (!grp_streams<T, FORM>(p)) {
         // Tiles of 128x128 once they fill three quarters of the chip: 1000 x 3884 x 1115 in 8 bits 24.5 us, in tiles of 64x64 31.1; 2048 x 770 x 3073
         // (112 tiles) 37.4 and 26.8.  In fp32 the matrix cores are the bound, and small tiles leave none idle: 1001 rows of 13 groups, 515 x 1030, 29
         // against 73 us, 5000 rows of 5 groups, 2047 x 4095, by the rows 720 against 827.
         if constexpr (ES < 4) {
-            if (grp_tiles<FORM>(p, 128, 128) >= 0.75 * places) return grouped_any<T, FORM, 128, 128, 2, 4>(p, st);
+            if (grp_tiles<FORM>(p, 128, 128) >= 0.75 * places) return grouped_any<T, FORM, 128, 128, 2, 4, 1>(p, st);
         }
-        return grouped_any<T, FORM, 64, 64, 2, 2>(p, st);
+        // While each compute unit has two tiles at most, twice the waves, which share every step's chunks: 64 x 1001 x 2049 in 8 bits 11.0 us for 12.1,
+        // 1001 fp32 rows of 13 groups, 515 x 1030, 25.2 for 26.9; at 5000 rows, 2047 x 4095, 697 and 693.
+        if constexpr (FORM != kWeights) {
+            if (grp_tiles<FORM>(p, 64, 64) <= 2 * places) return grouped_any<T, FORM, 64, 64, 2, 2, 2>(p, st);
+        }
+        return grouped_any<T, FORM, 64, 64, 2, 2, 1>(p, st);
     }
     if constexpr (ES == 4) {
         // (as above; 5000 rows of 5 groups, 2048 x 4096: forward 695 us in tiles of 64x64, 762 of 128x128, by the weights 682 and 657)

@@ -49,28 +49,48 @@ size_t in_size(int dt) { return dt == ALT_I8 ? 1 : dtype_size(dt); }
 
 // ---- operands whose rows are not whole 16-byte chunks, laid out anew -------------------------------------------------------------
 
-// dst[r] = src[r] filled up with zeros to `dst_bytes` a row (a multiple of 16).  A thread moves 32 bytes: the eight dwords they start in and the one
-// they end in, shifted together.  Bound by memory: 33 MB of 4099-byte rows in 15 us.
-__global__ __launch_bounds__(256) void grp_pack_kernel(const char *src, int64_t src_ld, int bytes, char *dst, int dst_bytes, uint32_t pieces, FastDiv per_row, uint32_t row0)
+// Rows of a matrix that are laid out anew: dst[r] = src[r] filled up with zeros to `dst_bytes` (a multiple of 16), in pieces of 32 bytes.
+struct PackJob {
+    const char *src;
+    char *dst;
+    int64_t ld;
+    int bytes, dst_bytes;
+    uint32_t pieces;
+    FastDiv per_row;
+};
+
+// A thread moves a piece: the eight dwords it starts in and the one it ends in, shifted together; behind a row's last byte no dword is touched.
+// Two matrices to a launch.  Bound by memory: MEASURE.
+__global__ __launch_bounds__(256) void grp_pack_kernel(const PackJob first, const PackJob second, uint32_t first_blocks)
 {
-    const uint32_t i = blockIdx.x * 256u + threadIdx.x;
-    if (i >= pieces) return;
-    const uint32_t r = fast_div(i, per_row), at = (i - r * per_row.d) * 32u;
-    const char *p = src + (int64_t)(row0 + r) * src_ld + at;
-    char *d = dst + (int64_t)(row0 + r) * dst_bytes + at;
-    const int exist = bytes - (int)at;
-    u32x4_t v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    const bool is_first = blockIdx.x < first_blocks;
+    const PackJob &j = is_first ? first : second;
+    const uint32_t i = (blockIdx.x - (is_first ? 0u : first_blocks)) * 256u + threadIdx.x;
+    if (i >= j.pieces) return;
+    const uint32_t r = fast_div(i, j.per_row), at = (i - r * j.per_row.d) * 32u;
+    const char *p = j.src + (int64_t)r * j.ld + at;
+    char *d = j.dst + (int64_t)r * j.dst_bytes + at;
+    const int exist = j.bytes - (int)at;
+    GrpPair<false> w;
     if (exist >= 32) {
-        GrpPair<false> w;
         w.load(p);
-        v[0] = w.chunk(0, (uint32_t)(uintptr_t)p);
-        v[1] = w.chunk(1, (uint32_t)(uintptr_t)p);
     } else {
-        v[0] = grp_load_chunk<1>(p, exist);
-        v[1] = grp_load_chunk<1>(p + 16, exist - 16);
+        const char *dword = (const char *)((uintptr_t)p & ~(uintptr_t)3);
+        uint32_t v[9];
+#pragma unroll
+        for (int q = 0; q < 9; ++q) v[q] = dword + q * 4 < p + exist ? *(const uint32_t *)(dword + q * 4) : 0u;
+        w.lo = (u32x4_t){v[0], v[1], v[2], v[3]};
+        w.hi = (u32x4_t){v[4], v[5], v[6], v[7]};
+        w.more = v[8];
+    }
+    u32x4_t v[2] = {w.chunk(0, (uint32_t)(uintptr_t)p), w.chunk(1, (uint32_t)(uintptr_t)p)};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const int left = exist - q * 4;                    // bytes of this dword that exist
+        v[q / 4][q % 4] = left >= 4 ? v[q / 4][q % 4] : left > 0 ? v[q / 4][q % 4] & ((1u << left * 8) - 1u) : 0u;
     }
     *(u32x4_t *)d = v[0];
-    if ((int)at + 16 < dst_bytes) *(u32x4_t *)(d + 16) = v[1];
+    if ((int)at + 16 < j.dst_bytes) *(u32x4_t *)(d + 16) = v[1];
 }
 
 struct Matrix {
@@ -79,6 +99,7 @@ struct Matrix {
     int64_t rows, bytes;                   // rows, and bytes of each that exist
     int64_t packed() const { return (bytes + 15) / 16 * 16; }
     int64_t size() const { return rows * packed(); }
+    int64_t pieces() const { return rows * ((packed() + 31) / 32); }
     bool whole() const { return ((uint64_t)*p | (uint64_t)*ld | (uint64_t)bytes) % 16 == 0; }
 };
 
@@ -89,9 +110,11 @@ void matrices(int form, int es, GroupedParams &p, Matrix &a, Matrix &b)
     b = {&p.b, &p.ldb, form == kWeights ? p.red : (int64_t)p.groups * (form == kForward ? p.cols : p.red), (int64_t)(form == kForward ? p.red : p.cols) * es};
 }
 
-// Bytes for operands laid out anew, 0 where that does not pay.  The kernel for any alignment takes 1.8 times as long as those for whole chunks at
-// least, but for what a tile costs whatever its reduction is, and that has to outweigh a copy (8191^3 in 8 bits 911 us, 500 laid out anew; 5000 rows of 5
-// experts, 2047 x 4095 bf16, by the weights 155 and 130; 1001 rows of 13, 515 x 1030, 16 and 26).
+// Bytes for operands laid out anew, 0 where that does not pay: the copy is held against what the kernels for whole chunks take for the reduction.  8191 x
+// 8191 x 8191 in 8 bits takes 500 us so, 852 in the kernel for any alignment; 5000 rows of 5 experts, 2047 x 4095 bf16, by the rows 126 and 137
+// (the copy 0.62 of the other's time, the forward product's 0.73: 145 and 147), 1497 x 3424 x 1117 (0.56) 40 and 32.  By the weights a group's length is
+// the reduction, and uneven groups cost the kernel for any alignment more: 4685 rows of 24 experts, 91 x 2432, 17.6 and 23.1 (0.59); 5000 rows of 5
+// 133 and 148 (0.45); 3424 x 1117 of 1497 rows 27.3 and 25.7 (0.28).
 size_t pack_bytes(int form, int dtype, GroupedParams &p)
 {
     if (dtype == ALT_F32 || p.rows == 0 || p.red == 0) return 0;
@@ -103,7 +126,7 @@ size_t pack_bytes(int form, int dtype, GroupedParams &p)
     double cost = 0;
     for (const Matrix *m : {&a, &b})
         if (!m->whole()) {
-            if (m->packed() > (1 << 22) || m->rows > 0x7fffffff) return 0;
+            if (m->packed() > (1 << 22) || m->rows > (1 << 30) || m->pieces() > (1 << 30)) return 0;
             need += (size_t)m->size();
             cost += 2.0 + 2.0 * (double)m->size() / 4.5e6;
         }
@@ -111,24 +134,24 @@ size_t pack_bytes(int form, int dtype, GroupedParams &p)
     if (form == kForward) grp_choose<kForward>(p, es, &t);
     else if (form == kInput) grp_choose<kInput>(p, es, &t);
     else grp_choose<kWeights>(p, es, &t);
-    return cost < 0.8 * t.reduction ? need : 0;
+    return cost < (form == kWeights ? 0.8 : 0.55) * t.reduction ? need : 0;
 }
 
-hipError_t pack(Matrix &m, char *to, hipStream_t st)
+hipError_t pack(Matrix &a, Matrix &b, char *to, hipStream_t st)
 {
-    const int64_t per_row = (m.packed() + 31) / 32;
-    // (a launch's index has 31 bits)
-    const int64_t most = (1ll << 30) / per_row;
-    for (int64_t r = 0; r < m.rows; r += most) {
-        const int64_t n = std::min(most, m.rows - r);
-        hipLaunchKernelGGL(grp_pack_kernel, dim3((unsigned)((n * per_row + 255) / 256)), dim3(256), 0, st, (const char *)*m.p, *m.ld, (int)m.bytes, to, (int)m.packed(),
-                           (uint32_t)(n * per_row), make_fastdiv((uint32_t)per_row), (uint32_t)r);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    *m.p = to;
-    *m.ld = m.packed();
-    return hipSuccess;
+    PackJob jobs[2] = {};
+    uint32_t blocks[2] = {0, 0};
+    int n = 0;
+    for (Matrix *m : {&a, &b})
+        if (!m->whole()) {
+            jobs[n] = {(const char *)*m->p, to, *m->ld, (int)m->bytes, (int)m->packed(), (uint32_t)m->pieces(), make_fastdiv((uint32_t)((m->packed() + 31) / 32))};
+            blocks[n++] = ((uint32_t)m->pieces() + 255) / 256;
+            *m->p = to;
+            *m->ld = m->packed();
+            to += m->size();
+        }
+    hipLaunchKernelGGL(grp_pack_kernel, dim3(blocks[0] + blocks[1]), dim3(256), 0, st, jobs[0], jobs[1], blocks[0]);
+    return hipGetLastError();
 }
 
 // What the problem takes of its operands' and outputs' extents, strides in bytes.
@@ -160,13 +183,7 @@ alt_status_t run(alt_handle_t h, const char *call, int dtype, int form, GroupedP
         if (need && need + (ws - (uintptr_t)workspace) <= ws_bytes) {
             Matrix a, b;
             matrices(form, dtype == ALT_I8 ? 1 : 2, p, a, b);
-            char *to = (char *)ws;
-            for (Matrix *m : {&a, &b})
-                if (!m->whole()) {
-                    const int64_t size = m->size();
-                    ALT_CHECK_HIP(h, pack(*m, to, st));
-                    to += size;
-                }
+            ALT_CHECK_HIP(h, pack(a, b, (char *)ws, st));
             p.flags |= kGrpPacked;
         }
     }
