@@ -1018,12 +1018,12 @@ struct GrpStream {
     }
 };
 
-// Tiles of 64x64 and 128x128: a workgroup's operands run through a ring of NS stages in LDS.  At the barrier of step s the stages of steps s and
+// Tiles of 64x64, 128x64 and 128x128: a workgroup's operands run through a ring of NS stages in LDS.  At the barrier of step s the stages of steps s and
 // s + 1 have landed and every wave has read stage s - 1 for the last time; then the loads of step s + NS - 1 go out into that stage, and each
 // chunk's fragments are read three chunks before they are used, across the barrier too (a read takes about as long as four matrix instructions).
 // A wave issues in order, and a matrix instruction hides eight other instructions at most: behind each stand a few operand reads and loads, and
 // the order is pinned.  Bound by latency on small calls (the loads of three steps in flight are what hides it: 64 x 4096 x 4096 in 8 bits 9.6 us,
-// 1.8 TB/s), by the matrix instructions and the loads' issue above (2048 x 768 x 3072 in 8 bits 13.8 us, 0.7 POP/s).
+// 1.8 TB/s), by operand delivery into LDS above (2048 x 768 x 3072 in 8 bits 13.3 us, 80 GB/s to a compute unit).
 template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB, int NS>
 struct GrpRing {
     using type = T;
@@ -1562,18 +1562,20 @@ inline bool grp_is_few(const GroupedParams &p)
     return p.rows <= 32 * spans;
 }
 
-// Tiles of 64x64 with a deep ring (one to a compute unit) or a shallow one (two), of 128x128, of 256x256, for operands of 8 or 16 bits; the constants
-// are those of 8-bit products of 32 .. 8192 rows, 768 .. 8192 columns and reductions of 512 .. 8192, which they give to 10 %; bf16 has the same
-// tiles in bytes.
-enum { kDeep, kShallow, kMiddle, kLarge };
+// Tiles of 64x64 with a deep ring (one to a compute unit) or a shallow one (two), of 128x64, of 128x128, of 256x256, for operands of 8 or 16 bits; the
+// constants are those of 8-bit products of 32 .. 8192 rows, 768 .. 8192 columns and reductions of 512 .. 8192, which they give to 10 %; bf16 has the
+// same tiles in bytes.  (128x64 for one round of the chip: 2048 x 1024 x 4096 17.2 us, 20.1 in tiles of 64x64, 19.9 of 128x128; the gradient by the rows
+// gains nothing: 2000 rows of 8, 768 x 1024, 10.1 and 9.4.)
+enum { kDeep, kShallow, kHalf, kMiddle, kLarge };
 template <int FORM>
 inline int grp_choose(const GroupedParams &p, int ES, GrpTime *time)
 {
     const double places = p.places, units = std::ceil((double)p.red * ES / 128.0 / (FORM == kWeights ? p.groups : 1)), n64 = grp_tiles<FORM>(p, 64, 64);
-    const GrpTime t[4] = {n64 <= places ? GrpTime{2.0, 0.21 * units} : GrpTime{1e30, 0.0}, grp_rounds(n64, 2 * places, units, 3.0, 0.43),
+    const GrpTime t[5] = {n64 <= places ? GrpTime{2.0, 0.21 * units} : GrpTime{1e30, 0.0}, grp_rounds(n64, 2 * places, units, 3.0, 0.43),
+                          FORM == kForward ? grp_rounds(grp_tiles<FORM>(p, 128, 64), places, units, 2.3, 0.33) : GrpTime{1e30, 0.0},
                           grp_rounds(grp_tiles<FORM>(p, 128, 128), places, units, 3.3, 0.54), grp_rounds(grp_tiles<FORM>(p, 256, 256), places, units, 8.6, 1.57)};
     int best = 0;
-    for (int i = 1; i < 4; ++i)
+    for (int i = 1; i < 5; ++i)
         if (t[i].fixed + t[i].reduction < t[best].fixed + t[best].reduction) best = i;
     *time = t[best];
     return best;
@@ -1615,6 +1617,9 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
         switch (grp_choose<FORM>(p, ES, &time)) {
             case kDeep: return grouped_tiles<GrpRing<T, FORM, 64, 64, 2, 2, 256, 4>>(p, st);
             case kShallow: return grouped_tiles<GrpRing<T, FORM, 64, 64, 2, 2, 128, 4>>(p, st);
+            case kHalf:
+                if constexpr (FORM == kForward) return grouped_tiles<GrpRing<T, FORM, 128, 64, 4, 2, 128, 4>>(p, st);
+                break;                                     // (of the forward product only)
             case kMiddle: return grouped_tiles<GrpRing<T, FORM, 128, 128, 2, 4, 128, 4>>(p, st);
         }
         if constexpr (FORM == kWeights) return grouped_tiles<GrpWide<T, FORM>>(p, st);
