@@ -1554,12 +1554,15 @@ inline GrpTime grp_rounds(double tiles, double places, double units, double fixe
     return {rounds * fixed, rounds * per_unit * units * (0.5 + 0.5 * tiles / (rounds * places))};
 }
 
-// Up to 32 rows each, the weights are what there is to read: 16 x 8192 x 8192 in 8 bits 14.8 us so, 39 us in tiles of 64 rows; at 33 to 64 rows
-// 64 x 4096 x 4096 takes 10.6 us so, 9.6 in tiles.
-inline bool grp_is_few(const GroupedParams &p)
+// Whether a forward product runs in tiles of 16 rows.  Up to 16 rows each, the weights are what there is to read, and they are read once: 16 x 4096 x
+// 4096 in 8 bits 6.6 us.  With more rows, where these tiles are so few that they all run at once, as the other kernels would leave most of the chip
+// idle: 64 x 1024 x 4096 (256 tiles) 6.6 us for 12.8, 512 x 64 x 4096 6.4 for 12.8; 32 x 8192 x 8192 (1024) 25.1 for 16.4, 64 x 3000 x 2048 (752) 8.4 for
+// 6.7.  In fp32 the others are slower and the line lies higher: 512 x 512 x 2048 (1024 tiles) 26.5 us for 42.8; 256 rows of 8 groups, 2048 x 2048
+// (2048), 51.5 for 47.2.
+inline bool grp_is_few(const GroupedParams &p, int ES)
 {
     const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows;
-    return p.rows <= 32 * spans;
+    return p.rows <= 16 * spans || grp_tiles<kForward>(p, 16, 16) <= (ES == 4 ? 4 : 2) * p.places;
 }
 
 // Tiles of 64x64 with a deep ring (one to a compute unit) or a shallow one (two), of 128x64, of 128x128, of 256x256, for operands of 8 or 16 bits; the
@@ -1589,17 +1592,15 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
     if constexpr (FORM == kForward) {
         // (columns in twos, four waves, where that fills the chip, else one by one and eight waves to a reduction: 16 x 4096 x 4096 6.6 against 8.5 us,
         // 32 x 4096 x 4096 10.4 against 8.6)
-        // Operands of any alignment go that way too while its tiles are few: 128 x 1001 x 2049 in 8 bits (504 tiles) 7.8 us for 11.0, 64 fp32 rows,
-        // 2047 x 2049 (512), 15.4 for 38.8; 40 x 4095 x 4097 in 8 bits (768) 18.2 for 17.4.
-        if (grp_is_few(p) || (!grp_streams<T, FORM>(p) && grp_tiles<FORM>(p, 16, 16) <= 2 * places))
+        if (grp_is_few(p, ES))
             return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 8, 2>(p, st) : grouped_few<T, 2, 4, 2>(p, st);
     }
     if (!grp_streams<T, FORM>(p)) {
-        // Tiles of 128x128 once they fill three quarters of the chip: 1000 x 3884 x 1115 in 8 bits 24.5 us, in tiles of 64x64 31.1; 2048 x 770 x 3073
-        // (112 tiles) 37.4 and 26.8.  In fp32 the matrix cores are the bound, and small tiles leave none idle: 1001 rows of 13 groups, 515 x 1030, 29
-        // against 73 us, 5000 rows of 5 groups, 2047 x 4095, by the rows 720 against 827.
+        // Tiles of 128x128 once they fill half the chip: 1500 x 1501 x 2049 in 8 bits (144 tiles) 21.8 us, in tiles of 64x64 27.2; 2048 x 770 x 3073 (112)
+        // 28.0 and 26.0.  In fp32 the matrix cores are the bound, and small tiles leave none idle: 1001 rows of 13 groups, 515 x 1030, 25 against 72 us,
+        // 5000 rows of 5 groups, 2047 x 4095, 708 against 760.
         if constexpr (ES < 4) {
-            if (grp_tiles<FORM>(p, 128, 128) >= 0.75 * places) return grouped_any<T, FORM, 128, 128, 2, 4, 1>(p, st);
+            if (grp_tiles<FORM>(p, 128, 128) >= 0.5 * places) return grouped_any<T, FORM, 128, 128, 2, 4, 1>(p, st);
         }
         // While each compute unit has two tiles at most, twice the waves, which share every step's chunks: 64 x 1001 x 2049 in 8 bits 11.0 us for 12.1,
         // 1001 fp32 rows of 13 groups, 515 x 1030, 25.2 for 26.9; at 5000 rows, 2047 x 4095, 697 and 693.

@@ -655,3 +655,41 @@ def test_quantize_rows_beyond_32_bits(h):
     torch.cuda.synchronize()
     want, scale = exact_rows(x)
     assert np.array_equal(q.cpu().numpy(), want) and np.array_equal(f64(s), scale)
+
+
+TILES = [([300], 1030, 272), ([1100], 1100, 256), ([1500], 1501, 528), ([40] * 40, 520, 256), ([33, 0, 700, 1, 129, 640], 1000, 144)]
+
+
+@pytest.mark.parametrize("counts,N,K", TILES, ids=["one_group", "one_round", "two_rounds", "many_groups", "uneven"])
+@pytest.mark.parametrize("pad", [0, 16, 1])
+@pytest.mark.parametrize("dtype", [alt.BF16, alt.F32, alt.I8])
+def test_tiles_of_every_size(h, counts, N, K, pad, dtype):
+    """More rows than tiles of 16 are for, at strides of whole chunks and not, with bias and ReLU; all sums exact."""
+    td, E, rows = TORCH[dtype], len(counts), sum(counts)
+    off = [0]
+    for c in counts:
+        off.append(off[-1] + c)
+    o, bias = make_offsets(off), torch.randint(-50, 50, (E, N), device="cuda").float()
+    x, w = matrix(small_integers((rows, K), torch.float32, 1), td, K + pad), matrix(small_integers((E, N, K), torch.float32, 2), td, K + pad)
+    one = dict(a_scale=torch.ones(rows, device="cuda"), b_scale=torch.ones(E, N, device="cuda")) if dtype == alt.I8 else {}
+    y = Canary(rows, N, torch.float32, N + pad)
+    d = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=alt.F32, epilogue=alt.EPI_BIAS | alt.EPI_RELU, lda=K + pad, ldb=K + pad, ldc=N + pad)
+    h.gemm_grouped(d, x, w, o, y, bias=bias, **one)
+    torch.cuda.synchronize()
+    assert y.untouched()
+    for e in range(E):
+        lo, hi = off[e], off[e + 1]
+        assert torch.equal(y.t[lo:hi], torch.relu(x[lo:hi].float() @ w[e].float().T + bias[e])), e
+    if dtype == alt.I8:
+        return
+    dy = matrix(small_integers((rows, N), torch.float32, 3), td, N + pad)
+    dx, dw, db = Canary(rows, K, torch.float32, K + pad), Canary(N, K, torch.float32, K + pad, lead=(E,)), torch.empty(E, N, device="cuda")
+    shape = dict(in_dtype=dtype, out_dtype=alt.F32, lda=K + pad, ldb=K + pad, ldc=N + pad)
+    h.gemm_grouped_dx(alt.grouped_desc(rows, E, N, K, epilogue=alt.EPI_RELU, **shape), dy, w, o, dx, relu_of=x)
+    h.gemm_grouped_dw(alt.grouped_desc(rows, E, N, K, epilogue=alt.EPI_BIAS, **shape), x, dy, o, dw, dbias=db)
+    torch.cuda.synchronize()
+    assert dx.untouched() and dw.untouched()
+    for e in range(E):
+        lo, hi = off[e], off[e + 1]
+        assert torch.equal(dx.t[lo:hi], (dy[lo:hi].float() @ w[e].float()) * (x[lo:hi] > 0)), e
+        assert torch.equal(dw.t[e], dy[lo:hi].float().T @ x[lo:hi].float()) and torch.equal(db[e], dy[lo:hi].float().sum(0)), e
