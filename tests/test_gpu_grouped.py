@@ -693,3 +693,12 @@ def test_tiles_of_every_size(h, counts, N, K, pad, dtype):
         lo, hi = off[e], off[e + 1]
         assert torch.equal(dx.t[lo:hi], (dy[lo:hi].float() @ w[e].float()) * (x[lo:hi] > 0)), e
         assert torch.equal(dw.t[e], dy[lo:hi].float().T @ x[lo:hi].float()) and torch.equal(db[e], dy[lo:hi].float().sum(0)), e
+
+
+@pytest.mark.parametrize("dtype", [alt.F32, alt.BF16])
+@pytest.mark.parametrize("cols,ldx", [(1000, 0), (1025, 0), (1999, 2003), (2048, 0), (2056, 0)])
+def test_quantize_many_rows(h, dtype, cols, ldx):
+    x = matrix(normal(cols, 515, cols) * torch.exp(normal(7, 515, 1)), TORCH[dtype], ldx)
+    q, s = quantize(h, x, dtype)
+    want, scale = exact_rows(x)
+    assert np.array_equal(q.cpu().numpy(), want) and np.array_equal(f64(s), scale)
