@@ -350,7 +350,8 @@ __device__ __forceinline__ void grp_store(const GroupedParams &p, char *y_row, i
 
 // ---- what the tile kernels share ---------------------------------------------------------------------------------------------
 
-// One workgroup's tile: rows [row0, row_end) of the output (at most BM of them), columns from col0, reduced over `red` steps from a0 and b0.
+// One workgroup's tile: rows of the output from row0 on, a tile's number of them at most and up to row_end (where the group's end), columns from
+// col0 on, reduced over `red` steps from a0 and b0.
 struct GrpProblem {
     int row0, row_end, col0, red, group;
     const char *a0, *b0;
@@ -1010,7 +1011,6 @@ struct GrpStream {
     }
     // RED: this lane's chunk lies behind the reduction's end, which is not the descriptor's but in the last row
     __device__ __forceinline__ uint32_t past() const { return RED && chunk >= left ? kOutOfRange : 0u; }
-    __device__ __forceinline__ void none() { left = 0; }
     __device__ __forceinline__ void next()
     {
         base += RED ? (uint64_t)BKB : (uint64_t)((int64_t)ld * Op::BK);
