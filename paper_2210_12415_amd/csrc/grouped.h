@@ -747,6 +747,107 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
     }
 }
 
+// The same for the gradient by the rows, whose right operand has its columns contiguous: tiles of 16 rows by 64 columns.  A lane takes four consecutive
+// columns (those of its lane % 16) of as many steps of the reduction as the matrix instruction takes of a lane (those of its lane / 16), so that each
+// row of 64 columns is read whole; matrix tile j has the columns 4 c + j.  Units of 64 bytes of the left operand.  Bound by latency: 19 rows, 2538 x
+// 128, fp32 17.7 us (two such units in flight: 22.2; sixteen waves: 20.4), 64 rows, 1024 x 4096, 10.9.
+template <typename T, int NW>
+__global__ __launch_bounds__(64 * NW) void grouped_few_dx_kernel(const GroupedParams p)
+{
+    constexpr int ES = GrpTraits<T>::ES, EPC = 16 / ES, UNIT = 4 * EPC, SUMS = GrpTraits<T>::SUMS;
+    typedef uint32_t cols4_t __attribute__((ext_vector_type(ES)));             // four columns: 16 bytes, or 8
+    __shared__ u32x4_t part[NW * 4 * 64];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    GrpProblem g;
+    if (!grp_problem<T, kInput, 16, 64>(p, lane, g)) return;
+    if (g.col0 + 64 > p.cols && p.cols >= 64) {            // (the last tile ends with the matrix)
+        g.b0 -= (int64_t)(g.col0 + 64 - p.cols) * ES;
+        g.col0 = p.cols - 64;
+    }
+    const bool narrow = p.cols < 64;
+    const int step = lane / 16 * EPC, col = lane % 16 * 4; // this lane's first step of a unit and first column of the tile
+    const char *ap = g.a0 + (int64_t)min(lane % 16, g.row_end - g.row0 - 1) * p.lda + step * ES;
+    const char *bp = g.b0 + (int64_t)step * p.ldb + col * ES;
+
+    typename GrpFew<T>::acc_t acc[4][SUMS];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < SUMS; ++q) acc[j][q] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+
+    auto mma = [&](const u32x4_t &a, const cols4_t (&b)[EPC]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4_t f;
+            if constexpr (ES == 4) {
+                f = (u32x4_t){b[0][j], b[1][j], b[2][j], b[3][j]};
+            } else {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) f[d] = __builtin_amdgcn_perm(b[2 * d + 1][j / 2], b[2 * d][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+            }
+            grp_mma16<T>(acc[j], f, a);
+        }
+    };
+    const int units = narrow ? 0 : g.red / UNIT;           // whole ones
+    auto load = [&](u32x4_t &a, cols4_t (&b)[EPC], int u) {
+        const int64_t n = (int64_t)u * UNIT;
+#pragma unroll
+        for (int i = 0; i < EPC; ++i) __builtin_memcpy(&b[i], bp + (n + i) * p.ldb, 4 * ES);
+        __builtin_memcpy(&a, ap + n * ES, 16);
+    };
+    if (wave < units) {
+        u32x4_t a[2];
+        cols4_t b[2][EPC];
+        load(a[0], b[0], wave);
+        for (int u = wave; u < units; u += 2 * NW) {
+            if (u + NW < units) load(a[1], b[1], u + NW);
+            mma(a[0], b[0]);
+            if (u + 2 * NW < units) load(a[0], b[0], u + 2 * NW);
+            if (u + NW < units) mma(a[1], b[1]);
+        }
+    }
+    // what is left: the reduction's end, or all of it for fewer than 64 columns
+    for (int n = (units + (wave + NW - units % NW) % NW) * UNIT; n < g.red; n += NW * UNIT) {
+        cols4_t b[EPC];
+#pragma unroll
+        for (int i = 0; i < EPC; ++i) {
+            const u32x4_t v = grp_load_chunk<ES>(bp + (int64_t)(n + i) * p.ldb, n + step + i < g.red ? min(p.cols - g.col0 - col, 4) : 0);
+            if constexpr (ES == 4) b[i] = v;
+            else b[i] = (cols4_t){v.x, v.y};
+        }
+        mma(grp_load_chunk<ES>(ap + (int64_t)n * ES, g.red - n - step), b);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (SUMS == 4) acc[j][0] = (acc[j][0] + acc[j][1]) + (acc[j][2] + acc[j][3]);
+        part[(wave * 4 + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[j][0]);
+    }
+    __syncthreads();
+    // each thread: four columns of a row, which lie in the four tiles' sums of one lane
+    const float *sums = (const float *)part;
+    for (int i = t; i < 256; i += NW * 64) {
+        const int r = i / 16, c = i % 16, row = g.row0 + r, first = g.col0 + c * 4;
+        if (row >= g.row_end || first >= p.cols) continue;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) v[j] += sums[((w * 4 + j) * 64 + c / 4 * 16 + r) * 4 + c % 4];
+        }
+        if (p.flags & kGrpMask) {
+            const char *m = (const char *)p.mask + (int64_t)row * p.ldmask + (int64_t)first * ES;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (first + j >= p.cols) break;
+                const uint32_t e = ES == 4 ? *(const uint32_t *)(m + j * 4) : *(const uint16_t *)(m + j * 2);
+                if (!grp_positive<ES>(e)) v[j] = 0.f;
+            }
+        }
+        grp_store<4>(p, g.y + (int64_t)row * p.ldy, first, v);
+    }
+}
+
 // ---- the kernel for any size, stride and alignment: operands go through registers --------------------------------------------
 //
 // Chunks of 16 bytes are loaded at whatever address they start at.  Rows and columns that do not exist repeat the tile's last ones (their sums are
@@ -1486,6 +1587,17 @@ hipError_t grouped_few(GroupedParams p, hipStream_t st)
     return hipGetLastError();
 }
 
+template <typename T>
+hipError_t grouped_few_dx(GroupedParams p, hipStream_t st)
+{
+    constexpr int NW = 8;
+    unsigned grid;
+    const hipError_t e = grp_grid<kInput, 16, 64>(p, 64 * NW, &grid);
+    if (e != hipSuccess || !grid) return e;
+    hipLaunchKernelGGL((grouped_few_dx_kernel<T, NW>), dim3(grid), dim3(64 * NW), 0, st, p);
+    return hipGetLastError();
+}
+
 // Whether the direct loads take a product: whole chunks at whole addresses, and a tile's rows (or steps) within a descriptor.
 template <typename T, int FORM>
 bool grp_streams(const GroupedParams &p)
@@ -1565,6 +1677,15 @@ inline bool grp_is_few(const GroupedParams &p, int ES)
     return p.rows <= 16 * spans || grp_tiles<kForward>(p, 16, 16) <= (ES == 4 ? 4 : 2) * p.places;
 }
 
+// The same for the gradient by the rows, in fp32 and where the direct loads do not take the operands (bf16 through those is as fast: 16 x 8192 x 8192
+// 26.3 us, 28.6 so).  fp32: 316 rows, 1536 x 265 (100 tiles), 14.0 us for 30.0, 256 rows of 8 groups, 2048 x 2048 (512), 32.2 for 45.4, 1000 of 5, 1030 x 515
+// (585), 30.9 for 24.6; bf16: one row, 3742 x 170, 12.9 for 17.1, 316 rows, 1536 x 265, 9.1 for 11.9.
+inline bool grp_is_few_dx(const GroupedParams &p, int ES)
+{
+    const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows;
+    return p.rows <= 16 * spans || grp_tiles<kInput>(p, 16, 64) <= (ES == 4 ? 2 : 1) * p.places;
+}
+
 // Tiles of 64x64 with a deep ring (one to a compute unit) or a shallow one (two), of 128x64, of 128x128, of 256x256, for operands of 8 or 16 bits; the
 // constants are those of 8-bit products of 32 .. 8192 rows, 768 .. 8192 columns and reductions of 512 .. 8192, which they give to 10 %; bf16 has the
 // same tiles in bytes.  (128x64 for one round of the chip: 2048 x 1024 x 4096 17.2 us, 20.1 in tiles of 64x64, 19.9 of 128x128; the gradient by the rows
@@ -1594,6 +1715,9 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
         // 32 x 4096 x 4096 10.4 against 8.6)
         if (grp_is_few(p, ES))
             return grp_tiles<FORM>(p, 16, 16) <= places ? grouped_few<T, 1, 8, 2>(p, st) : grouped_few<T, 2, 4, 2>(p, st);
+    }
+    if constexpr (FORM == kInput) {
+        if ((ES == 4 || !grp_streams<T, FORM>(p)) && grp_is_few_dx(p, ES)) return grouped_few_dx<T>(p, st);
     }
     if (!grp_streams<T, FORM>(p)) {
         // Tiles of 128x128 once they fill half the chip: 1500 x 1501 x 2049 in 8 bits (144 tiles) 21.8 us, in tiles of 64x64 27.2; 2048 x 770 x 3073 (112)

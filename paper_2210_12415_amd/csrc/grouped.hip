@@ -119,6 +119,7 @@ size_t pack_bytes(int form, int dtype, GroupedParams &p)
 {
     if (dtype == ALT_F32 || p.rows == 0 || p.red == 0) return 0;
     if (form == kForward && grp_is_few(p, dtype == ALT_I8 ? 1 : 2)) return 0;
+    if (form == kInput && grp_is_few_dx(p, 2)) return 0;
     const int es = dtype == ALT_I8 ? 1 : 2;
     Matrix a, b;
     matrices(form, es, p, a, b);

@@ -702,3 +702,29 @@ def test_quantize_many_rows(h, dtype, cols, ldx):
     q, s = quantize(h, x, dtype)
     want, scale = exact_rows(x)
     assert np.array_equal(q.cpu().numpy(), want) and np.array_equal(f64(s), scale)
+
+
+@pytest.mark.parametrize("counts,N,K", [([1], 3742, 170), ([19], 2538, 64), ([2, 0, 33, 1], 77, 65), ([5] * 70, 130, 63), ([16, 17], 1000, 3), ([40], 31, 127)])
+@pytest.mark.parametrize("pad", [0, 1, 8])
+@pytest.mark.parametrize("dtype", [alt.BF16, alt.F32])
+def test_gradient_by_few_rows(h, counts, N, K, pad, dtype):
+    """Fewer columns than a tile's, tiles moved back to end with the matrix, reductions that end inside a unit; rows of no expert; all sums exact."""
+    td, E, rows = TORCH[dtype], len(counts), sum(counts) + 3
+    off = [2]
+    for c in counts:
+        off.append(off[-1] + c)
+    x = matrix(small_integers((rows, K), torch.float32, 1), td, K + pad)
+    w = matrix(small_integers((E, N, K), torch.float32, 2), td, K + pad)
+    dy = matrix(small_integers((rows, N), torch.float32, 3), td, N + pad)
+    for epilogue, out in ((alt.EPI_RELU, alt.F32), (0, alt.F32), (alt.EPI_RELU, dtype)):
+        dx = Canary(rows, K, TORCH[out], K + pad)
+        d = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=out, epilogue=epilogue, lda=K + pad, ldb=K + pad, ldc=N + pad)
+        h.gemm_grouped_dx(d, dy, w, make_offsets(off), dx, relu_of=x if epilogue else None)
+        torch.cuda.synchronize()
+        assert dx.untouched() and not dx.t[:2].any() and not dx.t[off[-1]:].any()
+        for e in range(E):
+            lo, hi = off[e], off[e + 1]
+            want = dy[lo:hi].float() @ w[e].float()
+            if epilogue:
+                want = want * (x[lo:hi] > 0)
+            assert torch.equal(dx.t[lo:hi], want.to(TORCH[out])), (e, epilogue, out)
