@@ -507,7 +507,7 @@ alt_status_t alt_gemm_variant_name(alt_handle_t h, const alt_gemm_desc_t *d, int
 alt_status_t alt_quantize_rows(alt_handle_t h, alt_dtype_t dtype, int64_t rows, int64_t cols, const void *x, int64_t x_stride,
                                void *q, int64_t q_stride, float *scale, void *stream);
 
-#define ALT_I8_MAX_K 131072       /* products of two numbers in -128 .. 127 that a 32-bit sum holds */
+#define ALT_I8_MAX_K 131071       /* products of two numbers in -128 .. 127 that a 32-bit sum holds: 131072 * 128 * 128 is 2^31 */
 
 typedef struct {
     int64_t M, N, K;

@@ -173,6 +173,24 @@ def test_gemm_i8_sums_are_exact(h, M):
     assert torch.equal(y.cpu().double(), 2.0 * (q.double() @ w.double().T))
 
 
+@pytest.mark.parametrize("M,N,pad", [(1, 64, 1), (16, 33, 0), (512, 1040, 1), (512, 1040, 17), (513, 1024, 0)])
+def test_gemm_i8_longest_sums(h, M, N, pad):
+    """The longest reduction of the largest products, of either sign (2147467264 and -2130690176; the fp32 of the exact sum is one value), in tiles of
+    16 rows, whole chunks (131071 of 131072 bytes, laid out anew, among them) and any alignment."""
+    K = 131071
+    q, w = torch.full((M * (K + pad),), -128, dtype=torch.int8, device="cuda"), torch.full((N, K + pad), -128, dtype=torch.int8, device="cuda")
+    w[1::2] = 127
+    d = alt.gemm_i8_desc(M, N, K, out_dtype=alt.F32, lda=K + pad, ldb=K + pad)
+    need = h.gemm_i8_workspace_size(d)
+    want = torch.full((M, N), float(K * 128 * 128), device="cuda")
+    want[:, 1::2] = float(-K * 128 * 127)
+    for ws in ([0, need] if need else [0]):
+        y = torch.zeros(M, N, device="cuda")
+        h.gemm_i8(d, q, torch.ones(M, device="cuda"), w, torch.ones(N, device="cuda"), y, workspace=torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None,
+                  ws_bytes=ws)
+        assert torch.equal(y, want), ws
+
+
 def test_gemm_i8_rows_without_a_scale_are_nan(h):
     q, w = torch.ones(20, 64, dtype=torch.int8, device="cuda"), torch.ones(32, 64, dtype=torch.int8, device="cuda")
     s, t = torch.ones(20, device="cuda"), torch.ones(32, device="cuda")

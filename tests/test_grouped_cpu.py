@@ -85,6 +85,20 @@ def test_grouped_refuses_what_an_8_bit_layer_lacks(h):
     assert refused(lambda: h.gemm_grouped(far, a_scale=4096, b_scale=4096, stream=0, **a)) == UNSUPPORTED
 
 
+def test_8_bit_reductions_end_where_their_sums_fit(h):
+    """131071 products of -128 and -128 fit a 32-bit sum; 131072 are 2^31, which does not."""
+    assert 131071 * 128 * 128 < 2 ** 31 <= 131072 * 128 * 128
+    a = dict(CALLS["gemm_grouped"], a_scale=4096, b_scale=4096, stream=0)
+    for K in (131071, 131072):
+        one, layer = alt.gemm_i8_desc(4, 32, K), alt.grouped_desc(4, 2, 32, K, in_dtype=alt.I8)
+        if K == 131071:
+            h.gemm_i8_workspace_size(one), h.gemm_grouped_workspace_size(layer)
+            continue
+        assert refused(lambda: h.gemm_i8_workspace_size(one)) == UNSUPPORTED and refused(lambda: h.gemm_grouped_workspace_size(layer)) == UNSUPPORTED
+        assert refused(lambda: h.gemm_i8(one, 4096, 4096, 4096, 4096, 4096, stream=0)) == UNSUPPORTED
+        assert refused(lambda: h.gemm_grouped(layer, **a)) == UNSUPPORTED
+
+
 def test_grouped_refuses_epilogues_of_the_other_direction(h):
     d = alt.grouped_desc(4, 2, 32, 64, epilogue=alt.EPI_BIAS)
     assert refused(lambda: h.gemm_grouped_dx(d, stream=0, **CALLS["gemm_grouped_dx"])) == INVALID
