@@ -121,16 +121,33 @@ __device__ __forceinline__ int grp_scan(int v)                  // inclusive pre
     return v;
 }
 
-// Rows of span s: group s, and as spans `groups` and `groups + 1` the rows behind the last group and before the first.
-// (Clamped: whatever the offsets hold, rows stay inside the tensors.)
-__device__ __forceinline__ void grp_span(const GroupedParams &p, int s, int &beg, int &end)
+__device__ __forceinline__ int grp_scan_max(int v)              // inclusive prefix maximum over the wave, of values from 0 on
 {
-    beg = end = 0;
-    if (s < p.groups + 2) {
-        const int lo = s <= p.groups ? p.offsets[s] : 0, hi = s < p.groups ? p.offsets[s + 1] : s == p.groups ? p.rows : p.offsets[0];
-        beg = min(max(lo, 0), p.rows);
-        end = min(max(hi, beg), p.rows);
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true));
+    return v;
+}
+
+// Rows of the spans s0 to s0 + 63, one per lane: span s is group s, and the spans `groups` and `groups + 1` are the rows behind the last group and
+// before the first.  Offsets count as their running maximum, at most p.rows: whatever they hold, the spans are disjoint and together all rows, so that
+// there are never more tiles than the launch counts on, and no sum of them wraps.  `past`: that maximum over the spans before s0 (0 at first).
+__device__ __forceinline__ void grp_spans(const GroupedParams &p, int s0, int lane, int &past, int &beg, int &end)
+{
+    const int s = s0 + lane;
+    if (!p.offsets) {
+        beg = 0;
+        end = s == 0 ? p.rows : 0;
+        return;
     }
+    const int lo = s <= p.groups ? p.offsets[s] : 0, hi = s < p.groups ? p.offsets[s + 1] : s == p.groups ? p.rows : s == p.groups + 1 ? p.offsets[0] : 0;
+    const int top = max(grp_scan_max(min(max(lo, 0), p.rows)), past);
+    past = __builtin_amdgcn_readlane(top, 63);
+    beg = s <= p.groups ? top : 0;
+    end = min(max(hi, beg), p.rows);
 }
 
 // Tiles are numbered group by group, inside a group in panels of kPanel row tiles, rows fastest (tiles that run together share both
@@ -148,11 +165,10 @@ __device__ __forceinline__ void grp_order(const GroupedParams &p, int q, int til
 template <int BM>
 __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint32_t wg, GrpTile &t)
 {
-    int total = 0, upto = 0, beg = 0, end = 0;
+    int total = 0, upto = 0, past_rows = 0, beg = 0, end = 0;
     const int spans = p.offsets ? p.groups + 2 : 1;
     for (int s0 = 0; s0 < spans; s0 += 64) {
-        if (p.offsets) grp_span(p, s0 + lane, beg, end);
-        else { beg = 0; end = lane == 0 ? p.rows : 0; }
+        grp_spans(p, s0, lane, past_rows, beg, end);
         upto = grp_scan((end - beg + BM - 1) / BM);
         total += __builtin_amdgcn_readlane(upto, 63);
     }
@@ -161,9 +177,10 @@ __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint3
     if ((wg >> 3) >= per || logical >= tiles) return false;
     // the span that holds it
     int before = 0;
+    past_rows = 0;
     for (int s0 = 0; s0 < spans; s0 += 64) {
         if (spans > 64) {
-            grp_span(p, s0 + lane, beg, end);
+            grp_spans(p, s0, lane, past_rows, beg, end);
             upto = grp_scan((end - beg + BM - 1) / BM);
         }
         const uint64_t past = __ballot((uint32_t)(before + upto) * (uint32_t)p.tiles_n > logical);
@@ -176,7 +193,7 @@ __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint3
             t.group = min(s0 + l, p.groups);
             t.row_end = __builtin_amdgcn_readlane(end, l);
             t.row0 = __builtin_amdgcn_readlane(beg, l) + row_tile * BM;
-            return (unsigned)row_tile < (unsigned)mt && (unsigned)t.col_tile < (unsigned)p.tiles_n;    // (sums of offsets out of order may wrap)
+            return true;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
@@ -1416,19 +1433,13 @@ __device__ __forceinline__ void grp_rows(int len, int &large, int &small)
     small = rest > 0 && rest <= 128;
 }
 
-__device__ __forceinline__ void grp_span_rows(const GroupedParams &p, int s, int &beg, int &end)
-{
-    if (p.offsets) grp_span(p, s, beg, end);
-    else { beg = 0; end = s == 0 ? p.rows : 0; }
-}
-
 __device__ __forceinline__ void grp_schedule(const GroupedParams &p, int lane, GrpSchedule &h)
 {
-    int large = 0, small = 0;
+    int large = 0, small = 0, past_rows = 0;
     h.spans = p.offsets ? p.groups + 2 : 1;
     for (int s0 = 0; s0 < h.spans; s0 += 64) {
         int beg, end, l, m;
-        grp_span_rows(p, s0 + lane, beg, end);
+        grp_spans(p, s0, lane, past_rows, beg, end);
         grp_rows(end - beg, l, m);
         l = grp_scan(l);
         m = grp_scan(m);
@@ -1448,12 +1459,12 @@ __device__ __forceinline__ void grp_schedule(const GroupedParams &p, int lane, G
 __device__ __forceinline__ bool grp_row_tile(const GroupedParams &p, const GrpSchedule &h, int lane, bool is_small, uint32_t q, uint32_t per_row, int &span, int &beg, int &end,
                                              int &first, int &count)
 {
-    int before = 0;
+    int before = 0, past_rows = 0;
     for (int s0 = 0; s0 < h.spans; s0 += 64) {
         int b = h.beg, e = h.end, upto = is_small ? h.upto_small : h.upto_large;
         if (h.spans > 64) {
             int l, m;
-            grp_span_rows(p, s0 + lane, b, e);
+            grp_spans(p, s0, lane, past_rows, b, e);
             grp_rows(e - b, l, m);
             upto = grp_scan(is_small ? m : l);
         }
@@ -1492,7 +1503,6 @@ __device__ __forceinline__ bool grp_unit(const GroupedParams &p, const GrpSchedu
     if (!grp_row_tile(p, h, lane, false, q, p.tiles_n, span, beg, end, first, count)) return false;
     int mt, nt;
     grp_order(p, q - first * p.tiles_n, count, mt, nt);
-    if ((unsigned)mt >= (unsigned)count || (unsigned)nt >= (unsigned)p.tiles_n) return false;             // (sums of offsets out of order may wrap)
     grp_at<T, FORM>(p, min(span, p.groups), beg + mt * 256 + (sub >> 1) * 128, end, nt * 256 + (sub & 1) * 128, g);
     if (g.col0 >= p.cols) g.red = 0;                       // (nothing is left of the large tile there)
     return true;
@@ -1539,7 +1549,7 @@ hipError_t grouped_run_bf16(int form, const GroupedParams &p, hipStream_t st);
 hipError_t grouped_run_f32(int form, const GroupedParams &p, hipStream_t st);
 hipError_t grouped_run_i8(const GroupedParams &p, hipStream_t st);
 
-// Most tiles of BM rows that any offsets in order can make of p.rows rows: each span ends in one part tile at most.
+// Most tiles of BM rows that any offsets can make of p.rows rows: each span ends in one part tile at most.
 inline int64_t grp_row_tiles(const GroupedParams &p, int BM)
 {
     if (!p.offsets) return ((int64_t)p.rows + BM - 1) / BM;

@@ -497,6 +497,36 @@ def test_offsets_out_of_range_stay_in_the_buffers(h, off):
     assert torch.isfinite(dw.t).all()
 
 
+DISORDER = {"alternating": lambda rows, E: [(i % 2) * rows for i in range(E + 1)], "falling": lambda rows, E: [rows - i * rows // E for i in range(E + 1)],
+            "anywhere": lambda rows, E: np.random.default_rng(rows).integers(-2 ** 31, 2 ** 31, E + 1).tolist(),
+            "shuffled": lambda rows, E: np.random.default_rng(E).integers(0, rows + 1, E + 1).tolist()}
+
+
+@pytest.mark.parametrize("disorder", sorted(DISORDER))
+@pytest.mark.parametrize("rows,E,N,K", [(900, 70, 64, 128), (2500, 100, 136, 128), (2500, 100, 130, 130), (35840, 70, 4096, 128)],
+                         ids=["tiles_of_16", "whole_chunks", "any_alignment", "large_tiles"])
+def test_offsets_out_of_order_count_as_their_running_maximum(h, rows, E, N, K, disorder):
+    """Whatever the offsets hold, every row is one expert's or none's, and is computed once; all sums exact.  (The gradient by the weights takes an
+    expert's own two offsets.)"""
+    off = DISORDER[disorder](rows, E)
+    x, w, dy = small_integers((rows, K), torch.bfloat16, 1), small_integers((E, N, K), torch.bfloat16, 2), small_integers((rows, N), torch.bfloat16, 3)
+    y, dx, dw = Canary(rows, N, torch.float32), Canary(rows, K, torch.float32), Canary(N, K, torch.float32, lead=(E,))
+    d, o = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32), make_offsets(off)
+    h.gemm_grouped(d, x, w, o, y)
+    h.gemm_grouped_dx(d, dy, w, o, dx)
+    if rows < 10000:
+        h.gemm_grouped_dw(d, x, dy, o, dw)
+    torch.cuda.synchronize()
+    assert y.untouched() and dx.untouched() and dw.untouched()
+    at = np.maximum.accumulate(np.clip(off, 0, rows)).tolist()
+    assert not y.t[:at[0]].any() and not y.t[at[E]:].any() and not dx.t[:at[0]].any() and not dx.t[at[E]:].any()
+    for e, lo, hi in spans_of(at):
+        assert torch.equal(y.t[lo:hi], x[lo:hi].float() @ w[e].float().T) and torch.equal(dx.t[lo:hi], dy[lo:hi].float() @ w[e].float()), e
+    for e in range(E if rows < 10000 else 0):
+        lo, hi = min(max(off[e], 0), rows), min(max(off[e + 1], 0), rows)
+        assert torch.equal(dw.t[e], dy[lo:hi].float().T @ x[lo:hi].float()), e
+
+
 def test_no_rows(h):
     E, N, K = 3, 64, 64
     o = make_offsets([0, 0, 0, 0])
