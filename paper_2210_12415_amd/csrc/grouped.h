@@ -162,9 +162,59 @@ __device__ __forceinline__ void grp_order(const GroupedParams &p, int q, int til
     row_tile = panel * kPanel + rest - col_tile * pm;
 }
 
+// Of many groups no workgroup looks at every offset: each has a slot that may hold a row tile, and searches the offsets for its span, 64 probes at a time.
+// Spans here lie in the order of their rows (0: before the first group, s: group s - 1, groups + 1: behind the last), span s from row b(s) on.  Where
+// there are few rows each row is a slot, and its tile is the one that begins there; otherwise span s has the slots from b(s) / BM + s on, which are
+// never fewer than its tiles.  Offsets out of order lead a search anywhere, but to rows inside the tensors, and each workgroup to one tile at most.
+// A scan takes every workgroup two turns for each 64 groups, so that a launch grows with their square, and a search leaves slots empty, each of which takes a
+// compute unit's time where a tile's LDS is most of it: 128 groups of 128 rows, 1024 x 1024 bf16, 86 us with the scan and 90 with the search, 200 of 82
+// 127 and 118, 512 of 32 336 and 258; one row each, 64 x 64, 4096 groups 358 and 25, 65536 107 ms and 0.54, 2^20 9.0 ms with the search.
+constexpr int kScanSpans = 192;
+
+__host__ __device__ inline bool grp_searches(const GroupedParams &p) { return p.offsets && p.groups + 2 > kScanSpans; }
+__host__ __device__ inline bool grp_slot_per_row(const GroupedParams &p, int BM) { return p.rows <= p.rows / BM + p.groups + 2; }
+
+template <int BM>
+__device__ __forceinline__ bool grp_search(const GroupedParams &p, int lane, uint32_t wg, GrpTile &t)
+{
+    const bool per_row = grp_slot_per_row(p, BM);
+    const int spans = p.groups + 2, slots = per_row ? p.rows : p.rows / BM + spans;
+    const uint32_t tiles = (uint32_t)slots * (uint32_t)p.tiles_n, per = (tiles + 7) / 8;
+    const uint32_t logical = (wg & 7) * per + (wg >> 3);
+    if ((wg >> 3) >= per || logical >= tiles) return false;
+    const int slot = (int)(logical / (uint32_t)p.tiles_n);
+    auto begin = [&](int s) { return s == 0 ? 0 : s < spans ? min(max(p.offsets[s - 1], 0), p.rows) : p.rows; };
+    auto first_slot = [&](int s, int b) { return per_row ? b : b / BM + s; };
+    // the last span that begins at or before the slot, among the `left` ones from `span` on, of which the first does
+    int span = 0, left = spans;
+    while (left > 1) {
+        const int step = (left + 63) / 64, at = lane * step;
+        const bool before = lane == 0 || (at < left && first_slot(span + at, begin(span + at)) <= slot);
+        const int pick = (63 - __builtin_clzll(__ballot(before))) * step;
+        span += pick;
+        left = min(step, left - pick);
+    }
+    const int beg = begin(span), end = max(begin(span + 1), beg), mt = (end - beg + BM - 1) / BM, in = slot - first_slot(span, beg);
+    const uint32_t q = logical - (uint32_t)(slot - in) * (uint32_t)p.tiles_n;      // of the span's first slot's tiles
+    int row_tile;
+    if (per_row) {
+        if (in % BM || in >= end - beg) return false;
+        row_tile = in / BM;
+        t.col_tile = (int)(logical - (uint32_t)slot * (uint32_t)p.tiles_n);
+    } else {
+        if (q >= (uint32_t)mt * (uint32_t)p.tiles_n) return false;
+        grp_order(p, (int)q, mt, row_tile, t.col_tile);
+    }
+    t.group = span == 0 ? p.groups : span - 1;             // (span groups + 1: group `groups`, too)
+    t.row0 = beg + row_tile * BM;
+    t.row_end = end;
+    return true;
+}
+
 template <int BM>
 __device__ __forceinline__ bool grp_find(const GroupedParams &p, int lane, uint32_t wg, GrpTile &t)
 {
+    if (grp_searches(p)) return grp_search<BM>(p, lane, wg, t);
     int total = 0, upto = 0, past_rows = 0, beg = 0, end = 0;
     const int spans = p.offsets ? p.groups + 2 : 1;
     for (int s0 = 0; s0 < spans; s0 += 64) {
@@ -1508,6 +1558,10 @@ __device__ __forceinline__ bool grp_unit(const GroupedParams &p, const GrpSchedu
     return true;
 }
 
+// The walk scans the offsets for every tile, 64 at a time, which pays up to some number of groups: 256 rows each, 512 x 512 bf16, 1024 groups 250 us, 315 in
+// tiles of 128x128 that are searched for, 2048 594 and 619, 4096 1893 and 1269.
+constexpr int kWalkGroups = 2048;
+
 constexpr int kLargeThreads = 512;
 
 template <typename T, int FORM> struct GrpLarge {
@@ -1549,12 +1603,12 @@ hipError_t grouped_run_bf16(int form, const GroupedParams &p, hipStream_t st);
 hipError_t grouped_run_f32(int form, const GroupedParams &p, hipStream_t st);
 hipError_t grouped_run_i8(const GroupedParams &p, hipStream_t st);
 
-// Most tiles of BM rows that any offsets can make of p.rows rows: each span ends in one part tile at most.
+// Most tiles of BM rows that any offsets can make of p.rows rows: each span ends in one part tile at most, and each tile has a
+// row.  (As many slots grp_search counts on.)
 inline int64_t grp_row_tiles(const GroupedParams &p, int BM)
 {
     if (!p.offsets) return ((int64_t)p.rows + BM - 1) / BM;
-    const int64_t spans = (int64_t)p.groups + 2;
-    return p.rows / BM + (spans < p.rows ? spans : p.rows);
+    return std::min<int64_t>(p.rows, p.rows / BM + (int64_t)p.groups + 2);
 }
 
 // Sets the column tiles and works out the workgroups of a launch (0: nothing to do).
@@ -1758,6 +1812,7 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
             case kMiddle: return grouped_tiles<GrpRing<T, FORM, 128, 128, 2, 4, 128, 4>>(p, st);
         }
         if constexpr (FORM == kWeights) return grouped_tiles<GrpWide<T, FORM>>(p, st);
+        else if (p.offsets && p.groups > kWalkGroups) return grouped_tiles<GrpRing<T, FORM, 128, 128, 2, 4, 128, 4>>(p, st);
         else return grouped_large<T, FORM>(p, st);
     }
 }

@@ -527,6 +527,79 @@ def test_offsets_out_of_order_count_as_their_running_maximum(h, rows, E, N, K, d
         assert torch.equal(dw.t[e], dy[lo:hi].float().T @ x[lo:hi].float()), e
 
 
+@pytest.mark.parametrize("disorder", sorted(DISORDER))
+@pytest.mark.parametrize("rows,E,N,K", [(60, 3000, 64, 128), (3500, 230, 64, 128), (9000, 230, 136, 128), (9000, 230, 130, 130)],
+                         ids=["a_slot_for_a_row", "tiles_of_16", "whole_chunks", "any_alignment"])
+def test_offsets_out_of_order_of_many_experts(h, rows, E, N, K, disorder):
+    """Where a search finds the tiles: nothing outside the buffers, and of each row nothing but some expert's values, or zeros, or what was there."""
+    off = DISORDER[disorder](rows, E)
+    x, w, dy = small_integers((rows, K), torch.bfloat16, 1), small_integers((E, N, K), torch.bfloat16, 2), small_integers((rows, N), torch.bfloat16, 3)
+    y, dx, dw = Canary(rows, N, torch.float32), Canary(rows, K, torch.float32), Canary(N, K, torch.float32, lead=(E,))
+    d, o = alt.grouped_desc(rows, E, N, K, out_dtype=alt.F32), make_offsets(off)
+    h.gemm_grouped(d, x, w, o, y)
+    h.gemm_grouped_dx(d, dy, w, o, dx)
+    h.gemm_grouped_dw(d, x, dy, o, dw)
+    torch.cuda.synchronize()
+    assert y.untouched() and dx.untouched() and dw.untouched()
+    for got, most in ((y.t, 9 * K), (dx.t, 9 * N)):
+        assert bool((got.abs() <= most).all()) and torch.equal(got, got.round())
+
+
+@pytest.mark.parametrize("most,E,N,K,dtype", [(1, 63, 64, 64, alt.BF16), (3, 63, 70, 66, alt.F32), (1, 1000, 40, 72, alt.BF16), (1, 5000, 24, 32, alt.I8), (40, 100, 100, 64, alt.BF16), (40, 190, 48, 64, alt.BF16), (40, 191, 48, 66, alt.BF16), (300, 191, 64, 128, alt.BF16),
+                                              (40, 1000, 33, 17, alt.I8), (40, 1000, 64, 72, alt.BF16), (90, 300, 33, 70, alt.BF16), (90, 300, 20, 36, alt.F32), (300, 200, 64, 64, alt.I8),
+                                              (1, 1 << 20, 8, 8, alt.BF16), (2, 1 << 20, 8, 8, alt.I8)])
+def test_many_experts(h, most, E, N, K, dtype):
+    """More experts than a wave scans at once, of 0 to `most` rows, with rows of no expert before and behind; all sums exact."""
+    counts = np.random.default_rng(E + most).integers(0, most + 1, E)
+    counts[[0, E // 3, E // 2, E - 1]] = [most, 0, 0, 0]
+    off = np.concatenate([[0], np.cumsum(counts)]) + 5
+    rows, td = int(off[-1]) + 7, TORCH[dtype]
+    expert = torch.as_tensor(np.concatenate([np.full(5, -1), np.repeat(np.arange(E), counts), np.full(7, -1)]), device="cuda")
+    x, w, dy = small_integers((rows, K), td, 1), small_integers((E, N, K), td, 2), small_integers((rows, N), td, 3)
+    y, o = Canary(rows, N, torch.float32), torch.as_tensor(off.astype(np.int32), device="cuda")
+    one = dict(a_scale=torch.ones(rows, device="cuda"), b_scale=torch.ones(E, N, device="cuda")) if dtype == alt.I8 else {}
+    d = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=alt.F32)
+    h.gemm_grouped(d, x, w, o, y, **one)
+    dx = Canary(rows, K, torch.float32)
+    if dtype != alt.I8:
+        h.gemm_grouped_dx(d, dy, w, o, dx)
+    torch.cuda.synchronize()
+    assert y.untouched() and dx.untouched()
+    for lo in range(0, rows, 20000):
+        part = slice(lo, lo + 20000)
+        own = w[expert[part].clamp(min=0)].float() * (expert[part] >= 0)[:, None, None]
+        assert torch.equal(y.t[part], (own * x[part, None, :].float()).sum(2))
+        if dtype != alt.I8:
+            assert torch.equal(dx.t[part], (own * dy[part, :, None].float()).sum(1))
+
+
+@pytest.mark.parametrize("E,mean,N,K,dtype", [(70, 500, 2048, 512, alt.BF16), (130, 500, 1024, 1024, alt.I8), (130, 500, 1024, 1024, alt.BF16), (2100, 240, 1024, 64, alt.BF16)])
+def test_large_tiles_of_many_experts(h, E, mean, N, K, dtype):
+    """Groups that end anywhere in a tile, empty ones, rows of no expert before and behind, in large tiles and the small ones at their ends; all sums exact."""
+    counts = np.random.default_rng(E).integers(0, 2 * mean, E)
+    counts[[0, 1, 2, 3, 4, 5, 62, 63, 64, E - 1]] = [256, 0, 1, 128, 129, 511, 0, 255, 0, 384]
+    counts = counts * (E * mean) // counts.sum()
+    off = np.concatenate([[0], np.cumsum(counts)]) + 130
+    off, rows, td = off.tolist(), int(off[-1]) + 300, TORCH[dtype]
+    x, w, y = small_integers((rows, K), td, 1), small_integers((E, N, K), td, 2), Canary(rows, N, torch.float32)
+    one = dict(a_scale=torch.ones(rows, device="cuda"), b_scale=torch.ones(E, N, device="cuda")) if dtype == alt.I8 else {}
+    d, o = alt.grouped_desc(rows, E, N, K, in_dtype=dtype, out_dtype=alt.F32), make_offsets(off)
+    h.gemm_grouped(d, x, w, o, y, **one)
+    torch.cuda.synchronize()
+    assert y.untouched() and not y.t[:130].any() and not y.t[off[-1]:].any()
+    for e, lo, hi in spans_of(off):
+        assert torch.equal(y.t[lo:hi], x[lo:hi].float() @ w[e].float().T), e
+    if dtype == alt.I8:
+        return
+    dy, dx = small_integers((rows, N), td, 3), Canary(rows, K, torch.float32)
+    del y
+    h.gemm_grouped_dx(d, dy, w, o, dx)
+    torch.cuda.synchronize()
+    assert dx.untouched() and not dx.t[:130].any() and not dx.t[off[-1]:].any()
+    for e, lo, hi in spans_of(off):
+        assert torch.equal(dx.t[lo:hi], dy[lo:hi].float() @ w[e].float()), e
+
+
 def test_no_rows(h):
     E, N, K = 3, 64, 64
     o = make_offsets([0, 0, 0, 0])
