@@ -527,8 +527,8 @@ alt_status_t alt_gemm_i8_workspace_size(alt_handle_t h, const alt_gemm_i8_desc_t
 /* A layer of experts: `rows` tokens in the order of their experts, expert e owning the rows [offsets[e], offsets[e+1]).  `offsets` is an
  * int32 array of groups + 1 on the device, not decreasing, read when the kernels run; an expert may own no row.  Rows before offsets[0]
  * and from offsets[groups] on belong to no expert.  (Offsets outside 0 .. rows are clamped; with offsets out of order results are
- * unspecified, but nothing outside the buffers is read or written.)  2^30 rows, 2^20 experts and 2^22 elements between rows at most, here and
- * in alt_gemm_i8. */
+ * unspecified, but nothing outside the buffers is written, nor read but for the rest of the aligned dwords that they begin and end in.)
+ * 2^30 rows, 2^20 experts and 2^22 elements between rows at most, here and in alt_gemm_i8. */
 typedef struct {
     int64_t rows, N, K;           /* rows may be 0 */
     int64_t lda, ldb, ldc;        /* elements between rows of a and dx; of b and dw (an expert's matrix is N * ldb elements); of y and dy; 0 = dense */

@@ -48,8 +48,8 @@ enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpMask = 4, kGrpWhole = 8, kGrpPacked = 
 // (kGrpWhole: the columns are whole 16-byte chunks of the output, and whole fours; kGrpPacked: operand rows are filled up with zeros to whole chunks)
 
 template <typename T> struct GrpTraits;
-// (SUMS: sums per output.  fp32 keeps four, each over every fourth product, added at the end: that halves their rounding error, 5e-7 to 2.5e-7 of the
-// result in the 2-norm at reductions of 1000.)
+// (SUMS: sums per output and wave.  fp32 keeps four, each over every fourth product, added at the end: that halves their rounding error, 5.7e-7 to 2.9e-7
+// of the result in the 2-norm at reductions of 1000; the kernel for any alignment keeps two.)
 template <> struct GrpTraits<bf16_tag> { static constexpr int ES = 2, SUMS = 1; typedef floatx16_t acc_t; };
 template <> struct GrpTraits<float> { static constexpr int ES = 4, SUMS = 4; typedef floatx16_t acc_t; };
 typedef int intx16_t __attribute__((ext_vector_type(16)));
@@ -688,8 +688,9 @@ __device__ __forceinline__ void grp_mma16(typename GrpFew<T>::acc_t (&c)[GrpTrai
     }
 }
 
-// 32 bytes at p.  Memory takes more than twice as long over addresses inside a dword (16 x 6005 x 8192 in 8 bits 27.4 us, 14.3 at whole dwords), so
-// where there are such (!DW) they are the eight dwords they start in and, if they start inside one, the dword they end in, shifted together.
+// 32 bytes at p, or the aligned dwords that hold them.  Memory takes more than twice as long over addresses inside a dword (16 x 6005 x 8192 in 8 bits
+// 27.4 us, 14.3 at whole dwords), so where there are such (!DW) they are the eight dwords they start in and, if they start inside one, the dword they
+// end in, shifted together.
 template <bool DW>
 struct GrpPair {
     u32x4_t lo, hi;
@@ -920,9 +921,9 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_dx_kernel(const GroupedPa
 // Chunks of 16 bytes are loaded at whatever address they start at.  Rows and columns that do not exist repeat the tile's last ones (their sums are
 // never stored), or, where the outer index is contiguous, the last tile is moved back to end with the matrix (what two tiles both compute they
 // compute alike); so only the reduction's last step has chunks of which a part exists.  Loads are two steps ahead: those of step s + 2 go out
-// before step s is computed, and reach LDS behind it a step later (four steps ahead: 12.8 us for 12.0 at 64 x 1001 x 2049 in 8 bits).  WGK = 2: twice
+// before step s is computed, and reach LDS behind it a step later (four steps ahead: 12.4 us for 11.7 at 333 x 1001 x 2049 in 8 bits).  WGK = 2: twice
 // the waves, halves of every step's chunks to each half of them, whose sums meet in LDS.  Bound in 8 and 16 bits by the issue of loads, LDS
-// writes and reads (5000 rows of 5 groups, 2047 x 4095, bf16 147 us, 0.57 PFLOP/s), in fp32 by the matrix instructions (690 us, 122 TFLOP/s).
+// writes and reads (5000 rows of 5 groups, 2047 x 4095, bf16 132 to 147 us, 0.6 PFLOP/s), in fp32 by the matrix instructions (690 us, 122 TFLOP/s).
 template <int ES, bool RED, int OUTER, int BKB, int THREADS>
 struct GrpLoader {
     using Op = GrpOperand<ES, RED, OUTER, BKB>;
@@ -1051,7 +1052,8 @@ __global__ __launch_bounds__(64 * WGM * WGN * WGK) void grouped_any_kernel(const
         for (int i = 0; i < LB::NL; ++i) *(u32x4_t *)(d + A::BYTES + (i * THREADS + t) * 16) = vb[i];
     };
 
-    // (two sums for fp32: four take the registers of a third wave, and 1001 rows of 13 groups, 515 x 1030, 34 us forward for 30)
+    // (two sums for fp32: four take the registers of a third wave, and 1001 rows of 13 groups, 515 x 1030, 34 us forward for 30.  Their error is 4.0e-7
+    // at reductions of 1000, and with WGK = 2, which makes four of them, 2.9e-7)
     GrpSums<T, TM, TN, (ES == 4 ? 2 : 1)> acc;
     acc.clear();
     float sums[TM];                                        // kWeights: of this lane's row of the left operand
@@ -1187,11 +1189,11 @@ struct GrpStream {
 };
 
 // Tiles of 64x64, 128x64 and 128x128: a workgroup's operands run through a ring of NS stages in LDS.  At the barrier of step s the stages of steps s and
-// s + 1 have landed and every wave has read stage s - 1 for the last time; then the loads of step s + NS - 1 go out into that stage, and each
-// chunk's fragments are read three chunks before they are used, across the barrier too (a read takes about as long as four matrix instructions).
-// A wave issues in order, and a matrix instruction hides eight other instructions at most: behind each stand a few operand reads and loads, and
-// the order is pinned.  Bound by latency on small calls (the loads of three steps in flight are what hides it: 64 x 4096 x 4096 in 8 bits 9.6 us,
-// 1.8 TB/s), by operand delivery into LDS above (2048 x 768 x 3072 in 8 bits 13.3 us, 80 GB/s to a compute unit).
+// s + 1 have landed and every wave has read stage s - 1 for the last time; then the loads of step s + NS - 1 go out into that stage, and each chunk's
+// fragments are read three chunks before they are used, across the barrier too (a read takes about as long as four matrix instructions).  A wave issues
+// in order, and a matrix instruction hides eight other instructions at most: behind each stand a few operand reads and loads, and the order is pinned.
+// Bound by latency on small calls (the loads of three steps in flight are what hides it: 64 x 4096 x 4096 in 8 bits 9.6 us, 1.8 TB/s), by operand
+// delivery into LDS above (2048 x 768 x 3072 in 8 bits, 192 tiles of 128x64, 13.0 us: steps of 24 KB in 0.33 us, 73 GB/s to a compute unit).
 template <typename T, int FORM, int BM, int BN, int WGM, int WGN, int BKB, int NS>
 struct GrpRing {
     using type = T;
@@ -1319,13 +1321,13 @@ struct GrpRing {
     }
 };
 
-// Tiles of 256x256, eight waves of 128x64 each: 64 KB of operands for 128 bytes of the reduction.  A step takes whole cache lines (with steps of
-// 64 bytes each line comes to the L1 twice, and these requests are the bound: 8192 x 8192 x 8192 in bf16 870 us, so 785 us, 1.40 PFLOP/s; in 8
-// bits 470 and 433 us, 2.54 POP/s, where the chip's power is the bound: it runs at two thirds of its clock).  Two stages fit and a half, so the
-// ring has five units of one operand each, A and B in turn.  One barrier a step stands before its last chunk, whose fragments every wave has read
-// by then: the step's two units are free, the next step's have landed, and its first fragments are read behind the last chunk's matrix
-// instructions.  Into the freed units go B of the step after next (which has one step to land) and A of the one behind it (which has two), the
-// loads evenly behind the matrix instructions of this chunk and the next.
+// Tiles of 256x256, eight waves of 128x64 each: 64 KB of operands for 128 bytes of the reduction.  A step takes whole cache lines (with steps of 64
+// bytes each line comes to the L1 twice, and these requests are the bound: 8192 x 8192 x 8192 in bf16 870 us, so 780 us, 1.41 PFLOP/s, and a library's
+// product 673; in 8 bits 470 and 428 us, 2.57 POP/s, the library's 441, where the chip's power is the bound: it runs at two thirds of its clock).  Two
+// stages fit and a half, so the ring has five units of one operand each, A and B in turn.  One barrier a step stands before its last chunk, whose
+// fragments every wave has read by then: the step's two units are free, the next step's have landed, and its first fragments are read behind the last
+// chunk's matrix instructions.  Into the freed units go B of the step after next (which has one step to land) and A of the one behind it (which has
+// two), the loads evenly behind the matrix instructions of this chunk and the next.
 template <typename T, int FORM>
 struct GrpWide {
     using type = T;
@@ -1730,11 +1732,13 @@ inline GrpTime grp_rounds(double tiles, double places, double units, double fixe
     return {rounds * fixed, rounds * per_unit * units * (0.5 + 0.5 * tiles / (rounds * places))};
 }
 
-// Whether a forward product runs in tiles of 16 rows.  Up to 16 rows each, the weights are what there is to read, and they are read once: 16 x 4096 x
-// 4096 in 8 bits 6.6 us.  With more rows, where these tiles are so few that they all run at once, as the other kernels would leave most of the chip
-// idle: 64 x 1024 x 4096 (256 tiles) 6.6 us for 12.8, 512 x 64 x 4096 6.4 for 12.8; 32 x 8192 x 8192 (1024) 25.1 for 16.4, 64 x 3000 x 2048 (752) 8.4 for
-// 6.7.  In fp32 the others are slower and the line lies higher: 512 x 512 x 2048 (1024 tiles) 26.5 us for 42.8; 256 rows of 8 groups, 2048 x 2048
-// (2048), 51.5 for 47.2.
+// Whether a forward product runs in tiles of 16 rows.  With up to 16 rows a group in the mean, even groups' weights are what there is to read, and they
+// are read once: 16 x 4096 x 4096 in 8 bits 6.6 us.  A popular group's are read for every 16 of its rows, again from the caches, which takes about as
+// long as the weights of as many groups from memory and far longer than large tiles would: 1000 rows of 64 groups, 4096 x 4096 bf16, even 441 us, half
+// of them in one group 517, all in one 340 (that group alone, in larger tiles, 41); in 8 bits 225, 264 and 179 (25).  With more rows, where these tiles
+// are so few that they all run at once, as the other kernels would leave most of the chip idle: 64 x 1024 x 4096 (256 tiles) 6.6 us for 12.8, 512 x 64 x
+// 4096 6.4 for 12.8; 32 x 8192 x 8192 (1024) 25.1 for 16.4, 64 x 3000 x 2048 (752) 8.4 for 6.7.  In fp32 the others are slower and the line lies higher:
+// 512 x 512 x 2048 (1024 tiles) 26.5 us for 42.8; 256 rows of 8 groups, 2048 x 2048 (2048), 51.5 for 47.2.
 inline bool grp_is_few(const GroupedParams &p, int ES)
 {
     const int64_t spans = !p.offsets ? 1 : p.groups < p.rows ? p.groups : p.rows;
@@ -1790,8 +1794,8 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
         if constexpr (ES < 4) {
             if (grp_tiles<FORM>(p, 128, 128) >= 0.5 * places) return grouped_any<T, FORM, 128, 128, 2, 4, 1>(p, st);
         }
-        // While each compute unit has two tiles at most, twice the waves, which share every step's chunks: 64 x 1001 x 2049 in 8 bits 11.0 us for 12.1,
-        // 1001 fp32 rows of 13 groups, 515 x 1030, 25.2 for 26.9; at 5000 rows, 2047 x 4095, 697 and 693.
+        // While each compute unit has two tiles at most, twice the waves, which share every step's chunks: 333 x 1001 x 2049 in 8 bits 11.7 us for 13.1,
+        // 1001 fp32 rows of 13 groups, 515 x 1030, 25.9 for 27.1; at 5000 rows, 2047 x 4095, 697 and 693.
         if constexpr (FORM != kWeights) {
             if (grp_tiles<FORM>(p, 64, 64) <= 2 * places) return grouped_any<T, FORM, 64, 64, 2, 2, 2>(p, st);
         }

@@ -1,6 +1,7 @@
 // Rows to 8 bits: s = max|x| / 127 rounded up to 16 significant bits (at least 2^-126), q = x / s to the nearest whole number, ties
 // to even.  Bound by memory: one read of x, one write of q.  A row stays in the registers of its threads between the maximum and
-// the rounding; rows too long for that are read twice, the second time from the caches.  16384 x 4096 bf16: 33 to 37 us, 5.4 to 6 TB/s.
+// the rounding; rows too long for that are read twice, the second time from the caches.  16384 x 4096 bf16: 38 to 40 us, 5.1 to 5.3 TB/s,
+// inputs from memory (one input again and again comes in part from the last-level cache: 32 to 38).
 #include <hip/hip_runtime.h>
 
 #include "common.h"
@@ -155,8 +156,9 @@ template <int ELSZ>
 void quantize_run(const void *x, int64_t ldx, void *q, int64_t ldq, float *scale, int64_t rows, int cols, hipStream_t st)
 {
     // A wave for each of many short rows (16384 x 1000 10.9 us, 16.4 with a workgroup each; 16384 x 2048 bf16 19.6 and 22.6, fp32 26.8 and 25.7), a
-    // workgroup for the others (1 x 4096 2.6 us, 5.2 with a wave; 16384 x 4096 31.8 us, 6.3 TB/s, and 43.1), which keeps as many chunks as it needs
-    // up to 8192 columns (4096 x 8192 19.1 us with four to a thread, 22.2 with two, the rest read again; 16384 x 4096 31.8 with two, 33.4 with four).
+    // workgroup for the others (1 x 4096 2.6 us, 5.2 with a wave; 16384 x 4096 31.8 us and 43.1; each pair from one run, one input again and
+    // again), which keeps as many chunks as it needs up to 8192 columns (4096 x 8192 19.1 us with four to a thread, 22.2 with two, the rest read
+    // again; 16384 x 4096 31.8 with two, 33.4 with four).
     if constexpr (ELSZ == 2) {
         if (cols > 1024 && cols <= 2048 && rows >= 512) return quantize_launch<ELSZ, 64, 4>(x, ldx, q, ldq, scale, rows, cols, st);
     }
