@@ -562,6 +562,124 @@ alt_status_t alt_gemm_grouped_workspace_size(alt_handle_t h, const alt_grouped_d
 alt_status_t alt_gemm_grouped_dx_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);
 alt_status_t alt_gemm_grouped_dw_workspace_size(alt_handle_t h, const alt_grouped_desc_t *d, size_t *bytes);
 
+/* ---- what stands around the products of a layer ----------------------------
+ *
+ * Layer norm, the choice of experts, the exchange of rows between the order of the tokens and that of the experts (what alt_gemm_grouped and its
+ * gradients take), and a product with low-rank adapters.  As in the calls above, row strides are in elements, 0 = dense; buffers need the
+ * alignment of their elements and must not overlap; rows of 16-byte chunks at 16-byte addresses are fastest; all calls are asynchronous on
+ * `stream` and give the same bits for the same inputs, whatever runs beside them.  The handle's device has to be the current one (the calls
+ * refuse any other).  A workspace is the caller's, needs the bytes its size call names (at any address; less is ALT_WORKSPACE_TOO_SMALL), holds
+ * nothing between calls, and must not be in use by two streams at once.  2^30 rows, tokens or (token, choice) pairs, 2^24 columns at most. */
+
+typedef struct {
+    int64_t rows, cols;           /* rows may be 0 */
+    int64_t x_stride, y_stride;   /* elements between rows of x and dx; of y and dy */
+    int32_t in_dtype, out_dtype;  /* of x and dx; of y and dy: ALT_F32 or ALT_BF16 */
+    float eps;                    /* >= 0 */
+    int32_t reserved;
+} alt_norm_desc_t;
+
+/* mean[m] = sum_c x[m,c] / cols, rstd[m] = 1 / sqrt(sum_c (x[m,c] - mean[m])^2 / cols + eps),
+ * y[m,c] = (x[m,c] - mean[m]) * rstd[m] * gamma[c] + beta[c].
+ * gamma and beta (fp32) may be NULL: ones, zeros.  mean and rstd (fp32), which the gradient takes, may be NULL.  Everything between x and y is
+ * fp32; y is rounded once. */
+alt_status_t alt_layer_norm(alt_handle_t h, const alt_norm_desc_t *d, const void *x, const float *gamma, const float *beta, void *y, float *mean,
+                            float *rstd, void *stream);
+
+/* Gradients from dy, with u = (x - mean) * rstd and g = dy * gamma (mean and rstd as the forward call left them):
+ *   dx[m,c] = rstd[m] * (g[m,c] - mean_c(g[m]) - u[m,c] * mean_c(g[m] u[m])),  dgamma[c] = sum_m dy[m,c] u[m,c],  dbeta[c] = sum_m dy[m,c].
+ * gamma may be NULL as before; dgamma and dbeta (fp32) may be NULL where they are not wanted.  Without rows they are zeros. */
+alt_status_t alt_layer_norm_grad(alt_handle_t h, const alt_norm_desc_t *d, const void *dy, const void *x, const float *mean, const float *rstd,
+                                 const float *gamma, void *dx, float *dgamma, float *dbeta, void *workspace, size_t ws_bytes, void *stream);
+alt_status_t alt_layer_norm_grad_workspace_size(alt_handle_t h, const alt_norm_desc_t *d, size_t *bytes);
+
+#define ALT_SCORE_SOFTMAX 0
+#define ALT_SCORE_SIGMOID 1
+#define ALT_ROUTE_MAX_EXPERTS 1024
+#define ALT_ROUTE_MAX_TOP_K 32
+
+typedef struct {
+    int64_t tokens;               /* may be 0 */
+    int64_t stride;               /* elements between rows of logits and dlogits */
+    int32_t experts, top_k;       /* top_k <= top_groups * experts / groups */
+    int32_t groups, top_groups;   /* groups of experts / groups consecutive experts each, and how many of them a token chooses from; 1, 1 = no groups */
+    int32_t group_best;           /* 1 or 2: of how many choices a group's worth is the sum */
+    int32_t score;                /* ALT_SCORE_* */
+    int32_t renormalize;          /* 0 or 1 */
+    int32_t dtype;                /* of logits and dlogits: ALT_F32 or ALT_BF16 */
+    float scale;                  /* of the weights */
+    int32_t reserved;
+} alt_route_desc_t;
+
+/* The experts of each token, of its row of logits (tokens x experts):
+ *   score   softmax over the experts, or sigmoid;
+ *   choice  score + bias[e] where `bias` (fp32, may be NULL) is given, the logit itself otherwise;
+ *   groups  with top_groups < groups a group is worth the sum of the group_best largest choices in it (scores where there is no bias), and a
+ *           token chooses from the experts of its top_groups worthiest groups only;
+ *   experts[token][top_k]  the top_k experts of largest choice, in that order, ties by the lower index (of groups, too).  Choices are compared as if
+ *           computed in 64 bits;
+ *   weights[token][top_k]  score * scale, with `renormalize` divided by the sum of the token's chosen scores before (a sum of zero counts as one).
+ * A logit of -inf (or a choice that is -inf or NaN) takes its expert out, a group without experts too; what a token lacks of top_k experts is expert -1
+ * with weight 0, so a padded row of logits may be all -inf.  A row with a NaN (softmax: or +inf) has no experts and weights NaN.
+ * The order of the experts, as alt_gemm_grouped takes it: offsets[e] (groups + 1 = experts + 1 of them) is the first row of expert e, its rows
+ * ordered by token, then by choice, and rows[token][top_k] is the row of each choice, -1 for expert -1. */
+alt_status_t alt_route(alt_handle_t h, const alt_route_desc_t *d, const void *logits, const float *bias, int32_t *experts, float *weights, int32_t *rows,
+                       int32_t *offsets, void *workspace, size_t ws_bytes, void *stream);
+alt_status_t alt_route_workspace_size(alt_handle_t h, const alt_route_desc_t *d, size_t *bytes);
+
+/* Gradient by the logits from that of the weights, the choice being constant: for the chosen experts j of a token with scores s[j], sum Z,
+ *   ds[j] = scale * dweights[j],  with `renormalize`  ds[j] = scale / Z * (dweights[j] - sum_i dweights[i] s[i] / Z),
+ *   softmax  dlogits[e] = s[e] * (ds[e] - sum_j ds[j] s[j])  (ds[e] = 0 where e is not chosen),  sigmoid  dlogits[e] = ds[e] s[e] (1 - s[e]).
+ * `experts` is alt_route's.  Experts -1 (or outside 0 .. experts - 1) have no part, and a token without any has zeros. */
+alt_status_t alt_route_grad(alt_handle_t h, const alt_route_desc_t *d, const void *logits, const int32_t *experts, const float *dweights, void *dlogits,
+                            void *stream);
+
+typedef struct {
+    int64_t tokens;               /* rows of the tensors in the tokens' order; may be 0 */
+    int64_t rows;                 /* rows of the tensors in the experts' order; may be 0 */
+    int64_t cols;
+    int64_t token_stride, row_stride;   /* elements between rows of either */
+    int32_t top_k;                /* choices of a token, ALT_ROUTE_MAX_TOP_K at most */
+    int32_t dtype;                /* of all but weights: ALT_F32 or ALT_BF16 */
+} alt_exchange_desc_t;
+
+/* Tokens into the experts' order: y[rows[t][j]] = x[t] for every choice j.  `rows` (tokens x top_k, int32) is alt_route's: -1 (any number outside
+ * 0 .. d->rows - 1) is no row, and no row stands twice (if one does, which of the tokens it holds is unspecified).  Rows of y that no choice names
+ * are left as they were. */
+alt_status_t alt_dispatch_rows(alt_handle_t h, const alt_exchange_desc_t *d, const void *x, const int32_t *rows, void *y, void *stream);
+
+/* And back: y[t] = sum_j weights[t][j] * x[rows[t][j]], in the order of the choices, in fp32, rounded once.  A choice without a row is a row of zeros
+ * (so a token without any is zeros, or NaN where its weights are).  weights (fp32) may be NULL: ones, which makes this the gradient of
+ * alt_dispatch_rows (x = gradient by its y, y = gradient by its x). */
+alt_status_t alt_combine_rows(alt_handle_t h, const alt_exchange_desc_t *d, const void *x, const int32_t *rows, const float *weights, void *y,
+                              void *stream);
+
+/* Gradients of alt_combine_rows: dx[rows[t][j]] = weights[t][j] * dy[t], dweights[t][j] = sum_c dy[t,c] * x[rows[t][j],c] (0 for a choice without a
+ * row).  Rows of dx that no choice names are left as they were.  dweights may be NULL, and x with it; weights NULL: ones. */
+alt_status_t alt_combine_rows_grad(alt_handle_t h, const alt_exchange_desc_t *d, const void *dy, const void *x, const int32_t *rows,
+                                   const float *weights, void *dx, float *dweights, void *stream);
+
+#define ALT_ADAPTERS_MAX_RANK 512
+
+typedef struct {
+    int64_t M, N, K;              /* M may be 0 */
+    int64_t lda, ldb, ldc;        /* elements between rows of x, w and y */
+    int32_t adapters, rank;
+    int32_t in_dtype;             /* of x, w, a, b: ALT_BF16 or ALT_F32 */
+    int32_t out_dtype;            /* ALT_F32, or (not for ALT_F32 operands) ALT_BF16 */
+    int32_t epilogue;             /* ALT_EPI_* flags */
+    int32_t reserved;
+} alt_adapters_desc_t;
+
+/* A projection that all rows share with a low-rank one beside it for each row's request, g = adapter[m]:
+ *   y[m,n] = sum_k x[m,k] w[n,k] + scale[g] * sum_r (sum_k x[m,k] a[g,r,k]) b[g,n,r]  (+ bias[n], then max(., 0) by `epilogue`).
+ * x is M x K, w N x K; a (adapters x rank x K) and b (adapters x N x rank) are dense.  adapter (int32, M of them, on the device) may name any of the
+ * adapters in any order; -1 (any number outside 0 .. adapters - 1) is a row without one.  scale (fp32, of each adapter) may be NULL: ones.  The inner
+ * sum keeps 16 bits or more of its fp32 value; everything else is fp32, rounded once.  An infinity or NaN in an adapter reaches its own rows only. */
+alt_status_t alt_gemm_adapters(alt_handle_t h, const alt_adapters_desc_t *d, const void *x, const void *w, const int32_t *adapter, const void *a,
+                               const void *b, const float *scale, const float *bias, void *y, void *workspace, size_t ws_bytes, void *stream);
+alt_status_t alt_gemm_adapters_workspace_size(alt_handle_t h, const alt_adapters_desc_t *d, size_t *bytes);
+
 /* ---- joint tuning (Section 5.2: cross exploration — pick a layout, tune the
  *      loops under it, feed the best latency back; budget counted in on-device
  *      measurements as in Section 6) --------------------------------------- */

@@ -11,8 +11,8 @@ import os as _os
 # Only effective if set before the HIP runtime starts in this process.
 _os.environ.setdefault("HIP_FORCE_DEV_KERNARG", "1")
 
-from .binding import (AltError, Handle, Layout, ConvDesc, Conv3dDesc, ConvCall, GemmDesc, GemmI8Desc, GroupedDesc, TuneOpts, TuneReport,
-                      ChainPlan, GraphNode, GraphPlan, NODE_CONV, NODE_ADD, Prim, Peaks, F32, BF16, I8, EPI_BIAS, EPI_RELU,
+from .binding import (AltError, Handle, Layout, ConvDesc, Conv3dDesc, ConvCall, GemmDesc, GemmI8Desc, GroupedDesc, NormDesc, RouteDesc, ExchangeDesc, AdaptersDesc, TuneOpts, TuneReport,
+                      ChainPlan, GraphNode, GraphPlan, NODE_CONV, NODE_ADD, Prim, Peaks, F32, BF16, I8, EPI_BIAS, EPI_RELU, SCORE_SOFTMAX, SCORE_SIGMOID,
                       SplitkStatus, TransformPlan, MultiPlan, layout_parse, layout_from_prims, layout_physical_shape, layout_offset,
                       layout_index_of, plan_chain, plan_graph, graph_node, unfold_shape, split, reorder, fuse, version, lib,
-                      conv_desc, conv3d_desc, gemm_desc, gemm_i8_desc, grouped_desc, exported_symbols, library_path)
+                      conv_desc, conv3d_desc, gemm_desc, gemm_i8_desc, grouped_desc, norm_desc, route_desc, exchange_desc, adapters_desc, exported_symbols, library_path)

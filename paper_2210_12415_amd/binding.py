@@ -8,7 +8,7 @@ try:
     from . import _altcall as _native
 except ImportError:                       # built where Python's headers are (build.py)
     _native = None
-if not hasattr(_native, "gemm_grouped_dw"):   # (nor is one that an older source was built to)
+if not hasattr(_native, "gemm_adapters"):   # (nor is one that an older source was built to)
     _native = None
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -16,6 +16,7 @@ _LIBPATH = os.environ.get("ALT_LIBRARY", os.path.join(_HERE, "libalt.so"))   # A
 
 F32, BF16, I8 = 0, 1, 2
 EPI_BIAS, EPI_RELU = 1, 2
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 MAX_RANK, MAX_PRIMS, MAX_CAND, MAX_CHAIN = 8, 8, 16, 8
 
 _STATUS = ["ok", "invalid argument", "invalid layout", "shape mismatch", "unsupported",
@@ -88,6 +89,27 @@ class GemmI8Desc(ctypes.Structure):
 class GroupedDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("rows", "N", "K", "lda", "ldb", "ldc")] + \
                [(n, ctypes.c_int32) for n in ("groups", "in_dtype", "out_dtype", "epilogue")]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "cols", "x_stride", "y_stride")] + \
+               [("in_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("tokens", "stride")] + \
+               [(n, ctypes.c_int32) for n in ("experts", "top_k", "groups", "top_groups", "group_best", "score", "renormalize", "dtype")] + \
+               [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ExchangeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("tokens", "rows", "cols", "token_stride", "row_stride")] + \
+               [("top_k", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "K", "lda", "ldb", "ldc")] + \
+               [(n, ctypes.c_int32) for n in ("adapters", "rank", "in_dtype", "out_dtype", "epilogue", "reserved")]
 
 
 class TuneOpts(ctypes.Structure):
@@ -178,7 +200,8 @@ def lib():
         L.alt_version.restype = ctypes.c_char_p
         if _native is not None:
             _native.setup(*[ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _REPEATED],
-                          ctypes.c_void_p, ConvDesc, Conv3dDesc, GemmDesc, Layout, GemmI8Desc, GroupedDesc)
+                          ctypes.c_void_p, ConvDesc, Conv3dDesc, GemmDesc, Layout, GemmI8Desc, GroupedDesc, NormDesc, RouteDesc, ExchangeDesc,
+                          AdaptersDesc)
         _lib = L
     return _lib
 
@@ -193,13 +216,17 @@ _PROTOTYPES = {"alt_layout_transform": (_V, _I, _I, _V, _V, _V, _V, _V, _V), "al
                "alt_conv2d_transpose": _OPERATOR, "alt_conv3d_transpose": _OPERATOR,
                "alt_quantize_rows": (_V, _I, _L, _L, _V, _L, _V, _L, _V, _V), "alt_gemm_i8": (_V,) * 9 + (ctypes.c_size_t, _V),
                "alt_gemm_grouped": (_V,) * 10 + (ctypes.c_size_t, _V), "alt_gemm_grouped_dx": (_V,) * 8 + (ctypes.c_size_t, _V),
-               "alt_gemm_grouped_dw": (_V,) * 8 + (ctypes.c_size_t, _V)}
+               "alt_gemm_grouped_dw": (_V,) * 8 + (ctypes.c_size_t, _V), "alt_layer_norm": (_V,) * 9,
+               "alt_layer_norm_grad": (_V,) * 11 + (ctypes.c_size_t, _V), "alt_route": (_V,) * 9 + (ctypes.c_size_t, _V), "alt_route_grad": (_V,) * 7,
+               "alt_dispatch_rows": (_V,) * 6, "alt_combine_rows": (_V,) * 7, "alt_combine_rows_grad": (_V,) * 9,
+               "alt_gemm_adapters": (_V,) * 11 + (ctypes.c_size_t, _V)}
 _calls = {}
 
 # The same calls by the native module (native/altcall.c), for arguments of plain types; it answers None to others, and without the module
 # everything is another.  (A conversion's arguments took 1.8 us through ctypes, beside 3.5 for the launch.)
 _REPEATED = ("alt_conv2d", "alt_conv3d", "alt_conv2d_transpose", "alt_conv3d_transpose", "alt_gemm", "alt_layout_transform", "alt_eltwise_add",
-             "alt_quantize_rows", "alt_gemm_i8", "alt_gemm_grouped", "alt_gemm_grouped_dx", "alt_gemm_grouped_dw")
+             "alt_quantize_rows", "alt_gemm_i8", "alt_gemm_grouped", "alt_gemm_grouped_dx", "alt_gemm_grouped_dw", "alt_layer_norm",
+             "alt_layer_norm_grad", "alt_route", "alt_route_grad", "alt_dispatch_rows", "alt_combine_rows", "alt_combine_rows_grad", "alt_gemm_adapters")
 
 
 def _not_taken(*_):
@@ -214,6 +241,9 @@ _quick_conv2d, _quick_conv3d = _quick("conv2d"), _quick("conv3d")
 _quick_conv2d_transpose, _quick_conv3d_transpose = _quick("conv2d_transpose"), _quick("conv3d_transpose")
 _quick_quantize, _quick_gemm_i8 = _quick("quantize_rows"), _quick("gemm_i8")
 _quick_grouped, _quick_grouped_dx, _quick_grouped_dw = _quick("gemm_grouped"), _quick("gemm_grouped_dx"), _quick("gemm_grouped_dw")
+_quick_layer_norm, _quick_layer_norm_grad, _quick_route, _quick_route_grad = _quick("layer_norm"), _quick("layer_norm_grad"), _quick("route"), _quick("route_grad")
+_quick_dispatch_rows, _quick_combine_rows, _quick_combine_rows_grad = _quick("dispatch_rows"), _quick("combine_rows"), _quick("combine_rows_grad")
+_quick_gemm_adapters = _quick("gemm_adapters")
 _quick_gemm, _quick_transform, _quick_add, _quick_prepare = _quick("gemm"), _quick("layout_transform"), _quick("eltwise_add"), _quick("prepare_conv2d")
 
 
@@ -241,7 +271,9 @@ def exported_symbols():
             "alt_eltwise_add", "alt_tune_graph", "alt_plan_graph", "alt_unfold", "alt_unfold_shape",
             "alt_cache_save", "alt_cache_load", "alt_cache_clear", "alt_get_peak", "alt_layout_transform_plan", "alt_splitk_status", "alt_conv2d_static", "alt_layout_transform_pad",
             "alt_quantize_rows", "alt_gemm_i8", "alt_gemm_i8_workspace_size", "alt_gemm_grouped", "alt_gemm_grouped_dx", "alt_gemm_grouped_dw",
-            "alt_gemm_grouped_workspace_size", "alt_gemm_grouped_dx_workspace_size", "alt_gemm_grouped_dw_workspace_size"]
+            "alt_gemm_grouped_workspace_size", "alt_gemm_grouped_dx_workspace_size", "alt_gemm_grouped_dw_workspace_size",
+            "alt_layer_norm", "alt_layer_norm_grad", "alt_layer_norm_grad_workspace_size", "alt_route", "alt_route_workspace_size", "alt_route_grad",
+            "alt_dispatch_rows", "alt_combine_rows", "alt_combine_rows_grad", "alt_gemm_adapters", "alt_gemm_adapters_workspace_size"]
 
 
 def version():
@@ -443,6 +475,26 @@ def gemm_i8_desc(M, N, K, out_dtype=BF16, epilogue=0, lda=0, ldb=0, ldc=0):
 def grouped_desc(rows, groups, N, K, in_dtype=BF16, out_dtype=BF16, epilogue=0, lda=0, ldb=0, ldc=0):
     """A layer of experts: lda, ldb, ldc are the row strides of a (and dx), b (and dw), y (and dy) in elements, 0 where dense."""
     return GroupedDesc(rows, N, K, lda, ldb, ldc, groups, in_dtype, out_dtype, epilogue)
+
+
+def norm_desc(rows, cols, in_dtype=BF16, out_dtype=BF16, eps=1e-5, x_stride=0, y_stride=0):
+    """Layer norm: in_dtype and x_stride of x and dx, out_dtype and y_stride of y and dy."""
+    return NormDesc(rows, cols, x_stride, y_stride, in_dtype, out_dtype, eps, 0)
+
+
+def route_desc(tokens, experts, top_k, dtype=F32, score=SCORE_SOFTMAX, groups=1, top_groups=1, group_best=2, renormalize=False, scale=1.0, stride=0):
+    """The choice of top_k experts: dtype and stride of the logits and their gradient."""
+    return RouteDesc(tokens, stride, experts, top_k, groups, top_groups, group_best, score, operator.index(renormalize), dtype, scale, 0)
+
+
+def exchange_desc(tokens, top_k, rows, cols, dtype=BF16, token_stride=0, row_stride=0):
+    """Rows of `cols` elements: `tokens` of them in the tokens' order, token_stride apart, `rows` in the experts' order, row_stride apart."""
+    return ExchangeDesc(tokens, rows, cols, token_stride, row_stride, top_k, dtype)
+
+
+def adapters_desc(M, N, K, adapters, rank, in_dtype=BF16, out_dtype=BF16, epilogue=0, lda=0, ldb=0, ldc=0):
+    """A product with low-rank adapters beside it: lda, ldb, ldc are the row strides of x, w and y in elements, 0 where dense."""
+    return AdaptersDesc(M, N, K, lda, ldb, ldc, adapters, rank, in_dtype, out_dtype, epilogue, 0)
 
 
 # ----------------------------------------------------------------------- handle ----
@@ -746,6 +798,48 @@ class Handle:
 
     def gemm_grouped_dw(self, d, a, dy, offsets, dw, dbias=None, workspace=None, ws_bytes=0, stream=None):
         self._buffers(_quick_grouped_dw, "alt_gemm_grouped_dw", d, (a, dy, offsets, dw, dbias), workspace, ws_bytes, stream)
+
+    def _plain(self, quick, name, d, buffers, stream):
+        """A call of a handle, a descriptor and buffers."""
+        status = quick(self._h, d, *buffers, stream)
+        if status is None:
+            status = _call(name)(self._h, ctypes.byref(d), *[_address(b) for b in buffers], _stream_address(stream))
+        if status != 0:
+            _ck(status, self._h)
+
+    # around the layers' products
+    def layer_norm(self, d, x, y, gamma=None, beta=None, mean=None, rstd=None, stream=None):
+        self._plain(_quick_layer_norm, "alt_layer_norm", d, (x, gamma, beta, y, mean, rstd), stream)
+
+    def layer_norm_grad(self, d, dy, x, mean, rstd, dx, gamma=None, dgamma=None, dbeta=None, workspace=None, ws_bytes=0, stream=None):
+        self._buffers(_quick_layer_norm_grad, "alt_layer_norm_grad", d, (dy, x, mean, rstd, gamma, dx, dgamma, dbeta), workspace, ws_bytes, stream)
+
+    def layer_norm_grad_workspace_size(self, d):
+        return self._workspace_size("alt_layer_norm_grad_workspace_size", d)
+
+    def route(self, d, logits, experts, weights, rows, offsets, bias=None, workspace=None, ws_bytes=0, stream=None):
+        self._buffers(_quick_route, "alt_route", d, (logits, bias, experts, weights, rows, offsets), workspace, ws_bytes, stream)
+
+    def route_workspace_size(self, d):
+        return self._workspace_size("alt_route_workspace_size", d)
+
+    def route_grad(self, d, logits, experts, dweights, dlogits, stream=None):
+        self._plain(_quick_route_grad, "alt_route_grad", d, (logits, experts, dweights, dlogits), stream)
+
+    def dispatch_rows(self, d, x, rows, y, stream=None):
+        self._plain(_quick_dispatch_rows, "alt_dispatch_rows", d, (x, rows, y), stream)
+
+    def combine_rows(self, d, x, rows, y, weights=None, stream=None):
+        self._plain(_quick_combine_rows, "alt_combine_rows", d, (x, rows, weights, y), stream)
+
+    def combine_rows_grad(self, d, dy, x, rows, weights, dx, dweights=None, stream=None):
+        self._plain(_quick_combine_rows_grad, "alt_combine_rows_grad", d, (dy, x, rows, weights, dx, dweights), stream)
+
+    def gemm_adapters(self, d, x, w, adapter, a, b, y, scale=None, bias=None, workspace=None, ws_bytes=0, stream=None):
+        self._buffers(_quick_gemm_adapters, "alt_gemm_adapters", d, (x, w, adapter, a, b, scale, bias, y), workspace, ws_bytes, stream)
+
+    def gemm_adapters_workspace_size(self, d):
+        return self._workspace_size("alt_gemm_adapters_workspace_size", d)
 
     def _workspace_size(self, name, d):
         n = ctypes.c_size_t()

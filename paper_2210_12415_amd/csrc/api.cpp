@@ -1,5 +1,6 @@
 // Handle lifecycle, error reporting.
 #include "ops.h"
+#include "rows.h"
 
 namespace alt {
 
@@ -14,6 +15,16 @@ alt_status_t fail(alt_handle_t h, alt_status_t s, const char *fmt, ...)
         h->last_error = buf;
     }
     return s;
+}
+
+// The calls that work on rows refuse another device than the handle's: their kernels would run where the current one is.
+alt_status_t check_device(alt_handle_t h, const char *call)
+{
+    if (!h->has_gpu) return fail(h, ALT_HIP_ERROR, "no GPU device available");
+    int dev = -1;
+    ALT_CHECK_HIP(h, hipGetDevice(&dev));
+    if (dev != h->device) return fail(h, ALT_INVALID_ARG, "%s: the handle is of device %d, the current one is %d", call, h->device, dev);
+    return ALT_OK;
 }
 
 }  // namespace alt

@@ -22,6 +22,8 @@
 namespace alt {
 
 struct i8_tag {};
+struct bf16_adapted_tag {};    // bf16 and fp32 products with low-rank adapters beside them (kForward)
+struct f32_adapted_tag {};
 enum { kForward = 0, kInput = 1, kWeights = 2 };
 
 struct GroupedParams {
@@ -43,6 +45,11 @@ struct GroupedParams {
     int32_t places;            // compute units
     FastDiv d_panel;           // of kPanel * tiles_n
     int32_t flags;
+    // low-rank adapters beside the product (the adapted types below): each row's adapter, and its inner sums (grp_adapt says how they lie)
+    const int32_t *adapter;
+    const char *inner;
+    const char *up;            // [adapters][cols][rank]
+    int32_t adapters, rank, inner_bytes;
 };
 enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpMask = 4, kGrpWhole = 8, kGrpPacked = 16 };
 // (kGrpWhole: the columns are whole 16-byte chunks of the output, and whole fours; kGrpPacked: operand rows are filled up with zeros to whole chunks)
@@ -50,15 +57,17 @@ enum { kGrpRelu = 1, kGrpOutBf16 = 2, kGrpMask = 4, kGrpWhole = 8, kGrpPacked = 
 template <typename T> struct GrpTraits;
 // (SUMS: sums per output and wave.  fp32 keeps four, each over every fourth product, added at the end: that halves their rounding error, 5.7e-7 to 2.9e-7
 // of the result in the 2-norm at reductions of 1000; the kernel for any alignment keeps two.)
-template <> struct GrpTraits<bf16_tag> { static constexpr int ES = 2, SUMS = 1; typedef floatx16_t acc_t; };
-template <> struct GrpTraits<float> { static constexpr int ES = 4, SUMS = 4; typedef floatx16_t acc_t; };
+template <> struct GrpTraits<bf16_tag> { static constexpr int ES = 2, SUMS = 1; static constexpr bool ADAPT = false; typedef floatx16_t acc_t; };
+template <> struct GrpTraits<float> { static constexpr int ES = 4, SUMS = 4; static constexpr bool ADAPT = false; typedef floatx16_t acc_t; };
 typedef int intx16_t __attribute__((ext_vector_type(16)));
-template <> struct GrpTraits<i8_tag> { static constexpr int ES = 1, SUMS = 1; typedef intx16_t acc_t; };
+template <> struct GrpTraits<i8_tag> { static constexpr int ES = 1, SUMS = 1; static constexpr bool ADAPT = false; typedef intx16_t acc_t; };
+template <> struct GrpTraits<bf16_adapted_tag> : GrpTraits<bf16_tag> { static constexpr bool ADAPT = true; };
+template <> struct GrpTraits<f32_adapted_tag> : GrpTraits<float> { static constexpr bool ADAPT = true; };
 
 template <typename T, int SUMS>
 __device__ __forceinline__ void grp_mma(typename GrpTraits<T>::acc_t (&c)[SUMS], const u32x4_t &first, const u32x4_t &second)
 {
-    if constexpr (std::is_same<T, bf16_tag>::value) {
+    if constexpr (GrpTraits<T>::ES == 2) {
         c[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, first), __builtin_bit_cast(bf16x8_t, second), c[0], 0, 0, 0);
     } else if constexpr (std::is_same<T, i8_tag>::value) {
         typedef int i32x4v_t __attribute__((ext_vector_type(4)));
@@ -636,10 +645,57 @@ __device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProble
     }
 }
 
+// The adapters' part of a wave's tile: c[row][col] += sum_r inner[row][r] * up[g][col][r] for the adapter g of the row, one adapter that its rows have
+// after another, in registers: a product like the tile's own with `rank` more steps.  A row's inner sums lie one behind another, filled up to whole
+// matrix instructions with zeros (inner_bytes), in bf16 as two such rows, the value rounded and what that left, so that the adapters' part is as exact as the
+// tile's own.  Lanes hold rows: another adapter's rows take nothing of the sums, whatever they are.
+template <typename T, int TM, int TN, int SUMS>
+__device__ __forceinline__ void grp_adapt(const GroupedParams &p, const GrpProblem &g, GrpSums<T, TM, TN, SUMS> &acc, int wrow, int wcol, int lane)
+{
+    constexpr int ES = GrpTraits<T>::ES, PARTS = ES == 2 ? 2 : 1;
+    const int half = (lane >> 5) * 16;
+    if (g.col0 + wcol >= p.cols) return;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int row = g.row0 + wrow + i * 32 + (lane & 31), row_in = min(row, g.row_end - 1);
+        const int id = p.adapter[row_in];
+        const char *inner = p.inner + (int64_t)row_in * (PARTS * p.inner_bytes) + half;
+        uint64_t left = __ballot(row < g.row_end && id >= 0 && id < p.adapters);
+        while (left) {
+            const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+            const bool mine = id == one;
+            left &= ~__ballot(mine);
+            const char *up = p.up + ((int64_t)one * p.cols + g.col0 + wcol) * p.rank * ES + half;
+            typename GrpTraits<T>::acc_t part[TN][1];
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) part[j][0][e] = 0;
+            for (int at = 0; at < p.inner_bytes; at += 32) {
+                u32x4_t fa[PARTS];
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) fa[q] = *(const u32x4_t *)(inner + q * p.inner_bytes + at);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const int64_t col = min(j * 32 + (lane & 31), p.cols - 1 - g.col0 - wcol);
+                    const u32x4_t fb = grp_load_chunk<ES>(up + col * p.rank * ES + at, p.rank - (at + half) / ES);
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) grp_mma<T>(part[j], fb, fa[q]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc.c[i][j][0][e] += mine ? part[j][0][e] : 0.f;
+        }
+    }
+}
+
 template <typename T, int FORM, int TM, int TN, int SUMS>
-__device__ __forceinline__ void grp_epilogue(const GroupedParams &p, const GrpProblem &g, const GrpSums<T, TM, TN, SUMS> &acc, char *stage, int wrow, int wcol,
+__device__ __forceinline__ void grp_epilogue(const GroupedParams &p, const GrpProblem &g, GrpSums<T, TM, TN, SUMS> &acc, char *stage, int wrow, int wcol,
                                              int lane)
 {
+    if constexpr (GrpTraits<T>::ADAPT) grp_adapt(p, g, acc, wrow, wcol, lane);
     const bool bf16 = GrpTraits<T>::ES < 4 && (p.flags & kGrpOutBf16);
     if ((p.flags & kGrpWhole) || g.col0 + wcol + TN * 32 <= p.cols) {
         if (bf16) grp_emit<T, FORM, TM, TN, (GrpTraits<T>::ES < 4), true>(p, g, acc, stage, wrow, wcol, lane);
@@ -671,13 +727,15 @@ __device__ __forceinline__ void grp_store_sums(const GroupedParams &p, const Grp
 template <typename T> struct GrpFew;
 template <> struct GrpFew<bf16_tag> { typedef f32x4_t acc_t; };
 template <> struct GrpFew<float> { typedef f32x4_t acc_t; };
+template <> struct GrpFew<bf16_adapted_tag> : GrpFew<bf16_tag> {};
+template <> struct GrpFew<f32_adapted_tag> : GrpFew<float> {};
 typedef int i32x4s_t __attribute__((ext_vector_type(4)));
 template <> struct GrpFew<i8_tag> { typedef i32x4s_t acc_t; };
 
 template <typename T>
 __device__ __forceinline__ void grp_mma16(typename GrpFew<T>::acc_t (&c)[GrpTraits<T>::SUMS], const u32x4_t &first, const u32x4_t &second)
 {
-    if constexpr (std::is_same<T, bf16_tag>::value) {
+    if constexpr (GrpTraits<T>::ES == 2) {
         c[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, first), __builtin_bit_cast(bf16x8_t, second), c[0], 0, 0, 0);
     } else if constexpr (std::is_same<T, i8_tag>::value) {
         c[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4s_t, first), __builtin_bit_cast(i32x4s_t, second), c[0], 0, 0, 0);
@@ -780,6 +838,42 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
             const u32x4_t a = grp_load_chunk<ES>(ap + k, count);
 #pragma unroll
             for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[j], grp_load_chunk<ES>(bp[j] + k, count), a);
+        }
+    }
+    // the adapters' part (as grp_adapt has it), one adapter to a wave, then the next
+    if constexpr (GrpTraits<T>::ADAPT) {
+        constexpr int PARTS = ES == 2 ? 2 : 1;
+        const int quarter = lane / 16 * 16, row_in = g.row0 + min(lane % 16, rows_left - 1), id = p.adapter[row_in];
+        const char *inner = p.inner + (int64_t)row_in * (PARTS * p.inner_bytes);
+        uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
+        for (int n = 0; left; ++n) {
+            const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+            const bool mine = id == one;
+            left &= ~__ballot(mine);
+            if (n % NW != wave) continue;
+            typename GrpFew<T>::acc_t mid[NT][SUMS];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int s = 0; s < SUMS; ++s) mid[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+            for (int k = quarter; k - quarter < p.inner_bytes; k += 64) {
+                u32x4_t fa[PARTS];
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) fa[q] = k < p.inner_bytes ? *(const u32x4_t *)(inner + q * p.inner_bytes + k) : (u32x4_t){0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const int64_t col = (int64_t)one * p.cols + g.col0 + min(j * 16 + lane % 16, cols_left - 1);
+                    const u32x4_t fb = grp_load_chunk<ES>(p.up + col * p.rank * ES + k, p.rank - k / ES);
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) grp_mma16<T>(mid[j], fb, fa[q]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int s = 0; s < SUMS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[j][s][e] += mine ? mid[j][s][e] : 0.f;
         }
     }
 #pragma unroll
@@ -1604,6 +1698,8 @@ __global__ __launch_bounds__(kLargeThreads, 2) void grouped_large_kernel(const G
 hipError_t grouped_run_bf16(int form, const GroupedParams &p, hipStream_t st);
 hipError_t grouped_run_f32(int form, const GroupedParams &p, hipStream_t st);
 hipError_t grouped_run_i8(const GroupedParams &p, hipStream_t st);
+hipError_t grouped_run_adapted_bf16(const GroupedParams &p, hipStream_t st);
+hipError_t grouped_run_adapted_f32(const GroupedParams &p, hipStream_t st);
 
 // Most tiles of BM rows that any offsets can make of p.rows rows: each span ends in one part tile at most, and each tile has a
 // row.  (As many slots grp_search counts on.)

@@ -1,16 +1,10 @@
 // Entry points of the products over groups of rows and of the 8-bit product: their checks, and the problem each is.
 #include "grouped.h"
 #include "ops.h"
+#include "rows.h"
 
 namespace alt {
 namespace {
-
-struct Buffer {
-    const char *name;
-    const void *p;
-    size_t align;
-    bool used = true;
-};
 
 // What every call checks of its layer, dense strides filled in.
 alt_status_t check_layer(alt_handle_t h, const char *call, const alt_grouped_desc_t *d, bool gradient, alt_grouped_desc_t *out)
@@ -34,13 +28,10 @@ alt_status_t check_layer(alt_handle_t h, const char *call, const alt_grouped_des
     return ALT_OK;
 }
 
-alt_status_t check_buffers(alt_handle_t h, const char *call, std::initializer_list<Buffer> bufs)
+alt_status_t check_layer_buffers(alt_handle_t h, const char *call, std::initializer_list<RowsBuffer> bufs)
 {
-    for (const Buffer &b : bufs) {
-        if (!b.used) continue;
-        if (!b.p) return fail(h, ALT_INVALID_ARG, "%s: %s is null", call, b.name);
-        if ((uintptr_t)b.p % b.align) return fail(h, ALT_INVALID_ARG, "%s: %s is not aligned to its elements", call, b.name);
-    }
+    const alt_status_t s = check_buffers(h, call, bufs);
+    if (s != ALT_OK) return s;
     if (!h->has_gpu) return fail(h, ALT_HIP_ERROR, "no GPU device available");
     return ALT_OK;
 }
@@ -189,7 +180,7 @@ alt_status_t run(alt_handle_t h, const char *call, int dtype, int form, GroupedP
         }
     }
     p.b_group = form == kWeights ? 0 : (int64_t)(form == kForward ? p.cols : p.red) * p.ldb;
-    const hipError_t e = dtype == ALT_I8 ? grouped_run_i8(p, st) : dtype == ALT_BF16 ? grouped_run_bf16(form, p, st) : grouped_run_f32(form, p, st);
+    const hipError_t e = p.adapter ? (dtype == ALT_BF16 ? grouped_run_adapted_bf16(p, st) : grouped_run_adapted_f32(p, st)) : dtype == ALT_I8 ? grouped_run_i8(p, st) : dtype == ALT_BF16 ? grouped_run_bf16(form, p, st) : grouped_run_f32(form, p, st);
     if (e == hipErrorInvalidConfiguration) return fail(h, ALT_UNSUPPORTED, "%s: more output tiles than a launch holds", call);
     ALT_CHECK_HIP(h, e);
     return ALT_OK;
@@ -222,6 +213,39 @@ alt_status_t forward(alt_handle_t h, const char *call, const alt_grouped_desc_t 
     return run(h, call, l.in_dtype, kForward, p, workspace, ws_bytes, (hipStream_t)stream);
 }
 
+// A product with adapters as a layer of one group.
+alt_grouped_desc_t one_group(const alt_adapters_desc_t *d)
+{
+    alt_grouped_desc_t g{};
+    g.rows = d->M; g.N = d->N; g.K = d->K;
+    g.lda = d->lda; g.ldb = d->ldb; g.ldc = d->ldc;
+    g.groups = 1;
+    g.in_dtype = d->in_dtype; g.out_dtype = d->out_dtype; g.epilogue = d->epilogue;
+    return g;
+}
+
+alt_status_t check_adapters(alt_handle_t h, const char *call, const alt_adapters_desc_t *d, alt_grouped_desc_t *out)
+{
+    if (!h) return ALT_INVALID_ARG;
+    if (!d) return fail(h, ALT_INVALID_ARG, "%s: null descriptor", call);
+    if (d->in_dtype == ALT_I8) return fail(h, ALT_INVALID_ARG, "%s: bad in_dtype", call);
+    const alt_grouped_desc_t g = one_group(d);
+    const alt_status_t s = check_layer(h, call, &g, false, out);
+    if (s != ALT_OK) return s;
+    if (d->adapters < 1 || d->rank < 1) return fail(h, ALT_INVALID_ARG, "%s: bad size", call);
+    if (d->N > (1 << 24) || d->adapters > (1 << 20) || d->rank > ALT_ADAPTERS_MAX_RANK)
+        return fail(h, ALT_UNSUPPORTED, "%s: more than 2^24 columns, 2^20 adapters or a rank over %d", call, ALT_ADAPTERS_MAX_RANK);
+    return ALT_OK;
+}
+
+// Bytes for operands laid out anew, behind the rows' inner sums.
+size_t adapters_pack_bytes(alt_handle_t h, const alt_grouped_desc_t &l, const void *x, const void *w)
+{
+    GroupedParams p = problem(h, l, kForward, x, w, nullptr);
+    if (p.places == 0) p.places = 256;
+    return pack_bytes(kForward, l.in_dtype, p);
+}
+
 // The 8-bit product as a layer of one group.
 alt_grouped_desc_t one_group(const alt_gemm_i8_desc_t *d)
 {
@@ -247,7 +271,7 @@ extern "C" alt_status_t alt_gemm_grouped(alt_handle_t h, const alt_grouped_desc_
     if (l.rows == 0) return ALT_OK;
     const size_t es = in_size(l.in_dtype);
     const bool scaled = l.in_dtype == ALT_I8;
-    s = check_buffers(h, "alt_gemm_grouped", {{"a", a, es}, {"b", b, es}, {"offsets", offsets, 4}, {"y", y, dtype_size(l.out_dtype)}, {"a_scale", a_scale, 4, scaled},
+    s = check_layer_buffers(h, "alt_gemm_grouped", {{"a", a, es}, {"b", b, es}, {"offsets", offsets, 4}, {"y", y, dtype_size(l.out_dtype)}, {"a_scale", a_scale, 4, scaled},
                                               {"b_scale", b_scale, 4, scaled}, {"bias", bias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}});
     if (s != ALT_OK) return s;
     return forward(h, "alt_gemm_grouped", l, a, a_scale, b, b_scale, bias, offsets, y, workspace, ws_bytes, stream);
@@ -262,7 +286,7 @@ extern "C" alt_status_t alt_gemm_grouped_dx(alt_handle_t h, const alt_grouped_de
     if (l.epilogue & ALT_EPI_BIAS) return fail(h, ALT_INVALID_ARG, "alt_gemm_grouped_dx: a bias has no part in the gradient of x");
     if (l.rows == 0) return ALT_OK;
     const size_t es = in_size(l.in_dtype);
-    s = check_buffers(h, "alt_gemm_grouped_dx", {{"dy", dy, es}, {"b", b, es}, {"offsets", offsets, 4}, {"dx", dx, dtype_size(l.out_dtype)},
+    s = check_layer_buffers(h, "alt_gemm_grouped_dx", {{"dy", dy, es}, {"b", b, es}, {"offsets", offsets, 4}, {"dx", dx, dtype_size(l.out_dtype)},
                                                  {"relu_of", relu_of, es, (l.epilogue & ALT_EPI_RELU) != 0}});
     if (s != ALT_OK) return s;
     GroupedParams p = problem(h, l, kInput, dy, b, dx);
@@ -281,7 +305,7 @@ extern "C" alt_status_t alt_gemm_grouped_dw(alt_handle_t h, const alt_grouped_de
     if (l.epilogue & ALT_EPI_RELU) return fail(h, ALT_INVALID_ARG, "alt_gemm_grouped_dw: dy is the gradient before the ReLU");
     const size_t es = in_size(l.in_dtype);
     // (without rows the gradients are zeros, and a and dy need not exist)
-    s = check_buffers(h, "alt_gemm_grouped_dw", {{"a", a, es, l.rows > 0}, {"dy", dy, es, l.rows > 0}, {"offsets", offsets, 4},
+    s = check_layer_buffers(h, "alt_gemm_grouped_dw", {{"a", a, es, l.rows > 0}, {"dy", dy, es, l.rows > 0}, {"offsets", offsets, 4},
                                                  {"dw", dw, dtype_size(l.out_dtype)}, {"dbias", dbias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}});
     if (s != ALT_OK) return s;
     GroupedParams p = problem(h, l, kWeights, dy, a, dw);
@@ -315,7 +339,7 @@ extern "C" alt_status_t alt_gemm_i8(alt_handle_t h, const alt_gemm_i8_desc_t *d,
     alt_status_t s = check_layer(h, "alt_gemm_i8", &g, false, &l);
     if (s != ALT_OK) return s;
     if (l.rows == 0) return ALT_OK;
-    s = check_buffers(h, "alt_gemm_i8", {{"a", a, 1}, {"b", b, 1}, {"a_scale", a_scale, 4}, {"b_scale", b_scale, 4}, {"y", y, dtype_size(l.out_dtype)},
+    s = check_layer_buffers(h, "alt_gemm_i8", {{"a", a, 1}, {"b", b, 1}, {"a_scale", a_scale, 4}, {"b_scale", b_scale, 4}, {"y", y, dtype_size(l.out_dtype)},
                                          {"bias", bias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}});
     if (s != ALT_OK) return s;
     return forward(h, "alt_gemm_i8", l, a, a_scale, b, b_scale, bias, nullptr, y, workspace, ws_bytes, stream);
@@ -327,4 +351,53 @@ extern "C" alt_status_t alt_gemm_i8_workspace_size(alt_handle_t h, const alt_gem
     if (!d) return fail(h, ALT_INVALID_ARG, "alt_gemm_i8_workspace_size: null descriptor");
     const alt_grouped_desc_t g = one_group(d);
     return workspace_size(h, &g, kForward, true, "alt_gemm_i8_workspace_size", bytes);
+}
+
+extern "C" alt_status_t alt_gemm_adapters(alt_handle_t h, const alt_adapters_desc_t *d, const void *x, const void *w, const int32_t *adapter, const void *a, const void *b,
+                                          const float *scale, const float *bias, void *y, void *workspace, size_t ws_bytes, void *stream)
+{
+    alt_grouped_desc_t l;
+    alt_status_t s = check_adapters(h, "alt_gemm_adapters", d, &l);
+    if (s != ALT_OK) return s;
+    if (l.rows == 0) return ALT_OK;
+    const size_t es = in_size(l.in_dtype);
+    s = check_buffers(h, "alt_gemm_adapters", {{"x", x, es}, {"w", w, es}, {"adapter", adapter, 4}, {"a", a, es}, {"b", b, es}, {"scale", scale, 4, scale != nullptr},
+                                               {"bias", bias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}, {"y", y, dtype_size(l.out_dtype)}});
+    const size_t inner = adapters_inner_bytes(l.rows, d->rank, l.in_dtype);
+    if (s == ALT_OK) s = check_workspace(h, "alt_gemm_adapters", workspace, ws_bytes, inner + 16);
+    if (s == ALT_OK) s = check_device(h, "alt_gemm_adapters");
+    if (s != ALT_OK) return s;
+    char *ws = aligned_workspace(workspace);
+    AdaptersDown down{};
+    down.x = (const char *)x;
+    down.a = (const char *)a;
+    down.adapter = adapter;
+    down.scale = scale;
+    down.inner = ws;
+    down.ldx = l.lda * (int64_t)es;
+    down.rows = (int32_t)l.rows;
+    down.adapters = d->adapters;
+    down.rank = d->rank;
+    down.K = (int32_t)l.K;
+    ALT_CHECK_HIP(h, adapters_down(l.in_dtype, down, (hipStream_t)stream));
+    GroupedParams p = problem(h, l, kForward, x, w, y);
+    p.bias = l.epilogue & ALT_EPI_BIAS ? bias : nullptr;
+    if (l.epilogue & ALT_EPI_RELU) p.flags |= kGrpRelu;
+    p.adapter = adapter;
+    p.inner = ws;
+    p.up = (const char *)b;
+    p.adapters = d->adapters;
+    p.rank = d->rank;
+    p.inner_bytes = adapters_row_bytes(d->rank, l.in_dtype);
+    return run(h, "alt_gemm_adapters", l.in_dtype, kForward, p, ws + inner, (size_t)((char *)workspace + ws_bytes - (ws + inner)), (hipStream_t)stream);
+}
+
+extern "C" alt_status_t alt_gemm_adapters_workspace_size(alt_handle_t h, const alt_adapters_desc_t *d, size_t *bytes)
+{
+    alt_grouped_desc_t l;
+    const alt_status_t s = check_adapters(h, "alt_gemm_adapters_workspace_size", d, &l);
+    if (s != ALT_OK) return s;
+    if (!bytes) return fail(h, ALT_INVALID_ARG, "alt_gemm_adapters_workspace_size: null result");
+    *bytes = l.rows ? adapters_inner_bytes(l.rows, d->rank, l.in_dtype) + adapters_pack_bytes(h, l, nullptr, nullptr) + 16 : 0;
+    return ALT_OK;
 }

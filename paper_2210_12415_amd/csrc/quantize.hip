@@ -2,47 +2,11 @@
 // to even.  Bound by memory: one read of x, one write of q.  A row stays in the registers of its threads between the maximum and
 // the rounding; rows too long for that are read twice, the second time from the caches.  16384 x 4096 bf16: 38 to 40 us, 5.1 to 5.3 TB/s,
 // inputs from memory (one input again and again comes in part from the last-level cache: 32 to 38).
-#include <hip/hip_runtime.h>
-
 #include "common.h"
+#include "rows.h"
 
 namespace alt {
 namespace {
-
-typedef uint32_t w4_t __attribute__((ext_vector_type(4)));
-typedef float f4_t __attribute__((ext_vector_type(4)));
-
-template <int ELSZ>
-__device__ __forceinline__ float element(const char *p)
-{
-    if constexpr (ELSZ == 4) return *(const float *)p;
-    else return __builtin_bit_cast(float, (uint32_t)*(const uint16_t *)p << 16);
-}
-
-// A chunk of eight elements as it lies in memory, at any alignment of whole elements, and as floats.
-template <int ELSZ> struct Chunk { w4_t w[ELSZ / 2]; };
-
-template <int ELSZ>
-__device__ __forceinline__ Chunk<ELSZ> load_chunk(const char *p)
-{
-    Chunk<ELSZ> c;
-    __builtin_memcpy(&c, p, 8 * ELSZ);
-    return c;
-}
-
-template <int ELSZ>
-__device__ __forceinline__ void floats(const Chunk<ELSZ> &c, float (&v)[8])
-{
-    if constexpr (ELSZ == 4) {
-        const f4_t a = __builtin_bit_cast(f4_t, c.w[0]), b = __builtin_bit_cast(f4_t, c.w[1]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-    } else {
-        const f4_t lo = __builtin_bit_cast(f4_t, c.w[0] << 16), hi = __builtin_bit_cast(f4_t, c.w[0] & 0xffff0000u);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = lo[i]; v[2 * i + 1] = hi[i]; }
-    }
-}
 
 // The largest |v| so far, as bits: they order like the numbers, infinity and NaN above all.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }

@@ -8,7 +8,8 @@
 #include <stdint.h>
 #include <unistd.h>
 
-enum { CONV2D, CONV3D, CONV2D_TRANSPOSE, CONV3D_TRANSPOSE, GEMM, TRANSFORM, ADD, QUANTIZE, GEMM_I8, GROUPED, GROUPED_DX, GROUPED_DW, FUNCTIONS };
+enum { CONV2D, CONV3D, CONV2D_TRANSPOSE, CONV3D_TRANSPOSE, GEMM, TRANSFORM, ADD, QUANTIZE, GEMM_I8, GROUPED, GROUPED_DX, GROUPED_DW,
+       NORM, NORM_GRAD, ROUTE, ROUTE_GRAD, DISPATCH, COMBINE, COMBINE_GRAD, ADAPTERS, FUNCTIONS };
 
 typedef int (*operator_fn)(void *, const void *, const void *, const void *, const float *, void *, void *, size_t, void *);
 typedef int (*gemm_fn)(void *, const void *, const void *, const void *, void *, void *, size_t, void *);
@@ -17,10 +18,14 @@ typedef int (*quantize_fn)(void *, int, int64_t, int64_t, const void *, int64_t,
 typedef int (*buffers6_fn)(void *, const void *, void *, void *, void *, void *, void *, void *, size_t, void *);    /* handle, descriptor, buffers, workspace last, its size, stream */
 typedef int (*buffers7_fn)(void *, const void *, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
 typedef int (*buffers8_fn)(void *, const void *, void *, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
+typedef int (*buffers9_fn)(void *, const void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
+typedef int (*plain3_fn)(void *, const void *, void *, void *, void *, void *);      /* handle, descriptor, buffers, stream */
+typedef int (*plain4_fn)(void *, const void *, void *, void *, void *, void *, void *);
+typedef int (*plain6_fn)(void *, const void *, void *, void *, void *, void *, void *, void *, void *);
 typedef int (*add_fn)(void *, int, int64_t, const void *, const void *, void *, int, void *);
 
 static void *entry[FUNCTIONS];
-static PyObject *handle_type, *conv_type, *conv3d_type, *gemm_type, *layout_type, *gemm_i8_type, *grouped_type;
+static PyObject *handle_type, *conv_type, *conv3d_type, *gemm_type, *layout_type, *gemm_i8_type, *grouped_type, *norm_type, *route_type, *exchange_type, *adapters_type;
 static PyObject *raw_stream, *get_device;                  /* torch's, once it has initialised the device */
 static pid_t stream_pid;
 static PyObject *s_data_ptr, *s_cuda_stream;
@@ -210,7 +215,7 @@ static PyObject *py_quantize_rows(PyObject *m, PyObject *const *a, Py_ssize_t n)
 /* (h, d, buffers and the workspace, ws_bytes, stream) */
 static PyObject *buffers_call(int which, PyObject *type, int count, PyObject *const *a, Py_ssize_t n)
 {
-    void *h, *d, *b[8], *st, *fn = entry[which];
+    void *h, *d, *b[9], *st, *fn = entry[which];
     unsigned long long bytes;
     int status;
     if (n != count + 4 || !fn || handle_of(a[0], &h) || object_at(a[1], type, &d)) return not_taken();
@@ -221,7 +226,27 @@ static PyObject *buffers_call(int which, PyObject *type, int count, PyObject *co
     switch (count) {
         case 6: status = ((buffers6_fn)fn)(h, d, b[0], b[1], b[2], b[3], b[4], b[5], (size_t)bytes, st); break;
         case 7: status = ((buffers7_fn)fn)(h, d, b[0], b[1], b[2], b[3], b[4], b[5], b[6], (size_t)bytes, st); break;
-        default: status = ((buffers8_fn)fn)(h, d, b[0], b[1], b[2], b[3], b[4], b[5], b[6], b[7], (size_t)bytes, st);
+        case 8: status = ((buffers8_fn)fn)(h, d, b[0], b[1], b[2], b[3], b[4], b[5], b[6], b[7], (size_t)bytes, st); break;
+        default: status = ((buffers9_fn)fn)(h, d, b[0], b[1], b[2], b[3], b[4], b[5], b[6], b[7], b[8], (size_t)bytes, st);
+    }
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* (h, d, buffers, stream) */
+static PyObject *plain_call(int which, PyObject *type, int count, PyObject *const *a, Py_ssize_t n)
+{
+    void *h, *d, *b[6], *st, *fn = entry[which];
+    int status;
+    if (n != count + 3 || !fn || handle_of(a[0], &h) || object_at(a[1], type, &d)) return not_taken();
+    for (int i = 0; i < count; ++i)
+        if (address(a[2 + i], &b[i])) return not_taken();
+    if (stream_of(a[count + 2], &st)) return not_taken();
+    Py_BEGIN_ALLOW_THREADS
+    switch (count) {
+        case 3: status = ((plain3_fn)fn)(h, d, b[0], b[1], b[2], st); break;
+        case 4: status = ((plain4_fn)fn)(h, d, b[0], b[1], b[2], b[3], st); break;
+        default: status = ((plain6_fn)fn)(h, d, b[0], b[1], b[2], b[3], b[4], b[5], st);
     }
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
@@ -231,6 +256,15 @@ static PyObject *py_gemm_i8(PyObject *m, PyObject *const *a, Py_ssize_t n) { ret
 static PyObject *py_gemm_grouped(PyObject *m, PyObject *const *a, Py_ssize_t n) { return buffers_call(GROUPED, grouped_type, 8, a, n); }
 static PyObject *py_gemm_grouped_dx(PyObject *m, PyObject *const *a, Py_ssize_t n) { return buffers_call(GROUPED_DX, grouped_type, 6, a, n); }
 static PyObject *py_gemm_grouped_dw(PyObject *m, PyObject *const *a, Py_ssize_t n) { return buffers_call(GROUPED_DW, grouped_type, 6, a, n); }
+
+static PyObject *py_layer_norm(PyObject *m, PyObject *const *a, Py_ssize_t n) { return plain_call(NORM, norm_type, 6, a, n); }
+static PyObject *py_layer_norm_grad(PyObject *m, PyObject *const *a, Py_ssize_t n) { return buffers_call(NORM_GRAD, norm_type, 9, a, n); }
+static PyObject *py_route(PyObject *m, PyObject *const *a, Py_ssize_t n) { return buffers_call(ROUTE, route_type, 7, a, n); }
+static PyObject *py_route_grad(PyObject *m, PyObject *const *a, Py_ssize_t n) { return plain_call(ROUTE_GRAD, route_type, 4, a, n); }
+static PyObject *py_dispatch_rows(PyObject *m, PyObject *const *a, Py_ssize_t n) { return plain_call(DISPATCH, exchange_type, 3, a, n); }
+static PyObject *py_combine_rows(PyObject *m, PyObject *const *a, Py_ssize_t n) { return plain_call(COMBINE, exchange_type, 4, a, n); }
+static PyObject *py_combine_rows_grad(PyObject *m, PyObject *const *a, Py_ssize_t n) { return plain_call(COMBINE_GRAD, exchange_type, 6, a, n); }
+static PyObject *py_gemm_adapters(PyObject *m, PyObject *const *a, Py_ssize_t n) { return buffers_call(ADAPTERS, adapters_type, 9, a, n); }
 
 /* A call of conv2d with its arguments marshalled once.  It keeps what they came from, the owner of the handle among them. */
 typedef struct {
@@ -303,17 +337,17 @@ static PyObject *py_prepare_conv2d(PyObject *m, PyObject *const *a, Py_ssize_t n
     return (PyObject *)p;
 }
 
-/* (the entry points' addresses, then the types of handles, of the convolutions' and the product's descriptors, of layouts and of the layers' descriptors) */
+/* (the entry points' addresses, then the types of handles, of the convolutions' and the product's descriptors, of layouts, of the layers' descriptors and of those around them) */
 static PyObject *py_setup(PyObject *m, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != FUNCTIONS + 7) { PyErr_SetString(PyExc_TypeError, "setup: wrong number of arguments"); return NULL; }
+    if (n != FUNCTIONS + 11) { PyErr_SetString(PyExc_TypeError, "setup: wrong number of arguments"); return NULL; }
     void *at[FUNCTIONS];
     for (int i = 0; i < FUNCTIONS; ++i) {
         at[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return NULL;
     }
-    PyObject **types[7] = {&handle_type, &conv_type, &conv3d_type, &gemm_type, &layout_type, &gemm_i8_type, &grouped_type};
-    for (int i = 0; i < 7; ++i) { Py_INCREF(a[FUNCTIONS + i]); Py_XSETREF(*types[i], a[FUNCTIONS + i]); }
+    PyObject **types[11] = {&handle_type, &conv_type, &conv3d_type, &gemm_type, &layout_type, &gemm_i8_type, &grouped_type, &norm_type, &route_type, &exchange_type, &adapters_type};
+    for (int i = 0; i < 11; ++i) { Py_INCREF(a[FUNCTIONS + i]); Py_XSETREF(*types[i], a[FUNCTIONS + i]); }
     for (int i = 0; i < FUNCTIONS; ++i) entry[i] = at[i];
     Py_RETURN_NONE;
 }
@@ -330,7 +364,8 @@ static PyObject *py_streams(PyObject *m, PyObject *const *a, Py_ssize_t n)
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(conv2d), FAST(conv3d), FAST(conv2d_transpose), FAST(conv3d_transpose), FAST(gemm), FAST(layout_transform),
-                                FAST(eltwise_add), FAST(quantize_rows), FAST(gemm_i8), FAST(gemm_grouped), FAST(gemm_grouped_dx), FAST(gemm_grouped_dw), FAST(prepare_conv2d), FAST(setup), FAST(streams), {NULL, NULL, 0, NULL}};
+                                FAST(eltwise_add), FAST(quantize_rows), FAST(gemm_i8), FAST(gemm_grouped), FAST(gemm_grouped_dx), FAST(gemm_grouped_dw),
+                                FAST(layer_norm), FAST(layer_norm_grad), FAST(route), FAST(route_grad), FAST(dispatch_rows), FAST(combine_rows), FAST(combine_rows_grad), FAST(gemm_adapters), FAST(prepare_conv2d), FAST(setup), FAST(streams), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_altcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__altcall(void)
