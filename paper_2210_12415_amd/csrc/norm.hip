@@ -3,82 +3,357 @@
 //   mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),  u = (x - mean) rstd,  y = u gamma + beta
 //   dx = rstd (g - mean_c(g) - u mean_c(g u))  with g = dy gamma,  dgamma = sum_m dy u,  dbeta = sum_m dy
 //
-// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.
+// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.  TPR threads (a wave, or a workgroup) have a row, in chunks of
+// eight columns that stay in registers from the first sum to the last store, and take one row after another: a thread's columns are the same in all
+// of them, so gamma and beta are read once, dgamma and dbeta are summed in registers, and the next row is on its way while this one is reduced.  What the
+// workgroups have of dgamma and dbeta goes to the workspace and is joined by a second launch, in the order of the workgroups.  Rows of more than 16384
+// columns do not fit: they are read again for every sum.
 #include "common.h"
 #include "rows.h"
 
 namespace alt {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMostCols = 16384;                           // of a row in registers
 
-// The sum over a workgroup's threads, the same in all of them.
-__device__ __forceinline__ float block_sum(float v, float (&part)[kWaves])
-{
-    v = wave_sum(v);
-    __syncthreads();                                       // (the last sum is read)
-    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
-    __syncthreads();
-    v = part[0];
+// A thread's part of a row: chunks t, t + TPR, ... of `chunks`, and one element of the `rest` behind them.
+template <int ES, int TPR, int KEEP>
+struct Part {
+    Chunk<ES> c[KEEP];
+    float last;
+    __device__ __forceinline__ void load(const char *row, int t, int chunks, int rest)
+    {
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) v += part[i];
-    return v;
-}
+        for (int i = 0; i < KEEP; ++i)
+            if (i * TPR + t < chunks) c[i] = load_chunk<ES>(row + (int64_t)(i * TPR + t) * (8 * ES));
+        last = t < rest ? element<ES>(row + ((int64_t)chunks * 8 + t) * ES) : 0.f;
+    }
+};
 
-template <int XS, int YS>
-__global__ __launch_bounds__(kThreads) void norm_kernel(const char *x0, int64_t ldx, const float *gamma, const float *beta, char *y0, int64_t ldy, float *mean_out, float *rstd_out,
-                                                        int64_t rows, int cols, float eps)
+// Values of a thread's columns: those of its chunks and the one behind them.
+template <int KEEP>
+struct Columns {
+    float v[KEEP][8], last;
+    __device__ __forceinline__ void fill(float f)
+    {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[i][q] = f;
+        last = f;
+    }
+    template <int TPR>
+    __device__ __forceinline__ void load(const float *p, int t, int chunks, int rest)
+    {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (i * TPR + t < chunks) floats<4>(load_chunk<4>((const char *)(p + (i * TPR + t) * 8)), v[i]);
+        if (t < rest) last = p[chunks * 8 + t];
+    }
+};
+
+// N sums over the TPR threads of a row, the same in all of them, for the G rows of a workgroup at once.  Two sets of parts in turn, so that one barrier a
+// call is enough.
+template <int TPR, int G, int N>
+struct RowSum {
+    static constexpr int WAVES = TPR / 64;
+    typedef float Parts[2][G][WAVES][N];
+    Parts *part;
+    int turn = 0;
+    __device__ __forceinline__ void operator()(float (&v)[N])
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
+        if constexpr (WAVES > 1) {
+            const int group = threadIdx.x / TPR;
+            if (threadIdx.x % 64 == 0) {
+#pragma unroll
+                for (int n = 0; n < N; ++n) (*part)[turn][group][threadIdx.x % TPR / 64][n] = v[n];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                v[n] = (*part)[turn][group][0][n];
+#pragma unroll
+                for (int i = 1; i < WAVES; ++i) v[n] += (*part)[turn][group][i][n];
+            }
+            turn ^= 1;
+        }
+    }
+};
+
+template <int TPR> constexpr int kThreadsOf = TPR < 256 ? 256 : TPR;
+
+template <int XS, int YS, int TPR, int KEEP>
+__global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, int64_t ldx, const float *gamma, const float *beta, char *y, int64_t ldy, float *mean_out,
+                                                               float *rstd_out, int64_t rows, int cols, float eps)
 {
-    __shared__ float part[kWaves];
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    const char *x = x0 + row * ldx;
-    char *y = y0 + row * ldy;
-    float s = 0.f;
-    for (int c = threadIdx.x; c < cols; c += kThreads) s += element<XS>(x + (int64_t)c * XS);
-    const float mean = block_sum(s, part) / (float)cols;
-    s = 0.f;
-    for (int c = threadIdx.x; c < cols; c += kThreads) {
-        const float v = element<XS>(x + (int64_t)c * XS) - mean;
-        s += v * v;
-    }
-    const float rstd = 1.f / sqrtf(block_sum(s, part) / (float)cols + eps);
-    if (threadIdx.x == 0) {
-        if (mean_out) mean_out[row] = mean;
-        if (rstd_out) rstd_out[row] = rstd;
-    }
-    for (int c = threadIdx.x; c < cols; c += kThreads)
-        store_element<YS>(y + (int64_t)c * YS, (element<XS>(x + (int64_t)c * XS) - mean) * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f));
+    constexpr int G = kThreadsOf<TPR> / TPR;
+    __shared__ typename RowSum<TPR, G, 1>::Parts part;
+    RowSum<TPR, G, 1> sum{&part};
+    const int t = threadIdx.x % TPR, chunks = cols / 8, rest = cols % 8;
+    const int64_t step = (int64_t)gridDim.x * G;
+    int64_t row = (int64_t)blockIdx.x * G + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    if (row >= rows) return;
+    Part<XS, TPR, KEEP> next;
+    next.load(x + row * ldx, t, chunks, rest);
+    Columns<KEEP> g, b;
+    g.fill(1.f);
+    b.fill(0.f);
+    if (gamma) g.template load<TPR>(gamma, t, chunks, rest);
+    if (beta) b.template load<TPR>(beta, t, chunks, rest);
+    const float n = (float)cols;
+    for (; row < rows; row += step) {
+        const Part<XS, TPR, KEEP> mine = next;
+        if (row + step < rows) next.load(x + (row + step) * ldx, t, chunks, rest);
+        float v[KEEP][8], s[1] = {mine.last};
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (i * TPR + t < chunks) {
+                floats<XS>(mine.c[i], v[i]);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) s[0] += v[i][q];
+            }
+        sum(s);
+        const float mean = s[0] / n;
+        s[0] = t < rest ? (mine.last - mean) * (mine.last - mean) : 0.f;
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (i * TPR + t < chunks) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    v[i][q] -= mean;
+                    s[0] += v[i][q] * v[i][q];
+                }
+            }
+        sum(s);
+        const float rstd = 1.f / sqrtf(s[0] / n + eps);
+        if (t == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+        char *to = y + row * ldy;
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (i * TPR + t < chunks) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[i][q] = v[i][q] * rstd * g.v[i][q] + b.v[i][q];
+                put_chunk<YS>(to + (int64_t)(i * TPR + t) * (8 * YS), chunk_of<YS>(v[i]));
+            }
+        if (t < rest) store_element<YS>(to + ((int64_t)chunks * 8 + t) * YS, (mine.last - mean) * rstd * g.last + b.last);
     }
 }
 
-template <int XS, int YS>
-__global__ __launch_bounds__(kThreads) void norm_dx_kernel(const char *dy0, int64_t ldy, const char *x0, int64_t ldx, const float *mean_in, const float *rstd_in, const float *gamma,
-                                                           char *dx0, int64_t rows, int cols)
+// dx, and this workgroup's part of dgamma and dbeta (`sums`: 2 x cols for each workgroup, or null).  G rows at once; with one chunk a thread
+// keeps the next row on its way, with two there are no registers for that.
+template <int XS, int YS, int TPR, int KEEP, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int64_t ldy, const char *x, int64_t ldx, const float *mean, const float *rstd, const float *gamma,
+                                                            char *dx, float *sums, int64_t rows, int cols)
 {
-    __shared__ float part[kWaves];
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    const char *dy = dy0 + row * ldy, *x = x0 + row * ldx;
-    char *dx = dx0 + row * ldx;
-    const float mean = mean_in[row], rstd = rstd_in[row];
-    float sg = 0.f, sgu = 0.f;
-    for (int c = threadIdx.x; c < cols; c += kThreads) {
-        const float g = element<YS>(dy + (int64_t)c * YS) * (gamma ? gamma[c] : 1.f);
-        sg += g;
-        sgu += g * ((element<XS>(x + (int64_t)c * XS) - mean) * rstd);
+    constexpr int G = THREADS / TPR;
+    constexpr bool AHEAD = KEEP == 1;
+    __shared__ typename RowSum<TPR, G, 2>::Parts part;
+    RowSum<TPR, G, 2> sum{&part};
+    const int t = threadIdx.x % TPR, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), chunks = cols / 8, rest = cols % 8;
+    const int64_t step = (int64_t)gridDim.x * G;
+    Part<XS, TPR, KEEP> next_x;
+    Part<YS, TPR, KEEP> next_dy;
+    float next_m = 0.f, next_r = 0.f;
+    auto load = [&](int64_t row) {
+        if (row >= rows) return;
+        next_x.load(x + row * ldx, t, chunks, rest);
+        next_dy.load(dy + row * ldy, t, chunks, rest);
+        next_m = mean[row];
+        next_r = rstd[row];
+    };
+    Columns<KEEP> g, dg, db;
+    g.fill(1.f);
+    dg.fill(0.f);
+    db.fill(0.f);
+    if (AHEAD) load((int64_t)blockIdx.x * G + group);
+    if (gamma) g.template load<TPR>(gamma, t, chunks, rest);
+    const float n = (float)cols;
+    // (all groups go round as often as the first, for the barriers of their sums)
+    for (int64_t first = (int64_t)blockIdx.x * G; first < rows; first += step) {
+        const int64_t row = first + group;
+        const bool is = row < rows;
+        if constexpr (!AHEAD) {
+            load(row);
+        }
+        const Part<XS, TPR, KEEP> mine_x = next_x;
+        const Part<YS, TPR, KEEP> mine_dy = next_dy;
+        const float m = next_m, r = next_r;
+        if (AHEAD) load(row + step);
+        float u[KEEP][8], w[KEEP][8], s[2] = {0.f, 0.f}, last_u = 0.f, last_g = 0.f;
+        auto values = [&](int i, float mean, float (&u)[8], float (&w)[8]) {
+            floats<XS>(mine_x.c[i], u);
+            floats<YS>(mine_dy.c[i], w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) u[q] = (u[q] - mean) * r;
+        };
+        if (is) {
+            last_u = t < rest ? (mine_x.last - m) * r : 0.f;
+            last_g = mine_dy.last * g.last;
+            s[0] = last_g;
+            s[1] = last_g * last_u;
+            dg.last += mine_dy.last * last_u;
+            db.last += mine_dy.last;
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+                if (i * TPR + t < chunks) {
+                    values(i, m, u[i], w[i]);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        dg.v[i][q] += w[i][q] * u[i][q];
+                        db.v[i][q] += w[i][q];
+                        w[i][q] *= g.v[i][q];
+                        s[0] += w[i][q];
+                        s[1] += w[i][q] * u[i][q];
+                    }
+                }
+        }
+        sum(s);
+        if (!is) continue;
+        const float sg = s[0] / n, sgu = s[1] / n;
+        char *to = dx + row * ldx;
+        float again = m;
+        if constexpr (!AHEAD) asm volatile("" : "+v"(again));              // (what the sums were made of is made again, not kept)
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (i * TPR + t < chunks) {
+                if constexpr (!AHEAD) {
+                    values(i, again, u[i], w[i]);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) w[i][q] *= g.v[i][q];
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) w[i][q] = r * (w[i][q] - sg - u[i][q] * sgu);
+                put_chunk<XS>(to + (int64_t)(i * TPR + t) * (8 * XS), chunk_of<XS>(w[i]));
+            }
+        if (t < rest) store_element<XS>(to + ((int64_t)chunks * 8 + t) * XS, r * (last_g - sg - last_u * sgu));
     }
-    sg = block_sum(sg, part) / (float)cols;
-    sgu = block_sum(sgu, part) / (float)cols;
-    for (int c = threadIdx.x; c < cols; c += kThreads) {
-        const float g = element<YS>(dy + (int64_t)c * YS) * (gamma ? gamma[c] : 1.f), u = (element<XS>(x + (int64_t)c * XS) - mean) * rstd;
-        store_element<XS>(dx + (int64_t)c * XS, rstd * (g - sg - u * sgu));
+    if (!sums) return;
+    sums += (int64_t)blockIdx.x * 2 * cols;
+    if constexpr (G > 1) {                                 // the groups' sums one after another, into the last group's registers
+        __shared__ float to[2][KEEP * TPR * 8], ends[2][8];
+        for (int k = 0; k < G; ++k) {
+            __syncthreads();
+            if (k != group) continue;
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const int at = (i * 8 + q) * TPR + t;
+                    if (k) { dg.v[i][q] += to[0][at]; db.v[i][q] += to[1][at]; }
+                    to[0][at] = dg.v[i][q];
+                    to[1][at] = db.v[i][q];
+                }
+            if (t < rest) {
+                if (k) { dg.last += ends[0][t]; db.last += ends[1][t]; }
+                ends[0][t] = dg.last;
+                ends[1][t] = db.last;
+            }
+        }
+        if (group != G - 1) return;
     }
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (i * TPR + t < chunks) {
+            put_chunk<4>((char *)(sums + (i * TPR + t) * 8), chunk_of<4>(dg.v[i]));
+            put_chunk<4>((char *)(sums + cols + (i * TPR + t) * 8), chunk_of<4>(db.v[i]));
+        }
+    if (t < rest) {
+        sums[chunks * 8 + t] = dg.last;
+        sums[cols + chunks * 8 + t] = db.last;
     }
 }
 
-// dgamma and dbeta: a workgroup's columns over its share of the rows, then the shares one after another.
+// The workgroups' parts, in a fixed order: 32 columns to a workgroup, 32 threads to a column, each with eight of its parts on their way at once (four
+// at once with eight threads to a column took longer than the rest: 2048 x 768 13.2 us for both launches).
+constexpr int kJoinGroups = 32;
+
+__global__ __launch_bounds__(32 * kJoinGroups) void norm_join_kernel(const float *sums, int shares, int cols, float *dgamma, float *dbeta)
+{
+    __shared__ float part[kJoinGroups][32];
+    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x % 32, width = 2 * (int64_t)cols;
+    const int group = threadIdx.x / 32;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < width)
+        for (int i0 = group; i0 < shares; i0 += 8 * kJoinGroups) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (i0 + q * kJoinGroups < shares) s[q] += sums[(i0 + q * kJoinGroups) * width + c];
+        }
+    part[group][threadIdx.x % 32] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+    __syncthreads();
+    if (group || c >= width) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kJoinGroups; ++k) sum += part[k][threadIdx.x];
+    float *to = c < cols ? dgamma : dbeta;
+    if (to) to[c < cols ? c : c - cols] = sum;
+}
+
+// ---- rows that registers do not hold ---------------------------------------------------------------------------------------------
+
+constexpr int kThreads = 256;
+
 template <int XS, int YS>
-__global__ __launch_bounds__(kThreads) void norm_columns_kernel(const char *dy, int64_t ldy, const char *x, int64_t ldx, const float *mean, const float *rstd, float *part,
-                                                                int64_t rows, int cols)
+__global__ __launch_bounds__(kThreads) void norm_long_kernel(const char *x, int64_t ldx, const float *gamma, const float *beta, char *y, int64_t ldy, float *mean_out,
+                                                             float *rstd_out, int64_t rows, int cols, float eps)
+{
+    __shared__ typename RowSum<kThreads, 1, 1>::Parts part;
+    RowSum<kThreads, 1, 1> sum{&part};
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const char *from = x + row * ldx;
+        char *to = y + row * ldy;
+        float s[1] = {0.f};
+        for (int c = threadIdx.x; c < cols; c += kThreads) s[0] += element<XS>(from + (int64_t)c * XS);
+        sum(s);
+        const float mean = s[0] / (float)cols;
+        s[0] = 0.f;
+        for (int c = threadIdx.x; c < cols; c += kThreads) {
+            const float v = element<XS>(from + (int64_t)c * XS) - mean;
+            s[0] += v * v;
+        }
+        sum(s);
+        const float rstd = 1.f / sqrtf(s[0] / (float)cols + eps);
+        if (threadIdx.x == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+        for (int c = threadIdx.x; c < cols; c += kThreads)
+            store_element<YS>(to + (int64_t)c * YS, (element<XS>(from + (int64_t)c * XS) - mean) * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f));
+    }
+}
+
+template <int XS, int YS>
+__global__ __launch_bounds__(kThreads) void norm_long_dx_kernel(const char *dy, int64_t ldy, const char *x, int64_t ldx, const float *mean, const float *rstd, const float *gamma,
+                                                                char *dx, int64_t rows, int cols)
+{
+    __shared__ typename RowSum<kThreads, 1, 2>::Parts part;
+    RowSum<kThreads, 1, 2> sum{&part};
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const char *from = x + row * ldx, *up = dy + row * ldy;
+        const float m = mean[row], r = rstd[row];
+        float s[2] = {0.f, 0.f};
+        for (int c = threadIdx.x; c < cols; c += kThreads) {
+            const float g = element<YS>(up + (int64_t)c * YS) * (gamma ? gamma[c] : 1.f);
+            s[0] += g;
+            s[1] += g * ((element<XS>(from + (int64_t)c * XS) - m) * r);
+        }
+        sum(s);
+        const float sg = s[0] / (float)cols, sgu = s[1] / (float)cols;
+        for (int c = threadIdx.x; c < cols; c += kThreads) {
+            const float g = element<YS>(up + (int64_t)c * YS) * (gamma ? gamma[c] : 1.f), u = (element<XS>(from + (int64_t)c * XS) - m) * r;
+            store_element<XS>(dx + row * ldx + (int64_t)c * XS, r * (g - sg - u * sgu));
+        }
+    }
+}
+
+template <int XS, int YS>
+__global__ __launch_bounds__(kThreads) void norm_long_sums_kernel(const char *dy, int64_t ldy, const char *x, int64_t ldx, const float *mean, const float *rstd, float *sums,
+                                                                  int64_t rows, int cols)
 {
     const int c = blockIdx.x * kThreads + threadIdx.x;
     if (c >= cols) return;
@@ -88,22 +363,38 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(const char *dy, 
         dg += v * ((element<XS>(x + m * ldx + (int64_t)c * XS) - mean[m]) * rstd[m]);
         db += v;
     }
-    part[(int64_t)blockIdx.y * 2 * cols + c] = dg;
-    part[((int64_t)blockIdx.y * 2 + 1) * cols + c] = db;
+    sums[(int64_t)blockIdx.y * 2 * cols + c] = dg;
+    sums[((int64_t)blockIdx.y * 2 + 1) * cols + c] = db;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_join_kernel(const float *part, int shares, int cols, float *dgamma, float *dbeta)
+// ---- launches ----------------------------------------------------------------------------------------------------------------------
+
+// Threads of a row, and its chunks in each thread.
+struct Shape { int tpr, keep; };
+Shape shape_of(int64_t cols)
 {
-    const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (c >= 2 * (int64_t)cols) return;
-    float s = 0.f;
-    for (int i = 0; i < shares; ++i) s += part[(int64_t)i * 2 * cols + c];
-    float *to = c < cols ? dgamma : dbeta;
-    if (to) to[c < cols ? c : c - cols] = s;
+    if (cols <= 1024) return {64, cols <= 512 ? 1 : 2};
+    if (cols <= 4096) return {256, cols <= 2048 ? 1 : 2};
+    return {cols <= 8192 ? 512 : 1024, 2};
 }
 
-unsigned row_blocks(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 << 20); }
-int column_shares(int64_t rows) { return (int)std::min<int64_t>(rows, 64); }
+// The gradients': one chunk to a thread (two behind 8192 columns), and a workgroup of 512 threads to a compute unit, which takes several rows at once
+// where they are short: more of them keep no more of memory busy, but leave more sums to join (16384 x 4096 bf16 77 us, with two workgroups 82, with 1024
+// threads 78, with four workgroups of 256 threads, two chunks each, 99).
+constexpr int kGradThreads = 512;
+int grad_tpr(int64_t cols)
+{
+    int tpr = 64;
+    while (tpr < 1024 && tpr * 8 < cols) tpr *= 2;
+    return tpr;
+}
+unsigned workgroups(alt_handle_t h, int64_t rows, int64_t cols)
+{
+    const int tpr = grad_tpr(cols), threads = std::max(tpr, kGradThreads);
+    const int64_t per = threads / tpr, cus = h->compute_units > 0 ? h->compute_units : 256;
+    return (unsigned)std::min<int64_t>((rows + per - 1) / per, cus);
+}
+int long_shares(int64_t rows) { return (int)std::min<int64_t>(rows, 64); }
 
 // What both directions check, dense strides filled in.
 alt_status_t check(alt_handle_t h, const char *call, const alt_norm_desc_t *d, alt_norm_desc_t *out)
@@ -123,28 +414,78 @@ alt_status_t check(alt_handle_t h, const char *call, const alt_norm_desc_t *d, a
     return ALT_OK;
 }
 
-size_t grad_workspace(const alt_norm_desc_t &d) { return d.rows ? (size_t)column_shares(d.rows) * 2 * d.cols * 4 + 16 : 0; }
+int shares_of(alt_handle_t h, const alt_norm_desc_t &d) { return d.cols > kMostCols ? long_shares(d.rows) : (int)workgroups(h, d.rows, d.cols); }
 
-template <int XS, int YS>
-void forward_run(const alt_norm_desc_t &d, const void *x, const float *gamma, const float *beta, void *y, float *mean, float *rstd, hipStream_t st)
+size_t grad_workspace(alt_handle_t h, const alt_norm_desc_t &d) { return d.rows ? (size_t)shares_of(h, d) * 2 * d.cols * 4 + 16 : 0; }
+
+// f(std::integral_constant TPR, KEEP) of a row's shape.
+template <typename F>
+void by_shape(int64_t cols, F f)
 {
-    hipLaunchKernelGGL((norm_kernel<XS, YS>), dim3(row_blocks(d.rows)), dim3(kThreads), 0, st, (const char *)x, d.x_stride * XS, gamma, beta, (char *)y, d.y_stride * YS, mean,
-                       rstd, d.rows, (int)d.cols, d.eps);
+    const Shape s = shape_of(cols);
+    using std::integral_constant;
+    if (s.tpr == 64 && s.keep == 1) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (s.tpr == 64) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (s.tpr == 256 && s.keep == 1) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (s.tpr == 256) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else if (s.tpr == 512) f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+
+template <typename F>
+void grad_by_shape(int64_t cols, F f)
+{
+    using std::integral_constant;
+    switch (grad_tpr(cols)) {
+        case 64: f(integral_constant<int, 64>{}, integral_constant<int, 1>{}); break;
+        case 128: f(integral_constant<int, 128>{}, integral_constant<int, 1>{}); break;
+        case 256: f(integral_constant<int, 256>{}, integral_constant<int, 1>{}); break;
+        case 512: f(integral_constant<int, 512>{}, integral_constant<int, 1>{}); break;
+        default:
+            if (cols <= 8192) f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+            else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    }
 }
 
 template <int XS, int YS>
-void grad_run(const alt_norm_desc_t &d, const void *dy, const void *x, const float *mean, const float *rstd, const float *gamma, void *dx, float *dgamma, float *dbeta, float *part,
-              hipStream_t st)
+void forward_run(alt_handle_t h, const alt_norm_desc_t &d, const void *x, const float *gamma, const float *beta, void *y, float *mean, float *rstd, hipStream_t st)
 {
-    if (d.rows)
-        hipLaunchKernelGGL((norm_dx_kernel<XS, YS>), dim3(row_blocks(d.rows)), dim3(kThreads), 0, st, (const char *)dy, d.y_stride * YS, (const char *)x, d.x_stride * XS, mean, rstd,
-                           gamma, (char *)dx, d.rows, (int)d.cols);
-    if (!dgamma && !dbeta) return;
-    const int shares = column_shares(d.rows);
-    if (d.rows)
-        hipLaunchKernelGGL((norm_columns_kernel<XS, YS>), dim3((unsigned)((d.cols + kThreads - 1) / kThreads), (unsigned)shares), dim3(kThreads), 0, st, (const char *)dy,
-                           d.y_stride * YS, (const char *)x, d.x_stride * XS, mean, rstd, part, d.rows, (int)d.cols);
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((2 * d.cols + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, part, shares, (int)d.cols, dgamma, dbeta);
+    const int64_t ldx = d.x_stride * XS, ldy = d.y_stride * YS;
+    const int cols = (int)d.cols;
+    if (d.cols > kMostCols) {
+        hipLaunchKernelGGL((norm_long_kernel<XS, YS>), dim3((unsigned)std::min<int64_t>(d.rows, 1 << 20)), dim3(kThreads), 0, st, (const char *)x, ldx, gamma, beta, (char *)y, ldy, mean,
+                           rstd, d.rows, cols, d.eps);
+        return;
+    }
+    by_shape(d.cols, [&](auto tpr, auto keep) {
+        constexpr int TPR = decltype(tpr)::value;
+        const int64_t per = kThreadsOf<TPR> / TPR, all = (d.rows + per - 1) / per;
+        hipLaunchKernelGGL((norm_kernel<XS, YS, TPR, decltype(keep)::value>), dim3((unsigned)std::min<int64_t>(all, (int64_t)h->compute_units * (2048 / kThreadsOf<TPR>))),
+                           dim3(kThreadsOf<TPR>), 0, st, (const char *)x, ldx, gamma, beta, (char *)y, ldy, mean, rstd, d.rows, cols, d.eps);
+    });
+}
+
+template <int XS, int YS>
+void grad_run(alt_handle_t h, const alt_norm_desc_t &d, const void *dy, const void *x, const float *mean, const float *rstd, const float *gamma, void *dx, float *dgamma,
+              float *dbeta, float *sums, hipStream_t st)
+{
+    const int64_t ldx = d.x_stride * XS, ldy = d.y_stride * YS;
+    const int cols = (int)d.cols, shares = d.rows ? shares_of(h, d) : 0;
+    if (d.cols > kMostCols && d.rows) {
+        hipLaunchKernelGGL((norm_long_dx_kernel<XS, YS>), dim3((unsigned)std::min<int64_t>(d.rows, 1 << 20)), dim3(kThreads), 0, st, (const char *)dy, ldy, (const char *)x, ldx, mean,
+                           rstd, gamma, (char *)dx, d.rows, cols);
+        if (sums)
+            hipLaunchKernelGGL((norm_long_sums_kernel<XS, YS>), dim3((unsigned)((cols + kThreads - 1) / kThreads), (unsigned)shares), dim3(kThreads), 0, st, (const char *)dy, ldy,
+                               (const char *)x, ldx, mean, rstd, sums, d.rows, cols);
+    } else if (d.rows) {
+        grad_by_shape(d.cols, [&](auto tpr, auto keep) {
+            constexpr int TPR = decltype(tpr)::value, THREADS = TPR > kGradThreads ? TPR : kGradThreads;
+            hipLaunchKernelGGL((norm_grad_kernel<XS, YS, TPR, decltype(keep)::value, THREADS>), dim3(workgroups(h, d.rows, d.cols)), dim3(THREADS), 0, st, (const char *)dy, ldy,
+                               (const char *)x, ldx, mean, rstd, gamma, (char *)dx, sums, d.rows, cols);
+        });
+    }
+    if (dgamma || dbeta)
+        hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((2 * d.cols + 31) / 32)), dim3(32 * kJoinGroups), 0, st, sums, shares, cols, dgamma, dbeta);
 }
 
 }  // namespace
@@ -165,11 +506,11 @@ extern "C" alt_status_t alt_layer_norm(alt_handle_t h, const alt_norm_desc_t *de
     if (s != ALT_OK) return s;
     const hipStream_t st = (hipStream_t)stream;
     if (d.in_dtype == ALT_F32) {
-        if (d.out_dtype == ALT_F32) forward_run<4, 4>(d, x, gamma, beta, y, mean, rstd, st);
-        else forward_run<4, 2>(d, x, gamma, beta, y, mean, rstd, st);
+        if (d.out_dtype == ALT_F32) forward_run<4, 4>(h, d, x, gamma, beta, y, mean, rstd, st);
+        else forward_run<4, 2>(h, d, x, gamma, beta, y, mean, rstd, st);
     } else {
-        if (d.out_dtype == ALT_F32) forward_run<2, 4>(d, x, gamma, beta, y, mean, rstd, st);
-        else forward_run<2, 2>(d, x, gamma, beta, y, mean, rstd, st);
+        if (d.out_dtype == ALT_F32) forward_run<2, 4>(h, d, x, gamma, beta, y, mean, rstd, st);
+        else forward_run<2, 2>(h, d, x, gamma, beta, y, mean, rstd, st);
     }
     ALT_CHECK_HIP(h, hipGetLastError());
     return ALT_OK;
@@ -186,17 +527,17 @@ extern "C" alt_status_t alt_layer_norm_grad(alt_handle_t h, const alt_norm_desc_
     s = check_buffers(h, "alt_layer_norm_grad", {{"dy", dy, dtype_size(d.out_dtype), rows}, {"x", x, dtype_size(d.in_dtype), rows}, {"mean", mean, 4, rows}, {"rstd", rstd, 4, rows},
                                                  {"gamma", gamma, 4, gamma != nullptr}, {"dx", dx, dtype_size(d.in_dtype), rows}, {"dgamma", dgamma, 4, dgamma != nullptr},
                                                  {"dbeta", dbeta, 4, dbeta != nullptr}});
-    if (s == ALT_OK && columns) s = check_workspace(h, "alt_layer_norm_grad", workspace, ws_bytes, grad_workspace(d));
+    if (s == ALT_OK && columns) s = check_workspace(h, "alt_layer_norm_grad", workspace, ws_bytes, grad_workspace(h, d));
     if (s == ALT_OK) s = check_device(h, "alt_layer_norm_grad");
     if (s != ALT_OK) return s;
     float *part = columns && rows ? (float *)aligned_workspace(workspace) : nullptr;
     const hipStream_t st = (hipStream_t)stream;
     if (d.in_dtype == ALT_F32) {
-        if (d.out_dtype == ALT_F32) grad_run<4, 4>(d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
-        else grad_run<4, 2>(d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
+        if (d.out_dtype == ALT_F32) grad_run<4, 4>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
+        else grad_run<4, 2>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
     } else {
-        if (d.out_dtype == ALT_F32) grad_run<2, 4>(d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
-        else grad_run<2, 2>(d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
+        if (d.out_dtype == ALT_F32) grad_run<2, 4>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
+        else grad_run<2, 2>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
     }
     ALT_CHECK_HIP(h, hipGetLastError());
     return ALT_OK;
@@ -208,6 +549,6 @@ extern "C" alt_status_t alt_layer_norm_grad_workspace_size(alt_handle_t h, const
     const alt_status_t s = check(h, "alt_layer_norm_grad_workspace_size", desc, &d);
     if (s != ALT_OK) return s;
     if (!bytes) return fail(h, ALT_INVALID_ARG, "alt_layer_norm_grad_workspace_size: null result");
-    *bytes = grad_workspace(d);
+    *bytes = grad_workspace(h, d);
     return ALT_OK;
 }
