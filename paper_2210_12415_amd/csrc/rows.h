@@ -73,6 +73,36 @@ __device__ __forceinline__ void put_chunk(char *p, const Chunk<ELSZ> &c)
     __builtin_memcpy(p, &c, 8 * ELSZ);
 }
 
+// 16 bytes as floats, and 16 / ELSZ floats as 16 bytes, rounded to nearest even.
+template <int ELSZ>
+__device__ __forceinline__ void floats16(const w4_t &c, float (&v)[16 / ELSZ])
+{
+    if constexpr (ELSZ == 4) {
+        const f4_t a = __builtin_bit_cast(f4_t, c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i];
+    } else {
+        const f4_t lo = __builtin_bit_cast(f4_t, c << 16), hi = __builtin_bit_cast(f4_t, c & 0xffff0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = lo[i]; v[2 * i + 1] = hi[i]; }
+    }
+}
+
+template <int ELSZ>
+__device__ __forceinline__ w4_t chunk16_of(const float (&v)[16 / ELSZ])
+{
+    if constexpr (ELSZ == 4) return __builtin_bit_cast(w4_t, (f4_t){v[0], v[1], v[2], v[3]});
+    else return (w4_t){f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
+}
+
+// A store of 16 bytes, at any alignment of whole elements, that the caches give up first.  Lanes side by side have to store side by side: with gaps
+// between them lines go out in parts (rows of 8192 tokens to two places each, 4096 bf16, 31 us for 40; fp32 in pieces of 32 bytes a lane 120 for 83).
+__device__ __forceinline__ void put_streaming(char *p, const w4_t &c)
+{
+    typedef uint32_t any4_t __attribute__((ext_vector_type(4), aligned(2)));
+    __builtin_nontemporal_store(c, (any4_t *)p);
+}
+
 // The sum over a wave's lanes, the same in all of them (shifts inside rows of 16 lanes, then the rows' last lanes handed on: lane 63 holds it).
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp_add(float v)
