@@ -3,8 +3,8 @@
 //   mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),  u = (x - mean) rstd,  y = u gamma + beta
 //   dx = rstd (g - mean_c(g) - u mean_c(g u))  with g = dy gamma,  dgamma = sum_m dy u,  dbeta = sum_m dy
 //
-// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.  TPR threads (a wave, or a workgroup) have a row, in chunks of
-// eight columns that stay in registers from the first sum to the last store, and take one row after another: a thread's columns are the same in all
+// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.  TPR threads (a wave, or a workgroup) have a row, in chunks
+// that stay in registers from the first sum to the last store, and take one row after another: a thread's columns are the same in all
 // of them, so gamma and beta are read once, dgamma and dbeta are summed in registers, and the next row is on its way while this one is reduced.  What the
 // workgroups have of dgamma and dbeta goes to the workspace and is joined by a second launch, in the order of the workgroups.  Rows of more than 16384
 // columns do not fit: they are read again for every sum.
@@ -16,39 +16,71 @@ namespace {
 
 constexpr int kMostCols = 16384;                           // of a row in registers
 
-// A thread's part of a row: chunks t, t + TPR, ... of `chunks`, and one element of the `rest` behind them.
-template <int ES, int TPR, int KEEP>
+// Columns of a chunk: what is 16 bytes of x and y, so that lanes side by side load and store side by side; eight where one is bf16 and the other fp32.
+template <int XS, int YS> constexpr int kChunk = XS == 4 && YS == 4 ? 4 : 8;
+
+template <int ES, int E>
+__device__ __forceinline__ void chunk_floats(const char *p, float (&v)[E])
+{
+    if constexpr (E * ES == 16) {
+        w4_t c;
+        __builtin_memcpy(&c, p, 16);
+        floats16<ES>(c, v);
+    } else {
+        floats<ES>(load_chunk<ES>(p), v);
+    }
+}
+
+// A thread's part of a row: chunks t, t + TPR, ... of `chunks`, as they lie in memory, and one element of the `rest` behind them.
+template <int ES, int E, int TPR, int K>
 struct Part {
-    Chunk<ES> c[KEEP];
+    w4_t c[K][E * ES / 16];
     float last;
     __device__ __forceinline__ void load(const char *row, int t, int chunks, int rest)
     {
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i)
-            if (i * TPR + t < chunks) c[i] = load_chunk<ES>(row + (int64_t)(i * TPR + t) * (8 * ES));
-        last = t < rest ? element<ES>(row + ((int64_t)chunks * 8 + t) * ES) : 0.f;
+        for (int i = 0; i < K; ++i)
+            if (i * TPR + t < chunks) __builtin_memcpy(&c[i], row + (int64_t)(i * TPR + t) * (E * ES), E * ES);
+        last = t < rest ? element<ES>(row + ((int64_t)chunks * E + t) * ES) : 0.f;
+    }
+    __device__ __forceinline__ void values(int i, float (&v)[E]) const
+    {
+        if constexpr (E * ES == 16) {
+            floats16<ES>(c[i][0], v);
+        } else {
+            Chunk<ES> whole;
+            __builtin_memcpy(&whole, &c[i], sizeof whole);
+            floats<ES>(whole, v);
+        }
     }
 };
 
-// Values of a thread's columns: those of its chunks and the one behind them.
-template <int KEEP>
+template <int ES, int E>
+__device__ __forceinline__ void put_values(char *p, const float (&v)[E])
+{
+    if constexpr (E * ES == 16) put_streaming(p, chunk16_of<ES>(v));
+    else put_chunk<ES>(p, chunk_of<ES>(v));
+}
+
+// fp32 values of a thread's columns: those of its chunks and the one behind them.
+template <int E, int K>
 struct Columns {
-    float v[KEEP][8], last;
+    float v[K][E], last;
     __device__ __forceinline__ void fill(float f)
     {
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i)
+        for (int i = 0; i < K; ++i)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[i][q] = f;
+            for (int q = 0; q < E; ++q) v[i][q] = f;
         last = f;
     }
     template <int TPR>
     __device__ __forceinline__ void load(const float *p, int t, int chunks, int rest)
     {
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i)
-            if (i * TPR + t < chunks) floats<4>(load_chunk<4>((const char *)(p + (i * TPR + t) * 8)), v[i]);
-        if (t < rest) last = p[chunks * 8 + t];
+        for (int i = 0; i < K; ++i)
+            if (i * TPR + t < chunks) chunk_floats<4, E>((const char *)(p + (i * TPR + t) * E), v[i]);
+        if (t < rest) last = p[chunks * E + t];
     }
 };
 
@@ -82,46 +114,52 @@ struct RowSum {
     }
 };
 
+template <int E>
+__device__ __forceinline__ void put_sums(float *p, const float (&v)[E])
+{
+    __builtin_memcpy(p, v, E * 4);
+}
+
 template <int TPR> constexpr int kThreadsOf = TPR < 256 ? 256 : TPR;
 
 template <int XS, int YS, int TPR, int KEEP>
 __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, int64_t ldx, const float *gamma, const float *beta, char *y, int64_t ldy, float *mean_out,
                                                                float *rstd_out, int64_t rows, int cols, float eps)
 {
-    constexpr int G = kThreadsOf<TPR> / TPR;
+    constexpr int G = kThreadsOf<TPR> / TPR, E = kChunk<XS, YS>, K = KEEP * 8 / E;
     __shared__ typename RowSum<TPR, G, 1>::Parts part;
     RowSum<TPR, G, 1> sum{&part};
-    const int t = threadIdx.x % TPR, chunks = cols / 8, rest = cols % 8;
+    const int t = threadIdx.x % TPR, chunks = cols / E, rest = cols % E;
     const int64_t step = (int64_t)gridDim.x * G;
     int64_t row = (int64_t)blockIdx.x * G + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
     if (row >= rows) return;
-    Part<XS, TPR, KEEP> next;
+    Part<XS, E, TPR, K> next;
     next.load(x + row * ldx, t, chunks, rest);
-    Columns<KEEP> g, b;
+    Columns<E, K> g, b;
     g.fill(1.f);
     b.fill(0.f);
     if (gamma) g.template load<TPR>(gamma, t, chunks, rest);
     if (beta) b.template load<TPR>(beta, t, chunks, rest);
     const float n = (float)cols;
     for (; row < rows; row += step) {
-        const Part<XS, TPR, KEEP> mine = next;
+        const Part<XS, E, TPR, K> mine = next;
         if (row + step < rows) next.load(x + (row + step) * ldx, t, chunks, rest);
-        float v[KEEP][8], s[1] = {mine.last};
+        float v[K][E], s[1] = {mine.last};
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i)
+        for (int i = 0; i < K; ++i)
             if (i * TPR + t < chunks) {
-                floats<XS>(mine.c[i], v[i]);
+                mine.values(i, v[i]);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) s[0] += v[i][q];
+                for (int q = 0; q < E; ++q) s[0] += v[i][q];
             }
         sum(s);
         const float mean = s[0] / n;
         s[0] = t < rest ? (mine.last - mean) * (mine.last - mean) : 0.f;
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i)
+        for (int i = 0; i < K; ++i)
             if (i * TPR + t < chunks) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
+                for (int q = 0; q < E; ++q) {
                     v[i][q] -= mean;
                     s[0] += v[i][q] * v[i][q];
                 }
@@ -134,13 +172,13 @@ __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, in
         }
         char *to = y + row * ldy;
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i)
+        for (int i = 0; i < K; ++i)
             if (i * TPR + t < chunks) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[i][q] = v[i][q] * rstd * g.v[i][q] + b.v[i][q];
-                put_chunk<YS>(to + (int64_t)(i * TPR + t) * (8 * YS), chunk_of<YS>(v[i]));
+                for (int q = 0; q < E; ++q) v[i][q] = v[i][q] * rstd * g.v[i][q] + b.v[i][q];
+                put_values<YS, E>(to + (int64_t)(i * TPR + t) * (E * YS), v[i]);
             }
-        if (t < rest) store_element<YS>(to + ((int64_t)chunks * 8 + t) * YS, (mine.last - mean) * rstd * g.last + b.last);
+        if (t < rest) store_element<YS>(to + ((int64_t)chunks * E + t) * YS, (mine.last - mean) * rstd * g.last + b.last);
     }
 }
 
@@ -150,14 +188,14 @@ template <int XS, int YS, int TPR, int KEEP, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int64_t ldy, const char *x, int64_t ldx, const float *mean, const float *rstd, const float *gamma,
                                                             char *dx, float *sums, int64_t rows, int cols)
 {
-    constexpr int G = THREADS / TPR;
+    constexpr int G = THREADS / TPR, E = kChunk<XS, YS>, K = KEEP * 8 / E;
     constexpr bool AHEAD = KEEP == 1;
     __shared__ typename RowSum<TPR, G, 2>::Parts part;
     RowSum<TPR, G, 2> sum{&part};
-    const int t = threadIdx.x % TPR, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), chunks = cols / 8, rest = cols % 8;
+    const int t = threadIdx.x % TPR, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), chunks = cols / E, rest = cols % E;
     const int64_t step = (int64_t)gridDim.x * G;
-    Part<XS, TPR, KEEP> next_x;
-    Part<YS, TPR, KEEP> next_dy;
+    Part<XS, E, TPR, K> next_x;
+    Part<YS, E, TPR, K> next_dy;
     float next_m = 0.f, next_r = 0.f;
     auto load = [&](int64_t row) {
         if (row >= rows) return;
@@ -166,7 +204,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
         next_m = mean[row];
         next_r = rstd[row];
     };
-    Columns<KEEP> g, dg, db;
+    Columns<E, K> g, dg, db;
     g.fill(1.f);
     dg.fill(0.f);
     db.fill(0.f);
@@ -180,16 +218,16 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
         if constexpr (!AHEAD) {
             load(row);
         }
-        const Part<XS, TPR, KEEP> mine_x = next_x;
-        const Part<YS, TPR, KEEP> mine_dy = next_dy;
+        const Part<XS, E, TPR, K> mine_x = next_x;
+        const Part<YS, E, TPR, K> mine_dy = next_dy;
         const float m = next_m, r = next_r;
         if (AHEAD) load(row + step);
-        float u[KEEP][8], w[KEEP][8], s[2] = {0.f, 0.f}, last_u = 0.f, last_g = 0.f;
-        auto values = [&](int i, float mean, float (&u)[8], float (&w)[8]) {
-            floats<XS>(mine_x.c[i], u);
-            floats<YS>(mine_dy.c[i], w);
+        float u[K][E], w[K][E], s[2] = {0.f, 0.f}, last_u = 0.f, last_g = 0.f;
+        auto values = [&](int i, float mean, float (&u)[E], float (&w)[E]) {
+            mine_x.values(i, u);
+            mine_dy.values(i, w);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) u[q] = (u[q] - mean) * r;
+            for (int q = 0; q < E; ++q) u[q] = (u[q] - mean) * r;
         };
         if (is) {
             last_u = t < rest ? (mine_x.last - m) * r : 0.f;
@@ -199,11 +237,11 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
             dg.last += mine_dy.last * last_u;
             db.last += mine_dy.last;
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i)
+            for (int i = 0; i < K; ++i)
                 if (i * TPR + t < chunks) {
                     values(i, m, u[i], w[i]);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
+                    for (int q = 0; q < E; ++q) {
                         dg.v[i][q] += w[i][q] * u[i][q];
                         db.v[i][q] += w[i][q];
                         w[i][q] *= g.v[i][q];
@@ -219,31 +257,31 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
         float again = m;
         if constexpr (!AHEAD) asm volatile("" : "+v"(again));              // (what the sums were made of is made again, not kept)
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i)
+        for (int i = 0; i < K; ++i)
             if (i * TPR + t < chunks) {
                 if constexpr (!AHEAD) {
                     values(i, again, u[i], w[i]);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) w[i][q] *= g.v[i][q];
+                    for (int q = 0; q < E; ++q) w[i][q] *= g.v[i][q];
                 }
 #pragma unroll
-                for (int q = 0; q < 8; ++q) w[i][q] = r * (w[i][q] - sg - u[i][q] * sgu);
-                put_chunk<XS>(to + (int64_t)(i * TPR + t) * (8 * XS), chunk_of<XS>(w[i]));
+                for (int q = 0; q < E; ++q) w[i][q] = r * (w[i][q] - sg - u[i][q] * sgu);
+                put_values<XS, E>(to + (int64_t)(i * TPR + t) * (E * XS), w[i]);
             }
-        if (t < rest) store_element<XS>(to + ((int64_t)chunks * 8 + t) * XS, r * (last_g - sg - last_u * sgu));
+        if (t < rest) store_element<XS>(to + ((int64_t)chunks * E + t) * XS, r * (last_g - sg - last_u * sgu));
     }
     if (!sums) return;
     sums += (int64_t)blockIdx.x * 2 * cols;
     if constexpr (G > 1) {                                 // the groups' sums one after another, into the last group's registers
-        __shared__ float to[2][KEEP * TPR * 8], ends[2][8];
+        __shared__ float to[2][K * E * TPR], ends[2][E];
         for (int k = 0; k < G; ++k) {
             __syncthreads();
             if (k != group) continue;
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i)
+            for (int i = 0; i < K; ++i)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int at = (i * 8 + q) * TPR + t;
+                for (int q = 0; q < E; ++q) {
+                    const int at = (i * E + q) * TPR + t;
                     if (k) { dg.v[i][q] += to[0][at]; db.v[i][q] += to[1][at]; }
                     to[0][at] = dg.v[i][q];
                     to[1][at] = db.v[i][q];
@@ -257,14 +295,14 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
         if (group != G - 1) return;
     }
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
+    for (int i = 0; i < K; ++i)
         if (i * TPR + t < chunks) {
-            put_chunk<4>((char *)(sums + (i * TPR + t) * 8), chunk_of<4>(dg.v[i]));
-            put_chunk<4>((char *)(sums + cols + (i * TPR + t) * 8), chunk_of<4>(db.v[i]));
+            put_sums<E>(sums + (i * TPR + t) * E, dg.v[i]);
+            put_sums<E>(sums + cols + (i * TPR + t) * E, db.v[i]);
         }
     if (t < rest) {
-        sums[chunks * 8 + t] = dg.last;
-        sums[cols + chunks * 8 + t] = db.last;
+        sums[chunks * E + t] = dg.last;
+        sums[cols + chunks * E + t] = db.last;
     }
 }
 
