@@ -31,21 +31,43 @@ __device__ __forceinline__ void chunk_floats(const char *p, float (&v)[E])
     }
 }
 
-// A thread's part of a row: chunks t, t + TPR, ... of `chunks`, as they lie in memory, and one element of the `rest` behind them.
-template <int ES, int E, int TPR, int K>
+// A thread's part of a row: chunks t, t + TPR, ... of `chunks`, as they lie in memory, and one element of the `rest` behind them.  SHIFT: bf16 rows that may begin
+// inside a dword; they are loaded from that dword on, with the one that they end in, and shifted when their values are asked for, as memory takes longer
+// over addresses inside a dword (gradients of 16384 x 4096, rows 4097 apart, 106 us, so 90; where all rows begin at dwords 78, and 81 if they are looked at so).
+template <int ES, int E, int TPR, int K, bool SHIFT>
 struct Part {
+    static_assert(!SHIFT || (ES == 2 && E == 8), "bf16");
     w4_t c[K][E * ES / 16];
-    float last;
+    uint32_t more[SHIFT ? K : 1], shift;   // shift: bytes
+    uint32_t bits;                         // of the element
     __device__ __forceinline__ void load(const char *row, int t, int chunks, int rest)
     {
+        shift = SHIFT ? __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)row & 2u) : 0u;
 #pragma unroll
         for (int i = 0; i < K; ++i)
-            if (i * TPR + t < chunks) __builtin_memcpy(&c[i], row + (int64_t)(i * TPR + t) * (E * ES), E * ES);
-        last = t < rest ? element<ES>(row + ((int64_t)chunks * E + t) * ES) : 0.f;
+            if (i * TPR + t < chunks) {
+                const char *at = row + (int64_t)(i * TPR + t) * (E * ES) - shift;
+                __builtin_memcpy(&c[i], __builtin_assume_aligned(at, 4), E * ES);
+                if constexpr (SHIFT) {
+                    if (shift) more[i] = *(const uint32_t *)(at + 16);
+                }
+            }
+        bits = 0;
+        if (t < rest) {
+            const char *at = row + ((int64_t)chunks * E + t) * ES;
+            if constexpr (ES == 4) bits = *(const uint32_t *)at;
+            else bits = *(const uint16_t *)at;
+        }
     }
+    // (made of the bits when it is used: made when it is loaded it is waited for there, with all loads before it, 16384 x 4095 131 us for 77)
+    __device__ __forceinline__ float last() const { return __builtin_bit_cast(float, ES == 4 ? bits : bits << 16); }
     __device__ __forceinline__ void values(int i, float (&v)[E]) const
     {
-        if constexpr (E * ES == 16) {
+        if constexpr (SHIFT) {
+            const w4_t w = c[i][0];
+            floats16<2>((w4_t){__builtin_amdgcn_alignbyte(w.y, w.x, shift), __builtin_amdgcn_alignbyte(w.z, w.y, shift), __builtin_amdgcn_alignbyte(w.w, w.z, shift),
+                               __builtin_amdgcn_alignbyte(more[i], w.w, shift)}, v);
+        } else if constexpr (E * ES == 16) {
             floats16<ES>(c[i][0], v);
         } else {
             Chunk<ES> whole;
@@ -122,7 +144,7 @@ __device__ __forceinline__ void put_sums(float *p, const float (&v)[E])
 
 template <int TPR> constexpr int kThreadsOf = TPR < 256 ? 256 : TPR;
 
-template <int XS, int YS, int TPR, int KEEP>
+template <int XS, int YS, int TPR, int KEEP, bool SHIFT>
 __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, int64_t ldx, const float *gamma, const float *beta, char *y, int64_t ldy, float *mean_out,
                                                                float *rstd_out, int64_t rows, int cols, float eps)
 {
@@ -133,7 +155,7 @@ __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, in
     const int64_t step = (int64_t)gridDim.x * G;
     int64_t row = (int64_t)blockIdx.x * G + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
     if (row >= rows) return;
-    Part<XS, E, TPR, K> next;
+    Part<XS, E, TPR, K, SHIFT> next;
     next.load(x + row * ldx, t, chunks, rest);
     Columns<E, K> g, b;
     g.fill(1.f);
@@ -142,9 +164,9 @@ __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, in
     if (beta) b.template load<TPR>(beta, t, chunks, rest);
     const float n = (float)cols;
     for (; row < rows; row += step) {
-        const Part<XS, E, TPR, K> mine = next;
+        const Part<XS, E, TPR, K, SHIFT> mine = next;
         if (row + step < rows) next.load(x + (row + step) * ldx, t, chunks, rest);
-        float v[K][E], s[1] = {mine.last};
+        float v[K][E], s[1] = {mine.last()};
 #pragma unroll
         for (int i = 0; i < K; ++i)
             if (i * TPR + t < chunks) {
@@ -154,7 +176,7 @@ __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, in
             }
         sum(s);
         const float mean = s[0] / n;
-        s[0] = t < rest ? (mine.last - mean) * (mine.last - mean) : 0.f;
+        s[0] = t < rest ? (mine.last() - mean) * (mine.last() - mean) : 0.f;
 #pragma unroll
         for (int i = 0; i < K; ++i)
             if (i * TPR + t < chunks) {
@@ -178,13 +200,13 @@ __global__ __launch_bounds__(kThreadsOf<TPR>) void norm_kernel(const char *x, in
                 for (int q = 0; q < E; ++q) v[i][q] = v[i][q] * rstd * g.v[i][q] + b.v[i][q];
                 put_values<YS, E>(to + (int64_t)(i * TPR + t) * (E * YS), v[i]);
             }
-        if (t < rest) store_element<YS>(to + ((int64_t)chunks * E + t) * YS, (mine.last - mean) * rstd * g.last + b.last);
+        if (t < rest) store_element<YS>(to + ((int64_t)chunks * E + t) * YS, (mine.last() - mean) * rstd * g.last + b.last);
     }
 }
 
 // dx, and this workgroup's part of dgamma and dbeta (`sums`: 2 x cols for each workgroup, or null).  G rows at once; with one chunk a thread
 // keeps the next row on its way, with two there are no registers for that.
-template <int XS, int YS, int TPR, int KEEP, int THREADS>
+template <int XS, int YS, int TPR, int KEEP, int THREADS, bool SHIFT>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int64_t ldy, const char *x, int64_t ldx, const float *mean, const float *rstd, const float *gamma,
                                                             char *dx, float *sums, int64_t rows, int cols)
 {
@@ -194,8 +216,8 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
     RowSum<TPR, G, 2> sum{&part};
     const int t = threadIdx.x % TPR, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), chunks = cols / E, rest = cols % E;
     const int64_t step = (int64_t)gridDim.x * G;
-    Part<XS, E, TPR, K> next_x;
-    Part<YS, E, TPR, K> next_dy;
+    Part<XS, E, TPR, K, SHIFT> next_x;
+    Part<YS, E, TPR, K, SHIFT> next_dy;
     float next_m = 0.f, next_r = 0.f;
     auto load = [&](int64_t row) {
         if (row >= rows) return;
@@ -218,8 +240,8 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
         if constexpr (!AHEAD) {
             load(row);
         }
-        const Part<XS, E, TPR, K> mine_x = next_x;
-        const Part<YS, E, TPR, K> mine_dy = next_dy;
+        const Part<XS, E, TPR, K, SHIFT> mine_x = next_x;
+        const Part<YS, E, TPR, K, SHIFT> mine_dy = next_dy;
         const float m = next_m, r = next_r;
         if (AHEAD) load(row + step);
         float u[K][E], w[K][E], s[2] = {0.f, 0.f}, last_u = 0.f, last_g = 0.f;
@@ -230,12 +252,12 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const char *dy, int6
             for (int q = 0; q < E; ++q) u[q] = (u[q] - mean) * r;
         };
         if (is) {
-            last_u = t < rest ? (mine_x.last - m) * r : 0.f;
-            last_g = mine_dy.last * g.last;
+            last_u = t < rest ? (mine_x.last() - m) * r : 0.f;
+            last_g = mine_dy.last() * g.last;
             s[0] = last_g;
             s[1] = last_g * last_u;
-            dg.last += mine_dy.last * last_u;
-            db.last += mine_dy.last;
+            dg.last += mine_dy.last() * last_u;
+            db.last += mine_dy.last();
 #pragma unroll
             for (int i = 0; i < K; ++i)
                 if (i * TPR + t < chunks) {
@@ -485,7 +507,10 @@ void grad_by_shape(int64_t cols, F f)
     }
 }
 
-template <int XS, int YS>
+// Whether bf16 rows begin inside dwords.
+bool inside_dwords(const alt_norm_desc_t &d, const void *p, int64_t stride) { return (uintptr_t)p % 4 || (d.rows > 1 && stride % 2); }
+
+template <int XS, int YS, bool SHIFT = false>
 void forward_run(alt_handle_t h, const alt_norm_desc_t &d, const void *x, const float *gamma, const float *beta, void *y, float *mean, float *rstd, hipStream_t st)
 {
     const int64_t ldx = d.x_stride * XS, ldy = d.y_stride * YS;
@@ -498,12 +523,12 @@ void forward_run(alt_handle_t h, const alt_norm_desc_t &d, const void *x, const 
     by_shape(d.cols, [&](auto tpr, auto keep) {
         constexpr int TPR = decltype(tpr)::value;
         const int64_t per = kThreadsOf<TPR> / TPR, all = (d.rows + per - 1) / per;
-        hipLaunchKernelGGL((norm_kernel<XS, YS, TPR, decltype(keep)::value>), dim3((unsigned)std::min<int64_t>(all, (int64_t)h->compute_units * (2048 / kThreadsOf<TPR>))),
+        hipLaunchKernelGGL((norm_kernel<XS, YS, TPR, decltype(keep)::value, SHIFT>), dim3((unsigned)std::min<int64_t>(all, (int64_t)h->compute_units * (2048 / kThreadsOf<TPR>))),
                            dim3(kThreadsOf<TPR>), 0, st, (const char *)x, ldx, gamma, beta, (char *)y, ldy, mean, rstd, d.rows, cols, d.eps);
     });
 }
 
-template <int XS, int YS>
+template <int XS, int YS, bool SHIFT = false>
 void grad_run(alt_handle_t h, const alt_norm_desc_t &d, const void *dy, const void *x, const float *mean, const float *rstd, const float *gamma, void *dx, float *dgamma,
               float *dbeta, float *sums, hipStream_t st)
 {
@@ -518,7 +543,7 @@ void grad_run(alt_handle_t h, const alt_norm_desc_t &d, const void *dy, const vo
     } else if (d.rows) {
         grad_by_shape(d.cols, [&](auto tpr, auto keep) {
             constexpr int TPR = decltype(tpr)::value, THREADS = TPR > kGradThreads ? TPR : kGradThreads;
-            hipLaunchKernelGGL((norm_grad_kernel<XS, YS, TPR, decltype(keep)::value, THREADS>), dim3(workgroups(h, d.rows, d.cols)), dim3(THREADS), 0, st, (const char *)dy, ldy,
+            hipLaunchKernelGGL((norm_grad_kernel<XS, YS, TPR, decltype(keep)::value, THREADS, SHIFT>), dim3(workgroups(h, d.rows, d.cols)), dim3(THREADS), 0, st, (const char *)dy, ldy,
                                (const char *)x, ldx, mean, rstd, gamma, (char *)dx, sums, d.rows, cols);
         });
     }
@@ -548,6 +573,7 @@ extern "C" alt_status_t alt_layer_norm(alt_handle_t h, const alt_norm_desc_t *de
         else forward_run<4, 2>(h, d, x, gamma, beta, y, mean, rstd, st);
     } else {
         if (d.out_dtype == ALT_F32) forward_run<2, 4>(h, d, x, gamma, beta, y, mean, rstd, st);
+        else if (inside_dwords(d, x, d.x_stride)) forward_run<2, 2, true>(h, d, x, gamma, beta, y, mean, rstd, st);
         else forward_run<2, 2>(h, d, x, gamma, beta, y, mean, rstd, st);
     }
     ALT_CHECK_HIP(h, hipGetLastError());
@@ -575,6 +601,7 @@ extern "C" alt_status_t alt_layer_norm_grad(alt_handle_t h, const alt_norm_desc_
         else grad_run<4, 2>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
     } else {
         if (d.out_dtype == ALT_F32) grad_run<2, 4>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
+        else if (inside_dwords(d, x, d.x_stride) || inside_dwords(d, dy, d.y_stride)) grad_run<2, 2, true>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
         else grad_run<2, 2>(h, d, dy, x, mean, rstd, gamma, dx, dgamma, dbeta, part, st);
     }
     ALT_CHECK_HIP(h, hipGetLastError());
