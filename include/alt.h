@@ -569,7 +569,8 @@ alt_status_t alt_gemm_grouped_dw_workspace_size(alt_handle_t h, const alt_groupe
  * alignment of their elements and must not overlap; rows of 16-byte chunks at 16-byte addresses are fastest; all calls are asynchronous on
  * `stream` and give the same bits for the same inputs, whatever runs beside them.  The handle's device has to be the current one (the calls
  * refuse any other).  A workspace is the caller's, needs the bytes its size call names (at any address; less is ALT_WORKSPACE_TOO_SMALL), holds
- * nothing between calls, and must not be in use by two streams at once.  2^30 rows, tokens or (token, choice) pairs, 2^24 columns at most. */
+ * nothing between calls, and must not be in use by two streams at once.  2^30 rows, tokens or (token, choice) pairs, 2^24 columns
+ * and strides of 2^31 at most (alt_route and its gradient: 2^25 tokens; alt_gemm_adapters: strides of 2^22, 2^20 adapters). */
 
 typedef struct {
     int64_t rows, cols;           /* rows may be 0 */

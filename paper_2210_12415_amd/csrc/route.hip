@@ -2,163 +2,421 @@
 //
 //   score = softmax or sigmoid of a row of logits, choice = score + bias or the logit, the top_k largest choices (of the worthiest groups);
 //   a place for every (token, choice) in the order of expert, token, choice: offsets and rows
+//
+// There is little to read: 16384 x 256 fp32 logits are 3 us of memory.  The time goes into launches and into the selection, about 100 instructions of a
+// wave for each choice of its four rows, so lanes hold many experts and few lanes a row.  One launch chooses and ranks the choices inside each
+// workgroup's tokens; where there is one workgroup that is all, else the ranks are moved by what the workgroups before have of each expert.
 #include "common.h"
 #include "rows.h"
 
 namespace alt {
 namespace {
 
+constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
+
 struct RouteParams {
     const char *logits;
     const float *bias;
     int32_t *experts;
     float *weights;
-    int32_t *rows, *offsets, *counts;
+    int32_t *rows, *offsets;
+    int32_t *counts;                       // [workgroups][num]: choices of each expert; then [num]: of all workgroups (route_scan_kernel)
     int64_t ld;                            // bytes between rows of logits
-    int32_t tokens, num, top_k, groups, top_groups, group_best, softmax, renorm;
+    int32_t tokens, num, top_k, groups, top_groups, group_best, softmax, renorm, chunks;
+    FastDiv each;                          // experts of a group
     float scale;
 };
 
-__device__ __forceinline__ double wave_max(double v)
+// ---- values of the lanes that share a row ------------------------------------------------------------------------------------------
+
+template <int N, typename T>
+__device__ __forceinline__ T rotated(T v)                  // of the lane N before, in turn inside 16 lanes
 {
-    for (int i = 32; i; i /= 2) v = fmax(v, __shfl_xor(v, i));
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t w = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, 0x120 + N, 0xf, 0xf, true);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), 0x120 + N, 0xf, 0xf, true);
+        return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+    } else {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, true));
+    }
+}
+
+// f over the L (16 or 64) lanes of a row, the same in all of them.
+template <int L, typename T, typename F>
+__device__ __forceinline__ T over_row(T v, F f)
+{
+    v = f(v, rotated<8>(v));
+    v = f(v, rotated<4>(v));
+    v = f(v, rotated<2>(v));
+    v = f(v, rotated<1>(v));
+    if constexpr (L == 64) {
+        v = f(v, __shfl_xor(v, 16));
+        v = f(v, __shfl_xor(v, 32));
+    }
     return v;
 }
+template <int L, typename T> __device__ __forceinline__ T row_max(T v) { return over_row<L>(v, [](T a, T b) { return a > b ? a : b; }); }
+template <int L, typename T> __device__ __forceinline__ T row_min(T v) { return over_row<L>(v, [](T a, T b) { return a < b ? a : b; }); }
+template <int L, typename T> __device__ __forceinline__ T row_sum(T v) { return over_row<L>(v, [](T a, T b) { return a + b; }); }
 
-__device__ __forceinline__ double wave_sum(double v)
+// This lane's V logits, of the experts from e0 on; -inf behind the last.
+template <int ES, int V>
+__device__ __forceinline__ void load_logits(const char *row, int e0, int num, float (&l)[V])
 {
-    for (int i = 32; i; i /= 2) v += __shfl_xor(v, i);
-    return v;
-}
-
-// The largest value of the wave and the lowest index that has it.
-__device__ __forceinline__ void wave_best(double &v, int &at)
-{
-    for (int i = 32; i; i /= 2) {
-        const double w = __shfl_xor(v, i);
-        const int b = __shfl_xor(at, i);
-        if (w > v || (w == v && b < at)) { v = w; at = b; }
-    }
-}
-
-constexpr int kMax = ALT_ROUTE_MAX_EXPERTS;
-
-// A wave per token, lane l with the experts l, l + 64, ...
-template <int ES>
-__global__ __launch_bounds__(64) void route_kernel(const RouteParams p)
-{
-    constexpr int VPL = kMax / 64;
-    __shared__ double worth[kMax], group[kMax];
-    const int lane = threadIdx.x;
-    for (int64_t t = blockIdx.x; t < p.tokens; t += gridDim.x) {
-    __syncthreads();
-    const char *row = p.logits + t * p.ld;
-    double l[VPL], score[VPL], key[VPL], top = -INFINITY;
-    bool lost = false;
+    if (e0 + V <= num) {
+        if constexpr (V * ES >= 16) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        const int e = lane + 64 * i;
-        l[i] = e < p.num ? (double)element<ES>(row + e * ES) : -INFINITY;
-        lost |= l[i] != l[i] || (p.softmax && l[i] == INFINITY);
-        top = fmax(top, l[i]);
-    }
-    top = wave_max(top);
-    lost = __ballot(lost) != 0;
-    double sum = 0;
+            for (int i = 0; i < V * ES / 16; ++i) {
+                w4_t c;
+                float f[16 / ES];
+                __builtin_memcpy(&c, row + (int64_t)e0 * ES + i * 16, 16);
+                floats16<ES>(c, f);
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        score[i] = l[i] == -INFINITY ? 0.0 : p.softmax ? exp(l[i] - top) : 1.0 / (1.0 + exp(-l[i]));
-        sum += score[i];
-    }
-    sum = wave_sum(sum);
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        const int e = lane + 64 * i;
-        if (p.softmax && sum > 0) score[i] /= sum;
-        double w = score[i] + (p.bias && e < p.num ? (double)p.bias[e] : 0.0);
-        if (l[i] == -INFINITY || w != w || lost) w = -INFINITY;
-        key[i] = w == -INFINITY ? w : p.bias ? w : l[i];
-        worth[e] = w;
-    }
-    if (p.top_groups < p.groups) {
-        const int each = p.num / p.groups;
-        __syncthreads();
-        for (int g = lane; g < p.groups; g += 64) {
-            double one = -INFINITY, two = -INFINITY;
-            for (int e = g * each; e < (g + 1) * each; ++e) {
-                const double v = worth[e];
-                if (v > one) { two = one; one = v; }
-                else if (v > two) two = v;
+                for (int q = 0; q < 16 / ES; ++q) l[i * (16 / ES) + q] = f[q];
             }
-            group[g] = p.group_best == 2 && two > -INFINITY ? one + two : one;
-        }
-        __syncthreads();
+        } else {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            const int e = lane + 64 * i, g = e < p.num ? e / each : 0;
+            for (int i = 0; i < V; ++i) l[i] = element<ES>(row + (int64_t)(e0 + i) * ES);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) l[i] = e0 + i < num ? element<ES>(row + (int64_t)(e0 + i) * ES) : -INFINITY;
+    }
+}
+
+// What a wave's lanes have stored in LDS is there for its other lanes (a wave's LDS operations run in their order; this is for the compiler).
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ float exp_of(float v) { return expf(v); }
+__device__ __forceinline__ double exp_of(double v) { return exp(v); }
+
+// (by the exponential of what is negative: nothing overflows, and small results keep their digits)
+template <typename F>
+__device__ __forceinline__ F sigmoid_of(F v)
+{
+    const F e = exp_of(v < 0 ? v : -v);
+    return (v < 0 ? e : (F)1) / (1 + e);
+}
+
+// ---- the choice --------------------------------------------------------------------------------------------------------------------
+
+// What a row's lanes know of it: the largest logit, the sum of exp(logit - top), and whether it is lost to a NaN.
+struct RowStats { float top, sum; bool lost; };
+
+// The choices of a row by numbers of type F: lane j of the row gets the j-th expert in `mine`, or -1.  True: they are those of exact arithmetic.
+//
+// Logits that are compared themselves are exact.  Scores are not, and two choices nearer than what rounding can have moved them leave it open which is
+// the larger; the caller then asks again in 64 bits.  A sigmoid in fp32 is off by four roundings, two of them by 2^-21 of the row's largest score S; a
+// softmax by the roundings of its argument, sum and quotient, 2^-18 S; adding the bias rounds by 2^-24 of the choice.  Twice that is `near`.
+template <typename F, int L, int V>
+__device__ __forceinline__ bool choose(const RouteParams &p, const float (&l)[V], const RowStats &st, int sub, char *lds, int &mine)
+{
+    constexpr bool FAST = sizeof(F) == 4;
+    const F none = -INFINITY;
+    const bool scored = p.bias || p.top_groups < p.groups;
+    const int e0 = sub * V;
+    F key[V], most = 0;
+    bool sure = true;
+    if (scored) {
+        F sum = 1;
+        if (p.softmax) {
+            if constexpr (FAST) {
+                sum = st.sum;
+            } else {
+                sum = 0;
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0 : exp_of((F)l[i] - (F)st.top);
+                sum = row_sum<L>(sum);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const F s = p.softmax ? exp_of((F)l[i] - (F)st.top) / sum : sigmoid_of((F)l[i]);
+            F w = p.bias && e0 + i < p.num ? s + (F)p.bias[e0 + i] : s;
+            if (l[i] == -INFINITY || w != w || st.lost) w = none;
+            if (FAST && w != none) most = s > most ? s : most;
+            key[i] = w;
+        }
+        if constexpr (FAST) most = row_max<L>(most);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = st.lost ? none : (F)l[i];
+    }
+    const F near = most * (F)(p.softmax ? 0x1p-17 : 0x1p-20) + (F)0x1p-120;
+    if (p.top_groups < p.groups) {
+        // one after another in the row's LDS: the worths of its experts, of its groups, and which groups are kept; a lane has the groups sub, sub + L, ...
+        F *worth = (F *)lds, group[V];
+        const int each = (int)p.each.d;
+#pragma unroll
+        for (int i = 0; i < V; ++i) worth[e0 + i] = key[i];
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int g = sub + i * L;
+            F one = none, two = none;
+            if (g < p.groups)
+                for (int e = g * each; e < (g + 1) * each; ++e) {
+                    const F v = worth[e];
+                    two = v > one ? one : v > two ? v : two;
+                    one = v > one ? v : one;
+                }
+            group[i] = p.group_best == 2 && two > none ? one + two : one;
+        }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (sub + i * L < p.groups) worth[sub + i * L] = group[i];
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int g = sub + i * L;
+            const F v = group[i];
             int better = 0;
-            for (int o = 0; o < p.groups; ++o) better += group[o] > group[g] || (group[o] == group[g] && o < g);
-            if (better >= p.top_groups) key[i] = -INFINITY;
+            if (g < p.groups)
+                for (int o = 0; o < p.groups; ++o) {
+                    const F w = worth[o];
+                    better += w > v || (w == v && o < g);
+                    if constexpr (FAST) {
+                        const F size = v < 0 ? -v : v, apart = w > v ? w - v : v - w;
+                        if (o != g && v > none && w > none && !(apart > 2 * near + size * (F)0x1p-21)) sure = false;
+                    }
+                }
+            group[i] = better < p.top_groups ? (F)1 : (F)0;
+        }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (sub + i * L < p.groups) worth[sub + i * L] = group[i];
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const bool kept = e0 + i < p.num && worth[fast_div((uint32_t)(e0 + i), p.each)] != 0;
+            if (!kept) key[i] = none;
+            else if (!p.bias) key[i] = key[i] == none ? none : (F)l[i];
         }
     }
-    int mine = -1;                                         // lane j: the j-th choice and its score
-    double chosen = 0, total = 0;
-    for (int j = 0; j < p.top_k; ++j) {
-        double best = -INFINITY;
-        int at = kMax;
+    mine = -1;
+    F last = INFINITY;
+    const int picks = FAST && p.bias ? p.top_k + 1 : p.top_k;              // (one more, to see how near it is)
+    for (int j = 0; j < picks; ++j) {
+        F best = none;
+        int at = 0x7fffffff;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (key[i] > best) { best = key[i]; at = lane + 64 * i; }
-        wave_best(best, at);
-        if (best == -INFINITY) break;
-        double s = 0;
+        for (int i = 0; i < V; ++i) {
+            const bool more = key[i] > best;
+            best = more ? key[i] : best;
+            at = more ? e0 + i : at;
+        }
+        const F top = row_max<L>(best);
+        const bool is = top > none;
+        at = row_min<L>(best == top && is ? at : 0x7fffffff);
+        if constexpr (FAST) {
+            if (p.bias && is && j > 0) {
+                const F size = last < 0 ? -last : last;
+                if (!(last - top > near + size * (F)0x1p-22)) sure = false;
+            }
+        }
+        last = top;
+        if (sub == j && j < p.top_k && is) mine = at;
+        if (!__ballot(is)) break;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (at == lane + 64 * i) { s = score[i]; key[i] = -INFINITY; }
-        s = __shfl(s, at % 64);
-        total += s;
-        if (lane == j) { mine = at; chosen = s; }
+        for (int i = 0; i < V; ++i)
+            if (e0 + i == at) key[i] = none;
     }
-    if (lane < p.top_k) {
-        const int64_t to = t * p.top_k + lane;
-        if (p.renorm && total > 0) chosen /= total;
-        p.experts[to] = mine;
-        p.weights[to] = lost ? __builtin_nanf("") : (float)(chosen * (double)p.scale);
-        p.rows[to] = -1;
+    return sure;
+}
+
+// Sum over the lanes up to and with this one.
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
+    return v;
+}
+
+// The sum of v over the threads before this one of the workgroup (`part`: one number for each wave).
+__device__ __forceinline__ int before_thread(int v, int (&part)[kRouteWaves])
+{
+    const int upto = wave_scan(v), wave = threadIdx.x / 64;
+    if (threadIdx.x % 64 == 63) part[wave] = upto;
+    __syncthreads();
+    int before = upto - v;
+#pragma unroll
+    for (int i = 0; i < kRouteWaves; ++i) before += i < wave ? part[i] : 0;
+    return before;
+}
+
+// Bytes of LDS: the workgroup's choices and a row of counts for each wave, over the rows' group worths.
+__host__ __device__ constexpr int route_slots(int L) { return L == 16 ? 64 * 16 : 16 * ALT_ROUTE_MAX_TOP_K; }
+template <int L> constexpr int kRowsOf = kRouteThreads / L;
+inline size_t route_lds(int L, int V, int num, bool grouped)
+{
+    const size_t rank = (size_t)route_slots(L) * 2 + (size_t)kRouteWaves * num * 2, worth = grouped ? (size_t)kRouteThreads * V * 8 : 0;
+    return (std::max(rank, worth) + 15) / 16 * 16;
+}
+
+// L lanes to a row, V experts to a lane.
+template <int ES, int L, int V>
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteParams p)
+{
+    extern __shared__ char route_smem[];
+    __shared__ int part[kRouteWaves];
+    constexpr int ROWS = kRowsOf<L>;
+    const int t = threadIdx.x, sub = t % L, row_in = t / L, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64);
+    const int64_t first = (int64_t)blockIdx.x * ROWS, token = first + row_in;
+    const bool here = token < p.tokens;
+    float l[V];
+    if (here) {
+        load_logits<ES, V>(p.logits + token * p.ld, sub * V, p.num, l);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) l[i] = -INFINITY;
     }
+    RowStats st;
+    st.top = -INFINITY;
+    int lost = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        lost |= l[i] != l[i] || (p.softmax && l[i] == INFINITY);
+        st.top = l[i] > st.top ? l[i] : st.top;
+    }
+    st.top = row_max<L>(st.top);
+    st.lost = row_max<L>(lost) != 0;
+    st.sum = 1.f;
+    if (p.softmax && (!p.renorm || p.bias || p.top_groups < p.groups)) {
+        st.sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) st.sum += l[i] == -INFINITY ? 0.f : expf(l[i] - st.top);
+        st.sum = row_sum<L>(st.sum);
+    }
+    int mine;
+    char *lds = route_smem + (size_t)row_in * (L * V * 8);
+    if (__ballot(!choose<float, L, V>(p, l, st, sub, lds, mine))) choose<double, L, V>(p, l, st, sub, lds, mine);
+    // weights, a choice to a lane
+    if (here) {
+        const bool is = mine >= 0;
+        const float v = is ? element<ES>(p.logits + token * p.ld + (int64_t)mine * ES) : -INFINITY;
+        float w;
+        if (p.softmax) {
+            // (renormalized: of the chosen ones alone, by the largest of them, which keeps what would be lost beside a larger one that was not chosen)
+            const float top = p.renorm ? row_max<L>(v) : st.top;
+            w = is ? expf(v - top) : 0.f;
+            w = w / (p.renorm ? row_sum<L>(w) : st.sum);
+        } else {
+            w = is ? sigmoid_of(v) : 0.f;
+            if (p.renorm) {
+                const float sum = row_sum<L>(w);
+                w = w / (sum > 0.f ? sum : 1.f);
+            }
+        }
+        if (sub < p.top_k) {
+            p.experts[token * p.top_k + sub] = mine;
+            p.weights[token * p.top_k + sub] = st.lost ? __builtin_nanf("") : is ? w * p.scale : 0.f;
+        }
+    }
+    // the choices of the workgroup's tokens, a choice to a thread: its place among those of its expert
+    __syncthreads();                                       // (the group worths are read)
+    int16_t *slot = (int16_t *)route_smem;
+    uint16_t *count = (uint16_t *)(slot + route_slots(L));
+    const int n = (int)min((int64_t)ROWS, p.tokens - first) * p.top_k, waves = (n + 63) / 64;
+    if (sub < p.top_k && here) slot[row_in * p.top_k + sub] = (int16_t)mine;
+    for (int i = t; i < waves * p.num; i += kRouteThreads) count[i] = 0;
+    __syncthreads();
+    const int e = t < n ? slot[t] : -1;
+    int rank = 0;
+    if (wave < waves) {
+        uint64_t same = __ballot(e >= 0);
+        for (int b = 1; b < p.num; b *= 2) {
+            const uint64_t has = __ballot((e & b) != 0);
+            same &= (e & b) ? has : ~has;
+        }
+        rank = __popcll(same & ((1ull << lane) - 1));
+        if (e >= 0 && rank == 0) count[wave * p.num + e] = (uint16_t)__popcll(same);
+    }
+    __syncthreads();
+    int all = 0;
+    if (t < p.num)
+        for (int w = 0; w < waves; ++w) {
+            const int c = count[w * p.num + t];
+            count[w * p.num + t] = (uint16_t)all;
+            all += c;
+        }
+    int begin = 0;
+    if (p.chunks == 1) {                                   // (the only workgroup)
+        begin = before_thread(all, part);
+        if (t < p.num) p.offsets[t] = begin;
+        if (t == p.num - 1) p.offsets[p.num] = begin + all;
+        __syncthreads();
+        if (t < p.num)
+            for (int w = 0; w < waves; ++w) count[w * p.num + t] += (uint16_t)begin;
+    } else if (t < p.num) {
+        p.counts[(int64_t)blockIdx.x * p.num + t] = all;
+    }
+    __syncthreads();
+    if (t < n) p.rows[first * p.top_k + t] = e >= 0 ? count[wave * p.num + e] + rank : -1;
+}
+
+// What the workgroups before have of each expert, in place of what each has, and behind them what all have.  16 experts to a workgroup, 64 threads to an
+// expert, each with a run of the workgroups.
+__global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(const RouteParams p)
+{
+    __shared__ int part[64][17];
+    const int x = threadIdx.x % 16, run = threadIdx.x / 16, e = blockIdx.x * 16 + x, per = (p.chunks + 63) / 64, lo = run * per, hi = min(lo + per, p.chunks);
+    int sum = 0;
+    if (e < p.num) {
+#pragma unroll 8
+        for (int c = lo; c < hi; ++c) sum += p.counts[(int64_t)c * p.num + e];
+    }
+    part[run][x] = sum;
+    __syncthreads();
+    int before = 0;
+    for (int r = 0; r < run; ++r) before += part[r][x];
+    if (e >= p.num) return;
+    if (run == 63) p.counts[(int64_t)p.chunks * p.num + e] = before + sum;
+    for (int c = lo; c < hi; ++c) {
+        int32_t *at = p.counts + (int64_t)c * p.num + e;
+        const int v = *at;
+        *at = before;
+        before += v;
     }
 }
 
-// A workgroup per expert counts its choices; then it finds its first row and gives its choices theirs.
-__global__ __launch_bounds__(256) void route_count_kernel(const RouteParams p)
+// Moves the ranks of a workgroup's choices to their rows.
+template <int L>
+__global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteParams p)
 {
-    __shared__ int count;
-    if (threadIdx.x == 0) count = 0;
+    __shared__ int part[kRouteWaves], base[kRouteThreads];
+    const int t = threadIdx.x;
+    const int64_t first = (int64_t)blockIdx.x * kRowsOf<L> * p.top_k, n = min((int64_t)kRowsOf<L> * p.top_k, (int64_t)p.tokens * p.top_k - first);
+    const int all = t < p.num ? p.counts[(int64_t)p.chunks * p.num + t] : 0, mine = t < p.num ? p.counts[(int64_t)blockIdx.x * p.num + t] : 0;
+    const int begin = before_thread(all, part);
+    base[t] = begin + mine;
+    if (blockIdx.x == 0) {
+        if (t < p.num) p.offsets[t] = begin;
+        if (t == p.num - 1) p.offsets[p.num] = begin + all;
+    }
     __syncthreads();
-    const int n = p.tokens * p.top_k;
-    int mine = 0;
-    for (int i = threadIdx.x; i < n; i += 256) mine += p.experts[i] == (int)blockIdx.x;
-    atomicAdd(&count, mine);
-    __syncthreads();
-    if (threadIdx.x == 0) p.counts[blockIdx.x] = count;
+    for (int i = t; i < n; i += kRouteThreads) {
+        const int e = p.experts[first + i];
+        if (e >= 0) p.rows[first + i] += base[e];
+    }
 }
 
-__global__ __launch_bounds__(64) void route_order_kernel(const RouteParams p)
+__global__ __launch_bounds__(kRouteThreads) void route_nothing_kernel(int32_t *offsets, int num)
 {
-    const int e = blockIdx.x, lane = threadIdx.x, n = p.tokens * p.top_k;
-    int at = 0;
-    for (int i = 0; i < e; ++i) at += p.counts[i];
-    if (lane == 0) {
-        p.offsets[e] = at;
-        if (e == p.num - 1) p.offsets[e + 1] = at + p.counts[e];
-    }
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const bool is = i0 + lane < n && p.experts[i0 + lane] == e;
-        const uint64_t all = __ballot(is);
-        if (is) p.rows[i0 + lane] = at + __popcll(all & ((1ull << lane) - 1));
-        at += __popcll(all);
-    }
+    for (int i = threadIdx.x; i <= num; i += kRouteThreads) offsets[i] = 0;
 }
+
+// ---- the gradient ------------------------------------------------------------------------------------------------------------------
 
 struct RouteGradParams {
     const char *logits;
@@ -170,63 +428,179 @@ struct RouteGradParams {
     float scale;
 };
 
-template <int ES>
-__global__ __launch_bounds__(64) void route_grad_kernel(const RouteGradParams p)
+constexpr int kGradThreads = 256;
+
+// Bound by memory: it writes the row, and reads it where every expert's score has a part (softmax without renormalisation).  A lane has a choice, and
+// then V experts; the choices' gradients come to the experts' lanes through LDS.
+template <int ES, int L, int V>
+__global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGradParams p)
 {
-    constexpr int VPL = kMax / 64;
-    const int lane = threadIdx.x;
-    for (int64_t t = blockIdx.x; t < p.tokens; t += gridDim.x) {
-    __syncthreads();
-    const char *row = p.logits + t * p.ld;
-    double s[VPL], rest[VPL], ds[VPL], top = -INFINITY, sum = 0;
+    constexpr int ROWS = kGradThreads / L;
+    __shared__ float to[ROWS][L * V];
+    __shared__ int chosen[ROWS][ALT_ROUTE_MAX_TOP_K];
+    __shared__ float parts[ROWS][ALT_ROUTE_MAX_TOP_K];
+    const int sub = threadIdx.x % L, row_in = threadIdx.x / L, e0 = sub * V;
+    for (int64_t first = (int64_t)blockIdx.x * ROWS; first < p.tokens; first += (int64_t)gridDim.x * ROWS) {
+        const int64_t token = first + row_in;
+        const bool here = token < p.tokens;
+        const char *row = p.logits + token * p.ld;
+        float l[V], top = -INFINITY, sum = 1.f;
+        const bool whole = p.softmax && !p.renorm;
+        if (whole) {
+            if (here) {
+                load_logits<ES, V>(row, e0, p.num, l);
+            } else {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        const int e = lane + 64 * i;
-        s[i] = e < p.num ? (double)element<ES>(row + e * ES) : -INFINITY;
-        top = fmax(top, s[i]);
-        ds[i] = 0;
-    }
-    top = wave_max(top);
+                for (int i = 0; i < V; ++i) l[i] = -INFINITY;
+            }
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        rest[i] = 1.0 / (1.0 + exp(s[i]));
-        s[i] = s[i] == -INFINITY ? 0.0 : p.softmax ? exp(s[i] - top) : 1.0 / (1.0 + exp(-s[i]));
-        sum += s[i];
-    }
-    sum = wave_sum(sum);
+            for (int i = 0; i < V; ++i) top = l[i] > top ? l[i] : top;
+            top = row_max<L>(top);
+            sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i)
-        if (p.softmax && sum > 0) s[i] /= sum;
-    bool any = false;
-    double total = 0, along = 0;
-    auto each = [&](auto f) {
-        for (int j = 0; j < p.top_k; ++j) {
-            const int e = p.experts[t * p.top_k + j];
-            if (e < 0 || e >= p.num) continue;
-            double v = 0;
-#pragma unroll
-            for (int i = 0; i < VPL; ++i)
-                if (e == lane + 64 * i) v = s[i];
-            f(e, __shfl(v, e % 64), (double)p.dweights[t * p.top_k + j]);
+            for (int i = 0; i < V; ++i) {
+                l[i] = l[i] == -INFINITY ? 0.f : expf(l[i] - top);
+                sum += l[i];
+            }
+            sum = row_sum<L>(sum);
+            sum = sum == 0.f ? 1.f : sum;
         }
-    };
-    each([&](int, double v, double dw) { total += v; along += dw * v; any = true; });
-    if (!(total > 0)) total = 1;
-    double inner = 0;
-    each([&](int e, double v, double dw) {
-        const double d = p.renorm ? p.scale / total * (dw - along / total) : p.scale * dw;
-        inner += d * v;
+        // a choice to a lane: its score (or share of the chosen scores) and dlogits = share * (dweight - mean) * rest
+        int e = -1;
+        float v = -INFINITY, dw = 0.f;
+        if (here && sub < p.top_k) {
+            e = p.experts[token * p.top_k + sub];
+            if (e < 0 || e >= p.num) e = -1;
+            if (e >= 0) {
+                v = element<ES>(row + (int64_t)e * ES);
+                dw = p.dweights[token * p.top_k + sub] * p.scale;
+            }
+        }
+        const bool is = e >= 0 && v != -INFINITY;
+        float s, rest = 1.f, mean = 0.f;
+        if (p.softmax) {
+            if (p.renorm) top = row_max<L>(v);
+            s = is ? expf(v - top) : 0.f;
+            if (p.renorm) {
+                sum = row_sum<L>(s);
+                sum = sum == 0.f ? 1.f : sum;
+            }
+            s /= sum;
+        } else {
+            s = is ? sigmoid_of(v) : 0.f;
+            rest = is ? sigmoid_of(-v) : 0.f;
+            if (p.renorm) {
+                const float all = row_sum<L>(s);
+                s /= all > 0.f ? all : 1.f;
+            }
+        }
+        if (p.renorm || p.softmax) mean = row_sum<L>(s * dw);
+        const bool any = row_max<L>(e) >= 0;
+        // (softmax without renormalisation: every expert has - score * mean, the chosen ones score * dweight beside it)
+        const float mine = whole ? s * dw : s * (dw - mean) * rest;
+        if (sub < p.top_k) {
+            chosen[row_in][sub] = e;
+            parts[row_in][sub] = e >= 0 ? mine : 0.f;
+        }
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (e == lane + 64 * i) ds[i] += d;
+        for (int i = 0; i < V; ++i) to[row_in][e0 + i] = 0.f;
+        wave_sync();
+        if (e >= 0) {
+            float total = 0.f;                             // (an expert that stands twice: every one of its choices stores both parts)
+            for (int j = 0; j < p.top_k; ++j) total += chosen[row_in][j] == e ? parts[row_in][j] : 0.f;
+            to[row_in][e] = total;
+        }
+        wave_sync();
+        if (here) {
+            float out[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                out[i] = to[row_in][e0 + i];
+                if (whole) out[i] -= l[i] / sum * mean;
+                if (!any) out[i] = 0.f;
+            }
+            char *at = p.dlogits + token * p.ld + (int64_t)e0 * ES;
+            if (e0 + V <= p.num && V * ES >= 16) {
+                if constexpr (V * ES >= 16) {
+#pragma unroll
+                    for (int i = 0; i < V * ES / 16; ++i) {
+                        float f[16 / ES];
+#pragma unroll
+                        for (int q = 0; q < 16 / ES; ++q) f[q] = out[i * (16 / ES) + q];
+                        const w4_t c = chunk16_of<ES>(f);
+                        __builtin_memcpy(at + i * 16, &c, 16);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (e0 + i < p.num) store_element<ES>(at + i * ES, out[i]);
+            }
+        }
+        wave_sync();
+    }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------------------------
+
+// Lanes of a row and experts of a lane: 16 lanes as long as they hold the experts and the choices.
+struct Shape { int l, v; };
+Shape shape_of(const alt_route_desc_t &d)
+{
+    if (d.top_k <= 16 && d.experts <= 256) return {16, d.experts <= 64 ? 4 : d.experts <= 128 ? 8 : 16};
+    return {64, d.experts <= 256 ? 4 : d.experts <= 512 ? 8 : 16};
+}
+
+template <typename F>
+void by_shape(const alt_route_desc_t &d, F f)
+{
+    using std::integral_constant;
+    const Shape s = shape_of(d);
+    if (s.l == 16) {
+        if (s.v == 4) f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+        else if (s.v == 8) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+        else f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    } else {
+        if (s.v == 4) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+        else if (s.v == 8) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+        else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+    }
+}
+
+int64_t chunks_of(const alt_route_desc_t &d) { return (d.tokens + kRouteThreads / shape_of(d).l - 1) / (kRouteThreads / shape_of(d).l); }
+
+template <int ES>
+hipError_t route_run(const alt_route_desc_t &d, const RouteParams &p, hipStream_t st)
+{
+    hipError_t e = hipSuccess;
+    by_shape(d, [&](auto l, auto v) {
+        constexpr int L = decltype(l)::value, V = decltype(v)::value;
+        const size_t lds = route_lds(L, V, p.num, p.top_groups < p.groups);
+        if (lds > 64 * 1024) {
+            static bool attr_set = false;
+            if (!attr_set) {
+                e = hipFuncSetAttribute((const void *)route_kernel<ES, L, V>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 256);
+                if (e != hipSuccess) return;
+                attr_set = true;
+            }
+        }
+        hipLaunchKernelGGL((route_kernel<ES, L, V>), dim3((unsigned)p.chunks), dim3(kRouteThreads), lds, st, p);
+        if ((e = hipGetLastError()) != hipSuccess || p.chunks == 1) return;
+        hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)((p.num + 15) / 16)), dim3(kRouteThreads), 0, st, p);
+        hipLaunchKernelGGL(route_place_kernel<L>, dim3((unsigned)p.chunks), dim3(kRouteThreads), 0, st, p);
+        e = hipGetLastError();
     });
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        const int e = lane + 64 * i;
-        const double v = p.softmax ? s[i] * (ds[i] - inner) : ds[i] * s[i] * rest[i];
-        if (e < p.num) store_element<ES>(p.dlogits + t * p.ld + e * ES, any ? (float)v : 0.f);
-    }
-    }
+    return e;
+}
+
+template <int ES>
+void route_grad_run(const alt_route_desc_t &d, const RouteGradParams &p, hipStream_t st)
+{
+    by_shape(d, [&](auto l, auto v) {
+        constexpr int L = decltype(l)::value, ROWS = kGradThreads / L;
+        const int64_t blocks = ((int64_t)p.tokens + ROWS - 1) / ROWS;
+        hipLaunchKernelGGL((route_grad_kernel<ES, L, decltype(v)::value>), dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(kGradThreads), 0, st, p);
+    });
 }
 
 alt_status_t check(alt_handle_t h, const char *call, const alt_route_desc_t *d, alt_route_desc_t *out)
@@ -246,11 +620,11 @@ alt_status_t check(alt_handle_t h, const char *call, const alt_route_desc_t *d, 
     if (d->experts % d->groups) return fail(h, ALT_SHAPE_MISMATCH, "%s: %d experts make no %d groups", call, d->experts, d->groups);
     if (d->top_k > (int64_t)d->top_groups * (d->experts / d->groups)) return fail(h, ALT_SHAPE_MISMATCH, "%s: top_k is more than the experts that a token chooses from", call);
     if (d->experts > ALT_ROUTE_MAX_EXPERTS || d->top_k > ALT_ROUTE_MAX_TOP_K) return fail(h, ALT_UNSUPPORTED, "%s: more than 1024 experts or 32 choices", call);
-    if (d->tokens > (1 << 30) / d->top_k || out->stride > 0x7fffffff) return fail(h, ALT_UNSUPPORTED, "%s: more than 2^30 choices or a stride over 2^31", call);
+    if (d->tokens > (1 << 25) || out->stride > 0x7fffffff) return fail(h, ALT_UNSUPPORTED, "%s: more than 2^25 tokens or a stride over 2^31", call);
     return ALT_OK;
 }
 
-size_t route_workspace(const alt_route_desc_t &d) { return (size_t)d.experts * 4 + 16; }
+size_t route_workspace(const alt_route_desc_t &d) { return (size_t)(chunks_of(d) + 1) * d.experts * 4 + 16; }
 
 }  // namespace
 }  // namespace alt
@@ -281,13 +655,14 @@ extern "C" alt_status_t alt_route(alt_handle_t h, const alt_route_desc_t *desc, 
     p.softmax = d.score == ALT_SCORE_SOFTMAX;
     p.renorm = d.renormalize;
     p.scale = d.scale;
-    if (some) {
-        if (d.dtype == ALT_F32) hipLaunchKernelGGL(route_kernel<4>, dim3((unsigned)std::min<int64_t>(d.tokens, 1 << 20)), dim3(64), 0, st, p);
-        else hipLaunchKernelGGL(route_kernel<2>, dim3((unsigned)std::min<int64_t>(d.tokens, 1 << 20)), dim3(64), 0, st, p);
+    p.chunks = (int32_t)chunks_of(d);
+    p.each = make_fastdiv((uint32_t)(d.experts / d.groups));
+    if (!some) {
+        hipLaunchKernelGGL(route_nothing_kernel, dim3(1), dim3(kRouteThreads), 0, st, offsets, (int)d.experts);
+        ALT_CHECK_HIP(h, hipGetLastError());
+        return ALT_OK;
     }
-    hipLaunchKernelGGL(route_count_kernel, dim3((unsigned)d.experts), dim3(256), 0, st, p);
-    hipLaunchKernelGGL(route_order_kernel, dim3((unsigned)d.experts), dim3(64), 0, st, p);
-    ALT_CHECK_HIP(h, hipGetLastError());
+    ALT_CHECK_HIP(h, d.dtype == ALT_F32 ? route_run<4>(d, p, st) : route_run<2>(d, p, st));
     return ALT_OK;
 }
 
@@ -313,8 +688,8 @@ extern "C" alt_status_t alt_route_grad(alt_handle_t h, const alt_route_desc_t *d
     const hipStream_t st = (hipStream_t)stream;
     RouteGradParams p{(const char *)logits, experts, dweights, (char *)dlogits, d.stride * (int64_t)dtype_size(d.dtype), (int32_t)d.tokens, d.experts, d.top_k, d.score == ALT_SCORE_SOFTMAX,
                       d.renormalize, d.scale};
-    if (d.dtype == ALT_F32) hipLaunchKernelGGL(route_grad_kernel<4>, dim3((unsigned)std::min<int64_t>(d.tokens, 1 << 20)), dim3(64), 0, st, p);
-    else hipLaunchKernelGGL(route_grad_kernel<2>, dim3((unsigned)std::min<int64_t>(d.tokens, 1 << 20)), dim3(64), 0, st, p);
+    if (d.dtype == ALT_F32) route_grad_run<4>(d, p, st);
+    else route_grad_run<2>(d, p, st);
     ALT_CHECK_HIP(h, hipGetLastError());
     return ALT_OK;
 }
