@@ -22,7 +22,7 @@ struct RouteParams {
     int32_t *rows, *offsets;
     int32_t *counts;                       // [workgroups][num]: choices of each expert; then [num]: of all workgroups (route_scan_kernel)
     int64_t ld;                            // bytes between rows of logits
-    int32_t tokens, num, top_k, groups, top_groups, group_best, softmax, renorm, chunks;
+    int32_t tokens, num, top_k, groups, top_groups, group_best, softmax, renorm, chunks, size;     // size: bytes of a logit
     FastDiv each;                          // experts of a group
     float scale;
 };
@@ -103,132 +103,201 @@ __device__ __forceinline__ F sigmoid_of(F v)
     return (v < 0 ? e : (F)1) / (1 + e);
 }
 
+__device__ __forceinline__ float element_at(const char *row, int size, int e) { return size == 4 ? element<4>(row + (int64_t)e * 4) : element<2>(row + (int64_t)e * 2); }
+
 // ---- the choice --------------------------------------------------------------------------------------------------------------------
 
 // What a row's lanes know of it: the largest logit, the sum of exp(logit - top), and whether it is lost to a NaN.
 struct RowStats { float top, sum; bool lost; };
 
-// The choices of a row by numbers of type F: lane j of the row gets the j-th expert in `mine`, or -1.  True: they are those of exact arithmetic.
-//
-// Logits that are compared themselves are exact.  Scores are not, and two choices nearer than what rounding can have moved them leave it open which is
-// the larger; the caller then asks again in 64 bits.  A sigmoid in fp32 is off by four roundings, two of them by 2^-21 of the row's largest score S; a
-// softmax by the roundings of its argument, sum and quotient, 2^-18 S; adding the bias rounds by 2^-24 of the choice.  Twice that is `near`.
-template <typename F, int L, int V>
-__device__ __forceinline__ bool choose(const RouteParams &p, const float (&l)[V], const RowStats &st, int sub, char *lds, int &mine)
+// Score and bias of an expert, by numbers of type F; -inf for one that is out.
+template <typename F>
+__device__ __forceinline__ F worth_of(const RouteParams &p, float l, int e, const RowStats &st, F sum)
 {
-    constexpr bool FAST = sizeof(F) == 4;
-    const F none = -INFINITY;
-    const bool scored = p.bias || p.top_groups < p.groups;
-    const int e0 = sub * V;
-    F key[V], most = 0;
-    bool sure = true;
-    if (scored) {
-        F sum = 1;
-        if (p.softmax) {
-            if constexpr (FAST) {
-                sum = st.sum;
-            } else {
-                sum = 0;
+    const F s = p.softmax ? exp_of((F)l - (F)st.top) / sum : sigmoid_of((F)l);
+    const F w = p.bias ? s + (F)p.bias[e] : s;
+    return l == -INFINITY || w != w || st.lost ? (F)-INFINITY : w;
+}
+
+template <int L, int V>
+__device__ __forceinline__ double exact_sum(const RouteParams &p, const float (&l)[V], const RowStats &st)
+{
+    double sum = 0;
+    if (!p.softmax) return sum;
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0 : exp_of((F)l[i] - (F)st.top);
-                sum = row_sum<L>(sum);
+    for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)st.top);
+    return row_sum<L>(sum);
+}
+
+// Which of a lane's V experts are of the row's worthiest groups, as bits.  In the row's LDS: the worths of the experts (or of each lane's two best, where a
+// lane's experts are of one group), in their place those of the groups, in the place of those which groups are kept.  `apart`: by how much the least
+// worthy group that is kept is worth more than the worthiest that is not.
+template <typename F, int L, int V, typename W>
+__device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, F *worth, W worth_at, F &apart)
+{
+    const F none = -INFINITY;
+    const int each = (int)p.each.d;
+    const bool lanes = each % V == 0;
+    const int per = lanes ? each / V * 2 : each;           // numbers of a group
+    auto better_of = [](F v, F &one, F &two) {
+        two = v > one ? one : v > two ? v : two;
+        one = v > one ? v : one;
+    };
+    auto at = [](int i) { return i + (i >> 5); };          // (groups of 32 numbers begin at different banks)
+    F one = none, two = none;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const F v = worth_at(i);
+        if (lanes) better_of(v, one, two);
+        else worth[at(sub * V + i)] = v;
+    }
+    if (lanes) {
+        worth[at(sub * 2)] = one;
+        worth[at(sub * 2 + 1)] = two;
+    }
+    wave_sync();
+    for (int g = sub; g < p.groups; g += L) {
+        one = two = none;
+        for (int i = g * per; i < (g + 1) * per; ++i) better_of(worth[at(i)], one, two);
+        worth[at(g * per)] = p.group_best == 2 && two > none ? one + two : one;        // (these numbers are this lane's alone)
+    }
+    wave_sync();
+    uint32_t mine = 0;
+    F least = INFINITY, most = none;
+    for (int g = sub, i = 0; g < p.groups; g += L, ++i) {
+        const F v = worth[at(g * per)];
+        int better = 0;
+        for (int o = 0; o < p.groups; ++o) {
+            const F w = worth[at(o * per)];
+            better += w > v || (w == v && o < g);
+        }
+        if (better < p.top_groups) {
+            mine |= 1u << i;
+            if (v > none) least = v < least ? v : least;
+        } else {
+            most = v > most ? v : most;
+        }
+    }
+    wave_sync();
+    for (int g = sub, i = 0; g < p.groups; g += L, ++i) worth[at(g * per)] = mine >> i & 1 ? (F)1 : (F)0;
+    wave_sync();
+    uint32_t kept = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = sub * V + i;
+        if (e < p.num && worth[at((int)fast_div((uint32_t)e, p.each) * per)] != 0) kept |= 1u << i;
+    }
+    wave_sync();
+    least = row_min<L>(least);
+    most = row_max<L>(most);
+    apart = most > none ? least - most : (F)INFINITY;
+    return kept;
+}
+
+// The choices of a row: lane j of it gets the j-th expert, or -1.
+//
+// Logits that are compared themselves are exact.  Scores in fp32 are not, and where two are nearer than what rounding can have moved them (`near`) they are
+// computed again in 64 bits.  A sigmoid is off by 2^-22 of itself, a softmax by the roundings of its argument, sum and quotient, 2^-19 of the largest score
+// of the row, which is 1 / sum; adding the bias rounds by 2^-24 of the choice; `near`, and what is added to it, is twice that of two of them.  In 64 bits go: the worths of the
+// groups, where the last that is kept and the first that is not are near; the choices of the few experts, one to a lane, that are chosen or near the
+// last chosen one; all of them, where those are more than a row has lanes.
+template <int L, int V>
+__device__ __forceinline__ int choose(const RouteParams &p, const char *row, const float (&l)[V], const RowStats &st, int sub, char *lds)
+{
+    const float none = -INFINITY;
+    const bool grouped = p.top_groups < p.groups, scored = p.bias || grouped;
+    const int e0 = sub * V;
+    float key[V], near = 0.f;
+    uint32_t kept = ~0u;
+    if (scored) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = worth_of<float>(p, l[i], min(e0 + i, p.num - 1), st, st.sum);
+        near = (p.softmax ? 0x1p-17f / st.sum : 0x1p-20f) + 0x1p-120f;
+        if (grouped) {
+            float apart, size = 0.f;
+            kept = kept_experts<float, L, V>(p, sub, (float *)lds, [&](int i) { return key[i]; }, apart);
+#pragma unroll
+            for (int i = 0; i < V; ++i) size = fmaxf(size, key[i] == none ? 0.f : __builtin_fabsf(key[i]));
+            size = row_max<L>(size);
+            if (__ballot(!(apart > 4.f * near + size * 0x1p-20f))) {
+                const double sum = exact_sum<L, V>(p, l, st);
+                double exactly;
+                kept = kept_experts<double, L, V>(p, sub, (double *)lds, [&](int i) { return worth_of<double>(p, l[i], min(e0 + i, p.num - 1), st, sum); }, exactly);
             }
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const F s = p.softmax ? exp_of((F)l[i] - (F)st.top) / sum : sigmoid_of((F)l[i]);
-            F w = p.bias && e0 + i < p.num ? s + (F)p.bias[e0 + i] : s;
-            if (l[i] == -INFINITY || w != w || st.lost) w = none;
-            if (FAST && w != none) most = s > most ? s : most;
-            key[i] = w;
-        }
-        if constexpr (FAST) most = row_max<L>(most);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = st.lost ? none : (F)l[i];
     }
-    const F near = most * (F)(p.softmax ? 0x1p-17 : 0x1p-20) + (F)0x1p-120;
-    if (p.top_groups < p.groups) {
-        // one after another in the row's LDS: the worths of its experts, of its groups, and which groups are kept; a lane has the groups sub, sub + L, ...
-        F *worth = (F *)lds, group[V];
-        const int each = (int)p.each.d;
 #pragma unroll
-        for (int i = 0; i < V; ++i) worth[e0 + i] = key[i];
-        wave_sync();
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = sub + i * L;
-            F one = none, two = none;
-            if (g < p.groups)
-                for (int e = g * each; e < (g + 1) * each; ++e) {
-                    const F v = worth[e];
-                    two = v > one ? one : v > two ? v : two;
-                    one = v > one ? v : one;
-                }
-            group[i] = p.group_best == 2 && two > none ? one + two : one;
-        }
-        wave_sync();
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (sub + i * L < p.groups) worth[sub + i * L] = group[i];
-        wave_sync();
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = sub + i * L;
-            const F v = group[i];
-            int better = 0;
-            if (g < p.groups)
-                for (int o = 0; o < p.groups; ++o) {
-                    const F w = worth[o];
-                    better += w > v || (w == v && o < g);
-                    if constexpr (FAST) {
-                        const F size = v < 0 ? -v : v, apart = w > v ? w - v : v - w;
-                        if (o != g && v > none && w > none && !(apart > 2 * near + size * (F)0x1p-21)) sure = false;
-                    }
-                }
-            group[i] = better < p.top_groups ? (F)1 : (F)0;
-        }
-        wave_sync();
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (sub + i * L < p.groups) worth[sub + i * L] = group[i];
-        wave_sync();
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const bool kept = e0 + i < p.num && worth[fast_div((uint32_t)(e0 + i), p.each)] != 0;
-            if (!kept) key[i] = none;
-            else if (!p.bias) key[i] = key[i] == none ? none : (F)l[i];
-        }
+    for (int i = 0; i < V; ++i) {
+        const bool is = (kept >> i & 1) && !st.lost && (!scored || key[i] != none);
+        key[i] = !is ? none : p.bias ? key[i] : l[i];
     }
-    mine = -1;
-    F last = INFINITY;
-    const int picks = FAST && p.bias ? p.top_k + 1 : p.top_k;              // (one more, to see how near it is)
-    for (int j = 0; j < picks; ++j) {
-        F best = none;
+    int mine = -1, picks = 0;
+    float last = INFINITY, end = none;                     // the pick before, the last chosen one
+    bool sure = true, more = false;                        // more: what is left is near the last chosen one
+    for (; picks <= L; ++picks) {
+        if (!p.bias && picks == p.top_k) break;
+        float best = none;
         int at = 0x7fffffff;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const bool more = key[i] > best;
-            best = more ? key[i] : best;
-            at = more ? e0 + i : at;
+            const bool is = key[i] > best;
+            best = is ? key[i] : best;
+            at = is ? e0 + i : at;
         }
-        const F top = row_max<L>(best);
+        const float top = row_max<L>(best);
         const bool is = top > none;
-        at = row_min<L>(best == top && is ? at : 0x7fffffff);
-        if constexpr (FAST) {
-            if (p.bias && is && j > 0) {
-                const F size = last < 0 ? -last : last;
-                if (!(last - top > near + size * (F)0x1p-22)) sure = false;
-            }
+        if (p.bias) {
+            if (is && picks > 0 && picks <= p.top_k && !(last - top > near + __builtin_fabsf(last) * 0x1p-22f)) sure = false;
+            more = is && !(end - top > near + __builtin_fabsf(end) * 0x1p-22f);
         }
         last = top;
-        if (sub == j && j < p.top_k && is) mine = at;
-        if (!__ballot(is)) break;
+        if (picks == p.top_k - 1) end = top;
+        if (picks >= p.top_k && !__ballot(more)) break;
+        if (picks == L || !__ballot(is)) break;
+        at = row_min<L>(best == top && is ? at : 0x7fffffff);
+        if (sub == picks && is) mine = at;
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (e0 + i == at) key[i] = none;
     }
-    return sure;
+    if (p.bias && __ballot(!sure)) {
+        const double sum = exact_sum<L, V>(p, l, st), out = -INFINITY;
+        if (picks < L || !__ballot(more)) {
+            // the candidates' places
+            const double v = mine >= 0 ? worth_of<double>(p, element_at(row, p.size, mine), mine, st, sum) : out;
+            int place = 0;
+            for (int o = 0; o < picks; ++o) {
+                const double w = __shfl(v, o, L);
+                const int e = __shfl(mine, o, L);
+                place += w > v || (w == v && e < mine);
+            }
+            const int from = mine >= 0 ? place : -1, candidate = mine;
+            mine = -1;
+            for (int o = 0; o < picks; ++o) {
+                const int to = __shfl(from, o, L), e = __shfl(candidate, o, L);
+                if (to == sub) mine = e;
+            }
+        } else {
+            // everything, in the row's LDS
+            double *worth = (double *)lds;
+#pragma unroll
+            for (int i = 0; i < V; ++i) worth[i * L + sub] = e0 + i < p.num && (kept >> i & 1) ? worth_of<double>(p, l[i], e0 + i, st, sum) : out;
+            mine = -1;
+            for (int j = 0; j < p.top_k; ++j) {
+                double best = out;
+                int at = 0x7fffffff, slot = 0;
+                for (int i = 0; i < V; ++i) {
+                    const double v = worth[i * L + sub];
+                    if (v > best) { best = v; at = e0 + i; slot = i; }
+                }
+                const double top = row_max<L>(best);
+                const int first = row_min<L>(best == top && top > out ? at : 0x7fffffff);
+                if (sub == j && top > out) mine = first;
+                if (at == first) worth[slot * L + sub] = out;              // (a lane without any: at = first = none, and its first number is -inf already)
+            }
+        }
+    }
+    return sub < p.top_k ? mine : -1;
 }
 
 // Sum over the lanes up to and with this one.
@@ -258,9 +327,10 @@ __device__ __forceinline__ int before_thread(int v, int (&part)[kRouteWaves])
 // Bytes of LDS: the workgroup's choices and a row of counts for each wave, over the rows' group worths.
 __host__ __device__ constexpr int route_slots(int L) { return L == 16 ? 64 * 16 : 16 * ALT_ROUTE_MAX_TOP_K; }
 template <int L> constexpr int kRowsOf = kRouteThreads / L;
-inline size_t route_lds(int L, int V, int num, bool grouped)
+__host__ __device__ constexpr int route_row_bytes(int experts) { return (experts + experts / 32) * 8; }
+inline size_t route_lds(int L, int V, int num, bool scored)
 {
-    const size_t rank = (size_t)route_slots(L) * 2 + (size_t)kRouteWaves * num * 2, worth = grouped ? (size_t)kRouteThreads * V * 8 : 0;
+    const size_t rank = (size_t)route_slots(L) * 2 + (size_t)kRouteWaves * num * 2, worth = scored ? (size_t)(kRouteThreads / L) * route_row_bytes(L * V) : 0;
     return (std::max(rank, worth) + 15) / 16 * 16;
 }
 
@@ -298,9 +368,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteParams 
         for (int i = 0; i < V; ++i) st.sum += l[i] == -INFINITY ? 0.f : expf(l[i] - st.top);
         st.sum = row_sum<L>(st.sum);
     }
-    int mine;
-    char *lds = route_smem + (size_t)row_in * (L * V * 8);
-    if (__ballot(!choose<float, L, V>(p, l, st, sub, lds, mine))) choose<double, L, V>(p, l, st, sub, lds, mine);
+    const int mine = choose<L, V>(p, p.logits + (here ? token : 0) * p.ld, l, st, sub, route_smem + (size_t)row_in * route_row_bytes(L * V));
     // weights, a choice to a lane
     if (here) {
         const bool is = mine >= 0;
@@ -575,7 +643,7 @@ hipError_t route_run(const alt_route_desc_t &d, const RouteParams &p, hipStream_
     hipError_t e = hipSuccess;
     by_shape(d, [&](auto l, auto v) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
-        const size_t lds = route_lds(L, V, p.num, p.top_groups < p.groups);
+        const size_t lds = route_lds(L, V, p.num, p.bias || p.top_groups < p.groups);
         if (lds > 64 * 1024) {
             static bool attr_set = false;
             if (!attr_set) {
@@ -656,6 +724,7 @@ extern "C" alt_status_t alt_route(alt_handle_t h, const alt_route_desc_t *desc, 
     p.renorm = d.renormalize;
     p.scale = d.scale;
     p.chunks = (int32_t)chunks_of(d);
+    p.size = (int32_t)dtype_size(d.dtype);
     p.each = make_fastdiv((uint32_t)(d.experts / d.groups));
     if (!some) {
         hipLaunchKernelGGL(route_nothing_kernel, dim3(1), dim3(kRouteThreads), 0, st, offsets, (int)d.experts);
