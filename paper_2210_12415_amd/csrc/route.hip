@@ -56,8 +56,15 @@ __device__ __forceinline__ T over_row(T v, F f)
     }
     return v;
 }
-template <int L, typename T> __device__ __forceinline__ T row_max(T v) { return over_row<L>(v, [](T a, T b) { return a > b ? a : b; }); }
-template <int L, typename T> __device__ __forceinline__ T row_min(T v) { return over_row<L>(v, [](T a, T b) { return a < b ? a : b; }); }
+// (of numbers: no NaN comes here)
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return __builtin_fmax(a, b); }
+__device__ __forceinline__ int larger(int a, int b) { return max(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return __builtin_fminf(a, b); }
+__device__ __forceinline__ double smaller(double a, double b) { return __builtin_fmin(a, b); }
+__device__ __forceinline__ int smaller(int a, int b) { return min(a, b); }
+template <int L, typename T> __device__ __forceinline__ T row_max(T v) { return over_row<L>(v, [](T a, T b) { return larger(a, b); }); }
+template <int L, typename T> __device__ __forceinline__ T row_min(T v) { return over_row<L>(v, [](T a, T b) { return smaller(a, b); }); }
 template <int L, typename T> __device__ __forceinline__ T row_sum(T v) { return over_row<L>(v, [](T a, T b) { return a + b; }); }
 
 // This lane's V logits, of the experts from e0 on; -inf behind the last.
@@ -110,12 +117,19 @@ __device__ __forceinline__ float element_at(const char *row, int size, int e) { 
 // What a row's lanes know of it: the largest logit, the sum of exp(logit - top), and whether it is lost to a NaN.
 struct RowStats { float top, sum; bool lost; };
 
-// Score and bias of an expert, by numbers of type F; -inf for one that is out.
+// Score and bias of an expert, by numbers of type F; -inf for one that is out.  `sum`: of the exponentials, in 32 bits its reciprocal.
 template <typename F>
-__device__ __forceinline__ F worth_of(const RouteParams &p, float l, int e, const RowStats &st, F sum)
+__device__ __forceinline__ F worth_of(const RouteParams &p, float l, float bias, const RowStats &st, F sum)
 {
-    const F s = p.softmax ? exp_of((F)l - (F)st.top) / sum : sigmoid_of((F)l);
-    const F w = p.bias ? s + (F)p.bias[e] : s;
+    F s;
+    if constexpr (sizeof(F) == 4) {
+        // (the hardware's base-2 exponential and reciprocal, each off by 2^-23 of itself: what is near is computed again anyway)
+        const float x = p.softmax ? l - st.top : -__builtin_fabsf(l), e = __builtin_amdgcn_exp2f(x * 0x1.715476p+0f);
+        s = p.softmax ? e * sum : (l < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+    } else {
+        s = p.softmax ? exp_of((F)l - (F)st.top) / sum : sigmoid_of((F)l);
+    }
+    const F w = s + (F)bias;
     return l == -INFINITY || w != w || st.lost ? (F)-INFINITY : w;
 }
 
@@ -197,7 +211,8 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
 // The choices of a row: lane j of it gets the j-th expert, or -1.
 //
 // Logits that are compared themselves are exact.  Scores in fp32 are not, and where two are nearer than what rounding can have moved them (`near`) they are
-// computed again in 64 bits.  A sigmoid is off by 2^-22 of itself, a softmax by the roundings of its argument, sum and quotient, 2^-19 of the largest score
+// computed again in 64 bits.  A sigmoid is off by 2^-22 (its exponential by (1.5 |x| + 2) 2^-24 of
+// itself, which counts s (1 - s), the rest by 1.5 2^-23 s), a softmax by the roundings of its argument, sum and quotient, 2^-19 of the largest score
 // of the row, which is 1 / sum; adding the bias rounds by 2^-24 of the choice; `near`, and what is added to it, is twice that of two of them.  In 64 bits go: the worths of the
 // groups, where the last that is kept and the first that is not are near; the choices of the few experts, one to a lane, that are chosen or near the
 // last chosen one; all of them, where those are more than a row has lanes.
@@ -210,9 +225,14 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
     float key[V], near = 0.f;
     uint32_t kept = ~0u;
     if (scored) {
+        const float part = 1.f / st.sum;
+        float bias[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = worth_of<float>(p, l[i], min(e0 + i, p.num - 1), st, st.sum);
-        near = (p.softmax ? 0x1p-17f / st.sum : 0x1p-20f) + 0x1p-120f;
+        for (int i = 0; i < V; ++i) bias[i] = 0.f;
+        if (p.bias) load_logits<4, V>((const char *)p.bias, e0, p.num, bias);
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = worth_of<float>(p, l[i], bias[i], st, part);
+        near = (p.softmax ? 0x1.8p-17f * part : 0x1p-20f) + 0x1p-120f;
         if (grouped) {
             float apart, size = 0.f;
             kept = kept_experts<float, L, V>(p, sub, (float *)lds, [&](int i) { return key[i]; }, apart);
@@ -222,7 +242,7 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
             if (__ballot(!(apart > 4.f * near + size * 0x1p-20f))) {
                 const double sum = exact_sum<L, V>(p, l, st);
                 double exactly;
-                kept = kept_experts<double, L, V>(p, sub, (double *)lds, [&](int i) { return worth_of<double>(p, l[i], min(e0 + i, p.num - 1), st, sum); }, exactly);
+                kept = kept_experts<double, L, V>(p, sub, (double *)lds, [&](int i) { return worth_of<double>(p, l[i], p.bias ? p.bias[min(e0 + i, p.num - 1)] : 0.f, st, sum); }, exactly);
             }
         }
     }
@@ -236,14 +256,9 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
     bool sure = true, more = false;                        // more: what is left is near the last chosen one
     for (; picks <= L; ++picks) {
         if (!p.bias && picks == p.top_k) break;
-        float best = none;
-        int at = 0x7fffffff;
+        float best = key[0];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const bool is = key[i] > best;
-            best = is ? key[i] : best;
-            at = is ? e0 + i : at;
-        }
+        for (int i = 1; i < V; ++i) best = larger(best, key[i]);
         const float top = row_max<L>(best);
         const bool is = top > none;
         if (p.bias) {
@@ -254,7 +269,10 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
         if (picks == p.top_k - 1) end = top;
         if (picks >= p.top_k && !__ballot(more)) break;
         if (picks == L || !__ballot(is)) break;
-        at = row_min<L>(best == top && is ? at : 0x7fffffff);
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i) at = key[i] == top ? e0 + i : at;
+        at = row_min<L>(is ? at : 0x7fffffff);
         if (sub == picks && is) mine = at;
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -264,7 +282,7 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
         const double sum = exact_sum<L, V>(p, l, st), out = -INFINITY;
         if (picks < L || !__ballot(more)) {
             // the candidates' places
-            const double v = mine >= 0 ? worth_of<double>(p, element_at(row, p.size, mine), mine, st, sum) : out;
+            const double v = mine >= 0 ? worth_of<double>(p, element_at(row, p.size, mine), p.bias[mine], st, sum) : out;
             int place = 0;
             for (int o = 0; o < picks; ++o) {
                 const double w = __shfl(v, o, L);
@@ -281,7 +299,7 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
             // everything, in the row's LDS
             double *worth = (double *)lds;
 #pragma unroll
-            for (int i = 0; i < V; ++i) worth[i * L + sub] = e0 + i < p.num && (kept >> i & 1) ? worth_of<double>(p, l[i], e0 + i, st, sum) : out;
+            for (int i = 0; i < V; ++i) worth[i * L + sub] = e0 + i < p.num && (kept >> i & 1) ? worth_of<double>(p, l[i], p.bias[e0 + i], st, sum) : out;
             mine = -1;
             for (int j = 0; j < p.top_k; ++j) {
                 double best = out;
@@ -446,8 +464,12 @@ __global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(const RoutePa
     }
     part[run][x] = sum;
     __syncthreads();
-    int before = 0;
-    for (int r = 0; r < run; ++r) before += part[r][x];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;            // a wave for each of the 16 experts
+    const int upto = wave_scan(part[lane][wave]);
+    __syncthreads();
+    part[lane][wave] = upto;
+    __syncthreads();
+    int before = part[run][x] - sum;
     if (e >= p.num) return;
     if (run == 63) p.counts[(int64_t)p.chunks * p.num + e] = before + sum;
     for (int c = lo; c < hi; ++c) {
