@@ -773,14 +773,11 @@ struct GrpPair {
     }
 };
 
-template <typename T, int NT, int NW, int BATCH, bool DW>
-__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParams p)
+// This wave's sums of the tile `g`; `between` runs while its first loads are on their way.
+template <typename T, int NT, int NW, int BATCH, bool DW, typename F>
+__device__ __forceinline__ void grp_few_sums(const GroupedParams &p, const GrpProblem &g, int lane, int wave, typename GrpFew<T>::acc_t (&acc)[NT][GrpTraits<T>::SUMS], F between)
 {
     constexpr int ES = GrpTraits<T>::ES, UNIT = 128;
-    __shared__ u32x4_t part[NW * NT * 64];
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    GrpProblem g;
-    if (!grp_problem<T, kForward, 16, 16 * NT>(p, lane, g)) return;
     const int rows_left = g.row_end - g.row0, cols_left = p.cols - g.col0;
 
     // (rows and columns outside the tile's repeat its last one: their sums are never stored)
@@ -790,7 +787,6 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
     for (int j = 0; j < NT; ++j) bp[j] = g.b0 + (int64_t)min(j * 16 + lane % 16, cols_left - 1) * p.ldb + at;
 
     constexpr int SUMS = GrpTraits<T>::SUMS;
-    typename GrpFew<T>::acc_t acc[NT][SUMS];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -823,12 +819,15 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
     if (wave < units) {
         Batch x, y;
         load(x, wave);
+        between();
         for (int u = wave; u < units; u += 2 * STEP) {
             if (u + STEP < units) load(y, u + STEP);
             mma(x, u);
             if (u + 2 * STEP < units) load(x, u + 2 * STEP);
             if (u + STEP < units) mma(y, u + STEP);
         }
+    } else {
+        between();
     }
     // what the reduction ends with: less than a unit
     if (bytes % UNIT && wave == units % NW) {
@@ -840,56 +839,89 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
             for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[j], grp_load_chunk<ES>(bp[j] + k, count), a);
         }
     }
-    // the adapters' part (as grp_adapt has it), one adapter to a wave, then the next
-    if constexpr (GrpTraits<T>::ADAPT) {
-        constexpr int PARTS = ES == 2 ? 2 : 1;
-        const int quarter = lane / 16 * 16, row_in = g.row0 + min(lane % 16, rows_left - 1), id = p.adapter[row_in];
-        const char *inner = p.inner + (int64_t)row_in * (PARTS * p.inner_bytes);
-        uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
-        for (int n = 0; left; ++n) {
-            const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-            const bool mine = id == one;
-            left &= ~__ballot(mine);
-            if (n % NW != wave) continue;
-            typename GrpFew<T>::acc_t mid[NT][SUMS];
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int s = 0; s < SUMS; ++s) mid[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
-            for (int k = quarter; k - quarter < p.inner_bytes; k += 64) {
-                u32x4_t fa[PARTS];
-#pragma unroll
-                for (int q = 0; q < PARTS; ++q) fa[q] = k < p.inner_bytes ? *(const u32x4_t *)(inner + q * p.inner_bytes + k) : (u32x4_t){0, 0, 0, 0};
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const int64_t col = (int64_t)one * p.cols + g.col0 + min(j * 16 + lane % 16, cols_left - 1);
-                    const u32x4_t fb = grp_load_chunk<ES>(p.up + col * p.rank * ES + k, p.rank - k / ES);
-#pragma unroll
-                    for (int q = 0; q < PARTS; ++q) grp_mma16<T>(mid[j], fb, fa[q]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int s = 0; s < SUMS; ++s)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[j][s][e] += mine ? mid[j][s][e] : 0.f;
-        }
-    }
+}
+
+// The waves' sums added in the waves' order: f(tile, lane of it, sum) for each four columns (lane / 16 of the tile's) of a row (lane % 16).
+template <typename T, int NT, int NW, typename F>
+__device__ __forceinline__ void grp_few_join(u32x4_t (&part)[NW * NT * 64], typename GrpFew<T>::acc_t (&acc)[NT][GrpTraits<T>::SUMS], int lane, int wave, F f)
+{
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        if constexpr (SUMS == 4) acc[j][0] = (acc[j][0] + acc[j][1]) + (acc[j][2] + acc[j][3]);
+        if constexpr (GrpTraits<T>::SUMS == 4) acc[j][0] = (acc[j][0] + acc[j][1]) + (acc[j][2] + acc[j][3]);
         part[(wave * NT + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[j][0]);
     }
     __syncthreads();
-    // each thread: four columns (lane / 16 of a tile's) of one row (lane % 16)
-    const bool owned = g.group < p.groups;
-    for (int s = t; s < NT * 64; s += NW * 64) {
+    for (int s = threadIdx.x; s < NT * 64; s += NW * 64) {
         typename GrpFew<T>::acc_t sum = __builtin_bit_cast(typename GrpFew<T>::acc_t, part[s]);
 #pragma unroll
         for (int w = 1; w < NW; ++w) sum += __builtin_bit_cast(typename GrpFew<T>::acc_t, part[w * NT * 64 + s]);
-        const int tile = s / 64, l = s % 64, row = g.row0 + l % 16, col = g.col0 + tile * 16 + l / 16 * 4;
-        if (row >= g.row_end || col >= p.cols) continue;
+        f(s / 64, s % 64, sum);
+    }
+}
+
+// The adapters' part of a tile (as grp_adapt has it), one adapter to a wave, then the next.
+template <typename T, int NT, int NW>
+__device__ __forceinline__ void grp_few_adapt(const GroupedParams &p, const GrpProblem &g, int lane, int wave, typename GrpFew<T>::acc_t (&acc)[NT])
+{
+    constexpr int ES = GrpTraits<T>::ES, PARTS = ES == 2 ? 2 : 1, SUMS = GrpTraits<T>::SUMS;
+    const int rows_left = g.row_end - g.row0, cols_left = p.cols - g.col0;
+    const int quarter = lane / 16 * 16, row_in = g.row0 + min(lane % 16, rows_left - 1), id = p.adapter[row_in];
+    const char *inner = p.inner + (int64_t)row_in * (PARTS * p.inner_bytes);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+    uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
+    for (int n = 0; left; ++n) {
+        const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const bool mine = id == one;
+        left &= ~__ballot(mine);
+        if (n % NW != wave) continue;
+        typename GrpFew<T>::acc_t mid[NT][SUMS];
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int s = 0; s < SUMS; ++s) mid[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+        for (int k = quarter; k - quarter < p.inner_bytes; k += 64) {
+            u32x4_t fa[PARTS];
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) fa[q] = k < p.inner_bytes ? *(const u32x4_t *)(inner + q * p.inner_bytes + k) : (u32x4_t){0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int64_t col = (int64_t)one * p.cols + g.col0 + min(j * 16 + lane % 16, cols_left - 1);
+                const u32x4_t fb = grp_load_chunk<ES>(p.up + col * p.rank * ES + k, p.rank - k / ES);
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) grp_mma16<T>(mid[j], fb, fa[q]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            if constexpr (SUMS == 4) mid[j][0] = (mid[j][0] + mid[j][1]) + (mid[j][2] + mid[j][3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][e] += mine ? mid[j][0][e] : 0.f;
+        }
+    }
+}
+
+template <typename T, int NT, int NW, int BATCH, bool DW>
+__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParams p)
+{
+    constexpr int ES = GrpTraits<T>::ES;
+    __shared__ u32x4_t part[NW * NT * 64];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    GrpProblem g;
+    if (!grp_problem<T, kForward, 16, 16 * NT>(p, lane, g)) return;
+    typename GrpFew<T>::acc_t acc[NT][GrpTraits<T>::SUMS];
+    if constexpr (GrpTraits<T>::ADAPT) {
+        typename GrpFew<T>::acc_t beside[NT];
+        grp_few_sums<T, NT, NW, BATCH, DW>(p, g, lane, wave, acc, [&] { grp_few_adapt<T, NT, NW>(p, g, lane, wave, beside); });
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[j][0] += beside[j];
+    } else {
+        grp_few_sums<T, NT, NW, BATCH, DW>(p, g, lane, wave, acc, [] {});
+    }
+    const bool owned = g.group < p.groups;
+    grp_few_join<T, NT, NW>(part, acc, lane, wave, [&](int tile, int l, const typename GrpFew<T>::acc_t &sum) {
+        const int row = g.row0 + l % 16, col = g.col0 + tile * 16 + l / 16 * 4;
+        if (row >= g.row_end || col >= p.cols) return;
         float v[4], scale[4] = {1.f, 1.f, 1.f, 1.f}, bias[4] = {0.f, 0.f, 0.f, 0.f}, sa = 1.f;
         if (owned) {
             const int64_t c = (int64_t)g.group * p.cols + col;
@@ -906,7 +938,7 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
             else v[q] += bias[q];
         }
         grp_store<4>(p, g.y + (int64_t)row * p.ldy, col, v);
-    }
+    });
 }
 
 // The same for the gradient by the rows, whose right operand has its columns contiguous: tiles of 16 rows by 64 columns.  A lane takes four consecutive

@@ -379,6 +379,7 @@ extern "C" alt_status_t alt_gemm_adapters(alt_handle_t h, const alt_adapters_des
     down.adapters = d->adapters;
     down.rank = d->rank;
     down.K = (int32_t)l.K;
+    down.places = h->compute_units;
     ALT_CHECK_HIP(h, adapters_down(l.in_dtype, down, (hipStream_t)stream));
     GroupedParams p = problem(h, l, kForward, x, w, y);
     p.bias = l.epilogue & ALT_EPI_BIAS ? bias : nullptr;

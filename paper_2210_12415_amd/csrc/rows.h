@@ -160,7 +160,7 @@ struct AdaptersDown {
     const float *scale;
     char *inner;
     int64_t ldx;                           // bytes between rows of x
-    int32_t rows, adapters, rank, K;
+    int32_t rows, adapters, rank, K, places;
 };
 
 // inner[m][r] = scale[g] * sum_k x[m,k] a[g,r,k], as the products take it (grp_adapt in grouped.h): rows of whole 32 bytes, in bf16 two of them
