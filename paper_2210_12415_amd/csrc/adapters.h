@@ -1,0 +1,36 @@
+// Low-rank adapters beside a product: what grouped.hip (its entry point) and adapters.hip (its kernels) share.
+//
+// Every row's inner sums, inner[m][r] = scale[g] * sum_k x[m,k] a[g,r,k], come first.  Then there are two ways:
+//   fused   the product's tiles take the adapters' part into their sums (grp_adapt in grouped.h)
+//   beside  the product goes to the workspace in fp32, and a last pass adds each row's part to it, column by column: where there are few rows, whose tiles
+//           would wait for the loads of one adapter after another (32 rows of 32 requests, 4096 x 4096, rank 16: FUSED us fused, BESIDE beside)
+#pragma once
+
+#include "grouped.h"
+
+namespace alt {
+
+struct AdapterParams {
+    const char *x, *a, *b;
+    const int32_t *adapter;
+    const float *scale, *bias;
+    char *inner;
+    const float *base;                     // beside: the product, M x N
+    char *y;
+    int64_t ldx, ldy;                      // bytes between rows
+    int32_t rows, cols, K, rank, adapters, places, relu, out_bf16;
+    int32_t inner_bytes;                   // of a row (fused: of one of its parts)
+    int32_t slices;                        // beside: parts of the reduction, each with inner sums of its own
+    int32_t slots, tiles, col_tiles;       // workgroups for a tile's adapters; tiles of rows; tiles of the rank
+};
+
+// Sets what the sizes say of `p`: which way, its slices and the layout of its inner sums (the sizes and `places` are given).  True: beside.
+bool adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p);
+size_t adapters_inner_bytes(int dtype, const AdapterParams &p, bool beside);
+
+hipError_t adapters_down(int dtype, const AdapterParams &p, bool beside, hipStream_t st);
+// The inner sums and the product in one launch (product: of few rows, fp32 into p.base).
+hipError_t adapters_few(int dtype, const AdapterParams &p, const GroupedParams &product, hipStream_t st);
+hipError_t adapters_up(int dtype, const AdapterParams &p, hipStream_t st);
+
+}  // namespace alt

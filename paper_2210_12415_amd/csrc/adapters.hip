@@ -1,107 +1,275 @@
-// Low-rank adapters: the inner sums of every row, inner[m][r] = scale[g] * sum_k x[m,k] a[g,r,k] for its adapter g, as the products take them (grp_adapt).
-//
-// A product of few columns, in tiles of 16 rows by 16 or 32 of the rank whose waves share the reduction (as grouped_few_kernel's), once for each
-// adapter that a tile's rows have: prompts have one or two, which a workgroup takes in turn; sequences that decode have up to 16, so where there are few tiles
-// the adapters are spread over workgroups too.  Bound by memory: the rows once, and the adapters that they have.
-#include "grouped.h"
+// Low-rank adapters: the inner sums of every row, and the last pass over few rows.
+#include "adapters.h"
 #include "rows.h"
 
 namespace alt {
 namespace {
 
-template <typename T, int NT, int NW, int BATCH, bool DW>
-__global__ __launch_bounds__(64 * NW) void adapters_down_kernel(const GroupedParams p, const float *scale, char *inner, int slots)
-{
-    constexpr int ES = GrpTraits<T>::ES, PARTS = ES == 2 ? 2 : 1;
-    __shared__ u32x4_t part[NW * NT * 64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col_tile = (int)(blockIdx.x % (unsigned)p.tiles_n), rest = (int)(blockIdx.x / (unsigned)p.tiles_n), slot = rest % slots;
-    GrpProblem g;
-    g.row0 = rest / slots * 16;
-    g.row_end = min(g.row0 + 16, p.rows);
-    g.col0 = col_tile * 16 * NT;
-    g.red = p.red;
-    g.a0 = (const char *)p.a + (int64_t)g.row0 * p.lda;
-    const int id = p.adapter[g.row0 + min(lane % 16, g.row_end - 1 - g.row0)];
-    uint64_t left = __ballot(lane % 16 < g.row_end - g.row0 && id >= 0 && id < p.adapters);
-    for (int n = 0; left; ++n) {
-        const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-        left &= ~__ballot(id == one);
-        if (n % slots != slot) continue;
-        g.b0 = (const char *)p.b + (int64_t)one * p.b_group + (int64_t)g.col0 * p.ldb;
-        typename GrpFew<T>::acc_t acc[NT][GrpTraits<T>::SUMS];
-        grp_few_sums<T, NT, NW, BATCH, DW>(p, g, lane, wave, acc, [] {});
-        const float by = scale ? scale[one] : 1.f;
-        grp_few_join<T, NT, NW>(part, acc, lane, wave, [&](int tile, int l, const typename GrpFew<T>::acc_t &sum) {
-            const int row = g.row0 + l % 16, at = (g.col0 + tile * 16 + l / 16 * 4) * ES;
-            if (row >= g.row_end || at >= p.inner_bytes || p.adapter[row] != one) return;
-            char *to = inner + (int64_t)row * (PARTS * p.inner_bytes) + at;
-            float v[4];
+// ---- inner sums ----------------------------------------------------------------------------------------------------------------------
+//
+// Tiles of 16 rows by 16 NT of the rank, once for each adapter that a tile's rows have: prompts have one or two, sequences that decode up to 16, so the
+// adapters of a tile are spread over `slots` workgroups; those of a first adapter come first (a launch's second ones mostly have nothing to do).  Rows come
+// through LDS in steps of 512 bytes, which lanes side by side load side by side: straight into the fragments of the matrix instructions, 16 rows to
+// 16 lanes, every load touches 64 cache lines, and 8192 rows of 4096, rank 32, took 37 us.  Waves share a step's reduction; `slices` share the rest of it.
+constexpr int kStep = 512, kPitch = kStep + 16;            // (rows of LDS 16 bytes more than 64 banks apart)
+
+template <typename T, int NT, int NW>
+struct Down {
+    static constexpr int ES = GrpTraits<T>::ES, THREADS = 64 * NW, ROWS = 16 + 16 * NT, Q = ROWS * (kStep / 16) / THREADS, SUMS = GrpTraits<T>::SUMS;
+    static constexpr int kLds = 2 * ROWS * kPitch;
+    static_assert(ROWS * (kStep / 16) % THREADS == 0 && NW * NT * 1024 <= kLds, "pieces");
+
+    // slices == 0: of the fused form (one slice, in bf16 in two parts)
+    static __device__ __forceinline__ void run(const AdapterParams &p, uint32_t wg, char *lds)
+    {
+        constexpr int PARTS = ES == 2 ? 2 : 1;
+        const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        const uint32_t slices = max(p.slices, 1);
+        const int col0 = (int)(wg % (uint32_t)p.col_tiles) * 16 * NT;
+        uint32_t rest = wg / (uint32_t)p.col_tiles;
+        const int row0 = (int)(rest % (uint32_t)p.tiles) * 16;
+        rest /= (uint32_t)p.tiles;
+        const int slice = (int)(rest % slices), slot = (int)(rest / slices);
+        if (slot >= p.slots) return;
+        const int rows_left = p.rows - row0;
+        const int id = p.adapter[row0 + min(lane % 16, rows_left - 1)];
+        uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
+        const int bytes = p.K * ES, steps = (bytes + kStep - 1) / kStep, per = (steps + (int)slices - 1) / (int)slices, first = slice * per, end = min(first + per, steps);
+        for (int n = 0; left; ++n) {
+            const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+            left &= ~__ballot(id == one);
+            if (n % p.slots != slot) continue;
+            // a thread's pieces of a step: 16 bytes each, of rows of x and then of the adapter (behind the last ones the last again, which nobody stores)
+            const char *from[Q];
+            uint32_t to[Q];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = at / ES + q < p.cols ? sum[q] * by : 0.f;      // (zeros behind the rank)
-            if constexpr (ES == 4) {
-                *(f32x4_t *)to = (f32x4_t){v[0], v[1], v[2], v[3]};
-            } else {
-                const u32x2_t hi = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
-                float low[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t bits = q % 2 ? hi[q / 2] & 0xffff0000u : hi[q / 2] << 16;
-                    // (of an infinity or a NaN nothing is left)
-                    low[q] = (bits & 0x7f800000u) == 0x7f800000u ? 0.f : v[q] - __builtin_bit_cast(float, bits);
-                }
-                *(u32x2_t *)to = hi;
-                *(u32x2_t *)(to + p.inner_bytes) = (u32x2_t){f32x2_to_bf16x2(low[0], low[1]), f32x2_to_bf16x2(low[2], low[3])};
+            for (int q = 0; q < Q; ++q) {
+                const int piece = q * THREADS + t, r = piece / (kStep / 16), c = piece % (kStep / 16) * 16;
+                from[q] = (r < 16 ? p.x + (int64_t)(row0 + min(r, rows_left - 1)) * p.ldx
+                                  : p.a + ((int64_t)one * p.rank + min(col0 + r - 16, p.rank - 1)) * ((int64_t)p.K * ES)) + c;
+                to[q] = r * kPitch + c;
             }
-        });
-        if (left) __syncthreads();                         // (the parts are read)
+            u32x4_t v[2][Q];
+            auto load = [&](u32x4_t (&v)[Q], int s) {
+                if (s >= end) return;
+                if (s < bytes / kStep) {                   // whole
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], from[q] + (int64_t)s * kStep, 16);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) v[q] = grp_load_chunk<ES>(from[q] + (int64_t)s * kStep, (bytes - s * kStep - (int)(to[q] % kPitch)) / ES);
+                }
+            };
+            typename GrpFew<T>::acc_t acc[NT][SUMS];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int s = 0; s < SUMS; ++s) acc[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
+            auto step = [&](u32x4_t (&v)[Q], int s, char *stage) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) *(u32x4_t *)(stage + to[q]) = v[q];
+                load(v, s + 2);
+                __syncthreads();                           // (and the other stage's readers are through)
+#pragma unroll
+                for (int h = 0; h < kStep / NW / 64; ++h) {
+                    const char *at = stage + lane % 16 * kPitch + wave * (kStep / NW) + h * 64 + lane / 16 * 16;
+                    const u32x4_t fa = *(const u32x4_t *)at;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[j], *(const u32x4_t *)(at + (16 + j * 16) * kPitch), fa);
+                }
+            };
+            load(v[0], first);
+            load(v[1], first + 1);
+            for (int s = first; s < end; s += 2) {
+                step(v[0], s, lds);
+                if (s + 1 < end) step(v[1], s + 1, lds + ROWS * kPitch);
+            }
+            __syncthreads();                               // the stages' readers are through
+            const float by = p.scale ? p.scale[one] : 1.f;
+            grp_few_join<T, NT, NW>(*(u32x4_t (*)[NW * NT * 64])lds, acc, lane, wave, [&](int tile, int l, const typename GrpFew<T>::acc_t &sum) {
+                const int row = row0 + l % 16, col = col0 + tile * 16 + l / 16 * 4;
+                if (row >= p.rows || p.adapter[row] != one) return;
+                float f[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) f[q] = col + q < p.rank ? sum[q] * by : 0.f;       // (zeros behind the rank)
+                if (ES == 4 || p.slices) {
+                    if (col * 4 < p.inner_bytes) *(f32x4_t *)(p.inner + ((int64_t)slice * p.rows + row) * p.inner_bytes + col * 4) = (f32x4_t){f[0], f[1], f[2], f[3]};
+                } else if (col * 2 < p.inner_bytes) {
+                    const u32x2_t hi = {f32x2_to_bf16x2(f[0], f[1]), f32x2_to_bf16x2(f[2], f[3])};
+                    float low[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t bits = q % 2 ? hi[q / 2] & 0xffff0000u : hi[q / 2] << 16;
+                        // (of an infinity or a NaN nothing is left)
+                        low[q] = (bits & 0x7f800000u) == 0x7f800000u ? 0.f : f[q] - __builtin_bit_cast(float, bits);
+                    }
+                    char *at = p.inner + (int64_t)row * (PARTS * p.inner_bytes) + col * 2;
+                    *(u32x2_t *)at = hi;
+                    *(u32x2_t *)(at + p.inner_bytes) = (u32x2_t){f32x2_to_bf16x2(low[0], low[1]), f32x2_to_bf16x2(low[2], low[3])};
+                }
+            });
+            if (left) __syncthreads();                     // (the parts are read)
+        }
+    }
+};
+
+template <typename T, int NT, int NW>
+__global__ __launch_bounds__(64 * NW) void adapters_down_kernel(const AdapterParams p)
+{
+    __shared__ uint4 lds[Down<T, NT, NW>::kLds / 16];
+    Down<T, NT, NW>::run(p, blockIdx.x, (char *)lds);
+}
+
+// The inner sums in the first `down` workgroups, the product of few rows in the others: neither needs the other.
+template <typename T, int NT, int NW, int BATCH, bool DW>
+__global__ __launch_bounds__(64 * NW) void adapters_few_kernel(const AdapterParams p, const GroupedParams product, uint32_t down)
+{
+    __shared__ uint4 lds[Down<T, 1, NW>::kLds / 16];
+    static_assert(NW * NT * 1024 <= sizeof lds, "LDS");
+    if (blockIdx.x < down) Down<T, 1, NW>::run(p, blockIdx.x, (char *)lds);
+    else grp_few<T, NT, NW, BATCH, DW>(product, blockIdx.x - down, *(u32x4_t (*)[NW * NT * 64])lds);
+}
+
+// ---- the last pass over few rows -------------------------------------------------------------------------------------------------------
+//
+// y[m][n] = base[m][n] + sum_r inner[m][r] * b[g][n][r] + bias[n].  A thread has a column of R rows, and reads its row of b again only where the next row has
+// another adapter.  Bound by memory: b of the adapters that the rows have, and the product, which is still in the caches.
+template <int ES, int R>
+__global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p, int col_blocks)
+{
+    constexpr int E = 16 / ES, PIECE = 64;                 // of the rank at a time
+    __shared__ float inner[R][PIECE];
+    const int t = threadIdx.x, row0 = (int)(blockIdx.x / (unsigned)col_blocks) * R, col = (int)(blockIdx.x % (unsigned)col_blocks) * 256 + t, width = p.inner_bytes / 4;
+    int ids[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int id = row0 + i < p.rows ? p.adapter[row0 + i] : -1;
+        ids[i] = id < p.adapters ? id : -1;
+    }
+    float sum[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) sum[i] = row0 + i < p.rows && col < p.cols ? p.base[(int64_t)(row0 + i) * p.cols + col] : 0.f;
+    const float bias = p.bias && col < p.cols ? p.bias[col] : 0.f;
+    const char *b = p.b + (int64_t)min(col, p.cols - 1) * p.rank * ES;
+    const int64_t b_adapter = (int64_t)p.cols * p.rank * ES;
+    for (int r0 = 0; r0 < p.rank; r0 += PIECE) {
+        __syncthreads();
+        for (int i = t; i < R * PIECE; i += 256) {
+            const int row = row0 + i / PIECE, r = r0 + i % PIECE;
+            float f = 0.f;
+            if (r < p.rank && row < p.rows) {
+                const int id = p.adapter[row];
+                if (id >= 0 && id < p.adapters)
+                    for (int s = 0; s < p.slices; ++s) f += *(const float *)(p.inner + (((int64_t)s * p.rows + row) * width + r) * 4);
+            }
+            inner[i / PIECE][i % PIECE] = f;
+        }
+        __syncthreads();
+        const int here = min(PIECE, p.rank - r0);
+        for (int r = 0; r < here; r += E) {
+            u32x4_t v = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if (ids[i] < 0) continue;
+                if (i == 0 || ids[i] != ids[i - 1]) v = grp_load_chunk<ES>(b + ids[i] * b_adapter + (int64_t)(r0 + r) * ES, here - r);
+                float f[E];
+                floats16<ES>(v, f);
+#pragma unroll
+                for (int q = 0; q < E; ++q) sum[i] += r + q < here ? inner[i][r + q] * f[q] : 0.f;
+            }
+        }
+    }
+    if (col >= p.cols) return;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (row0 + i >= p.rows) return;
+        float f = sum[i] + bias;
+        if (p.relu) f = grp_relu(f);
+        char *to = p.y + (int64_t)(row0 + i) * p.ldy;
+        if (p.out_bf16) ((uint16_t *)to)[col] = f32_to_bf16_rne(f);
+        else ((float *)to)[col] = f;
     }
 }
 
-template <typename T, int NT, int NW, int BATCH>
-hipError_t launch(GroupedParams p, const float *scale, char *inner, hipStream_t st)
+template <typename T, int NT, int NW>
+hipError_t down(AdapterParams p, hipStream_t st)
 {
-    p.tiles_n = (p.cols + 16 * NT - 1) / (16 * NT);
-    const int64_t tiles = ((int64_t)p.rows + 15) / 16 * p.tiles_n;
-    // (as many workgroups for a tile's adapters as it may have, while the chip has places for them)
-    const int slots = (int)std::min<int64_t>(std::min(p.adapters, 16), std::max<int64_t>(1, 2 * p.places / tiles));
-    if (tiles * slots * 64 * NW > 0xffffffffll) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)(tiles * slots)), block(64 * NW);
-    if constexpr (GrpTraits<T>::ES < 4) {
-        if (((uint64_t)p.a | (uint64_t)p.b | (uint64_t)p.lda | (uint64_t)p.ldb | (uint64_t)p.b_group) % 4) {
-            hipLaunchKernelGGL((adapters_down_kernel<T, NT, NW, BATCH, false>), grid, block, 0, st, p, scale, inner, slots);
-            return hipGetLastError();
-        }
-    }
-    hipLaunchKernelGGL((adapters_down_kernel<T, NT, NW, BATCH, true>), grid, block, 0, st, p, scale, inner, slots);
+    p.col_tiles = (p.rank + 16 * NT - 1) / (16 * NT);
+    const int64_t n = (int64_t)p.tiles * p.col_tiles * std::max(p.slices, 1) * p.slots;
+    if (n * 64 * NW > 0xffffffffll) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((adapters_down_kernel<T, NT, NW>), dim3((unsigned)n), dim3(64 * NW), 0, st, p);
     return hipGetLastError();
 }
 
-template <typename T>
-hipError_t run(const GroupedParams &p, const float *scale, char *inner, hipStream_t st)
+template <typename T, int NT, int NW>
+hipError_t few(AdapterParams p, GroupedParams product, hipStream_t st)
 {
-    return p.cols <= 16 ? launch<T, 1, 8, 2>(p, scale, inner, st) : launch<T, 2, 4, 2>(p, scale, inner, st);
+    p.col_tiles = (p.rank + 15) / 16;
+    const int64_t downs = ((int64_t)p.tiles * p.col_tiles * p.slices * p.slots + 7) / 8 * 8;       // (the product's workgroups go to their XCDs as ever)
+    unsigned grid;
+    const hipError_t e = grp_grid<kForward, 16, 16 * NT>(product, 64 * NW, &grid);
+    if (e != hipSuccess) return e;
+    if ((grid + downs) * 64 * NW > 0xffffffffll) return hipErrorInvalidConfiguration;
+    if constexpr (GrpTraits<T>::ES < 4) {
+        if (((uint64_t)product.a | (uint64_t)product.b | (uint64_t)product.lda | (uint64_t)product.ldb) % 4) {
+            hipLaunchKernelGGL((adapters_few_kernel<T, NT, NW, 2, false>), dim3(grid + (unsigned)downs), dim3(64 * NW), 0, st, p, product, (uint32_t)downs);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((adapters_few_kernel<T, NT, NW, 2, true>), dim3(grid + (unsigned)downs), dim3(64 * NW), 0, st, p, product, (uint32_t)downs);
+    return hipGetLastError();
+}
+
+template <int ES, int R>
+hipError_t up(const AdapterParams &p, hipStream_t st)
+{
+    const int64_t cols = ((int64_t)p.cols + 255) / 256, n = ((int64_t)p.rows + R - 1) / R * cols;
+    if (n * 256 > 0xffffffffll) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((adapters_up_kernel<ES, R>), dim3((unsigned)n), dim3(256), 0, st, p, (int)cols);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t adapters_down(int dtype, const AdaptersDown &d, hipStream_t st)
+bool adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p)
 {
-    const int64_t es = (int64_t)dtype_size(dtype);
-    GroupedParams p{};
-    p.a = d.x;
-    p.b = d.a;
-    p.lda = d.ldx;
-    p.ldb = d.K * es;
-    p.b_group = d.rank * p.ldb;
-    p.rows = d.rows;
-    p.cols = d.rank;
-    p.red = d.K;
-    p.adapter = d.adapter;
-    p.adapters = d.adapters;
-    p.places = d.places;
-    p.inner_bytes = adapters_row_bytes(d.rank, dtype);
-    return dtype == ALT_F32 ? run<float>(p, d.scale, d.inner, st) : run<bf16_tag>(p, d.scale, d.inner, st);
+    const int es = (int)dtype_size(dtype);
+    // beside: few rows, or as many as the last pass takes about 10 us for
+    const bool few_rows = grp_is_few(product, es), beside = few_rows || (double)p.rows * p.cols * (8 + p.rank * es) <= 64e6;
+    const int steps = (int)(((int64_t)p.K * es + kStep - 1) / kStep);
+    p.tiles = (p.rows + 15) / 16;
+    const int64_t work = (int64_t)p.tiles * ((p.rank + 15) / 16);
+    // workgroups for a tile's adapters, two at least and up to as many as the chip has places for
+    p.slots = (int)std::min<int64_t>(std::min(std::min(p.adapters, 16), p.rows), std::max<int64_t>(2, p.places / work));
+    p.slices = !beside ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(8, steps), p.places / (work * p.slots)));
+    p.inner_bytes = beside ? (p.rank + 15) / 16 * 64 : (p.rank * es + 31) / 32 * 32;
+    return beside;
+}
+
+size_t adapters_inner_bytes(int dtype, const AdapterParams &p, bool beside)
+{
+    return (size_t)p.rows * p.inner_bytes * (beside ? p.slices : dtype == ALT_BF16 ? 2 : 1);
+}
+
+hipError_t adapters_down(int dtype, const AdapterParams &p, bool, hipStream_t st)
+{
+    if (dtype == ALT_F32) return p.rank <= 16 ? down<float, 1, 4>(p, st) : down<float, 2, 4>(p, st);
+    return p.rank <= 16 ? down<bf16_tag, 1, 4>(p, st) : down<bf16_tag, 2, 4>(p, st);
+}
+
+hipError_t adapters_few(int dtype, const AdapterParams &p, const GroupedParams &product, hipStream_t st)
+{
+    const bool narrow = grp_tiles<kForward>(product, 16, 16) <= product.places;                // (as in grouped_run)
+    if (dtype == ALT_F32) return narrow ? few<float, 1, 8>(p, product, st) : few<float, 2, 4>(p, product, st);
+    return narrow ? few<bf16_tag, 1, 8>(p, product, st) : few<bf16_tag, 2, 4>(p, product, st);
+}
+
+hipError_t adapters_up(int dtype, const AdapterParams &p, hipStream_t st)
+{
+    // (a row to a workgroup while that fills the chip twice at most)
+    const bool one = (int64_t)p.rows * ((p.cols + 255) / 256) <= 2 * (int64_t)p.places;
+    if (dtype == ALT_F32) return one ? up<4, 1>(p, st) : up<4, 4>(p, st);
+    return one ? up<2, 1>(p, st) : up<2, 4>(p, st);
 }
 
 }  // namespace alt

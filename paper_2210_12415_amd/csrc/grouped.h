@@ -471,14 +471,14 @@ __device__ __forceinline__ int grp_by_length(const GroupedParams &p, int lane, i
 }
 
 template <typename T, int FORM, int BM, int BN>
-__device__ __forceinline__ bool grp_problem(const GroupedParams &p, int lane, GrpProblem &g)
+__device__ __forceinline__ bool grp_problem(const GroupedParams &p, int lane, uint32_t wg, GrpProblem &g)
 {
     constexpr int ES = GrpTraits<T>::ES;
     if constexpr (FORM == kWeights) {
         const int tiles_m = (p.rows + BM - 1) / BM, tiles = tiles_m * p.tiles_n, per = grp_weight_tiles(tiles);
-        g.group = (int)(blockIdx.x / (unsigned)per);
+        g.group = (int)(wg / (unsigned)per);
         if (p.groups <= 64 && gridDim.x > 2u * (unsigned)p.places) g.group = grp_by_length(p, lane, g.group);
-        int q = (int)(blockIdx.x % (unsigned)per), mt, nt;
+        int q = (int)(wg % (unsigned)per), mt, nt;
         if (tiles >= 64) q = (q & 7) * (per / 8) + (q >> 3);
         if (q >= tiles) return false;
         grp_order(p, q, tiles_m, mt, nt);
@@ -492,7 +492,7 @@ __device__ __forceinline__ bool grp_problem(const GroupedParams &p, int lane, Gr
         g.y = (char *)p.y + (int64_t)g.group * p.y_group;
     } else {
         GrpTile tile;
-        if (!grp_find<BM>(p, lane, blockIdx.x, tile)) return false;
+        if (!grp_find<BM>(p, lane, wg, tile)) return false;
         grp_at<T, FORM>(p, tile.group, tile.row0, tile.row_end, tile.col_tile * BN, g);
     }
     return true;
@@ -652,18 +652,22 @@ __device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProble
 template <typename T, int TM, int TN, int SUMS>
 __device__ __forceinline__ void grp_adapt(const GroupedParams &p, const GrpProblem &g, GrpSums<T, TM, TN, SUMS> &acc, int wrow, int wcol, int lane)
 {
-    constexpr int ES = GrpTraits<T>::ES, PARTS = ES == 2 ? 2 : 1;
+    constexpr int ES = GrpTraits<T>::ES, PARTS = ES == 2 ? 2 : 1, STEPS = 2;           // of which the loads go out together
     const int half = (lane >> 5) * 16;
     if (g.col0 + wcol >= p.cols) return;
+    int ids[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int row = g.row0 + wrow + i * 32 + (lane & 31), row_in = min(row, g.row_end - 1);
-        const int id = p.adapter[row_in];
-        const char *inner = p.inner + (int64_t)row_in * (PARTS * p.inner_bytes) + half;
-        uint64_t left = __ballot(row < g.row_end && id >= 0 && id < p.adapters);
+        const int row = g.row0 + wrow + i * 32 + (lane & 31), id = p.adapter[min(row, g.row_end - 1)];
+        ids[i] = row < g.row_end && id < p.adapters ? id : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const char *inner = p.inner + (int64_t)min(g.row0 + wrow + i * 32 + (lane & 31), g.row_end - 1) * (PARTS * p.inner_bytes) + half;
+        uint64_t left = __ballot(ids[i] >= 0);
         while (left) {
-            const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-            const bool mine = id == one;
+            const int one = __builtin_amdgcn_readlane(ids[i], __builtin_ctzll(left));
+            const bool mine = ids[i] == one;
             left &= ~__ballot(mine);
             const char *up = p.up + ((int64_t)one * p.cols + g.col0 + wcol) * p.rank * ES + half;
             typename GrpTraits<T>::acc_t part[TN][1];
@@ -671,17 +675,29 @@ __device__ __forceinline__ void grp_adapt(const GroupedParams &p, const GrpProbl
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) part[j][0][e] = 0;
-            for (int at = 0; at < p.inner_bytes; at += 32) {
-                u32x4_t fa[PARTS];
+            for (int at = 0; at < p.inner_bytes; at += 32 * STEPS) {
+                u32x4_t fa[STEPS][PARTS], fb[STEPS][TN];
 #pragma unroll
-                for (int q = 0; q < PARTS; ++q) fa[q] = *(const u32x4_t *)(inner + q * p.inner_bytes + at);
+                for (int s = 0; s < STEPS; ++s) {
+                    const int from = at + s * 32;
+                    const bool in = from < p.inner_bytes;
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const int64_t col = min(j * 32 + (lane & 31), p.cols - 1 - g.col0 - wcol);
-                    const u32x4_t fb = grp_load_chunk<ES>(up + col * p.rank * ES + at, p.rank - (at + half) / ES);
+                    for (int q = 0; q < PARTS; ++q) {
+                        fa[s][q] = (u32x4_t){0, 0, 0, 0};
+                        if (in) fa[s][q] = *(const u32x4_t *)(inner + q * p.inner_bytes + from);
+                    }
 #pragma unroll
-                    for (int q = 0; q < PARTS; ++q) grp_mma<T>(part[j], fb, fa[q]);
+                    for (int j = 0; j < TN; ++j) {
+                        const int64_t col = min(j * 32 + (lane & 31), p.cols - 1 - g.col0 - wcol);
+                        fb[s][j] = grp_load_chunk<ES>(up + col * p.rank * ES + from, p.rank - (from + half) / ES);
+                    }
                 }
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q) grp_mma<T>(part[j], fb[s][j], fa[s][q]);
             }
 #pragma unroll
             for (int j = 0; j < TN; ++j)
@@ -727,8 +743,6 @@ __device__ __forceinline__ void grp_store_sums(const GroupedParams &p, const Grp
 template <typename T> struct GrpFew;
 template <> struct GrpFew<bf16_tag> { typedef f32x4_t acc_t; };
 template <> struct GrpFew<float> { typedef f32x4_t acc_t; };
-template <> struct GrpFew<bf16_adapted_tag> : GrpFew<bf16_tag> {};
-template <> struct GrpFew<f32_adapted_tag> : GrpFew<float> {};
 typedef int i32x4s_t __attribute__((ext_vector_type(4)));
 template <> struct GrpFew<i8_tag> { typedef i32x4s_t acc_t; };
 
@@ -773,9 +787,9 @@ struct GrpPair {
     }
 };
 
-// This wave's sums of the tile `g`; `between` runs while its first loads are on their way.
-template <typename T, int NT, int NW, int BATCH, bool DW, typename F>
-__device__ __forceinline__ void grp_few_sums(const GroupedParams &p, const GrpProblem &g, int lane, int wave, typename GrpFew<T>::acc_t (&acc)[NT][GrpTraits<T>::SUMS], F between)
+// This wave's sums of the tile `g`.
+template <typename T, int NT, int NW, int BATCH, bool DW>
+__device__ __forceinline__ void grp_few_sums(const GroupedParams &p, const GrpProblem &g, int lane, int wave, typename GrpFew<T>::acc_t (&acc)[NT][GrpTraits<T>::SUMS])
 {
     constexpr int ES = GrpTraits<T>::ES, UNIT = 128;
     const int rows_left = g.row_end - g.row0, cols_left = p.cols - g.col0;
@@ -819,15 +833,12 @@ __device__ __forceinline__ void grp_few_sums(const GroupedParams &p, const GrpPr
     if (wave < units) {
         Batch x, y;
         load(x, wave);
-        between();
         for (int u = wave; u < units; u += 2 * STEP) {
             if (u + STEP < units) load(y, u + STEP);
             mma(x, u);
             if (u + 2 * STEP < units) load(x, u + 2 * STEP);
             if (u + STEP < units) mma(y, u + STEP);
         }
-    } else {
-        between();
     }
     // what the reduction ends with: less than a unit
     if (bytes % UNIT && wave == units % NW) {
@@ -859,65 +870,16 @@ __device__ __forceinline__ void grp_few_join(u32x4_t (&part)[NW * NT * 64], type
     }
 }
 
-// The adapters' part of a tile (as grp_adapt has it), one adapter to a wave, then the next.
-template <typename T, int NT, int NW>
-__device__ __forceinline__ void grp_few_adapt(const GroupedParams &p, const GrpProblem &g, int lane, int wave, typename GrpFew<T>::acc_t (&acc)[NT])
-{
-    constexpr int ES = GrpTraits<T>::ES, PARTS = ES == 2 ? 2 : 1, SUMS = GrpTraits<T>::SUMS;
-    const int rows_left = g.row_end - g.row0, cols_left = p.cols - g.col0;
-    const int quarter = lane / 16 * 16, row_in = g.row0 + min(lane % 16, rows_left - 1), id = p.adapter[row_in];
-    const char *inner = p.inner + (int64_t)row_in * (PARTS * p.inner_bytes);
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
-    uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
-    for (int n = 0; left; ++n) {
-        const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-        const bool mine = id == one;
-        left &= ~__ballot(mine);
-        if (n % NW != wave) continue;
-        typename GrpFew<T>::acc_t mid[NT][SUMS];
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int s = 0; s < SUMS; ++s) mid[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
-        for (int k = quarter; k - quarter < p.inner_bytes; k += 64) {
-            u32x4_t fa[PARTS];
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q) fa[q] = k < p.inner_bytes ? *(const u32x4_t *)(inner + q * p.inner_bytes + k) : (u32x4_t){0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int64_t col = (int64_t)one * p.cols + g.col0 + min(j * 16 + lane % 16, cols_left - 1);
-                const u32x4_t fb = grp_load_chunk<ES>(p.up + col * p.rank * ES + k, p.rank - k / ES);
-#pragma unroll
-                for (int q = 0; q < PARTS; ++q) grp_mma16<T>(mid[j], fb, fa[q]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            if constexpr (SUMS == 4) mid[j][0] = (mid[j][0] + mid[j][1]) + (mid[j][2] + mid[j][3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[j][e] += mine ? mid[j][0][e] : 0.f;
-        }
-    }
-}
-
+// Workgroup `wg` of a launch; `part` is LDS.
 template <typename T, int NT, int NW, int BATCH, bool DW>
-__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParams p)
+__device__ __forceinline__ void grp_few(const GroupedParams &p, uint32_t wg, u32x4_t (&part)[NW * NT * 64])
 {
     constexpr int ES = GrpTraits<T>::ES;
-    __shared__ u32x4_t part[NW * NT * 64];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     GrpProblem g;
-    if (!grp_problem<T, kForward, 16, 16 * NT>(p, lane, g)) return;
+    if (!grp_problem<T, kForward, 16, 16 * NT>(p, lane, wg, g)) return;
     typename GrpFew<T>::acc_t acc[NT][GrpTraits<T>::SUMS];
-    if constexpr (GrpTraits<T>::ADAPT) {
-        typename GrpFew<T>::acc_t beside[NT];
-        grp_few_sums<T, NT, NW, BATCH, DW>(p, g, lane, wave, acc, [&] { grp_few_adapt<T, NT, NW>(p, g, lane, wave, beside); });
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[j][0] += beside[j];
-    } else {
-        grp_few_sums<T, NT, NW, BATCH, DW>(p, g, lane, wave, acc, [] {});
-    }
+    grp_few_sums<T, NT, NW, BATCH, DW>(p, g, lane, wave, acc);
     const bool owned = g.group < p.groups;
     grp_few_join<T, NT, NW>(part, acc, lane, wave, [&](int tile, int l, const typename GrpFew<T>::acc_t &sum) {
         const int row = g.row0 + l % 16, col = g.col0 + tile * 16 + l / 16 * 4;
@@ -941,6 +903,13 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParam
     });
 }
 
+template <typename T, int NT, int NW, int BATCH, bool DW>
+__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(const GroupedParams p)
+{
+    __shared__ u32x4_t part[NW * NT * 64];
+    grp_few<T, NT, NW, BATCH, DW>(p, blockIdx.x, part);
+}
+
 // The same for the gradient by the rows, whose right operand has its columns contiguous: tiles of 16 rows by 64 columns.  A lane takes four consecutive
 // columns (those of its lane % 16) of as many steps of the reduction as the matrix instruction takes of a lane (those of its lane / 16), so that each
 // row of 64 columns is read whole; matrix tile j has the columns 4 c + j.  Units of 64 bytes of the left operand.  Bound by latency: 19 rows, 2538 x
@@ -953,7 +922,7 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_dx_kernel(const GroupedPa
     __shared__ u32x4_t part[NW * 4 * 64];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     GrpProblem g;
-    if (!grp_problem<T, kInput, 16, 64>(p, lane, g)) return;
+    if (!grp_problem<T, kInput, 16, 64>(p, lane, blockIdx.x, g)) return;
     if (g.col0 + 64 > p.cols && p.cols >= 64) {            // (the last tile ends with the matrix)
         g.b0 -= (int64_t)(g.col0 + 64 - p.cols) * ES;
         g.col0 = p.cols - 64;
@@ -1154,7 +1123,7 @@ __global__ __launch_bounds__(64 * WGM * WGN * WGK) void grouped_any_kernel(const
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wk = wave / TILES, tile = wave % TILES, wm = tile / WGN, wn = tile % WGN;
     GrpProblem g;
-    if (!grp_problem<T, FORM, BM, BN>(p, lane, g)) return;
+    if (!grp_problem<T, FORM, BM, BN>(p, lane, blockIdx.x, g)) return;
     if (FORM != kForward && g.col0 + BN > p.cols && p.cols >= BN) {
         g.b0 -= (int64_t)(g.col0 + BN - p.cols) * ES;
         g.col0 = p.cols - BN;
@@ -1587,7 +1556,7 @@ __global__ __launch_bounds__(K::THREADS, K::kLds > 80 * 1024 ? (K::NW + 3) / 4 :
 {
     extern __shared__ uint4 smem_u4[];
     GrpProblem only;
-    if (!grp_problem<typename K::type, K::kForm, K::kBM, K::kBN>(p, threadIdx.x & 63, only)) return;
+    if (!grp_problem<typename K::type, K::kForm, K::kBM, K::kBN>(p, threadIdx.x & 63, blockIdx.x, only)) return;
     K::tile(p, only, (char *)smem_u4);
 }
 
@@ -1906,7 +1875,7 @@ hipError_t grouped_run(const GroupedParams &p, hipStream_t st)
 {
     constexpr int ES = GrpTraits<T>::ES;
     const double places = p.places;
-    if constexpr (FORM == kForward) {
+    if constexpr (FORM == kForward && !GrpTraits<T>::ADAPT) {      // (few rows with adapters: adapters.hip)
         // (columns in twos, four waves, where that fills the chip, else one by one and eight waves to a reduction: 16 x 4096 x 4096 6.6 against 8.5 us,
         // 32 x 4096 x 4096 10.4 against 8.6)
         if (grp_is_few(p, ES))

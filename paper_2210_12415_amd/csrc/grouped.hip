@@ -1,5 +1,5 @@
 // Entry points of the products over groups of rows and of the 8-bit product: their checks, and the problem each is.
-#include "grouped.h"
+#include "adapters.h"
 #include "ops.h"
 #include "rows.h"
 
@@ -238,13 +238,49 @@ alt_status_t check_adapters(alt_handle_t h, const char *call, const alt_adapters
     return ALT_OK;
 }
 
-// Bytes for operands laid out anew, behind the rows' inner sums.
-size_t adapters_pack_bytes(alt_handle_t h, const alt_grouped_desc_t &l, const void *x, const void *w)
+// A product with adapters as both of its parts see it, and the layout of its workspace: inner sums, where the product goes beside them its fp32 results, and
+// operands laid out anew.
+struct AdapterCall {
+    GroupedParams product;
+    AdapterParams adapters;
+    bool beside, few;
+    size_t inner, base, pack;
+};
+
+AdapterCall adapter_call(alt_handle_t h, const alt_adapters_desc_t *d, const alt_grouped_desc_t &l, const void *x, const void *w, void *y)
 {
-    GroupedParams p = problem(h, l, kForward, x, w, nullptr);
+    AdapterCall c{};
+    GroupedParams &p = c.product;
+    p = problem(h, l, kForward, x, w, y);
     if (p.places == 0) p.places = 256;
-    return pack_bytes(kForward, l.in_dtype, p);
+    AdapterParams &q = c.adapters;
+    q.x = (const char *)x;
+    q.y = (char *)y;
+    q.ldx = p.lda;
+    q.ldy = p.ldy;
+    q.rows = p.rows; q.cols = p.cols; q.K = p.red;
+    q.rank = d->rank; q.adapters = d->adapters; q.places = p.places;
+    q.relu = (l.epilogue & ALT_EPI_RELU) != 0;
+    q.out_bf16 = l.out_dtype == ALT_BF16;
+    c.beside = adapters_plan(l.in_dtype, p, q);
+    c.few = grp_is_few(p, (int)in_size(l.in_dtype));
+    c.inner = adapters_inner_bytes(l.in_dtype, q, c.beside);
+    c.base = c.beside ? (size_t)l.rows * l.N * 4 : 0;
+    if (c.beside) {                                        // the product's results: dense fp32
+        p.ldy = l.N * 4;
+        p.flags = l.N % 4 == 0 ? kGrpWhole : 0;
+    } else {
+        p.rank = d->rank;
+        p.adapters = d->adapters;
+        p.inner_bytes = q.inner_bytes;
+        if (q.relu) p.flags |= kGrpRelu;
+    }
+    c.pack = pack_bytes(kForward, l.in_dtype, p);
+    return c;
 }
+
+// What there is of the workspace beside operands that are laid out anew, which may be left as they are.
+size_t adapters_need(const AdapterCall &c) { return c.inner + (c.base + 15) / 16 * 16 + 16; }
 
 // The 8-bit product as a layer of one group.
 alt_grouped_desc_t one_group(const alt_gemm_i8_desc_t *d)
@@ -363,34 +399,44 @@ extern "C" alt_status_t alt_gemm_adapters(alt_handle_t h, const alt_adapters_des
     const size_t es = in_size(l.in_dtype);
     s = check_buffers(h, "alt_gemm_adapters", {{"x", x, es}, {"w", w, es}, {"adapter", adapter, 4}, {"a", a, es}, {"b", b, es}, {"scale", scale, 4, scale != nullptr},
                                                {"bias", bias, 4, (l.epilogue & ALT_EPI_BIAS) != 0}, {"y", y, dtype_size(l.out_dtype)}});
-    const size_t inner = adapters_inner_bytes(l.rows, d->rank, l.in_dtype);
-    if (s == ALT_OK) s = check_workspace(h, "alt_gemm_adapters", workspace, ws_bytes, inner + 16);
+    if (s != ALT_OK) return s;
+    AdapterCall c = adapter_call(h, d, l, x, w, y);
+    s = check_workspace(h, "alt_gemm_adapters", workspace, ws_bytes, adapters_need(c));
     if (s == ALT_OK) s = check_device(h, "alt_gemm_adapters");
     if (s != ALT_OK) return s;
+    const hipStream_t st = (hipStream_t)stream;
     char *ws = aligned_workspace(workspace);
-    AdaptersDown down{};
-    down.x = (const char *)x;
-    down.a = (const char *)a;
-    down.adapter = adapter;
-    down.scale = scale;
-    down.inner = ws;
-    down.ldx = l.lda * (int64_t)es;
-    down.rows = (int32_t)l.rows;
-    down.adapters = d->adapters;
-    down.rank = d->rank;
-    down.K = (int32_t)l.K;
-    down.places = h->compute_units;
-    ALT_CHECK_HIP(h, adapters_down(l.in_dtype, down, (hipStream_t)stream));
-    GroupedParams p = problem(h, l, kForward, x, w, y);
-    p.bias = l.epilogue & ALT_EPI_BIAS ? bias : nullptr;
-    if (l.epilogue & ALT_EPI_RELU) p.flags |= kGrpRelu;
-    p.adapter = adapter;
-    p.inner = ws;
-    p.up = (const char *)b;
-    p.adapters = d->adapters;
-    p.rank = d->rank;
-    p.inner_bytes = adapters_row_bytes(d->rank, l.in_dtype);
-    return run(h, "alt_gemm_adapters", l.in_dtype, kForward, p, ws + inner, (size_t)((char *)workspace + ws_bytes - (ws + inner)), (hipStream_t)stream);
+    AdapterParams &q = c.adapters;
+    GroupedParams &p = c.product;
+    q.a = (const char *)a;
+    q.b = (const char *)b;
+    q.adapter = adapter;
+    q.scale = scale;
+    q.bias = l.epilogue & ALT_EPI_BIAS ? bias : nullptr;
+    q.inner = ws;
+    if (c.beside) {
+        q.base = (const float *)(ws + c.inner);
+        p.y = ws + c.inner;
+    } else {
+        p.bias = q.bias;
+        p.adapter = adapter;
+        p.inner = ws;
+        p.up = (const char *)b;
+    }
+    hipError_t e;
+    if (c.beside && c.few) {
+        e = adapters_few(l.in_dtype, q, p, st);
+    } else {
+        ALT_CHECK_HIP(h, adapters_down(l.in_dtype, q, c.beside, st));
+        char *more = ws + c.inner + (c.base + 15) / 16 * 16;
+        s = run(h, "alt_gemm_adapters", l.in_dtype, kForward, p, more, (size_t)((char *)workspace + ws_bytes - more), st);
+        if (s != ALT_OK) return s;
+        e = hipSuccess;
+    }
+    if (e == hipSuccess && c.beside) e = adapters_up(l.in_dtype, q, st);
+    if (e == hipErrorInvalidConfiguration) return fail(h, ALT_UNSUPPORTED, "alt_gemm_adapters: more workgroups than a launch holds");
+    ALT_CHECK_HIP(h, e);
+    return ALT_OK;
 }
 
 extern "C" alt_status_t alt_gemm_adapters_workspace_size(alt_handle_t h, const alt_adapters_desc_t *d, size_t *bytes)
@@ -399,6 +445,11 @@ extern "C" alt_status_t alt_gemm_adapters_workspace_size(alt_handle_t h, const a
     const alt_status_t s = check_adapters(h, "alt_gemm_adapters_workspace_size", d, &l);
     if (s != ALT_OK) return s;
     if (!bytes) return fail(h, ALT_INVALID_ARG, "alt_gemm_adapters_workspace_size: null result");
-    *bytes = l.rows ? adapters_inner_bytes(l.rows, d->rank, l.in_dtype) + adapters_pack_bytes(h, l, nullptr, nullptr) + 16 : 0;
+    if (l.rows == 0) {
+        *bytes = 0;
+        return ALT_OK;
+    }
+    const AdapterCall c = adapter_call(h, d, l, nullptr, nullptr, nullptr);
+    *bytes = adapters_need(c) + (c.pack ? c.pack + 16 : 0);
     return ALT_OK;
 }

@@ -152,20 +152,4 @@ inline alt_status_t check_workspace(alt_handle_t h, const char *call, const void
 }
 inline char *aligned_workspace(void *workspace) { return (char *)(((uintptr_t)workspace + 15) / 16 * 16); }
 
-// ---- the inner sums of low-rank adapters (adapters.hip) --------------------------------------------------------------------------------
-
-struct AdaptersDown {
-    const char *x, *a;
-    const int32_t *adapter;
-    const float *scale;
-    char *inner;
-    int64_t ldx;                           // bytes between rows of x
-    int32_t rows, adapters, rank, K, places;
-};
-
-// inner[m][r] = scale[g] * sum_k x[m,k] a[g,r,k], as the products take it (grp_adapt in grouped.h): rows of whole 32 bytes, in bf16 two of them
-inline int32_t adapters_row_bytes(int rank, int dtype) { return (rank * (int)dtype_size(dtype) + 31) / 32 * 32; }
-inline size_t adapters_inner_bytes(int64_t rows, int rank, int dtype) { return (size_t)rows * adapters_row_bytes(rank, dtype) * (dtype == ALT_BF16 ? 2 : 1); }
-hipError_t adapters_down(int dtype, const AdaptersDown &p, hipStream_t st);
-
 }  // namespace alt
