@@ -15,9 +15,10 @@ constexpr int kStep = 512, kPitch = kStep + 16;            // (rows of LDS 16 by
 
 template <typename T, int NT, int NW>
 struct Down {
-    static constexpr int ES = GrpTraits<T>::ES, THREADS = 64 * NW, ROWS = 16 + 16 * NT, Q = ROWS * (kStep / 16) / THREADS, SUMS = GrpTraits<T>::SUMS;
+    static constexpr int ES = GrpTraits<T>::ES, THREADS = 64 * NW, ROWS = 16 + 16 * NT, STRIDE = THREADS / (kStep / 16), Q = ROWS / STRIDE, XQ = 16 / STRIDE, AHEAD = 2,
+                         SUMS = GrpTraits<T>::SUMS;             // STRIDE: rows of a piece of all threads
     static constexpr int kLds = 2 * ROWS * kPitch;
-    static_assert(ROWS * (kStep / 16) % THREADS == 0 && NW * NT * 1024 <= kLds, "pieces");
+    static_assert(16 % STRIDE == 0 && AHEAD % 2 == 0 && NW * NT * 1024 <= kLds, "pieces");
 
     // slices == 0: of the fused form (one slice, in bf16 in two parts)
     static __device__ __forceinline__ void run(const AdapterParams &p, uint32_t wg, char *lds)
@@ -34,42 +35,35 @@ struct Down {
         const int rows_left = p.rows - row0;
         const int id = p.adapter[row0 + min(lane % 16, rows_left - 1)];
         uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
-        const int bytes = p.K * ES, steps = (bytes + kStep - 1) / kStep, per = (steps + (int)slices - 1) / (int)slices, first = slice * per, end = min(first + per, steps);
+        const int64_t row_bytes = (int64_t)p.K * ES;
+        const int bytes = (int)row_bytes, whole = bytes / kStep, steps = (bytes + kStep - 1) / kStep, per = (steps + (int)slices - 1) / (int)slices, first = slice * per, end = min(first + per, steps);
         for (int n = 0; left; ++n) {
             const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
             left &= ~__ballot(id == one);
             if (n % p.slots != slot) continue;
-            // a thread's pieces of a step: 16 bytes each, of rows of x and then of the adapter (behind the last ones the last again, which nobody stores)
-            const char *from[Q];
-            uint32_t to[Q];
+            // A thread's pieces of a step, 16 bytes each: XQ of rows of x, then of the adapter (behind the last row the last again, which nobody stores).
+            const char *x = p.x + (int64_t)row0 * p.ldx, *a = p.a + ((int64_t)one * p.rank + col0) * row_bytes;
+            const int r = t / (kStep / 16), c = t % (kStep / 16) * 16;
+            uint32_t from[Q];
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const int piece = q * THREADS + t, r = piece / (kStep / 16), c = piece % (kStep / 16) * 16;
-                from[q] = (r < 16 ? p.x + (int64_t)(row0 + min(r, rows_left - 1)) * p.ldx
-                                  : p.a + ((int64_t)one * p.rank + min(col0 + r - 16, p.rank - 1)) * ((int64_t)p.K * ES)) + c;
-                to[q] = r * kPitch + c;
-            }
-            u32x4_t v[2][Q];
+            for (int q = 0; q < Q; ++q)
+                from[q] = q < XQ ? (uint32_t)(min(q * STRIDE + r, rows_left - 1) * (int)p.ldx + c)
+                                 : (uint32_t)(min(q * STRIDE + r - 16, p.rank - col0 - 1) * (int)row_bytes + c);
+            char *to = lds + r * kPitch + c;
+            u32x4_t v[AHEAD][Q];
+            const int last = min(end, whole);              // of the whole steps
             auto load = [&](u32x4_t (&v)[Q], int s) {
-                if (s >= end) return;
-                if (s < bytes / kStep) {                   // whole
+                if (s >= last) return;
+                const char *xs = x + (int64_t)s * kStep, *as = a + (int64_t)s * kStep;
 #pragma unroll
-                    for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], from[q] + (int64_t)s * kStep, 16);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < Q; ++q) v[q] = grp_load_chunk<ES>(from[q] + (int64_t)s * kStep, (bytes - s * kStep - (int)(to[q] % kPitch)) / ES);
-                }
+                for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], (q < XQ ? xs : as) + from[q], 16);
             };
             typename GrpFew<T>::acc_t acc[NT][SUMS];
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int s = 0; s < SUMS; ++s) acc[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
-            auto step = [&](u32x4_t (&v)[Q], int s, char *stage) {
-#pragma unroll
-                for (int q = 0; q < Q; ++q) *(u32x4_t *)(stage + to[q]) = v[q];
-                load(v, s + 2);
-                __syncthreads();                           // (and the other stage's readers are through)
+            auto multiply = [&](const char *stage) {
 #pragma unroll
                 for (int h = 0; h < kStep / NW / 64; ++h) {
                     const char *at = stage + lane % 16 * kPitch + wave * (kStep / NW) + h * 64 + lane / 16 * 16;
@@ -78,11 +72,30 @@ struct Down {
                     for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[j], *(const u32x4_t *)(at + (16 + j * 16) * kPitch), fa);
                 }
             };
-            load(v[0], first);
-            load(v[1], first + 1);
-            for (int s = first; s < end; s += 2) {
-                step(v[0], s, lds);
-                if (s + 1 < end) step(v[1], s + 1, lds + ROWS * kPitch);
+            auto step = [&](u32x4_t (&v)[Q], int s, int stage) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) *(u32x4_t *)(to + stage + q * STRIDE * kPitch) = v[q];
+                load(v, s + AHEAD);
+                __syncthreads();                           // (and the other stage's readers are through)
+                multiply(lds + stage);
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) load(v[i], first + i);
+            for (int s = first; s < last; s += AHEAD) {
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+                    if (s + i < last) step(v[i], s + i, i % 2 * (ROWS * kPitch));
+            }
+            if (end > whole && first < end) {              // what the reduction ends with
+                __syncthreads();
+                const int count = (bytes - whole * kStep - c) / ES;
+#pragma unroll 1
+                for (int q = 0; q < Q; ++q) {
+                    const char *at = (q < XQ ? x + (int64_t)min(q * STRIDE + r, rows_left - 1) * p.ldx : a + (int64_t)min(q * STRIDE + r - 16, p.rank - col0 - 1) * row_bytes) + c;
+                    *(u32x4_t *)(to + q * STRIDE * kPitch) = grp_load_chunk<ES>(at + (int64_t)whole * kStep, count);
+                }
+                __syncthreads();
+                multiply(lds);
             }
             __syncthreads();                               // the stages' readers are through
             const float by = p.scale ? p.scale[one] : 1.f;
@@ -114,7 +127,7 @@ struct Down {
 };
 
 template <typename T, int NT, int NW>
-__global__ __launch_bounds__(64 * NW) void adapters_down_kernel(const AdapterParams p)
+__global__ __launch_bounds__(64 * NW, 3) void adapters_down_kernel(const AdapterParams p)
 {
     __shared__ uint4 lds[Down<T, NT, NW>::kLds / 16];
     Down<T, NT, NW>::run(p, blockIdx.x, (char *)lds);
@@ -153,6 +166,14 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p,
     const char *b = p.b + (int64_t)min(col, p.cols - 1) * p.rank * ES;
     const int64_t b_adapter = (int64_t)p.cols * p.rank * ES;
     for (int r0 = 0; r0 < p.rank; r0 += PIECE) {
+        const int here = min(PIECE, p.rank - r0);
+        // (one row: its row of b is on its way before the inner sums are asked for, 5.1 us for 4096 columns of 32 rows, rank 16, so 4.6)
+        u32x4_t ahead[R == 1 ? PIECE / E : 1];
+        if constexpr (R == 1) {
+#pragma unroll
+            for (int k = 0; k < PIECE / E; ++k)
+                if (k * E < here && ids[0] >= 0) ahead[k] = grp_load_chunk<ES>(b + ids[0] * b_adapter + (int64_t)(r0 + k * E) * ES, here - k * E);
+        }
         __syncthreads();
         for (int i = t; i < R * PIECE; i += 256) {
             const int row = row0 + i / PIECE, r = r0 + i % PIECE;
@@ -165,7 +186,17 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p,
             inner[i / PIECE][i % PIECE] = f;
         }
         __syncthreads();
-        const int here = min(PIECE, p.rank - r0);
+        if constexpr (R == 1) {
+#pragma unroll
+            for (int k = 0; k < PIECE / E; ++k) {
+                if (k * E >= here || ids[0] < 0) continue;
+                float f[E];
+                floats16<ES>(ahead[k], f);
+#pragma unroll
+                for (int q = 0; q < E; ++q) sum[0] += k * E + q < here ? inner[0][k * E + q] * f[q] : 0.f;
+            }
+            continue;
+        }
         for (int r = 0; r < here; r += E) {
             u32x4_t v = {0, 0, 0, 0};
 #pragma unroll
@@ -234,8 +265,12 @@ hipError_t up(const AdapterParams &p, hipStream_t st)
 bool adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p)
 {
     const int es = (int)dtype_size(dtype);
-    // beside: few rows, or as many as the last pass takes about 10 us for
-    const bool few_rows = grp_is_few(product, es), beside = few_rows || (double)p.rows * p.cols * (8 + p.rank * es) <= 64e6;
+    // beside: few rows, or where the last pass, at 5 TB/s and 3 us for its launch, takes less than the tiles' waiting, 0.7 us for each adapter of 32 rows
+    // (of those that there can be most are taken to be): 256 rows of 256 requests and 32 adapters, 4096 x 4096, 41 us for 50; 2048 rows of four
+    // adapters, 768 x 768, rank 8, 22 for 16
+    const bool few_rows = grp_is_few(product, es);
+    const double rounds = std::ceil(grp_tiles<kForward>(product, 128, 128) / p.places), wait = 0.5 * std::min(p.adapters, 32) * rounds;
+    const bool beside = few_rows || 3 + (double)p.rows * p.cols * (8 + p.rank * es) / 5e6 < wait;
     const int steps = (int)(((int64_t)p.K * es + kStep - 1) / kStep);
     p.tiles = (p.rows + 15) / 16;
     const int64_t work = (int64_t)p.tiles * ((p.rank + 15) / 16);
