@@ -11,26 +11,27 @@
 namespace alt {
 
 struct AdapterParams {
-    const char *x, *a, *b;
+    const char *x, *w, *a, *b;
     const int32_t *adapter;
     const float *scale, *bias;
     char *inner;
-    const float *base;                     // beside: the product, M x N
+    float *base;                           // beside: the product, M x N, base_slices of them to be added
     char *y;
-    int64_t ldx, ldy;                      // bytes between rows
+    int64_t ldx, ldw, ldy;                 // bytes between rows
     int32_t rows, cols, K, rank, adapters, places, relu, out_bf16;
+    // what follows from these (adapters_plan)
+    bool beside, few;                      // few: the product in one launch with the inner sums, beside
     int32_t inner_bytes;                   // of a row (fused: of one of its parts)
-    int32_t slices;                        // beside: parts of the reduction, each with inner sums of its own
+    int32_t slices, base_slices;           // beside: parts of the reductions, each with sums of its own
     int32_t slots, tiles, col_tiles;       // workgroups for a tile's adapters; tiles of rows; tiles of the rank
+    int32_t few_cols;                      // column tiles of 16 to a workgroup of the product
 };
 
-// Sets what the sizes say of `p`: which way, its slices and the layout of its inner sums (the sizes and `places` are given).  True: beside.
-bool adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p);
-size_t adapters_inner_bytes(int dtype, const AdapterParams &p, bool beside);
+void adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p);
+size_t adapters_inner_bytes(int dtype, const AdapterParams &p);
 
-hipError_t adapters_down(int dtype, const AdapterParams &p, bool beside, hipStream_t st);
-// The inner sums and the product in one launch (product: of few rows, fp32 into p.base).
-hipError_t adapters_few(int dtype, const AdapterParams &p, const GroupedParams &product, hipStream_t st);
+hipError_t adapters_down(int dtype, const AdapterParams &p, hipStream_t st);
+hipError_t adapters_few(int dtype, const AdapterParams &p, hipStream_t st);
 hipError_t adapters_up(int dtype, const AdapterParams &p, hipStream_t st);
 
 }  // namespace alt

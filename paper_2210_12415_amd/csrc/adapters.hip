@@ -5,26 +5,138 @@
 namespace alt {
 namespace {
 
-// ---- inner sums ----------------------------------------------------------------------------------------------------------------------
+// ---- products of few rows ------------------------------------------------------------------------------------------------------------
 //
-// Tiles of 16 rows by 16 NT of the rank, once for each adapter that a tile's rows have: prompts have one or two, sequences that decode up to 16, so the
-// adapters of a tile are spread over `slots` workgroups; those of a first adapter come first (a launch's second ones mostly have nothing to do).  Rows come
-// through LDS in steps of 512 bytes, which lanes side by side load side by side: straight into the fragments of the matrix instructions, 16 rows to
-// 16 lanes, every load touches 64 cache lines, and 8192 rows of 4096, rank 32, took 37 us.  Waves share a step's reduction; `slices` share the rest of it.
-constexpr int kStep = 512, kPitch = kStep + 16;            // (rows of LDS 16 bytes more than 64 banks apart)
+// Tiles of 16 RT rows by 16 NT columns whose operands, both with the reduction contiguous, come through LDS in steps of 512 bytes a row, which lanes side by
+// side load side by side.  (Straight into the fragments of the 16-row matrix instructions every load touches 64 cache lines: the inner sums of 8192 rows
+// of 4096, rank 32, took 37 us, so 25; 32 x 4096 x 4096 bf16 14.3, so TIME.)  AHEAD steps are on their way in registers; the waves share a step's reduction, and
+// workgroups the rest of it where there are few.  Chunk c of LDS row r lies at c ^ (r % 16), so that 16 rows' chunks are at distinct banks.
+constexpr int kStep = 512;
 
+template <typename T, int RT, int NT, int NW, int AHEAD>
+struct Core {
+    static constexpr int ES = GrpTraits<T>::ES, SUMS = GrpTraits<T>::SUMS, THREADS = 64 * NW, A = 16 * RT, ROWS = A + 16 * NT;
+    static constexpr int STRIDE = THREADS / (kStep / 16), Q = ROWS / STRIDE, AQ = A / STRIDE;              // rows of a piece of all threads; pieces of a step
+    static constexpr int kLds = 2 * ROWS * kStep;
+    static_assert(A % STRIDE == 0 && AHEAD % 2 == 0 && NW * RT * NT * 1024 <= kLds && kLds <= 64 * 1024, "pieces");
+    typedef typename GrpFew<T>::acc_t acc_t;
+
+    // This wave's sums of rows a (a_rows of them, lda bytes apart) by rows b, over the steps first .. end - 1 of `bytes` of each.  (Behind the last row the
+    // last again, whose sums nobody stores.)
+    static __device__ __forceinline__ void sums(const char *a, int64_t lda, int a_rows, const char *b, int64_t ldb, int b_rows, int bytes, int first, int end, char *lds,
+                                                acc_t (&acc)[RT][NT][SUMS])
+    {
+        const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        const int r = t / (kStep / 16), c = t % (kStep / 16), whole = bytes / kStep, last = min(end, whole);
+        uint32_t from[Q], to[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int row = q * STRIDE + r;
+            from[q] = (uint32_t)(q < AQ ? min(row, a_rows - 1) * (int)lda : min(row - A, b_rows - 1) * (int)ldb) + c * 16;
+            to[q] = row * kStep + (c ^ (row & 15)) * 16;
+        }
+        u32x4_t v[AHEAD][Q];
+        auto load = [&](u32x4_t (&v)[Q], int s) {
+            if (s >= last) return;
+            const char *as = a + (int64_t)s * kStep, *bs = b + (int64_t)s * kStep;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], (q < AQ ? as : bs) + from[q], 16);
+        };
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int s = 0; s < SUMS; ++s) acc[i][j][s] = (acc_t){0, 0, 0, 0};
+        auto multiply = [&](const char *stage) {
+#pragma unroll
+            for (int h = 0; h < kStep / NW / 64; ++h) {
+                const char *at = stage + lane % 16 * kStep + (((wave * (kStep / NW) + h * 64) / 16 + lane / 16) ^ (lane % 16)) * 16;
+                u32x4_t fa[RT];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) fa[i] = *(const u32x4_t *)(at + i * 16 * kStep);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const u32x4_t fb = *(const u32x4_t *)(at + (A + j * 16) * kStep);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) grp_mma16<T>(acc[i][j], fb, fa[i]);
+                }
+            }
+        };
+        auto step = [&](u32x4_t (&v)[Q], int s, char *stage) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) *(u32x4_t *)(stage + to[q]) = v[q];
+            load(v, s + AHEAD);
+            __syncthreads();                               // (and the other stage's readers are through)
+            multiply(stage);
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load(v[i], first + i);
+        for (int s = first; s < last; s += AHEAD) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (s + i < last) step(v[i], s + i, lds + i % 2 * (ROWS * kStep));
+        }
+        if (end > whole && first < end) {                  // what the reduction ends with
+            __syncthreads();
+            const int count = (bytes - whole * kStep - c * 16) / ES;
+#pragma unroll 1
+            for (int q = 0; q < Q; ++q) {
+                const int row = q * STRIDE + r;
+                const char *at = (row < A ? a + (int64_t)min(row, a_rows - 1) * lda : b + (int64_t)min(row - A, b_rows - 1) * ldb) + c * 16;
+                *(u32x4_t *)(lds + row * kStep + (c ^ (row & 15)) * 16) = grp_load_chunk<ES>(at + (int64_t)whole * kStep, count);
+            }
+            __syncthreads();
+            multiply(lds);
+        }
+        __syncthreads();                                   // the stages' readers are through
+    }
+
+    // The waves' sums added in the waves' order: f(row, first of four columns, sum), of the tile.
+    template <typename F>
+    static __device__ __forceinline__ void join(char *lds, acc_t (&acc)[RT][NT][SUMS], F f)
+    {
+        u32x4_t *part = (u32x4_t *)lds;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if constexpr (SUMS == 4) acc[i][j][0] = (acc[i][j][0] + acc[i][j][1]) + (acc[i][j][2] + acc[i][j][3]);
+                part[((wave * RT + i) * NT + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[i][j][0]);
+            }
+        __syncthreads();
+        for (int s = threadIdx.x; s < RT * NT * 64; s += THREADS) {
+            acc_t sum = __builtin_bit_cast(acc_t, part[s]);
+#pragma unroll
+            for (int w = 1; w < NW; ++w) sum += __builtin_bit_cast(acc_t, part[w * RT * NT * 64 + s]);
+            f(s / 64 / NT * 16 + s % 16, s / 64 % NT * 16 + s % 64 / 16 * 4, sum);
+        }
+    }
+};
+
+// Steps of one of `slices` parts of a reduction.
+__device__ __forceinline__ void slice_steps(int bytes, int slices, int slice, int &first, int &end)
+{
+    const int steps = (bytes + kStep - 1) / kStep, per = (steps + slices - 1) / slices;
+    first = slice * per;
+    end = min(first + per, steps);
+}
+
+// ---- inner sums: such a product once for each adapter that 16 rows have
+//
+// Prompts have one or two, sequences that decode up to 16, so the adapters of a tile are spread over `slots` workgroups, those of a first adapter before the
+// others (which mostly have nothing to do).
 template <typename T, int NT, int NW>
 struct Down {
-    static constexpr int ES = GrpTraits<T>::ES, THREADS = 64 * NW, ROWS = 16 + 16 * NT, STRIDE = THREADS / (kStep / 16), Q = ROWS / STRIDE, XQ = 16 / STRIDE, AHEAD = 2,
-                         SUMS = GrpTraits<T>::SUMS;             // STRIDE: rows of a piece of all threads
-    static constexpr int kLds = 2 * ROWS * kPitch;
-    static_assert(16 % STRIDE == 0 && AHEAD % 2 == 0 && NW * NT * 1024 <= kLds, "pieces");
+    using C = Core<T, 1, NT, NW, 2>;
+    static constexpr int ES = C::ES, kLds = C::kLds;
 
     // slices == 0: of the fused form (one slice, in bf16 in two parts)
     static __device__ __forceinline__ void run(const AdapterParams &p, uint32_t wg, char *lds)
     {
         constexpr int PARTS = ES == 2 ? 2 : 1;
-        const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        const int lane = threadIdx.x & 63;
         const uint32_t slices = max(p.slices, 1);
         const int col0 = (int)(wg % (uint32_t)p.col_tiles) * 16 * NT;
         uint32_t rest = wg / (uint32_t)p.col_tiles;
@@ -36,71 +148,17 @@ struct Down {
         const int id = p.adapter[row0 + min(lane % 16, rows_left - 1)];
         uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
         const int64_t row_bytes = (int64_t)p.K * ES;
-        const int bytes = (int)row_bytes, whole = bytes / kStep, steps = (bytes + kStep - 1) / kStep, per = (steps + (int)slices - 1) / (int)slices, first = slice * per, end = min(first + per, steps);
+        int first, end;
+        slice_steps((int)row_bytes, (int)slices, slice, first, end);
         for (int n = 0; left; ++n) {
             const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
             left &= ~__ballot(id == one);
             if (n % p.slots != slot) continue;
-            // A thread's pieces of a step, 16 bytes each: XQ of rows of x, then of the adapter (behind the last row the last again, which nobody stores).
-            const char *x = p.x + (int64_t)row0 * p.ldx, *a = p.a + ((int64_t)one * p.rank + col0) * row_bytes;
-            const int r = t / (kStep / 16), c = t % (kStep / 16) * 16;
-            uint32_t from[Q];
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-                from[q] = q < XQ ? (uint32_t)(min(q * STRIDE + r, rows_left - 1) * (int)p.ldx + c)
-                                 : (uint32_t)(min(q * STRIDE + r - 16, p.rank - col0 - 1) * (int)row_bytes + c);
-            char *to = lds + r * kPitch + c;
-            u32x4_t v[AHEAD][Q];
-            const int last = min(end, whole);              // of the whole steps
-            auto load = [&](u32x4_t (&v)[Q], int s) {
-                if (s >= last) return;
-                const char *xs = x + (int64_t)s * kStep, *as = a + (int64_t)s * kStep;
-#pragma unroll
-                for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], (q < XQ ? xs : as) + from[q], 16);
-            };
-            typename GrpFew<T>::acc_t acc[NT][SUMS];
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int s = 0; s < SUMS; ++s) acc[j][s] = (typename GrpFew<T>::acc_t){0, 0, 0, 0};
-            auto multiply = [&](const char *stage) {
-#pragma unroll
-                for (int h = 0; h < kStep / NW / 64; ++h) {
-                    const char *at = stage + lane % 16 * kPitch + wave * (kStep / NW) + h * 64 + lane / 16 * 16;
-                    const u32x4_t fa = *(const u32x4_t *)at;
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) grp_mma16<T>(acc[j], *(const u32x4_t *)(at + (16 + j * 16) * kPitch), fa);
-                }
-            };
-            auto step = [&](u32x4_t (&v)[Q], int s, int stage) {
-#pragma unroll
-                for (int q = 0; q < Q; ++q) *(u32x4_t *)(to + stage + q * STRIDE * kPitch) = v[q];
-                load(v, s + AHEAD);
-                __syncthreads();                           // (and the other stage's readers are through)
-                multiply(lds + stage);
-            };
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) load(v[i], first + i);
-            for (int s = first; s < last; s += AHEAD) {
-#pragma unroll
-                for (int i = 0; i < AHEAD; ++i)
-                    if (s + i < last) step(v[i], s + i, i % 2 * (ROWS * kPitch));
-            }
-            if (end > whole && first < end) {              // what the reduction ends with
-                __syncthreads();
-                const int count = (bytes - whole * kStep - c) / ES;
-#pragma unroll 1
-                for (int q = 0; q < Q; ++q) {
-                    const char *at = (q < XQ ? x + (int64_t)min(q * STRIDE + r, rows_left - 1) * p.ldx : a + (int64_t)min(q * STRIDE + r - 16, p.rank - col0 - 1) * row_bytes) + c;
-                    *(u32x4_t *)(to + q * STRIDE * kPitch) = grp_load_chunk<ES>(at + (int64_t)whole * kStep, count);
-                }
-                __syncthreads();
-                multiply(lds);
-            }
-            __syncthreads();                               // the stages' readers are through
+            typename C::acc_t acc[1][NT][C::SUMS];
+            C::sums(p.x + (int64_t)row0 * p.ldx, p.ldx, rows_left, p.a + ((int64_t)one * p.rank + col0) * row_bytes, row_bytes, p.rank - col0, (int)row_bytes, first, end, lds, acc);
             const float by = p.scale ? p.scale[one] : 1.f;
-            grp_few_join<T, NT, NW>(*(u32x4_t (*)[NW * NT * 64])lds, acc, lane, wave, [&](int tile, int l, const typename GrpFew<T>::acc_t &sum) {
-                const int row = row0 + l % 16, col = col0 + tile * 16 + l / 16 * 4;
+            C::join(lds, acc, [&](int r, int at, const typename C::acc_t &sum) {
+                const int row = row0 + r, col = col0 + at;
                 if (row >= p.rows || p.adapter[row] != one) return;
                 float f[4];
 #pragma unroll
@@ -133,14 +191,39 @@ __global__ __launch_bounds__(64 * NW, 3) void adapters_down_kernel(const Adapter
     Down<T, NT, NW>::run(p, blockIdx.x, (char *)lds);
 }
 
-// The inner sums in the first `down` workgroups, the product of few rows in the others: neither needs the other.
-template <typename T, int NT, int NW, int BATCH, bool DW>
-__global__ __launch_bounds__(64 * NW) void adapters_few_kernel(const AdapterParams p, const GroupedParams product, uint32_t down)
+// The inner sums in the first `down` workgroups, the shared product in the others: neither needs the other.  Column tiles that run together are one XCD's
+// (workgroups go to the XCDs in turn), rows first, so that a tile of w is read from memory once.
+template <typename T, int RT, int NT>
+__global__ __launch_bounds__(512) void adapters_few_kernel(const AdapterParams p, uint32_t down)
 {
-    __shared__ uint4 lds[Down<T, 1, NW>::kLds / 16];
-    static_assert(NW * NT * 1024 <= sizeof lds, "LDS");
-    if (blockIdx.x < down) Down<T, 1, NW>::run(p, blockIdx.x, (char *)lds);
-    else grp_few<T, NT, NW, BATCH, DW>(product, blockIdx.x - down, *(u32x4_t (*)[NW * NT * 64])lds);
+    using C = Core<T, RT, NT, 8, 4>;
+    constexpr int ES = C::ES;
+    __shared__ uint4 lds[(C::kLds > Down<T, 1, 8>::kLds ? C::kLds : Down<T, 1, 8>::kLds) / 16];
+    if (blockIdx.x < down) {
+        Down<T, 1, 8>::run(p, blockIdx.x, (char *)lds);
+        return;
+    }
+    const uint32_t wg = blockIdx.x - down, row_tiles = (uint32_t)(p.rows + 16 * RT - 1) / (16 * RT), col_tiles = (uint32_t)(p.cols + 16 * NT - 1) / (16 * NT);
+    const uint32_t tiles = row_tiles * col_tiles * (uint32_t)p.base_slices, per = (tiles + 7) / 8, tile = (wg & 7) * per + (wg >> 3);
+    if ((wg >> 3) >= per || tile >= tiles) return;
+    const int row0 = (int)(tile % row_tiles) * 16 * RT, col0 = (int)(tile / row_tiles % col_tiles) * 16 * NT, slice = (int)(tile / row_tiles / col_tiles);
+    int first, end;
+    slice_steps(p.K * ES, p.base_slices, slice, first, end);
+    typename C::acc_t acc[RT][NT][C::SUMS];
+    C::sums(p.x + (int64_t)row0 * p.ldx, p.ldx, p.rows - row0, p.w + (int64_t)col0 * p.ldw, p.ldw, p.cols - col0, p.K * ES, first, end, (char *)lds, acc);
+    float *base = p.base + (int64_t)slice * p.rows * p.cols;
+    C::join((char *)lds, acc, [&](int r, int at, const typename C::acc_t &sum) {
+        const int row = row0 + r, col = col0 + at;
+        if (row >= p.rows || col >= p.cols) return;
+        float *to = base + (int64_t)row * p.cols + col;
+        if (p.cols % 4 == 0) {
+            *(f32x4_t *)to = (f32x4_t){sum[0], sum[1], sum[2], sum[3]};
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (col + q < p.cols) to[q] = sum[q];
+        }
+    });
 }
 
 // ---- the last pass over few rows -------------------------------------------------------------------------------------------------------
@@ -161,7 +244,11 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p,
     }
     float sum[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i) sum[i] = row0 + i < p.rows && col < p.cols ? p.base[(int64_t)(row0 + i) * p.cols + col] : 0.f;
+    for (int i = 0; i < R; ++i) {
+        sum[i] = 0.f;
+        if (row0 + i < p.rows && col < p.cols)
+            for (int s = 0; s < p.base_slices; ++s) sum[i] += p.base[((int64_t)s * p.rows + row0 + i) * p.cols + col];
+    }
     const float bias = p.bias && col < p.cols ? p.bias[col] : 0.f;
     const char *b = p.b + (int64_t)min(col, p.cols - 1) * p.rank * ES;
     const int64_t b_adapter = (int64_t)p.cols * p.rank * ES;
@@ -232,23 +319,23 @@ hipError_t down(AdapterParams p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <typename T, int NT, int NW>
-hipError_t few(AdapterParams p, GroupedParams product, hipStream_t st)
+template <typename T, int RT, int NT>
+hipError_t few(AdapterParams p, hipStream_t st)
 {
     p.col_tiles = (p.rank + 15) / 16;
-    const int64_t downs = ((int64_t)p.tiles * p.col_tiles * p.slices * p.slots + 7) / 8 * 8;       // (the product's workgroups go to their XCDs as ever)
-    unsigned grid;
-    const hipError_t e = grp_grid<kForward, 16, 16 * NT>(product, 64 * NW, &grid);
-    if (e != hipSuccess) return e;
-    if ((grid + downs) * 64 * NW > 0xffffffffll) return hipErrorInvalidConfiguration;
-    if constexpr (GrpTraits<T>::ES < 4) {
-        if (((uint64_t)product.a | (uint64_t)product.b | (uint64_t)product.lda | (uint64_t)product.ldb) % 4) {
-            hipLaunchKernelGGL((adapters_few_kernel<T, NT, NW, 2, false>), dim3(grid + (unsigned)downs), dim3(64 * NW), 0, st, p, product, (uint32_t)downs);
-            return hipGetLastError();
-        }
-    }
-    hipLaunchKernelGGL((adapters_few_kernel<T, NT, NW, 2, true>), dim3(grid + (unsigned)downs), dim3(64 * NW), 0, st, p, product, (uint32_t)downs);
+    const int64_t downs = ((int64_t)p.tiles * p.col_tiles * p.slices * p.slots + 7) / 8 * 8;
+    const int64_t tiles = ((int64_t)p.rows + 16 * RT - 1) / (16 * RT) * ((p.cols + 16 * NT - 1) / (16 * NT)) * p.base_slices;
+    const int64_t n = downs + (tiles + 7) / 8 * 8;
+    if (n * 512 > 0xffffffffll) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((adapters_few_kernel<T, RT, NT>), dim3((unsigned)n), dim3(512), 0, st, p, (uint32_t)downs);
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t few(const AdapterParams &p, hipStream_t st)
+{
+    if (p.rows <= 16) return few<T, 1, 1>(p, st);
+    return p.few_cols == 1 ? few<T, 2, 1>(p, st) : few<T, 2, 2>(p, st);
 }
 
 template <int ES, int R>
@@ -262,42 +349,48 @@ hipError_t up(const AdapterParams &p, hipStream_t st)
 
 }  // namespace
 
-bool adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p)
+void adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p)
 {
     const int es = (int)dtype_size(dtype);
-    // beside: few rows, or where the last pass, at 5 TB/s and 3 us for its launch, takes less than the tiles' waiting, 0.7 us for each adapter of 32 rows
-    // (of those that there can be most are taken to be): 256 rows of 256 requests and 32 adapters, 4096 x 4096, 41 us for 50; 2048 rows of four
-    // adapters, 768 x 768, rank 8, 22 for 16
-    const bool few_rows = grp_is_few(product, es);
-    const double rounds = std::ceil(grp_tiles<kForward>(product, 128, 128) / p.places), wait = 0.5 * std::min(p.adapters, 32) * rounds;
-    const bool beside = few_rows || 3 + (double)p.rows * p.cols * (8 + p.rank * es) / 5e6 < wait;
-    const int steps = (int)(((int64_t)p.K * es + kStep - 1) / kStep);
+    const double places = p.places;
+    const int64_t steps = ((int64_t)p.K * es + kStep - 1) / kStep;
+    const int64_t rt = p.rows <= 16 ? 1 : 2, row_tiles = (p.rows + 16 * rt - 1) / (16 * rt);
+    p.few_cols = rt == 2 && row_tiles * ((p.cols + 31) / 32) >= p.places ? 2 : 1;
+    const int64_t tiles = row_tiles * ((p.cols + 16 * p.few_cols - 1) / (16 * p.few_cols));
+    // Times in us.  The last pass runs at 5 TB/s behind its launch; the fused tiles wait 0.7 for each adapter of 32 rows, and most of those that there can be
+    // are taken to be.  The product of few rows takes its tiles' loads from the caches at 13 TB/s (fp32, whose matrix instructions take longer, at 7); others
+    // come after the launch of the inner sums.  bf16, rank 16, either way: 128 x 4096 x 4096 30 of few rows and 36 otherwise, 256 x 4096 x 4096 48 and 41, 256 x
+    // 1024 x 4096 19 and 34, 200 x 8192 x 2048 42 and 31, 64 x 8192 x 8192 56 and 63; fp32 60 x 4096 x 4096 43 and 105.
+    const double rounds = std::ceil(grp_tiles<kForward>(product, 128, 128) / places), wait = 0.5 * std::min(p.adapters, 32) * rounds;
+    const double last = 3 + (double)p.rows * p.cols * (8 + p.rank * es) / 5e6, loads = (double)tiles * 16 * (rt + p.few_cols) * p.K * es;
+    GrpTime t;
+    (void)grp_choose<kForward>(product, es, &t);
+    const double few = 4 + loads / (es == 4 ? 7e6 : 13e6) + last;
+    const double other = 10 + (es == 4 ? 8 + 2.0 * p.rows * p.cols * p.K / 50e6 : t.fixed + t.reduction) + std::min(last, wait);
+    p.few = p.rows <= 16 || few < other;
+    p.beside = p.few || last < wait;
+    // (as many workgroups as the chip has places for share a product's reduction, each with eight steps at least)
+    p.base_slices = p.few ? (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, steps / 8), p.places / tiles)) : 1;
     p.tiles = (p.rows + 15) / 16;
     const int64_t work = (int64_t)p.tiles * ((p.rank + 15) / 16);
     // workgroups for a tile's adapters, two at least and up to as many as the chip has places for
     p.slots = (int)std::min<int64_t>(std::min(std::min(p.adapters, 16), p.rows), std::max<int64_t>(2, p.places / work));
-    p.slices = !beside ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(8, steps), p.places / (work * p.slots)));
-    p.inner_bytes = beside ? (p.rank + 15) / 16 * 64 : (p.rank * es + 31) / 32 * 32;
-    return beside;
+    p.slices = !p.beside ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, steps), p.places / (work * p.slots)));
+    p.inner_bytes = p.beside ? (p.rank + 15) / 16 * 64 : (p.rank * es + 31) / 32 * 32;
 }
 
-size_t adapters_inner_bytes(int dtype, const AdapterParams &p, bool beside)
+size_t adapters_inner_bytes(int dtype, const AdapterParams &p)
 {
-    return (size_t)p.rows * p.inner_bytes * (beside ? p.slices : dtype == ALT_BF16 ? 2 : 1);
+    return (size_t)p.rows * p.inner_bytes * (p.beside ? p.slices : dtype == ALT_BF16 ? 2 : 1);
 }
 
-hipError_t adapters_down(int dtype, const AdapterParams &p, bool, hipStream_t st)
+hipError_t adapters_down(int dtype, const AdapterParams &p, hipStream_t st)
 {
     if (dtype == ALT_F32) return p.rank <= 16 ? down<float, 1, 4>(p, st) : down<float, 2, 4>(p, st);
     return p.rank <= 16 ? down<bf16_tag, 1, 4>(p, st) : down<bf16_tag, 2, 4>(p, st);
 }
 
-hipError_t adapters_few(int dtype, const AdapterParams &p, const GroupedParams &product, hipStream_t st)
-{
-    const bool narrow = grp_tiles<kForward>(product, 16, 16) <= product.places;                // (as in grouped_run)
-    if (dtype == ALT_F32) return narrow ? few<float, 1, 8>(p, product, st) : few<float, 2, 4>(p, product, st);
-    return narrow ? few<bf16_tag, 1, 8>(p, product, st) : few<bf16_tag, 2, 4>(p, product, st);
-}
+hipError_t adapters_few(int dtype, const AdapterParams &p, hipStream_t st) { return dtype == ALT_F32 ? few<float>(p, st) : few<bf16_tag>(p, st); }
 
 hipError_t adapters_up(int dtype, const AdapterParams &p, hipStream_t st)
 {

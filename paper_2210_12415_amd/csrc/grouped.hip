@@ -243,7 +243,6 @@ alt_status_t check_adapters(alt_handle_t h, const char *call, const alt_adapters
 struct AdapterCall {
     GroupedParams product;
     AdapterParams adapters;
-    bool beside, few;
     size_t inner, base, pack;
 };
 
@@ -255,6 +254,8 @@ AdapterCall adapter_call(alt_handle_t h, const alt_adapters_desc_t *d, const alt
     if (p.places == 0) p.places = 256;
     AdapterParams &q = c.adapters;
     q.x = (const char *)x;
+    q.w = (const char *)w;
+    q.ldw = p.ldb;
     q.y = (char *)y;
     q.ldx = p.lda;
     q.ldy = p.ldy;
@@ -262,11 +263,10 @@ AdapterCall adapter_call(alt_handle_t h, const alt_adapters_desc_t *d, const alt
     q.rank = d->rank; q.adapters = d->adapters; q.places = p.places;
     q.relu = (l.epilogue & ALT_EPI_RELU) != 0;
     q.out_bf16 = l.out_dtype == ALT_BF16;
-    c.beside = adapters_plan(l.in_dtype, p, q);
-    c.few = grp_is_few(p, (int)in_size(l.in_dtype));
-    c.inner = adapters_inner_bytes(l.in_dtype, q, c.beside);
-    c.base = c.beside ? (size_t)l.rows * l.N * 4 : 0;
-    if (c.beside) {                                        // the product's results: dense fp32
+    adapters_plan(l.in_dtype, p, q);
+    c.inner = adapters_inner_bytes(l.in_dtype, q);
+    c.base = q.beside ? (size_t)q.base_slices * l.rows * l.N * 4 : 0;
+    if (q.beside) {                                        // the product's results: dense fp32
         p.ldy = l.N * 4;
         p.flags = l.N % 4 == 0 ? kGrpWhole : 0;
     } else {
@@ -275,7 +275,7 @@ AdapterCall adapter_call(alt_handle_t h, const alt_adapters_desc_t *d, const alt
         p.inner_bytes = q.inner_bytes;
         if (q.relu) p.flags |= kGrpRelu;
     }
-    c.pack = pack_bytes(kForward, l.in_dtype, p);
+    c.pack = q.few ? 0 : pack_bytes(kForward, l.in_dtype, p);
     return c;
 }
 
@@ -414,8 +414,8 @@ extern "C" alt_status_t alt_gemm_adapters(alt_handle_t h, const alt_adapters_des
     q.scale = scale;
     q.bias = l.epilogue & ALT_EPI_BIAS ? bias : nullptr;
     q.inner = ws;
-    if (c.beside) {
-        q.base = (const float *)(ws + c.inner);
+    if (q.beside) {
+        q.base = (float *)(ws + c.inner);
         p.y = ws + c.inner;
     } else {
         p.bias = q.bias;
@@ -424,16 +424,16 @@ extern "C" alt_status_t alt_gemm_adapters(alt_handle_t h, const alt_adapters_des
         p.up = (const char *)b;
     }
     hipError_t e;
-    if (c.beside && c.few) {
-        e = adapters_few(l.in_dtype, q, p, st);
+    if (q.few) {
+        e = adapters_few(l.in_dtype, q, st);
     } else {
-        ALT_CHECK_HIP(h, adapters_down(l.in_dtype, q, c.beside, st));
+        ALT_CHECK_HIP(h, adapters_down(l.in_dtype, q, st));
         char *more = ws + c.inner + (c.base + 15) / 16 * 16;
         s = run(h, "alt_gemm_adapters", l.in_dtype, kForward, p, more, (size_t)((char *)workspace + ws_bytes - more), st);
         if (s != ALT_OK) return s;
         e = hipSuccess;
     }
-    if (e == hipSuccess && c.beside) e = adapters_up(l.in_dtype, q, st);
+    if (e == hipSuccess && q.beside) e = adapters_up(l.in_dtype, q, st);
     if (e == hipErrorInvalidConfiguration) return fail(h, ALT_UNSUPPORTED, "alt_gemm_adapters: more workgroups than a launch holds");
     ALT_CHECK_HIP(h, e);
     return ALT_OK;
