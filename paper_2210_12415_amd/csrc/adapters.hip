@@ -9,15 +9,15 @@ namespace {
 //
 // Tiles of 16 RT rows by 16 NT columns whose operands, both with the reduction contiguous, come through LDS in steps of 512 bytes a row, which lanes side by
 // side load side by side.  (Straight into the fragments of the 16-row matrix instructions every load touches 64 cache lines: the inner sums of 8192 rows
-// of 4096, rank 32, took 37 us, so 25; 32 x 4096 x 4096 bf16 14.3, so TIME.)  AHEAD steps are on their way in registers; the waves share a step's reduction, and
+// of 4096, rank 32, took 37 us, so 25; the sums and the product of 32 x 4096 x 4096 bf16, rank 16, 14.3, so 12.5.)  AHEAD steps are on their way in registers; the waves share a step's reduction, and
 // workgroups the rest of it where there are few.  Chunk c of LDS row r lies at c ^ (r % 16), so that 16 rows' chunks are at distinct banks.
 constexpr int kStep = 512;
 
 template <typename T, int RT, int NT, int NW, int AHEAD>
 struct Core {
-    static constexpr int ES = GrpTraits<T>::ES, SUMS = GrpTraits<T>::SUMS, THREADS = 64 * NW, A = 16 * RT, ROWS = A + 16 * NT;
-    static constexpr int STRIDE = THREADS / (kStep / 16), Q = ROWS / STRIDE, AQ = A / STRIDE;              // rows of a piece of all threads; pieces of a step
-    static constexpr int kLds = 2 * ROWS * kStep;
+    static constexpr int STEP = kStep, ES = GrpTraits<T>::ES, SUMS = GrpTraits<T>::SUMS, THREADS = 64 * NW, A = 16 * RT, ROWS = A + 16 * NT;
+    static constexpr int STRIDE = THREADS / (STEP / 16), Q = ROWS / STRIDE, AQ = A / STRIDE;              // rows of a piece of all threads; pieces of a step
+    static constexpr int kLds = 2 * ROWS * STEP;
     static_assert(A % STRIDE == 0 && AHEAD % 2 == 0 && NW * RT * NT * 1024 <= kLds && kLds <= 64 * 1024, "pieces");
     typedef typename GrpFew<T>::acc_t acc_t;
 
@@ -27,18 +27,17 @@ struct Core {
                                                 acc_t (&acc)[RT][NT][SUMS])
     {
         const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-        const int r = t / (kStep / 16), c = t % (kStep / 16), whole = bytes / kStep, last = min(end, whole);
+        const int r = t / (STEP / 16), c = t % (STEP / 16), whole = bytes / STEP, last = min(end, whole);
         uint32_t from[Q], to[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int row = q * STRIDE + r;
             from[q] = (uint32_t)(q < AQ ? min(row, a_rows - 1) * (int)lda : min(row - A, b_rows - 1) * (int)ldb) + c * 16;
-            to[q] = row * kStep + (c ^ (row & 15)) * 16;
+            to[q] = row * STEP + (c ^ (row & 15)) * 16;
         }
         u32x4_t v[AHEAD][Q];
         auto load = [&](u32x4_t (&v)[Q], int s) {
-            if (s >= last) return;
-            const char *as = a + (int64_t)s * kStep, *bs = b + (int64_t)s * kStep;
+            const char *as = a + (int64_t)s * STEP, *bs = b + (int64_t)s * STEP;
 #pragma unroll
             for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], (q < AQ ? as : bs) + from[q], 16);
         };
@@ -50,41 +49,50 @@ struct Core {
                 for (int s = 0; s < SUMS; ++s) acc[i][j][s] = (acc_t){0, 0, 0, 0};
         auto multiply = [&](const char *stage) {
 #pragma unroll
-            for (int h = 0; h < kStep / NW / 64; ++h) {
-                const char *at = stage + lane % 16 * kStep + (((wave * (kStep / NW) + h * 64) / 16 + lane / 16) ^ (lane % 16)) * 16;
+            for (int h = 0; h < STEP / NW / 64; ++h) {
+                const char *at = stage + lane % 16 * STEP + (((wave * (STEP / NW) + h * 64) / 16 + lane / 16) ^ (lane % 16)) * 16;
                 u32x4_t fa[RT];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) fa[i] = *(const u32x4_t *)(at + i * 16 * kStep);
+                for (int i = 0; i < RT; ++i) fa[i] = *(const u32x4_t *)(at + i * 16 * STEP);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    const u32x4_t fb = *(const u32x4_t *)(at + (A + j * 16) * kStep);
+                    const u32x4_t fb = *(const u32x4_t *)(at + (A + j * 16) * STEP);
 #pragma unroll
                     for (int i = 0; i < RT; ++i) grp_mma16<T>(acc[i][j], fb, fa[i]);
                 }
             }
         };
-        auto step = [&](u32x4_t (&v)[Q], int s, char *stage) {
+        auto step = [&](u32x4_t (&v)[Q], int s, char *stage, auto MORE) {
 #pragma unroll
             for (int q = 0; q < Q; ++q) *(u32x4_t *)(stage + to[q]) = v[q];
-            load(v, s + AHEAD);
-            __syncthreads();                               // (and the other stage's readers are through)
+            if (decltype(MORE)::value || s + AHEAD < last) load(v, s + AHEAD);
+            lds_barrier();                                 // (and the other stage's readers are through; the loads stay on their way)
             multiply(stage);
         };
+        // (without branches around the loads while there are more, so that no step waits for more of them than it needs: 8192 rows of 4096, rank 32, 25 us
+        // with them; what there is none of is the last again)
+        if (first < last) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) load(v[i], first + i);
-        for (int s = first; s < last; s += AHEAD) {
+            for (int i = 0; i < AHEAD; ++i) load(v[i], min(first + i, last - 1));
+            int s = first;
+            for (; s + 2 * AHEAD <= last; s += AHEAD) {
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i)
-                if (s + i < last) step(v[i], s + i, lds + i % 2 * (ROWS * kStep));
+                for (int i = 0; i < AHEAD; ++i) step(v[i], s + i, lds + i % 2 * (ROWS * STEP), std::true_type{});
+            }
+            for (; s < last; s += AHEAD) {
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+                    if (s + i < last) step(v[i], s + i, lds + i % 2 * (ROWS * STEP), std::false_type{});
+            }
         }
         if (end > whole && first < end) {                  // what the reduction ends with
             __syncthreads();
-            const int count = (bytes - whole * kStep - c * 16) / ES;
+            const int count = (bytes - whole * STEP - c * 16) / ES;
 #pragma unroll 1
             for (int q = 0; q < Q; ++q) {
                 const int row = q * STRIDE + r;
                 const char *at = (row < A ? a + (int64_t)min(row, a_rows - 1) * lda : b + (int64_t)min(row - A, b_rows - 1) * ldb) + c * 16;
-                *(u32x4_t *)(lds + row * kStep + (c ^ (row & 15)) * 16) = grp_load_chunk<ES>(at + (int64_t)whole * kStep, count);
+                *(u32x4_t *)(lds + row * STEP + (c ^ (row & 15)) * 16) = grp_load_chunk<ES>(at + (int64_t)whole * STEP, count);
             }
             __syncthreads();
             multiply(lds);
@@ -130,7 +138,7 @@ __device__ __forceinline__ void slice_steps(int bytes, int slices, int slice, in
 template <typename T, int NT, int NW>
 struct Down {
     using C = Core<T, 1, NT, NW, 2>;
-    static constexpr int ES = C::ES, kLds = C::kLds;
+    static constexpr int ES = C::ES, ROWS = C::A, kLds = C::kLds;
 
     // slices == 0: of the fused form (one slice, in bf16 in two parts)
     static __device__ __forceinline__ void run(const AdapterParams &p, uint32_t wg, char *lds)
@@ -140,13 +148,13 @@ struct Down {
         const uint32_t slices = max(p.slices, 1);
         const int col0 = (int)(wg % (uint32_t)p.col_tiles) * 16 * NT;
         uint32_t rest = wg / (uint32_t)p.col_tiles;
-        const int row0 = (int)(rest % (uint32_t)p.tiles) * 16;
+        const int row0 = (int)(rest % (uint32_t)p.tiles) * ROWS;
         rest /= (uint32_t)p.tiles;
         const int slice = (int)(rest % slices), slot = (int)(rest / slices);
         if (slot >= p.slots) return;
         const int rows_left = p.rows - row0;
-        const int id = p.adapter[row0 + min(lane % 16, rows_left - 1)];
-        uint64_t left = __ballot(lane % 16 < rows_left && id >= 0 && id < p.adapters);
+        const int id = p.adapter[row0 + min(lane % ROWS, rows_left - 1)];
+        uint64_t left = __ballot(lane % ROWS < rows_left && id >= 0 && id < p.adapters);
         const int64_t row_bytes = (int64_t)p.K * ES;
         int first, end;
         slice_steps((int)row_bytes, (int)slices, slice, first, end);
@@ -184,11 +192,12 @@ struct Down {
     }
 };
 
-template <typename T, int NT, int NW>
-__global__ __launch_bounds__(64 * NW, 3) void adapters_down_kernel(const AdapterParams p)
+template <typename T, int NT>
+__global__ __launch_bounds__(256, 3) void adapters_down_kernel(const AdapterParams p)
 {
-    __shared__ uint4 lds[Down<T, NT, NW>::kLds / 16];
-    Down<T, NT, NW>::run(p, blockIdx.x, (char *)lds);
+    using D = Down<T, NT, 4>;
+    __shared__ uint4 lds[D::kLds / 16];
+    D::run(p, blockIdx.x, (char *)lds);
 }
 
 // The inner sums in the first `down` workgroups, the shared product in the others: neither needs the other.  Column tiles that run together are one XCD's
@@ -309,13 +318,13 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p,
     }
 }
 
-template <typename T, int NT, int NW>
+template <typename T, int NT>
 hipError_t down(AdapterParams p, hipStream_t st)
 {
     p.col_tiles = (p.rank + 16 * NT - 1) / (16 * NT);
     const int64_t n = (int64_t)p.tiles * p.col_tiles * std::max(p.slices, 1) * p.slots;
-    if (n * 64 * NW > 0xffffffffll) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((adapters_down_kernel<T, NT, NW>), dim3((unsigned)n), dim3(64 * NW), 0, st, p);
+    if (n * 256 > 0xffffffffll) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((adapters_down_kernel<T, NT>), dim3((unsigned)n), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
@@ -359,8 +368,9 @@ void adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p)
     const int64_t tiles = row_tiles * ((p.cols + 16 * p.few_cols - 1) / (16 * p.few_cols));
     // Times in us.  The last pass runs at 5 TB/s behind its launch; the fused tiles wait 0.7 for each adapter of 32 rows, and most of those that there can be
     // are taken to be.  The product of few rows takes its tiles' loads from the caches at 13 TB/s (fp32, whose matrix instructions take longer, at 7); others
-    // come after the launch of the inner sums.  bf16, rank 16, either way: 128 x 4096 x 4096 30 of few rows and 36 otherwise, 256 x 4096 x 4096 48 and 41, 256 x
-    // 1024 x 4096 19 and 34, 200 x 8192 x 2048 42 and 31, 64 x 8192 x 8192 56 and 63; fp32 60 x 4096 x 4096 43 and 105.
+    // come after the launch of the inner sums.  bf16, rank 16, either way: 128 x 4096 x 4096 30 of few rows and 36 otherwise, 256 x 4096 x 4096 44 and 37, 256 x
+    // 1024 x 4096 20 and 33, 200 x 8192 x 2048 41 and 30, 64 x 8192 x 8192 56 and 62 (the one of these that is
+    // taken on the slower side); fp32 60 x 4096 x 4096 43 and 101.
     const double rounds = std::ceil(grp_tiles<kForward>(product, 128, 128) / places), wait = 0.5 * std::min(p.adapters, 32) * rounds;
     const double last = 3 + (double)p.rows * p.cols * (8 + p.rank * es) / 5e6, loads = (double)tiles * 16 * (rt + p.few_cols) * p.K * es;
     GrpTime t;
@@ -386,8 +396,8 @@ size_t adapters_inner_bytes(int dtype, const AdapterParams &p)
 
 hipError_t adapters_down(int dtype, const AdapterParams &p, hipStream_t st)
 {
-    if (dtype == ALT_F32) return p.rank <= 16 ? down<float, 1, 4>(p, st) : down<float, 2, 4>(p, st);
-    return p.rank <= 16 ? down<bf16_tag, 1, 4>(p, st) : down<bf16_tag, 2, 4>(p, st);
+    if (dtype == ALT_F32) return p.rank <= 16 ? down<float, 1>(p, st) : down<float, 2>(p, st);
+    return p.rank <= 16 ? down<bf16_tag, 1>(p, st) : down<bf16_tag, 2>(p, st);
 }
 
 hipError_t adapters_few(int dtype, const AdapterParams &p, hipStream_t st) { return dtype == ALT_F32 ? few<float>(p, st) : few<bf16_tag>(p, st); }
