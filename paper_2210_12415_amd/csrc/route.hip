@@ -143,31 +143,32 @@ __device__ __forceinline__ double exact_sum(const RouteParams &p, const float (&
     return row_sum<L>(sum);
 }
 
-// Which of a lane's V experts are of the row's worthiest groups, as bits.  In the row's LDS: the worths of the experts (or of each lane's two best, where a
-// lane's experts are of one group), in their place those of the groups, in the place of those which groups are kept.  `apart`: by how much the least
+template <typename F>
+__device__ __forceinline__ void better_of(F v, F &one, F &two)
+{
+    two = v > one ? one : v > two ? v : two;
+    one = v > one ? v : one;
+}
+
+// Which of a lane's V experts are of the row's worthiest groups, as bits.  In the row's LDS: the worths of the experts (or of each lane's two best, of
+// `best_two`, where a lane's experts are of one group), in their place those of the groups, in the place of those which groups are kept.  `apart`: by how much the least
 // worthy group that is kept is worth more than the worthiest that is not.
-template <typename F, int L, int V, typename W>
-__device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, F *worth, W worth_at, F &apart)
+template <typename F, int L, int V, typename W, typename B>
+__device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, F *worth, W worth_at, B best_two, F &apart)
 {
     const F none = -INFINITY;
     const int each = (int)p.each.d;
     const bool lanes = each % V == 0;
     const int per = lanes ? each / V * 2 : each;           // numbers of a group
-    auto better_of = [](F v, F &one, F &two) {
-        two = v > one ? one : v > two ? v : two;
-        one = v > one ? v : one;
-    };
     auto at = [](int i) { return i + (i >> 5); };          // (groups of 32 numbers begin at different banks)
     F one = none, two = none;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const F v = worth_at(i);
-        if (lanes) better_of(v, one, two);
-        else worth[at(sub * V + i)] = v;
-    }
     if (lanes) {
+        best_two(one, two);
         worth[at(sub * 2)] = one;
         worth[at(sub * 2 + 1)] = two;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) worth[at(sub * V + i)] = worth_at(i);
     }
     wave_sync();
     for (int g = sub; g < p.groups; g += L) {
@@ -235,14 +236,30 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
         near = (p.softmax ? 0x1.8p-17f * part : 0x1p-20f) + 0x1p-120f;
         if (grouped) {
             float apart, size = 0.f;
-            kept = kept_experts<float, L, V>(p, sub, (float *)lds, [&](int i) { return key[i]; }, apart);
+            float one = none, two = none;
+#pragma unroll
+            for (int i = 0; i < V; ++i) better_of(key[i], one, two);
+            kept = kept_experts<float, L, V>(p, sub, (float *)lds, [&](int i) { return key[i]; }, [&](float &a, float &b) { a = one; b = two; }, apart);
 #pragma unroll
             for (int i = 0; i < V; ++i) size = fmaxf(size, key[i] == none ? 0.f : __builtin_fabsf(key[i]));
             size = row_max<L>(size);
             if (__ballot(!(apart > 4.f * near + size * 0x1p-20f))) {
                 const double sum = exact_sum<L, V>(p, l, st);
                 double exactly;
-                kept = kept_experts<double, L, V>(p, sub, (double *)lds, [&](int i) { return worth_of<double>(p, l[i], p.bias ? p.bias[min(e0 + i, p.num - 1)] : 0.f, st, sum); }, exactly);
+                // (a lane's two best are among those not below the second by more than `near`)
+                const float from = two == none ? none : two - (near + __builtin_fabsf(two) * 0x1p-22f);
+                uint32_t few = 0;
+#pragma unroll
+                for (int i = 0; i < V; ++i) few |= key[i] != none && key[i] >= from ? 1u << i : 0u;
+                kept = kept_experts<double, L, V>(
+                    p, sub, (double *)lds, [&](int i) { return worth_of<double>(p, l[i], p.bias ? p.bias[min(e0 + i, p.num - 1)] : 0.f, st, sum); },
+                    [&](double &a, double &b) {
+                        for (; few; few &= few - 1) {
+                            const int e = e0 + __builtin_ctz(few);
+                            better_of(worth_of<double>(p, element_at(row, p.size, e), p.bias ? p.bias[e] : 0.f, st, sum), a, b);
+                        }
+                    },
+                    exactly);
             }
         }
     }
