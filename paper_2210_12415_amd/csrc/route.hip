@@ -497,14 +497,48 @@ __global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(const RoutePa
     }
 }
 
-// Moves the ranks of a workgroup's choices to their rows.
-template <int L>
+// Moves the ranks of a workgroup's choices to their rows.  COUNT: every workgroup adds up what those before it have, and all, itself.
+template <int L, bool COUNT>
 __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteParams p)
 {
     __shared__ int part[kRouteWaves], base[kRouteThreads];
     const int t = threadIdx.x;
     const int64_t first = (int64_t)blockIdx.x * kRowsOf<L> * p.top_k, n = min((int64_t)kRowsOf<L> * p.top_k, (int64_t)p.tokens * p.top_k - first);
-    const int all = t < p.num ? p.counts[(int64_t)p.chunks * p.num + t] : 0, mine = t < p.num ? p.counts[(int64_t)blockIdx.x * p.num + t] : 0;
+    int all = 0, mine = 0;
+    if constexpr (COUNT) {
+        // a thread has an expert of every so many workgroups: lanes side by side have experts side by side
+        __shared__ int sums[2][kRouteThreads];
+        int width = 1;
+        while (width < p.num) width *= 2;
+        const int e = t & (width - 1), runs = kRouteThreads / width;
+        int before = 0, total = 0;
+        for (int c0 = t / width; c0 < p.chunks; c0 += 16 * runs) {
+            int v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = p.counts[(int64_t)min(c0 + i * runs, p.chunks - 1) * p.num + min(e, p.num - 1)];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int c = c0 + i * runs;
+                total += c < p.chunks ? v[i] : 0;
+                before += c < (int)blockIdx.x ? v[i] : 0;
+            }
+        }
+        for (int w = width; w < 64; w *= 2) {              // (the runs of a wave)
+            total += __shfl_xor(total, w);
+            before += __shfl_xor(before, w);
+        }
+        sums[0][t] = total;
+        sums[1][t] = before;
+        __syncthreads();
+        if (t < p.num)
+            for (int r = t; r < kRouteThreads; r += max(width, 64)) {
+                all += sums[0][r];
+                mine += sums[1][r];
+            }
+    } else if (t < p.num) {
+        all = p.counts[(int64_t)p.chunks * p.num + t];
+        mine = p.counts[(int64_t)blockIdx.x * p.num + t];
+    }
     const int begin = before_thread(all, part);
     base[t] = begin + mine;
     if (blockIdx.x == 0) {
@@ -537,16 +571,47 @@ struct RouteGradParams {
 
 constexpr int kGradThreads = 256;
 
+// Four elements, at any alignment of whole elements.
+template <int ES>
+__device__ __forceinline__ void load_four(const char *at, float *f)
+{
+    if constexpr (ES == 4) {
+        f4_t c;
+        __builtin_memcpy(&c, at, 16);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) f[q] = c[q];
+    } else {
+        uint32_t c[2];
+        __builtin_memcpy(c, at, 8);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) f[q] = __builtin_bit_cast(float, q % 2 ? c[q / 2] & 0xffff0000u : c[q / 2] << 16);
+    }
+}
+
+template <int ES>
+__device__ __forceinline__ void store_four(char *at, const float *f)
+{
+    if constexpr (ES == 4) {
+        const f4_t c = {f[0], f[1], f[2], f[3]};
+        __builtin_memcpy(at, &c, 16);
+    } else {
+        const uint32_t c[2] = {f32x2_to_bf16x2(f[0], f[1]), f32x2_to_bf16x2(f[2], f[3])};
+        __builtin_memcpy(at, c, 8);
+    }
+}
+
 // Bound by memory: it writes the row, and reads it where every expert's score has a part (softmax without renormalisation).  A lane has a choice, and
-// then V experts; the choices' gradients come to the experts' lanes through LDS.
+// then V experts, four side by side and the next four behind those of the other lanes (16384 x 256 fp32 7.0 us,
+// where a lane has 16 side by side 11.4); the choices' gradients come to the experts' lanes through LDS.
 template <int ES, int L, int V>
 __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGradParams p)
 {
     constexpr int ROWS = kGradThreads / L;
-    __shared__ float to[ROWS][L * V];
+    __shared__ __attribute__((aligned(16))) float to[ROWS][L * V];
     __shared__ int chosen[ROWS][ALT_ROUTE_MAX_TOP_K];
     __shared__ float parts[ROWS][ALT_ROUTE_MAX_TOP_K];
-    const int sub = threadIdx.x % L, row_in = threadIdx.x / L, e0 = sub * V;
+    const int sub = threadIdx.x % L, row_in = threadIdx.x / L;
+    auto first_of = [&](int i) { return (i * L + sub) * 4; };              // expert of the i-th four
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < p.tokens; first += (int64_t)gridDim.x * ROWS) {
         const int64_t token = first + row_in;
         const bool here = token < p.tokens;
@@ -554,11 +619,15 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGra
         float l[V], top = -INFINITY, sum = 1.f;
         const bool whole = p.softmax && !p.renorm;
         if (whole) {
-            if (here) {
-                load_logits<ES, V>(row, e0, p.num, l);
-            } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) l[i] = -INFINITY;
+            for (int i = 0; i < V / 4; ++i) {
+                const int e0 = first_of(i);
+                if (here && e0 + 4 <= p.num) {
+                    load_four<ES>(row + (int64_t)e0 * ES, l + i * 4);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) l[i * 4 + q] = here && e0 + q < p.num ? element<ES>(row + (int64_t)(e0 + q) * ES) : -INFINITY;
+                }
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) top = l[i] > top ? l[i] : top;
@@ -603,6 +672,7 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGra
         }
         if (p.renorm || p.softmax) mean = row_sum<L>(s * dw);
         const bool any = row_max<L>(e) >= 0;
+        const float share = mean / sum;                    // (of an expert's exponential, where the whole row has a part)
         // (softmax without renormalisation: every expert has - score * mean, the chosen ones score * dweight beside it)
         const float mine = whole ? s * dw : s * (dw - mean) * rest;
         if (sub < p.top_k) {
@@ -610,7 +680,7 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGra
             parts[row_in][sub] = e >= 0 ? mine : 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) to[row_in][e0 + i] = 0.f;
+        for (int i = 0; i < V / 4; ++i) *(f4_t *)&to[row_in][first_of(i)] = (f4_t){0.f, 0.f, 0.f, 0.f};
         wave_sync();
         if (e >= 0) {
             float total = 0.f;                             // (an expert that stands twice: every one of its choices stores both parts)
@@ -619,29 +689,25 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGra
         }
         wave_sync();
         if (here) {
-            float out[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                out[i] = to[row_in][e0 + i];
-                if (whole) out[i] -= l[i] / sum * mean;
-                if (!any) out[i] = 0.f;
-            }
-            char *at = p.dlogits + token * p.ld + (int64_t)e0 * ES;
-            if (e0 + V <= p.num && V * ES >= 16) {
-                if constexpr (V * ES >= 16) {
+            for (int i = 0; i < V / 4; ++i) {
+                const int e0 = first_of(i);
+                const f4_t part = *(const f4_t *)&to[row_in][e0];
+                float out[4];
 #pragma unroll
-                    for (int i = 0; i < V * ES / 16; ++i) {
-                        float f[16 / ES];
-#pragma unroll
-                        for (int q = 0; q < 16 / ES; ++q) f[q] = out[i * (16 / ES) + q];
-                        const w4_t c = chunk16_of<ES>(f);
-                        __builtin_memcpy(at + i * 16, &c, 16);
-                    }
+                for (int q = 0; q < 4; ++q) {
+                    out[q] = part[q];
+                    if (whole) out[q] -= l[i * 4 + q] * share;
+                    if (!any) out[q] = 0.f;
                 }
-            } else {
+                char *at = p.dlogits + token * p.ld + (int64_t)e0 * ES;
+                if (e0 + 4 <= p.num) {
+                    store_four<ES>(at, out);
+                } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (e0 + i < p.num) store_element<ES>(at + i * ES, out[i]);
+                    for (int q = 0; q < 4; ++q)
+                        if (e0 + q < p.num) store_element<ES>(at + q * ES, out[q]);
+                }
             }
         }
         wave_sync();
@@ -674,6 +740,10 @@ void by_shape(const alt_route_desc_t &d, F f)
     }
 }
 
+// Up to so many counts every workgroup reads them all, beyond them they have a launch of their own: 16384 tokens of 64 experts, two choices (16384 counts),
+// 10.1 us the one way and 11.7 the other; 16384 of 256, eight choices (65536) 31.9 and 31.6, 32768 of 256 52 and 35.
+constexpr int64_t kCountsEach = 16384;
+
 int64_t chunks_of(const alt_route_desc_t &d) { return (d.tokens + kRouteThreads / shape_of(d).l - 1) / (kRouteThreads / shape_of(d).l); }
 
 template <int ES>
@@ -693,8 +763,12 @@ hipError_t route_run(const alt_route_desc_t &d, const RouteParams &p, hipStream_
         }
         hipLaunchKernelGGL((route_kernel<ES, L, V>), dim3((unsigned)p.chunks), dim3(kRouteThreads), lds, st, p);
         if ((e = hipGetLastError()) != hipSuccess || p.chunks == 1) return;
-        hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)((p.num + 15) / 16)), dim3(kRouteThreads), 0, st, p);
-        hipLaunchKernelGGL(route_place_kernel<L>, dim3((unsigned)p.chunks), dim3(kRouteThreads), 0, st, p);
+        if ((int64_t)p.chunks * p.num <= kCountsEach) {
+            hipLaunchKernelGGL((route_place_kernel<L, true>), dim3((unsigned)p.chunks), dim3(kRouteThreads), 0, st, p);
+        } else {
+            hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)((p.num + 15) / 16)), dim3(kRouteThreads), 0, st, p);
+            hipLaunchKernelGGL((route_place_kernel<L, false>), dim3((unsigned)p.chunks), dim3(kRouteThreads), 0, st, p);
+        }
         e = hipGetLastError();
     });
     return e;
