@@ -4,7 +4,8 @@
 //   a place for every (token, choice) in the order of expert, token, choice: offsets and rows
 //
 // There is little to read: 16384 x 256 fp32 logits are 3 us of memory.  The time goes into launches and into the selection, about 100 instructions of a
-// wave for each choice of its four rows, so lanes hold many experts and few lanes a row.  One launch chooses and ranks the choices inside each
+// wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 26.2 us, 23.2 without groups, 19.5
+// without biases, and of them 8 for the ranks' two launches.  One launch chooses and ranks the choices inside each
 // workgroup's tokens; where there is one workgroup that is all, else the ranks are moved by what the workgroups before have of each expert.
 #include "common.h"
 #include "rows.h"
@@ -42,7 +43,7 @@ __device__ __forceinline__ T rotated(T v)                  // of the lane N befo
     }
 }
 
-// f over the L (16 or 64) lanes of a row, the same in all of them.
+// f over the L (16, 32 or 64) lanes of a row, the same in all of them.
 template <int L, typename T, typename F>
 __device__ __forceinline__ T over_row(T v, F f)
 {
@@ -50,10 +51,8 @@ __device__ __forceinline__ T over_row(T v, F f)
     v = f(v, rotated<4>(v));
     v = f(v, rotated<2>(v));
     v = f(v, rotated<1>(v));
-    if constexpr (L == 64) {
-        v = f(v, __shfl_xor(v, 16));
-        v = f(v, __shfl_xor(v, 32));
-    }
+    if constexpr (L >= 32) v = f(v, __shfl_xor(v, 16));
+    if constexpr (L == 64) v = f(v, __shfl_xor(v, 32));
     return v;
 }
 // (of numbers: no NaN comes here)
@@ -111,6 +110,19 @@ __device__ __forceinline__ F sigmoid_of(F v)
 }
 
 __device__ __forceinline__ float element_at(const char *row, int size, int e) { return size == 4 ? element<4>(row + (int64_t)e * 4) : element<2>(row + (int64_t)e * 2); }
+
+// Sum over the lanes of the row up to and with this one.
+template <int L>
+__device__ __forceinline__ int row_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    if constexpr (L >= 32) v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);
+    if constexpr (L == 64) v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
+    return v;
+}
 
 // ---- the choice --------------------------------------------------------------------------------------------------------------------
 
@@ -182,6 +194,7 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
     for (int g = sub, i = 0; g < p.groups; g += L, ++i) {
         const F v = worth[at(g * per)];
         int better = 0;
+#pragma unroll 8
         for (int o = 0; o < p.groups; ++o) {
             const F w = worth[at(o * per)];
             better += w > v || (w == v && o < g);
@@ -197,16 +210,145 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
     for (int g = sub, i = 0; g < p.groups; g += L, ++i) worth[at(g * per)] = mine >> i & 1 ? (F)1 : (F)0;
     wave_sync();
     uint32_t kept = 0;
+    if (lanes) {
+        if (sub * V < p.num && worth[at((int)fast_div((uint32_t)(sub * V), p.each) * per)] != 0) kept = ~0u;
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = sub * V + i;
-        if (e < p.num && worth[at((int)fast_div((uint32_t)e, p.each) * per)] != 0) kept |= 1u << i;
+        for (int i = 0; i < V; ++i) {
+            const int e = sub * V + i;
+            if (e < p.num && worth[at((int)fast_div((uint32_t)e, p.each) * per)] != 0) kept |= 1u << i;
+        }
     }
     wave_sync();
     least = row_min<L>(least);
     most = row_max<L>(most);
     apart = most > none ? least - most : (F)INFINITY;
     return kept;
+}
+
+// ---- the largest numbers of a row ------------------------------------------------------------------------------------------------------
+//
+// A choice and its expert are one double: the choice, exactly, and in the bits that it leaves free the expert, so that of equal ones the lower is larger.
+// Lists of the K largest, in order, are merged lane by lane: the larger of each number and its counterpart from the list's other end are the K
+// largest of both, first up and then down, and a few exchanges order them.
+constexpr double kNoChoice = -0x1p1000;
+// Up to eight choices, more than four, come of lists, others one after another: with a list of eight 16384 tokens of 256 experts take 19.6 us for eight choices
+// and 19.5 for six, one after another 22.0 and 19.9 (a list of four 18.1 for four and 18.2 for one; one after another 19.0 and 16.7).
+constexpr int kListed = 8;
+
+__device__ __forceinline__ double choice_of(float key, int e)
+{
+    const double v = __builtin_fmin((double)(key + 0.f), 0x1p200);                            // (0 for -0; a number for an infinity)
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v) | (uint64_t)(key < 0.f ? e : 1023 - e);
+    return key == -INFINITY ? kNoChoice : __builtin_bit_cast(double, bits);
+}
+
+__device__ __forceinline__ int expert_of(double v)
+{
+    const int low = (int)(__builtin_bit_cast(uint64_t, v) & 1023);
+    return v == kNoChoice ? -1 : v < 0 ? low : 1023 - low;
+}
+
+__device__ __forceinline__ void exchange(double &a, double &b)
+{
+    const double lo = smaller(a, b);
+    a = larger(a, b);
+    b = lo;
+}
+
+// Descending, of a list that goes up and then down (or the other way).
+template <int K>
+__device__ __forceinline__ void order_merged(double (&v)[K])
+{
+#pragma unroll
+    for (int d = K / 2; d; d /= 2)
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (!(i & d)) exchange(v[i], v[i | d]);
+}
+
+// Descending, N at a time; then the K largest of all V (V < K: behind them nothing).
+template <int K, int V>
+__device__ __forceinline__ void order_own(const double (&v)[V], double (&list)[K])
+{
+    constexpr int N = V < K ? V : K;
+#pragma unroll
+    for (int at = 0; at < V; at += N) {
+        double part[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[i] = v[at + i];
+#pragma unroll
+        for (int size = 2; size <= N; size *= 2)
+#pragma unroll
+            for (int d = size / 2; d; d /= 2)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (!(i & d)) {
+                        if (i & size) exchange(part[i | d], part[i]);
+                        else exchange(part[i], part[i | d]);
+                    }
+        if (at == 0) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) list[i] = i < N ? part[i < N ? i : 0] : kNoChoice;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) list[i] = larger(list[i], part[N - 1 - i]);
+            order_merged(list);
+        }
+    }
+}
+
+template <int CTRL>
+__device__ __forceinline__ double moved(double v)
+{
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+template <int K, typename F>
+__device__ __forceinline__ void merge_with(double (&v)[K], F other)
+{
+    double o[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) o[i] = other(v[i]);
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] = larger(v[i], o[K - 1 - i]);
+    order_merged(v);
+}
+
+// The row's K largest, the same in all of its lanes.
+template <int L, int K, int V>
+__device__ __forceinline__ void row_largest(const float (&key)[V], int e0, double (&list)[K])
+{
+    double own[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) own[i] = choice_of(key[i], e0 + i);
+    order_own<K, V>(own, list);
+    merge_with(list, [](double v) { return moved<0xb1>(v); });         // the lane beside; the other pair of four; the other four of eight; the other eight
+    merge_with(list, [](double v) { return moved<0x4e>(v); });
+    merge_with(list, [](double v) { return moved<0x141>(v); });
+    merge_with(list, [](double v) { return moved<0x140>(v); });
+    if constexpr (L >= 32) merge_with(list, [](double v) { return __shfl_xor(v, 16); });
+    if constexpr (L == 64) merge_with(list, [](double v) { return __shfl_xor(v, 32); });
+}
+
+// Lane j's choice of the row's top_k <= K, the last of them, and whether two of them are so near that their order isn't sure.
+template <int L, int K, int V>
+__device__ __forceinline__ int choose_largest(const RouteParams &p, const float (&key)[V], float near, int sub, float &end, bool &sure)
+{
+    double list[K];
+    row_largest<L, K, V>(key, sub * V, list);
+    double mine = kNoChoice;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        if (i == sub) mine = list[i];
+        if (i == p.top_k - 1 && list[i] != kNoChoice) end = (float)list[i];
+        if (i + 1 < K && i + 1 < p.top_k && list[i + 1 < K ? i + 1 : i] != kNoChoice)
+            sure &= list[i] - list[i + 1 < K ? i + 1 : i] > (double)near + __builtin_fabs(list[i]) * 0x1p-22;
+    }
+    return sub < p.top_k ? expert_of(mine) : -1;
 }
 
 // The choices of a row: lane j of it gets the j-th expert, or -1.
@@ -216,7 +358,8 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
 // itself, which counts s (1 - s), the rest by 1.5 2^-23 s), a softmax by the roundings of its argument, sum and quotient, 2^-19 of the largest score
 // of the row, which is 1 / sum; adding the bias rounds by 2^-24 of the choice; `near`, and what is added to it, is twice that of two of them.  In 64 bits go: the worths of the
 // groups, where the last that is kept and the first that is not are near; the choices of the few experts, one to a lane, that are chosen or near the
-// last chosen one; all of them, where those are more than a row has lanes.
+// last chosen one; all of them, where those are more than a row has lanes.  There are such rows in every launch of thousands, and the launch ends with
+// them, so they are short: 16384 tokens of 256 experts in eight groups took 5 us more where a near group had all its experts computed.
 template <int L, int V>
 __device__ __forceinline__ int choose(const RouteParams &p, const char *row, const float (&l)[V], const RowStats &st, int sub, char *lds)
 {
@@ -268,50 +411,62 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
         const bool is = (kept >> i & 1) && !st.lost && (!scored || key[i] != none);
         key[i] = !is ? none : p.bias ? key[i] : l[i];
     }
-    int mine = -1, picks = 0;
-    float last = INFINITY, end = none;                     // the pick before, the last chosen one
-    bool sure = true, more = false;                        // more: what is left is near the last chosen one
-    for (; picks <= L; ++picks) {
-        if (!p.bias && picks == p.top_k) break;
-        float best = key[0];
+    int mine = -1;
+    float end = none;                                      // the last chosen one
+    bool sure = true;
+    uint32_t few = 0;                                      // this lane's experts that are chosen or near the last chosen one
+    if (p.top_k > 4 && p.top_k <= kListed) {
+        mine = choose_largest<L, kListed, V>(p, key, near, sub, end, sure);
+    } else {
+        float last = INFINITY;                             // the pick before
+        for (int picks = 0; picks < p.top_k; ++picks) {
+            float best = key[0];
 #pragma unroll
-        for (int i = 1; i < V; ++i) best = larger(best, key[i]);
-        const float top = row_max<L>(best);
-        const bool is = top > none;
-        if (p.bias) {
-            if (is && picks > 0 && picks <= p.top_k && !(last - top > near + __builtin_fabsf(last) * 0x1p-22f)) sure = false;
-            more = is && !(end - top > near + __builtin_fabsf(end) * 0x1p-22f);
+            for (int i = 1; i < V; ++i) best = larger(best, key[i]);
+            const float top = row_max<L>(best);
+            const bool is = top > none;
+            if (!__ballot(is)) break;
+            if (is && picks > 0 && !(last - top > near + __builtin_fabsf(last) * 0x1p-22f)) sure = false;
+            last = top;
+            if (picks == p.top_k - 1) end = top;
+            int at = 0x7fffffff;
+#pragma unroll
+            for (int i = V - 1; i >= 0; --i) at = key[i] == top ? e0 + i : at;
+            at = row_min<L>(is ? at : 0x7fffffff);
+            if (sub == picks && is) mine = at;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (e0 + i == at) key[i] = none;
+            }
+            if (p.bias && at >= e0 && at < e0 + V) few |= 1u << (at - e0);
         }
-        last = top;
-        if (picks == p.top_k - 1) end = top;
-        if (picks >= p.top_k && !__ballot(more)) break;
-        if (picks == L || !__ballot(is)) break;
-        int at = 0x7fffffff;
-#pragma unroll
-        for (int i = V - 1; i >= 0; --i) at = key[i] == top ? e0 + i : at;
-        at = row_min<L>(is ? at : 0x7fffffff);
-        if (sub == picks && is) mine = at;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (e0 + i == at) key[i] = none;
     }
-    if (p.bias && __ballot(!sure)) {
+    if (!p.bias) return mine;
+    const float from = end - (near + __builtin_fabsf(end) * 0x1p-22f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) few |= key[i] != none && !(key[i] < from) ? 1u << i : 0u;
+    const int own = __popc(few), count = row_sum<L>(own);
+    if (__ballot(!sure || count > p.top_k)) {
         const double sum = exact_sum<L, V>(p, l, st), out = -INFINITY;
-        if (picks < L || !__ballot(more)) {
-            // the candidates' places
-            const double v = mine >= 0 ? worth_of<double>(p, element_at(row, p.size, mine), p.bias[mine], st, sum) : out;
+        if (!__ballot(count > L)) {
+            // the candidates' places, a candidate to a lane
+            int *slot = (int *)lds, *chosen = slot + 3 * L;
+            double *worth = (double *)(slot + L);
+            slot[sub] = chosen[sub] = -1;
+            wave_sync();
+            for (int at = row_scan<L>(own) - own; few; few &= few - 1) slot[at++] = e0 + __builtin_ctz(few);
+            wave_sync();
+            const int e = slot[sub];
+            const double v = e >= 0 ? worth_of<double>(p, element_at(row, p.size, e), p.bias[e], st, sum) : out;
+            worth[sub] = v;
+            wave_sync();
             int place = 0;
-            for (int o = 0; o < picks; ++o) {
-                const double w = __shfl(v, o, L);
-                const int e = __shfl(mine, o, L);
-                place += w > v || (w == v && e < mine);
-            }
-            const int from = mine >= 0 ? place : -1, candidate = mine;
-            mine = -1;
-            for (int o = 0; o < picks; ++o) {
-                const int to = __shfl(from, o, L), e = __shfl(candidate, o, L);
-                if (to == sub) mine = e;
-            }
+            for (int o = 0; o < count; o += 8)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) place += worth[o + q] > v || (worth[o + q] == v && slot[o + q] < e);
+            if (e >= 0) chosen[place] = e;
+            wave_sync();
+            mine = chosen[sub];
         } else {
             // everything, in the row's LDS
             double *worth = (double *)lds;
@@ -335,22 +490,10 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
     return sub < p.top_k ? mine : -1;
 }
 
-// Sum over the lanes up to and with this one.
-__device__ __forceinline__ int wave_scan(int v)
-{
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
-    return v;
-}
-
 // The sum of v over the threads before this one of the workgroup (`part`: one number for each wave).
 __device__ __forceinline__ int before_thread(int v, int (&part)[kRouteWaves])
 {
-    const int upto = wave_scan(v), wave = threadIdx.x / 64;
+    const int upto = row_scan<64>(v), wave = threadIdx.x / 64;
     if (threadIdx.x % 64 == 63) part[wave] = upto;
     __syncthreads();
     int before = upto - v;
@@ -360,7 +503,7 @@ __device__ __forceinline__ int before_thread(int v, int (&part)[kRouteWaves])
 }
 
 // Bytes of LDS: the workgroup's choices and a row of counts for each wave, over the rows' group worths.
-__host__ __device__ constexpr int route_slots(int L) { return L == 16 ? 64 * 16 : 16 * ALT_ROUTE_MAX_TOP_K; }
+__host__ __device__ constexpr int route_slots(int L) { return kRouteThreads / L * (L == 16 ? 16 : ALT_ROUTE_MAX_TOP_K); }
 template <int L> constexpr int kRowsOf = kRouteThreads / L;
 __host__ __device__ constexpr int route_row_bytes(int experts) { return (experts + experts / 32) * 8; }
 inline size_t route_lds(int L, int V, int num, bool scored)
@@ -482,7 +625,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(const RoutePa
     part[run][x] = sum;
     __syncthreads();
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;            // a wave for each of the 16 experts
-    const int upto = wave_scan(part[lane][wave]);
+    const int upto = row_scan<64>(part[lane][wave]);
     __syncthreads();
     part[lane][wave] = upto;
     __syncthreads();
@@ -716,12 +859,14 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGra
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------------
 
-// Lanes of a row and experts of a lane: 16 lanes as long as they hold the experts and the choices.
+// Lanes of a row and experts of a lane: as few lanes as hold the experts, 16 to a lane, and the choices (16384 tokens of 512 experts,
+// eight choices: 32 lanes 30 us, 64 lanes 44).
 struct Shape { int l, v; };
 Shape shape_of(const alt_route_desc_t &d)
 {
     if (d.top_k <= 16 && d.experts <= 256) return {16, d.experts <= 64 ? 4 : d.experts <= 128 ? 8 : 16};
-    return {64, d.experts <= 256 ? 4 : d.experts <= 512 ? 8 : 16};
+    if (d.experts <= 512) return {32, d.experts <= 256 ? 8 : 16};
+    return {64, 16};
 }
 
 template <typename F>
@@ -734,9 +879,9 @@ void by_shape(const alt_route_desc_t &d, F f)
         else if (s.v == 8) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
         else f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
     } else {
-        if (s.v == 4) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-        else if (s.v == 8) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-        else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+        if (s.l == 64) f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+        else if (s.v == 8) f(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+        else f(integral_constant<int, 32>{}, integral_constant<int, 16>{});
     }
 }
 

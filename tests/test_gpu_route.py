@@ -158,6 +158,34 @@ def test_route_compares_choices_beyond_32_bits(h):
     check(h, big, alt.route_desc(T, E, 8, score=alt.SCORE_SIGMOID, renormalize=True))
 
 
+@pytest.mark.parametrize("E,k", [(8, 5), (64, 8), (200, 7), (256, 9), (257, 6), (300, 17), (512, 8), (512, 20), (1024, 8), (1000, 31), (256, 32)])
+def test_route_orders_of_every_shape(h, E, k):
+    """Equal logits, both zeros, all negative, few left, near each other and, by the bias, more of them near the last choice than a row has lanes."""
+    T = 150
+    g = torch.Generator().manual_seed(E + k)
+    steps = torch.randint(-3, 3, (T, E), generator=g).float()
+    signs = torch.where(torch.rand(T, E, generator=g) < 0.5, -0.0, 0.0)
+    few = logits(T, E, 3, masked=0.9)
+    near = normal(5, T, E, std=2.0 ** -18) - 12
+    largest = torch.where(torch.rand(T, E, generator=g) < 0.1, torch.finfo(torch.float32).max, 0.0)
+    largest[torch.rand(T, E, generator=g) < 0.02] = INF
+    for l in (steps, signs, steps - 8, few, near, -largest, logits(T, E, 9)):
+        l = matrix(l, torch.float32)
+        for bias in (None, torch.linspace(0, 2.0 ** -30, E).cuda(), normal(3, E, std=0.1).cuda()):
+            check(h, l, alt.route_desc(T, E, k, score=alt.SCORE_SIGMOID, renormalize=True), bias)
+            check(h, l, alt.route_desc(T, E, k, score=alt.SCORE_SOFTMAX), bias)
+    check(h, matrix(largest, torch.float32), alt.route_desc(T, E, k, score=alt.SCORE_SIGMOID))
+
+
+@pytest.mark.parametrize("E,groups,top_groups,k", [(512, 8, 4, 8), (512, 64, 20, 12), (300, 10, 3, 8), (300, 3, 2, 20)])
+def test_route_by_groups_of_more_experts(h, E, groups, top_groups, k):
+    for l in (logits(333, E, 3, masked=0.15), normal(5, 333, E, std=2.0 ** -18) - 12):
+        l = matrix(l, torch.float32)
+        for bias in (None, normal(E, E, std=0.1).cuda(), torch.ones(E).cuda()):
+            for best in (1, 2):
+                check(h, l, alt.route_desc(333, E, k, score=alt.SCORE_SIGMOID, groups=groups, top_groups=top_groups, group_best=best, renormalize=True), bias)
+
+
 def test_route_biases_that_bar_or_force(h):
     T, E = 100, 40
     l = matrix(logits(T, E, 7), torch.float32)
