@@ -7,39 +7,36 @@ namespace {
 
 // ---- products of few rows ------------------------------------------------------------------------------------------------------------
 //
-// Tiles of 16 RT rows by 16 NT columns whose operands, both with the reduction contiguous, come through LDS in steps of 512 bytes a row, which lanes side by
-// side load side by side.  (Straight into the fragments of the 16-row matrix instructions every load touches 64 cache lines: the inner sums of 8192 rows
-// of 4096, rank 32, took 37 us, so 25; the sums and the product of 32 x 4096 x 4096 bf16, rank 16, 14.3, so 12.5.)  AHEAD steps are on their way in registers; the waves share a step's reduction, and
-// workgroups the rest of it where there are few.  Chunk c of LDS row r lies at c ^ (r % 16), so that 16 rows' chunks are at distinct banks.
-constexpr int kStep = 512;
+// Tiles of 16 RT rows by 16 NT columns whose operands, both with the reduction contiguous, come in pieces of 128 bytes a row, whole cache lines, the waves'
+// in turn.  A wave takes its pieces through LDS of its own and waits for no other: 100 x 2048 x 2048 bf16 with 50 adapters of rank 16 14.6 us, where the waves
+// shared all pieces at barriers 15.6.  (Straight into the fragments of the 16-row matrix instructions every load touches 64 cache lines: the inner sums of 8192
+// rows of 4096, rank 32, took 37 us, so 24.)  AHEAD pieces are on their way in registers; four instead of two, eight waves instead of four and 32 rows
+// instead of 16 took 25 to 30.  Chunk c of a piece of row r lies at c ^ (r % 8), so that 16 rows' chunks are at distinct banks.
+constexpr int kPiece = 128, kWaves = 4, kStep = kWaves * kPiece;
 
-template <typename T, int RT, int NT, int NW, int AHEAD>
+template <typename T, int RT, int NT, int AHEAD>
 struct Core {
-    static constexpr int STEP = kStep, ES = GrpTraits<T>::ES, SUMS = GrpTraits<T>::SUMS, THREADS = 64 * NW, A = 16 * RT, ROWS = A + 16 * NT;
-    static constexpr int STRIDE = THREADS / (STEP / 16), Q = ROWS / STRIDE, AQ = A / STRIDE;              // rows of a piece of all threads; pieces of a step
-    static constexpr int kLds = 2 * ROWS * STEP;
-    static_assert(A % STRIDE == 0 && AHEAD % 2 == 0 && NW * RT * NT * 1024 <= kLds && kLds <= 64 * 1024, "pieces");
+    static constexpr int ES = GrpTraits<T>::ES, SUMS = GrpTraits<T>::SUMS, THREADS = 64 * kWaves, A = 16 * RT, ROWS = A + 16 * NT;
+    static constexpr int Q = ROWS / 8, AQ = A / 8, kLds = ROWS * kStep;                                   // loads of a piece; of its rows of a
+    static_assert(kWaves * RT * NT * 1024 <= kLds && kLds <= 64 * 1024, "LDS");
     typedef typename GrpFew<T>::acc_t acc_t;
 
-    // This wave's sums of rows a (a_rows of them, lda bytes apart) by rows b, over the steps first .. end - 1 of `bytes` of each.  (Behind the last row the
-    // last again, whose sums nobody stores.)
+    // This wave's sums of rows a (a_rows of them, lda bytes apart) by rows b, over the steps first .. end - 1 of kStep of `bytes` of each.  (Behind the last row
+    // the last again, whose sums nobody stores.)
     static __device__ __forceinline__ void sums(const char *a, int64_t lda, int a_rows, const char *b, int64_t ldb, int b_rows, int bytes, int first, int end, char *lds,
                                                 acc_t (&acc)[RT][NT][SUMS])
     {
-        const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-        const int r = t / (STEP / 16), c = t % (STEP / 16), whole = bytes / STEP, last = min(end, whole);
-        uint32_t from[Q], to[Q];
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane / 8, c = lane % 8;
+        const int whole = bytes / kPiece, from_piece = first * kWaves + wave, n = max(0, (min(end * kWaves, whole) - from_piece + kWaves - 1) / kWaves);
+        char *const stage = lds + wave * (ROWS * kPiece);
+        uint32_t from[Q];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const int row = q * STRIDE + r;
-            from[q] = (uint32_t)(q < AQ ? min(row, a_rows - 1) * (int)lda : min(row - A, b_rows - 1) * (int)ldb) + c * 16;
-            to[q] = row * STEP + (c ^ (row & 15)) * 16;
-        }
+        for (int q = 0; q < Q; ++q) from[q] = (uint32_t)(q < AQ ? min(q * 8 + r, a_rows - 1) * (int)lda : min(q * 8 + r - A, b_rows - 1) * (int)ldb) + c * 16;
         u32x4_t v[AHEAD][Q];
-        auto load = [&](u32x4_t (&v)[Q], int s) {
-            const char *as = a + (int64_t)s * STEP, *bs = b + (int64_t)s * STEP;
+        auto load = [&](u32x4_t (&v)[Q], int k) {
+            const int64_t at = (int64_t)(from_piece + k * kWaves) * kPiece;
 #pragma unroll
-            for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], (q < AQ ? as : bs) + from[q], 16);
+            for (int q = 0; q < Q; ++q) __builtin_memcpy(&v[q], (q < AQ ? a : b) + at + from[q], 16);
         };
 #pragma unroll
         for (int i = 0; i < RT; ++i)
@@ -47,55 +44,55 @@ struct Core {
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int s = 0; s < SUMS; ++s) acc[i][j][s] = (acc_t){0, 0, 0, 0};
-        auto multiply = [&](const char *stage) {
+        auto put = [&](const u32x4_t (&v)[Q]) {
 #pragma unroll
-            for (int h = 0; h < STEP / NW / 64; ++h) {
-                const char *at = stage + lane % 16 * STEP + (((wave * (STEP / NW) + h * 64) / 16 + lane / 16) ^ (lane % 16)) * 16;
+            for (int q = 0; q < Q; ++q) *(u32x4_t *)(stage + q * (8 * kPiece) + r * kPiece + (c ^ r) * 16) = v[q];
+        };
+        auto multiply = [&] {
+            wave_sync();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const char *at = stage + lane % 16 * kPiece + ((h * 4 + lane / 16) ^ (lane % 8)) * 16;
                 u32x4_t fa[RT];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) fa[i] = *(const u32x4_t *)(at + i * 16 * STEP);
+                for (int i = 0; i < RT; ++i) fa[i] = *(const u32x4_t *)(at + i * 16 * kPiece);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    const u32x4_t fb = *(const u32x4_t *)(at + (A + j * 16) * STEP);
+                    const u32x4_t fb = *(const u32x4_t *)(at + (A + j * 16) * kPiece);
 #pragma unroll
                     for (int i = 0; i < RT; ++i) grp_mma16<T>(acc[i][j], fb, fa[i]);
                 }
             }
+            wave_sync();
         };
-        auto step = [&](u32x4_t (&v)[Q], int s, char *stage, auto MORE) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) *(u32x4_t *)(stage + to[q]) = v[q];
-            if (decltype(MORE)::value || s + AHEAD < last) load(v, s + AHEAD);
-            lds_barrier();                                 // (and the other stage's readers are through; the loads stay on their way)
-            multiply(stage);
+        auto step = [&](u32x4_t (&v)[Q], int k, auto MORE) {
+            put(v);
+            if (decltype(MORE)::value || k + AHEAD < n) load(v, k + AHEAD);
+            multiply();
         };
-        // (without branches around the loads while there are more, so that no step waits for more of them than it needs: 8192 rows of 4096, rank 32, 25 us
-        // with them; what there is none of is the last again)
-        if (first < last) {
+        // (without branches around the loads while there are more, so that no piece waits for more of them than it needs; what there is none of is the last
+        // again)
+        if (n > 0) {
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) load(v[i], min(first + i, last - 1));
-            int s = first;
-            for (; s + 2 * AHEAD <= last; s += AHEAD) {
+            for (int i = 0; i < AHEAD; ++i) load(v[i], min(i, n - 1));
+            int k = 0;
+            for (; k + 2 * AHEAD <= n; k += AHEAD) {
 #pragma unroll
-                for (int i = 0; i < AHEAD; ++i) step(v[i], s + i, lds + i % 2 * (ROWS * STEP), std::true_type{});
+                for (int i = 0; i < AHEAD; ++i) step(v[i], k + i, std::true_type{});
             }
-            for (; s < last; s += AHEAD) {
+            for (; k < n; k += AHEAD) {
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i)
-                    if (s + i < last) step(v[i], s + i, lds + i % 2 * (ROWS * STEP), std::false_type{});
+                    if (k + i < n) step(v[i], k + i, std::false_type{});
             }
         }
-        if (end > whole && first < end) {                  // what the reduction ends with
-            __syncthreads();
-            const int count = (bytes - whole * STEP - c * 16) / ES;
-#pragma unroll 1
-            for (int q = 0; q < Q; ++q) {
-                const int row = q * STRIDE + r;
-                const char *at = (row < A ? a + (int64_t)min(row, a_rows - 1) * lda : b + (int64_t)min(row - A, b_rows - 1) * ldb) + c * 16;
-                *(u32x4_t *)(lds + row * STEP + (c ^ (row & 15)) * 16) = grp_load_chunk<ES>(at + (int64_t)whole * STEP, count);
-            }
-            __syncthreads();
-            multiply(lds);
+        if (bytes > whole * kPiece && whole >= from_piece && whole < end * kWaves && whole % kWaves == wave) {     // what the reduction ends with
+            const int count = (bytes - whole * kPiece - c * 16) / ES;
+            u32x4_t last[Q];
+#pragma unroll
+            for (int q = 0; q < Q; ++q) last[q] = grp_load_chunk<ES>((q < AQ ? a : b) + (int64_t)whole * kPiece + from[q], count);
+            put(last);
+            multiply();
         }
         __syncthreads();                                   // the stages' readers are through
     }
@@ -117,7 +114,7 @@ struct Core {
         for (int s = threadIdx.x; s < RT * NT * 64; s += THREADS) {
             acc_t sum = __builtin_bit_cast(acc_t, part[s]);
 #pragma unroll
-            for (int w = 1; w < NW; ++w) sum += __builtin_bit_cast(acc_t, part[w * RT * NT * 64 + s]);
+            for (int w = 1; w < kWaves; ++w) sum += __builtin_bit_cast(acc_t, part[w * RT * NT * 64 + s]);
             f(s / 64 / NT * 16 + s % 16, s / 64 % NT * 16 + s % 64 / 16 * 4, sum);
         }
     }
@@ -135,9 +132,9 @@ __device__ __forceinline__ void slice_steps(int bytes, int slices, int slice, in
 //
 // Prompts have one or two, sequences that decode up to 16, so the adapters of a tile are spread over `slots` workgroups, those of a first adapter before the
 // others (which mostly have nothing to do).
-template <typename T, int NT, int NW>
+template <typename T, int NT>
 struct Down {
-    using C = Core<T, 1, NT, NW, 2>;
+    using C = Core<T, 1, NT, 2>;
     static constexpr int ES = C::ES, ROWS = C::A, kLds = C::kLds;
 
     // slices == 0: of the fused form (one slice, in bf16 in two parts)
@@ -193,9 +190,9 @@ struct Down {
 };
 
 template <typename T, int NT>
-__global__ __launch_bounds__(256, 3) void adapters_down_kernel(const AdapterParams p)
+__global__ __launch_bounds__(64 * kWaves) void adapters_down_kernel(const AdapterParams p)
 {
-    using D = Down<T, NT, 4>;
+    using D = Down<T, NT>;
     __shared__ uint4 lds[D::kLds / 16];
     D::run(p, blockIdx.x, (char *)lds);
 }
@@ -203,13 +200,13 @@ __global__ __launch_bounds__(256, 3) void adapters_down_kernel(const AdapterPara
 // The inner sums in the first `down` workgroups, the shared product in the others: neither needs the other.  Column tiles that run together are one XCD's
 // (workgroups go to the XCDs in turn), rows first, so that a tile of w is read from memory once.
 template <typename T, int RT, int NT>
-__global__ __launch_bounds__(512) void adapters_few_kernel(const AdapterParams p, uint32_t down)
+__global__ __launch_bounds__(64 * kWaves) void adapters_few_kernel(const AdapterParams p, uint32_t down)
 {
-    using C = Core<T, RT, NT, 8, 4>;
+    using C = Core<T, RT, NT, 2>;
     constexpr int ES = C::ES;
-    __shared__ uint4 lds[(C::kLds > Down<T, 1, 8>::kLds ? C::kLds : Down<T, 1, 8>::kLds) / 16];
+    __shared__ uint4 lds[(C::kLds > Down<T, 1>::kLds ? C::kLds : Down<T, 1>::kLds) / 16];
     if (blockIdx.x < down) {
-        Down<T, 1, 8>::run(p, blockIdx.x, (char *)lds);
+        Down<T, 1>::run(p, blockIdx.x, (char *)lds);
         return;
     }
     const uint32_t wg = blockIdx.x - down, row_tiles = (uint32_t)(p.rows + 16 * RT - 1) / (16 * RT), col_tiles = (uint32_t)(p.cols + 16 * NT - 1) / (16 * NT);
@@ -323,8 +320,8 @@ hipError_t down(AdapterParams p, hipStream_t st)
 {
     p.col_tiles = (p.rank + 16 * NT - 1) / (16 * NT);
     const int64_t n = (int64_t)p.tiles * p.col_tiles * std::max(p.slices, 1) * p.slots;
-    if (n * 256 > 0xffffffffll) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((adapters_down_kernel<T, NT>), dim3((unsigned)n), dim3(256), 0, st, p);
+    if (n * 64 * kWaves > 0xffffffffll) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((adapters_down_kernel<T, NT>), dim3((unsigned)n), dim3(64 * kWaves), 0, st, p);
     return hipGetLastError();
 }
 
@@ -335,8 +332,8 @@ hipError_t few(AdapterParams p, hipStream_t st)
     const int64_t downs = ((int64_t)p.tiles * p.col_tiles * p.slices * p.slots + 7) / 8 * 8;
     const int64_t tiles = ((int64_t)p.rows + 16 * RT - 1) / (16 * RT) * ((p.cols + 16 * NT - 1) / (16 * NT)) * p.base_slices;
     const int64_t n = downs + (tiles + 7) / 8 * 8;
-    if (n * 512 > 0xffffffffll) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((adapters_few_kernel<T, RT, NT>), dim3((unsigned)n), dim3(512), 0, st, p, (uint32_t)downs);
+    if (n * 64 * kWaves > 0xffffffffll) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((adapters_few_kernel<T, RT, NT>), dim3((unsigned)n), dim3(64 * kWaves), 0, st, p, (uint32_t)downs);
     return hipGetLastError();
 }
 
@@ -368,9 +365,9 @@ void adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p)
     const int64_t tiles = row_tiles * ((p.cols + 16 * p.few_cols - 1) / (16 * p.few_cols));
     // Times in us.  The last pass runs at 5 TB/s behind its launch; the fused tiles wait 0.7 for each adapter of 32 rows, and most of those that there can be
     // are taken to be.  The product of few rows takes its tiles' loads from the caches at 13 TB/s (fp32, whose matrix instructions take longer, at 7); others
-    // come after the launch of the inner sums.  bf16, rank 16, either way: 128 x 4096 x 4096 30 of few rows and 36 otherwise, 256 x 4096 x 4096 44 and 37, 256 x
-    // 1024 x 4096 20 and 33, 200 x 8192 x 2048 41 and 30, 64 x 8192 x 8192 56 and 62 (the one of these that is
-    // taken on the slower side); fp32 60 x 4096 x 4096 43 and 101.
+    // come after the launch of the inner sums.  bf16, rank 16, either way: 128 x 4096 x 4096 29 of few rows and 36 otherwise, 256 x 4096 x 4096 44 and 37, 256 x
+    // 1024 x 4096 18 and 33, 200 x 8192 x 2048 41 and 30, 64 x 8192 x 8192 56 and 62 (the one of these that is taken on the slower side); fp32 60 x 4096 x 4096
+    // 42 and 101.
     const double rounds = std::ceil(grp_tiles<kForward>(product, 128, 128) / places), wait = 0.5 * std::min(p.adapters, 32) * rounds;
     const double last = 3 + (double)p.rows * p.cols * (8 + p.rank * es) / 5e6, loads = (double)tiles * 16 * (rt + p.few_cols) * p.K * es;
     GrpTime t;

@@ -93,13 +93,6 @@ __device__ __forceinline__ void load_logits(const char *row, int e0, int num, fl
     }
 }
 
-// What a wave's lanes have stored in LDS is there for its other lanes (a wave's LDS operations run in their order; this is for the compiler).
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 __device__ __forceinline__ float exp_of(float v) { return expf(v); }
 __device__ __forceinline__ double exp_of(double v) { return exp(v); }
 

@@ -121,6 +121,13 @@ __device__ __forceinline__ float wave_sum(float v)
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
+// What a wave's lanes have stored in LDS is there for its other lanes (a wave's LDS operations run in their order; this is for the compiler).
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---- host side -------------------------------------------------------------------------------------------------------------------
 
 // The handle's device has to be the current one.
