@@ -77,6 +77,14 @@ def test_adapters(h, M, N, K, G, r, dtype):
     check(h, M, N, K, G, r, requests(M, G), dtype)
 
 
+@pytest.mark.parametrize("K", [1, 2, 31, 63, 64, 65, 129, 255, 256, 257, 511, 1000, 2047, 4096, 9999])
+@pytest.mark.parametrize("M,G,r", [(5, 3, 16), (16, 2, 40), (20, 20, 5), (48, 3, 17), (600, 4, 20)])
+@pytest.mark.parametrize("dtype", [alt.BF16, alt.F32])
+def test_adapters_of_every_reduction(h, M, G, r, K, dtype):
+    """Reductions that end inside the pieces, the steps and the slices that they are cut into."""
+    check(h, M, 80, K, G, r, requests(M, G, K), dtype)
+
+
 @pytest.mark.parametrize("M,N,K", [(40, 3000, 512), (2100, 2048, 512), (5000, 2048, 128)])
 @pytest.mark.parametrize("out", [alt.BF16, alt.F32])
 def test_adapters_in_large_tiles(h, M, N, K, out):

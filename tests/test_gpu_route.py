@@ -226,6 +226,11 @@ def test_route_without_tokens(h):
     h.route_grad(d, None, None, None, None)
 
 
+@pytest.mark.parametrize("T,E,k", [(4096, 256, 2), (4097, 256, 2), (16384, 64, 1), (16385, 64, 1), (9000, 1000, 3), (3000, 300, 20)])
+def test_route_ranks_of_few_and_many_workgroups(h, T, E, k):
+    check(h, matrix(logits(T, E, 2, masked=0.2, padded=0.1), torch.bfloat16), alt.route_desc(T, E, k, dtype=alt.BF16))
+
+
 def test_route_many_tokens(h):
     T, E, k = (1 << 20) + 333, 8, 2
     l = torch.randn(T, E, device="cuda")
