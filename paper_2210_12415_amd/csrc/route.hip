@@ -4,7 +4,7 @@
 //   a place for every (token, choice) in the order of expert, token, choice: offsets and rows
 //
 // There is little to read: 16384 x 256 fp32 logits are 3 us of memory.  The time goes into launches and into the selection, about 100 instructions of a
-// wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 26.2 us, 23.2 without groups, 19.5
+// wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 23.8 us, 20.6 without groups, 18.4
 // without biases, and of them 8 for the ranks' two launches.  One launch chooses and ranks the choices inside each
 // workgroup's tokens; where there is one workgroup that is all, else the ranks are moved by what the workgroups before have of each expert.
 #include <atomic>
@@ -140,14 +140,26 @@ __device__ __forceinline__ F worth_of(const RouteParams &p, float l, float bias,
     return l == -INFINITY || w != w || st.lost ? (F)-INFINITY : w;
 }
 
+// (What is computed again is read again, in loops: all of it at once, from registers, takes scalar registers from what is always computed: 16384 tokens of 256
+// experts, eight choices with biases, 23.2 us, so 20.6.)
 template <int L, int V>
-__device__ __forceinline__ double exact_sum(const RouteParams &p, const float (&l)[V], const RowStats &st)
+__device__ __forceinline__ double exact_sum(const RouteParams &p, const char *row, int e0, const RowStats &st)
 {
     double sum = 0;
     if (!p.softmax) return sum;
-#pragma unroll
-    for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)st.top);
+#pragma unroll 4
+    for (int i = 0; i < V; ++i) {
+        const float l = e0 + i < p.num ? element_at(row, p.size, e0 + i) : -INFINITY;
+        sum += l == -INFINITY ? 0.0 : exp((double)l - (double)st.top);
+    }
     return row_sum<L>(sum);
+}
+
+// The worth in 64 bits of an expert that may be behind the last.
+__device__ __forceinline__ double exact_worth(const RouteParams &p, const char *row, int e, const RowStats &st, double sum)
+{
+    const bool is = e < p.num;
+    return worth_of<double>(p, is ? element_at(row, p.size, e) : -INFINITY, is && p.bias ? p.bias[e] : 0.f, st, sum);
 }
 
 template <typename F>
@@ -173,6 +185,9 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
         best_two(one, two);
         worth[at(sub * 2)] = one;
         worth[at(sub * 2 + 1)] = two;
+    } else if constexpr (sizeof(F) == 8) {
+#pragma unroll 2
+        for (int i = 0; i < V; ++i) worth[at(sub * V + i)] = worth_at(i);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) worth[at(sub * V + i)] = worth_at(i);
@@ -226,22 +241,23 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
 // A choice and its expert are one double: the choice, exactly, and in the bits that it leaves free the expert, so that of equal ones the lower is larger.
 // Lists of the K largest, in order, are merged lane by lane: the larger of each number and its counterpart from the list's other end are the K
 // largest of both, first up and then down, and a few exchanges order them.
-constexpr double kNoChoice = -0x1p1000;
+constexpr double kNoChoice = -0x1p1000;                    // (what is below it is none)
 // Up to eight choices, more than four, come of lists, others one after another: with a list of eight 16384 tokens of 256 experts take 19.6 us for eight choices
 // and 19.5 for six, one after another 22.0 and 19.9 (a list of four 18.1 for four and 18.2 for one; one after another 19.0 and 16.7).
 constexpr int kListed = 8;
 
 __device__ __forceinline__ double choice_of(float key, int e)
 {
-    const double v = __builtin_fmin((double)(key + 0.f), 0x1p200);                            // (0 for -0; a number for an infinity)
-    const uint64_t bits = __builtin_bit_cast(uint64_t, v) | (uint64_t)(key < 0.f ? e : 1023 - e);
-    return key == -INFINITY ? kNoChoice : __builtin_bit_cast(double, bits);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, (double)(key + 0.f));               // (0 for -0)
+    // infinities become 2^1023 and -2^1023: the positive numbers end there as signed integers, the negative ones as unsigned
+    const uint32_t high = min((uint32_t)min((int)(bits >> 32), 0x7fe00000), 0xffe00000u), low = (uint32_t)bits | (uint32_t)(key < 0.f ? e : 1023 - e);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
 }
 
 __device__ __forceinline__ int expert_of(double v)
 {
     const int low = (int)(__builtin_bit_cast(uint64_t, v) & 1023);
-    return v == kNoChoice ? -1 : v < 0 ? low : 1023 - low;
+    return v < kNoChoice ? -1 : v < 0 ? low : 1023 - low;
 }
 
 __device__ __forceinline__ void exchange(double &a, double &b)
@@ -284,7 +300,7 @@ __device__ __forceinline__ void order_own(const double (&v)[V], double (&list)[K
                     }
         if (at == 0) {
 #pragma unroll
-            for (int i = 0; i < K; ++i) list[i] = i < N ? part[i < N ? i : 0] : kNoChoice;
+            for (int i = 0; i < K; ++i) list[i] = i < N ? part[i < N ? i : 0] : 2 * kNoChoice;
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) list[i] = larger(list[i], part[N - 1 - i]);
@@ -335,12 +351,12 @@ __device__ __forceinline__ int choose_largest(const RouteParams &p, const float 
 {
     double list[K];
     row_largest<L, K, V>(key, sub * V, list);
-    double mine = kNoChoice;
+    double mine = 2 * kNoChoice;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
         if (i == sub) mine = list[i];
-        if (i == p.top_k - 1 && list[i] != kNoChoice) end = (float)list[i];
-        if (i + 1 < K && i + 1 < p.top_k && list[i + 1 < K ? i + 1 : i] != kNoChoice)
+        if (i == p.top_k - 1 && list[i] > kNoChoice) end = (float)list[i];
+        if (i + 1 < K && i + 1 < p.top_k && list[i + 1 < K ? i + 1 : i] > kNoChoice)
             sure &= list[i] - list[i + 1 < K ? i + 1 : i] > (double)near + __builtin_fabs(list[i]) * 0x1p-22;
     }
     return sub < p.top_k ? expert_of(mine) : -1;
@@ -382,7 +398,7 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
             for (int i = 0; i < V; ++i) size = fmaxf(size, key[i] == none ? 0.f : __builtin_fabsf(key[i]));
             size = row_max<L>(size);
             if (__ballot(!(apart > 4.f * near + size * 0x1p-20f))) {
-                const double sum = exact_sum<L, V>(p, l, st);
+                const double sum = exact_sum<L, V>(p, row, e0, st);
                 double exactly;
                 // (a lane's two best are among those not below the second by more than `near`)
                 const float from = two == none ? none : two - (near + __builtin_fabsf(two) * 0x1p-22f);
@@ -390,21 +406,23 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
 #pragma unroll
                 for (int i = 0; i < V; ++i) few |= key[i] != none && key[i] >= from ? 1u << i : 0u;
                 kept = kept_experts<double, L, V>(
-                    p, sub, (double *)lds, [&](int i) { return worth_of<double>(p, l[i], p.bias ? p.bias[min(e0 + i, p.num - 1)] : 0.f, st, sum); },
+                    p, sub, (double *)lds, [&](int i) { return exact_worth(p, row, e0 + i, st, sum); },
                     [&](double &a, double &b) {
                         for (; few; few &= few - 1) {
-                            const int e = e0 + __builtin_ctz(few);
-                            better_of(worth_of<double>(p, element_at(row, p.size, e), p.bias ? p.bias[e] : 0.f, st, sum), a, b);
+                            better_of(exact_worth(p, row, e0 + __builtin_ctz(few), st, sum), a, b);
                         }
                     },
                     exactly);
             }
         }
     }
+    if (!p.bias) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const bool is = (kept >> i & 1) && !st.lost && (!scored || key[i] != none);
-        key[i] = !is ? none : p.bias ? key[i] : l[i];
+        for (int i = 0; i < V; ++i) key[i] = st.lost || (scored && key[i] == none) ? none : l[i];
+    }
+    if (grouped) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = kept >> i & 1 ? key[i] : none;
     }
     int mine = -1;
     float end = none;                                      // the last chosen one
@@ -442,7 +460,7 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
     for (int i = 0; i < V; ++i) few |= key[i] != none && !(key[i] < from) ? 1u << i : 0u;
     const int own = __popc(few), count = row_sum<L>(own);
     if (__ballot(!sure || count > p.top_k)) {
-        const double sum = exact_sum<L, V>(p, l, st), out = -INFINITY;
+        const double sum = exact_sum<L, V>(p, row, e0, st), out = -INFINITY;
         if (!__ballot(count > L)) {
             // the candidates' places, a candidate to a lane
             int *slot = (int *)lds, *chosen = slot + 3 * L;
@@ -452,7 +470,7 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
             for (int at = row_scan<L>(own) - own; few; few &= few - 1) slot[at++] = e0 + __builtin_ctz(few);
             wave_sync();
             const int e = slot[sub];
-            const double v = e >= 0 ? worth_of<double>(p, element_at(row, p.size, e), p.bias[e], st, sum) : out;
+            const double v = e >= 0 ? exact_worth(p, row, e, st, sum) : out;
             worth[sub] = v;
             wave_sync();
             int place = 0;
@@ -465,8 +483,8 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
         } else {
             // everything, in the row's LDS
             double *worth = (double *)lds;
-#pragma unroll
-            for (int i = 0; i < V; ++i) worth[i * L + sub] = e0 + i < p.num && (kept >> i & 1) ? worth_of<double>(p, l[i], p.bias[e0 + i], st, sum) : out;
+#pragma unroll 2
+            for (int i = 0; i < V; ++i) worth[i * L + sub] = kept >> i & 1 ? exact_worth(p, row, e0 + i, st, sum) : out;
             mine = -1;
             for (int j = 0; j < p.top_k; ++j) {
                 double best = out;
@@ -529,10 +547,13 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteParams 
     int lost = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        lost |= l[i] != l[i] || (p.softmax && l[i] == INFINITY);
+        lost |= l[i] != l[i];
         st.top = l[i] > st.top ? l[i] : st.top;
     }
-    st.top = row_max<L>(st.top);
+    if (p.softmax) {
+        st.top = row_max<L>(st.top);
+        lost |= st.top == INFINITY;
+    }
     st.lost = row_max<L>(lost) != 0;
     st.sum = 1.f;
     if (p.softmax && (!p.renorm || p.bias || p.top_groups < p.groups)) {
