@@ -4,7 +4,7 @@
 //   a place for every (token, choice) in the order of expert, token, choice: offsets and rows
 //
 // There is little to read: 16384 x 256 fp32 logits are 3 us of memory.  The time goes into launches and into the selection, about 100 instructions of a
-// wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 23.8 us, 20.6 without groups, 18.4
+// wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 23.2 us, 20 without groups, 18
 // without biases, and of them 8 for the ranks' two launches.  One launch chooses and ranks the choices inside each
 // workgroup's tokens; where there is one workgroup that is all, else the ranks are moved by what the workgroups before have of each expert.
 #include <atomic>
@@ -23,7 +23,8 @@ struct RouteParams {
     int32_t *experts;
     float *weights;
     int32_t *rows, *offsets;
-    int32_t *counts;                       // [workgroups][num]: choices of each expert; then [num]: of all workgroups (route_scan_kernel)
+    uint16_t *counts;                      // [workgroups][num]: choices of each expert
+    int32_t *before;                       // [workgroups][num]: those of the workgroups before; then [num]: of all (route_scan_kernel)
     int64_t ld;                            // bytes between rows of logits
     int32_t tokens, num, top_k, groups, top_groups, group_best, softmax, renorm, chunks, size;     // size: bytes of a logit
     FastDiv each;                          // experts of a group
@@ -621,14 +622,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteParams 
         if (t < p.num)
             for (int w = 0; w < waves; ++w) count[w * p.num + t] += (uint16_t)begin;
     } else if (t < p.num) {
-        p.counts[(int64_t)blockIdx.x * p.num + t] = all;
+        p.counts[(int64_t)blockIdx.x * p.num + t] = (uint16_t)all;
     }
     __syncthreads();
     if (t < n) p.rows[first * p.top_k + t] = e >= 0 ? count[wave * p.num + e] + rank : -1;
 }
 
-// What the workgroups before have of each expert, in place of what each has, and behind them what all have.  16 experts to a workgroup, 64 threads to an
-// expert, each with a run of the workgroups.
+// What the workgroups before have of each expert, and behind them what all have.  16 experts to a workgroup, 64 threads to an expert, each with a run of the
+// workgroups.
 __global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(const RouteParams p)
 {
     __shared__ int part[64][17];
@@ -647,12 +648,11 @@ __global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(const RoutePa
     __syncthreads();
     int before = part[run][x] - sum;
     if (e >= p.num) return;
-    if (run == 63) p.counts[(int64_t)p.chunks * p.num + e] = before + sum;
+    if (run == 63) p.before[(int64_t)p.chunks * p.num + e] = before + sum;
+#pragma unroll 8
     for (int c = lo; c < hi; ++c) {
-        int32_t *at = p.counts + (int64_t)c * p.num + e;
-        const int v = *at;
-        *at = before;
-        before += v;
+        p.before[(int64_t)c * p.num + e] = before;
+        before += p.counts[(int64_t)c * p.num + e];
     }
 }
 
@@ -663,18 +663,20 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteP
     __shared__ int part[kRouteWaves], base[kRouteThreads];
     const int t = threadIdx.x;
     const int64_t first = (int64_t)blockIdx.x * kRowsOf<L> * p.top_k, n = min((int64_t)kRowsOf<L> * p.top_k, (int64_t)p.tokens * p.top_k - first);
+    static_assert(kRowsOf<L> * (L == 16 ? 16 : ALT_ROUTE_MAX_TOP_K) <= kRouteThreads, "a choice to a thread");
+    const int e = t < n ? p.experts[first + t] : -1, rank = t < n ? p.rows[first + t] : 0;
     int all = 0, mine = 0;
     if constexpr (COUNT) {
         // a thread has an expert of every so many workgroups: lanes side by side have experts side by side
         __shared__ int sums[2][kRouteThreads];
         int width = 1;
         while (width < p.num) width *= 2;
-        const int e = t & (width - 1), runs = kRouteThreads / width;
+        const int at = t & (width - 1), runs = kRouteThreads / width;
         int before = 0, total = 0;
         for (int c0 = t / width; c0 < p.chunks; c0 += 16 * runs) {
             int v[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = p.counts[(int64_t)min(c0 + i * runs, p.chunks - 1) * p.num + min(e, p.num - 1)];
+            for (int i = 0; i < 16; ++i) v[i] = p.counts[(int64_t)min(c0 + i * runs, p.chunks - 1) * p.num + min(at, p.num - 1)];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int c = c0 + i * runs;
@@ -695,8 +697,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteP
                 mine += sums[1][r];
             }
     } else if (t < p.num) {
-        all = p.counts[(int64_t)p.chunks * p.num + t];
-        mine = p.counts[(int64_t)blockIdx.x * p.num + t];
+        all = p.before[(int64_t)p.chunks * p.num + t];
+        mine = p.before[(int64_t)blockIdx.x * p.num + t];
     }
     const int begin = before_thread(all, part);
     base[t] = begin + mine;
@@ -705,10 +707,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteP
         if (t == p.num - 1) p.offsets[p.num] = begin + all;
     }
     __syncthreads();
-    for (int i = t; i < n; i += kRouteThreads) {
-        const int e = p.experts[first + i];
-        if (e >= 0) p.rows[first + i] += base[e];
-    }
+    if (e >= 0) p.rows[first + t] = rank + base[e];
 }
 
 __global__ __launch_bounds__(kRouteThreads) void route_nothing_kernel(int32_t *offsets, int num)
@@ -902,8 +901,9 @@ void by_shape(const alt_route_desc_t &d, F f)
 }
 
 // Up to so many counts every workgroup reads them all, beyond them they have a launch of their own: 16384 tokens of 64 experts, two choices (16384 counts),
-// 10.1 us the one way and 11.7 the other; 16384 of 256, eight choices (65536) 31.9 and 31.6, 32768 of 256 52 and 35.
+// 9.7 us the one way and 11.7 the other; 16384 of 256, eight choices (65536) 25.2 and 23.2, 32768 of 256 (131072) 44 and 25.
 constexpr int64_t kCountsEach = 16384;
+bool counts_each(int64_t chunks, int num) { return chunks * num <= kCountsEach; }
 
 int64_t chunks_of(const alt_route_desc_t &d) { return (d.tokens + kRouteThreads / shape_of(d).l - 1) / (kRouteThreads / shape_of(d).l); }
 
@@ -925,7 +925,7 @@ hipError_t route_run(const alt_route_desc_t &d, const RouteParams &p, int device
         }
         hipLaunchKernelGGL((route_kernel<ES, L, V>), dim3((unsigned)p.chunks), dim3(kRouteThreads), lds, st, p);
         if ((e = hipGetLastError()) != hipSuccess || p.chunks == 1) return;
-        if ((int64_t)p.chunks * p.num <= kCountsEach) {
+        if (counts_each(p.chunks, p.num)) {
             hipLaunchKernelGGL((route_place_kernel<L, true>), dim3((unsigned)p.chunks), dim3(kRouteThreads), 0, st, p);
         } else {
             hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)((p.num + 15) / 16)), dim3(kRouteThreads), 0, st, p);
@@ -967,7 +967,12 @@ alt_status_t check(alt_handle_t h, const char *call, const alt_route_desc_t *d, 
     return ALT_OK;
 }
 
-size_t route_workspace(const alt_route_desc_t &d) { return (size_t)(chunks_of(d) + 1) * d.experts * 4 + 16; }
+// The workspace: what each workgroup counts, and, where that has a launch of its own, what those before have.
+size_t counts_bytes(const alt_route_desc_t &d) { return ((size_t)chunks_of(d) * d.experts * 2 + 15) / 16 * 16; }
+size_t route_workspace(const alt_route_desc_t &d)
+{
+    return counts_bytes(d) + (counts_each(chunks_of(d), d.experts) ? 0 : (size_t)(chunks_of(d) + 1) * d.experts * 4) + 16;
+}
 
 }  // namespace
 }  // namespace alt
@@ -991,7 +996,8 @@ extern "C" alt_status_t alt_route(alt_handle_t h, const alt_route_desc_t *desc, 
     p.logits = (const char *)logits;
     p.bias = bias;
     p.experts = experts; p.weights = weights; p.rows = rows; p.offsets = offsets;
-    p.counts = (int32_t *)aligned_workspace(workspace);
+    p.counts = (uint16_t *)aligned_workspace(workspace);
+    p.before = (int32_t *)(aligned_workspace(workspace) + counts_bytes(d));
     p.ld = d.stride * (int64_t)dtype_size(d.dtype);
     p.tokens = (int32_t)d.tokens;
     p.num = d.experts; p.top_k = d.top_k; p.groups = d.groups; p.top_groups = d.top_groups; p.group_best = d.group_best;
