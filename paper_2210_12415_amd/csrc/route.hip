@@ -26,7 +26,7 @@ struct RouteParams {
     uint16_t *counts;                      // [workgroups][num]: choices of each expert
     int32_t *before;                       // [workgroups][num]: those of the workgroups before; then [num]: of all (route_scan_kernel)
     int64_t ld;                            // bytes between rows of logits
-    int32_t tokens, num, top_k, groups, top_groups, group_best, softmax, renorm, chunks, size;     // size: bytes of a logit
+    int32_t tokens, num, top_k, groups, top_groups, group_best, softmax, renorm, chunks, size, listed;     // size: bytes of a logit; listed: choices of lists
     FastDiv each;                          // experts of a group
     float scale;
 };
@@ -243,8 +243,10 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
 // Lists of the K largest, in order, are merged lane by lane: the larger of each number and its counterpart from the list's other end are the K
 // largest of both, first up and then down, and a few exchanges order them.
 constexpr double kNoChoice = -0x1p1000;                    // (what is below it is none)
-// Up to eight choices, more than four, come of lists, others one after another: with a list of eight 16384 tokens of 256 experts take 19.6 us for eight choices
-// and 19.5 for six, one after another 22.0 and 19.9 (a list of four 18.1 for four and 18.2 for one; one after another 19.0 and 16.7).
+// Five to eight choices come of lists where compute units have several waves to a vector unit, others one after another.  Of 256 experts, six choices and eight:
+// 16384 tokens 19.5 and 19.6 us with lists of eight, 19.9 and 22.0 one after another (lists of four: four choices 18.1 for 19.0, one 18.2 for 16.7).  Eight choices
+// with biases and groups: 64 tokens 13.6 and 16.4, but 32 tokens, eight waves, 12.6 and 11.7, 16 tokens 12.2 and 10.3: a wave alone waits for
+// the longer way's instructions.
 constexpr int kListed = 8;
 
 __device__ __forceinline__ double choice_of(float key, int e)
@@ -429,7 +431,7 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
     float end = none;                                      // the last chosen one
     bool sure = true;
     uint32_t few = 0;                                      // this lane's experts that are chosen or near the last chosen one
-    if (p.top_k > 4 && p.top_k <= kListed) {
+    if (p.listed) {
         mine = choose_largest<L, kListed, V>(p, key, near, sub, end, sure);
     } else {
         float last = INFINITY;                             // the pick before
@@ -1006,6 +1008,7 @@ extern "C" alt_status_t alt_route(alt_handle_t h, const alt_route_desc_t *desc, 
     p.scale = d.scale;
     p.chunks = (int32_t)chunks_of(d);
     p.size = (int32_t)dtype_size(d.dtype);
+    p.listed = d.top_k > 4 && d.top_k <= kListed && d.tokens * shape_of(d).l > 512;
     p.each = make_fastdiv((uint32_t)(d.experts / d.groups));
     if (!some) {
         hipLaunchKernelGGL(route_nothing_kernel, dim3(1), dim3(kRouteThreads), 0, st, offsets, (int)d.experts);
