@@ -105,6 +105,21 @@ __device__ __forceinline__ F sigmoid_of(F v)
     return (v < 0 ? e : (F)1) / (1 + e);
 }
 
+// A chosen expert's share of the chosen scores of its row: s, the sigmoid of v, to a lane (`is`: where there is one).  From -87 down exponentials lose digits in
+// 32 bits and then all; where the scores are small, so that 1 + exp(v) is 1, their shares are those of a softmax, which keeps them.  (Scores that are zero in 64 bits are zero.)
+template <int L>
+__device__ __forceinline__ float sigmoid_share(float s, float v, bool is)
+{
+    const float sum = row_sum<L>(s);
+    const bool small = sum < 0x1p-32f;
+    float share = s / (sum > 0.f ? sum : 1.f);
+    if (__ballot(is && small)) {
+        const float top = row_max<L>(is ? v : -INFINITY), e = is && top > -745.13f ? expf(v - top) : 0.f, all = row_sum<L>(e);
+        if (small) share = all > 0.f ? e / all : 0.f;
+    }
+    return share;
+}
+
 __device__ __forceinline__ float element_at(const char *row, int size, int e) { return size == 4 ? element<4>(row + (int64_t)e * 4) : element<2>(row + (int64_t)e * 2); }
 
 // Sum over the lanes of the row up to and with this one.
@@ -578,10 +593,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteParams 
             w = w / (p.renorm ? row_sum<L>(w) : st.sum);
         } else {
             w = is ? sigmoid_of(v) : 0.f;
-            if (p.renorm) {
-                const float sum = row_sum<L>(w);
-                w = w / (sum > 0.f ? sum : 1.f);
-            }
+            if (p.renorm) w = sigmoid_share<L>(w, v, is);
         }
         if (sub < p.top_k) {
             p.experts[token * p.top_k + sub] = mine;
@@ -825,10 +837,7 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(const RouteGra
         } else {
             s = is ? sigmoid_of(v) : 0.f;
             rest = is ? sigmoid_of(-v) : 0.f;
-            if (p.renorm) {
-                const float all = row_sum<L>(s);
-                s /= all > 0.f ? all : 1.f;
-            }
+            if (p.renorm) s = sigmoid_share<L>(s, v, is);
         }
         if (p.renorm || p.softmax) mean = row_sum<L>(s * dw);
         const bool any = row_max<L>(e) >= 0;
