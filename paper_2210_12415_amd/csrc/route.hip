@@ -418,11 +418,11 @@ __device__ __forceinline__ int choose(const RouteParams &p, const char *row, con
             if (__ballot(!(apart > 4.f * near + size * 0x1p-20f))) {
                 const double sum = exact_sum<L, V>(p, row, e0, st);
                 double exactly;
-                // (a lane's two best are among those not below the second by more than `near`)
+                // (a lane's two best are among those not below the second by more than `near`; where the second is infinite `from` is NaN and all are looked at)
                 const float from = two == none ? none : two - (near + __builtin_fabsf(two) * 0x1p-22f);
                 uint32_t few = 0;
 #pragma unroll
-                for (int i = 0; i < V; ++i) few |= key[i] != none && key[i] >= from ? 1u << i : 0u;
+                for (int i = 0; i < V; ++i) few |= key[i] != none && !(key[i] < from) ? 1u << i : 0u;
                 kept = kept_experts<double, L, V>(
                     p, sub, (double *)lds, [&](int i) { return exact_worth(p, row, e0 + i, st, sum); },
                     [&](double &a, double &b) {

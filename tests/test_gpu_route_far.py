@@ -1,4 +1,5 @@
-"""Routing where values leave the range of 32 bits, against the definition in 64: renormalized sigmoid weights of logits far below zero, and their gradients.
+"""Routing where values leave the range of 32 bits, against the definition in 64: renormalized sigmoid weights of logits far below zero, and their gradients;
+biases of infinity by groups.
 
 Shares of the chosen scores are quotients of exponentials: each is off by (|x| + 2) * 2^-24 of itself, x the difference of two logits, which is itself rounded, the sum
 of up to 32 of them by 32 * 2^-24 more, and a handful of single roundings."""
@@ -95,3 +96,32 @@ def test_renormalized_sigmoid_of_two_logits(h):
     h.route_grad(d, l, experts, torch.tensor([[2.0, -1.0]] * (len(at) + 1), device="cuda"), out)
     mean = 2 * first - (1 - first)
     close(out, np.array([[0, (1 - first) * (-1 - mean), first * (2 - mean), 0]] * len(at) + [[0.0] * 4]), 32 * EPS)
+
+
+@pytest.mark.parametrize("score", [alt.SCORE_SOFTMAX, alt.SCORE_SIGMOID])
+@pytest.mark.parametrize("best", [1, 2])
+@pytest.mark.parametrize("E,groups,top_groups,k", [(64, 8, 3, 6), (128, 8, 2, 5), (256, 8, 4, 8), (512, 16, 3, 8), (1024, 8, 3, 20), (60, 12, 4, 6), (256, 4, 1, 16)])
+def test_biases_of_infinity_by_groups(h, E, groups, top_groups, k, best, score):
+    """Experts that a bias of infinity forces, several of them side by side: their groups are worth infinity, ties go to the lower index."""
+    T, each = 90, E // groups
+    l = normal(E, T, E)
+    l[torch.rand(T, E, generator=torch.Generator().manual_seed(E)) < 0.2] = -INF
+    bias = normal(7, E, std=0.1)
+    last = (groups - 1) * each
+    bias[[last, last + 1, last + 2, each, each + 1]] = INF
+    bias[2 * each] = INF
+    l = matrix(l, torch.float32)
+    experts = run(h, l, alt.route_desc(T, E, k, score=score, groups=groups, top_groups=top_groups, group_best=best), bias.cuda())[0]
+    full, add = f64(l), f64(bias)
+    if score == alt.SCORE_SOFTMAX:
+        e = np.exp(full - full.max(1, keepdims=True))
+        s = e / e.sum(1, keepdims=True)
+    else:
+        s = 1 / (1 + np.exp(-full))
+    key = np.where(full == -INF, -INF, s + add)
+    two = -np.sort(-key.reshape(T, groups, each), axis=2)[:, :, :best]
+    worth = np.where(two[:, :, 0] == -INF, -INF, np.where(two == -INF, 0, two).sum(2))
+    place = np.argsort(np.argsort(-worth, axis=1, kind="stable"), axis=1, kind="stable")
+    key = np.where(np.repeat(place >= top_groups, each, axis=1), -INF, key)
+    order = np.argsort(-key, axis=1, kind="stable")[:, :k]
+    equal(experts, np.where(np.take_along_axis(key, order, 1) == -INF, -1, order), "experts")
