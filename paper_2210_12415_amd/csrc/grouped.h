@@ -645,10 +645,24 @@ __device__ __forceinline__ void grp_emit(const GroupedParams &p, const GrpProble
     }
 }
 
+// bf16 numbers, infinities and NaN among them zeros.
+__device__ __forceinline__ u32x4_t grp_finite(const u32x4_t &v)
+{
+    typedef int16_t i16x2_t __attribute__((ext_vector_type(2)));
+    u32x4_t out;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {                          // (an exponent of ones becomes its half's top bit)
+        const i16x2_t all = __builtin_bit_cast(i16x2_t, (v[q] & 0x7f807f80u) + 0x00800080u) >> (int16_t)15;
+        out[q] = v[q] & ~__builtin_bit_cast(uint32_t, all);
+    }
+    return out;
+}
+
 // The adapters' part of a wave's tile: c[row][col] += sum_r inner[row][r] * up[g][col][r] for the adapter g of the row, one adapter that its rows have
 // after another, in registers: a product like the tile's own with `rank` more steps.  A row's inner sums lie one behind another, filled up to whole
 // matrix instructions with zeros (inner_bytes), in bf16 as two such rows, the value rounded and what that left, so that the adapters' part is as exact as the
-// tile's own.  Lanes hold rows: another adapter's rows take nothing of the sums, whatever they are.
+// tile's own.  Lanes hold rows: another adapter's rows take nothing of the sums, whatever they are.  What of `up` is not finite meets the first part alone, which
+// makes of it what the whole sum would: beside it the second, zero or of another sign, would make NaN of infinities.
 template <typename T, int TM, int TN, int SUMS>
 __device__ __forceinline__ void grp_adapt(const GroupedParams &p, const GrpProblem &g, GrpSums<T, TM, TN, SUMS> &acc, int wrow, int wcol, int lane)
 {
@@ -695,9 +709,10 @@ __device__ __forceinline__ void grp_adapt(const GroupedParams &p, const GrpProbl
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int q = 0; q < PARTS; ++q) grp_mma<T>(part[j], fb[s][j], fa[s][q]);
+                    for (int j = 0; j < TN; ++j) {
+                        grp_mma<T>(part[j], fb[s][j], fa[s][0]);
+                        if constexpr (PARTS == 2) grp_mma<T>(part[j], grp_finite(fb[s][j]), fa[s][1]);
+                    }
             }
 #pragma unroll
             for (int j = 0; j < TN; ++j)
