@@ -190,26 +190,26 @@ struct Down {
 };
 
 template <typename T, int NT>
-__global__ __launch_bounds__(64 * kWaves) void adapters_down_kernel(const AdapterParams p)
+__global__ __launch_bounds__(64 * kWaves) void adapters_down_kernel(const AdapterParams p, uint32_t begin)
 {
     using D = Down<T, NT>;
     __shared__ uint4 lds[D::kLds / 16];
-    D::run(p, blockIdx.x, (char *)lds);
+    D::run(p, begin + blockIdx.x, (char *)lds);
 }
 
 // The inner sums in the first `down` workgroups, the shared product in the others: neither needs the other.  Column tiles that run together are one XCD's
 // (workgroups go to the XCDs in turn), rows first, so that a tile of w is read from memory once.
 template <typename T, int RT, int NT>
-__global__ __launch_bounds__(64 * kWaves) void adapters_few_kernel(const AdapterParams p, uint32_t down)
+__global__ __launch_bounds__(64 * kWaves) void adapters_few_kernel(const AdapterParams p, uint32_t begin, uint32_t down)
 {
     using C = Core<T, RT, NT, 2>;
     constexpr int ES = C::ES;
     __shared__ uint4 lds[(C::kLds > Down<T, 1>::kLds ? C::kLds : Down<T, 1>::kLds) / 16];
-    if (blockIdx.x < down) {
-        Down<T, 1>::run(p, blockIdx.x, (char *)lds);
+    if (begin + blockIdx.x < down) {
+        Down<T, 1>::run(p, begin + blockIdx.x, (char *)lds);
         return;
     }
-    const uint32_t wg = blockIdx.x - down, row_tiles = (uint32_t)(p.rows + 16 * RT - 1) / (16 * RT), col_tiles = (uint32_t)(p.cols + 16 * NT - 1) / (16 * NT);
+    const uint32_t wg = begin + blockIdx.x - down, row_tiles = (uint32_t)(p.rows + 16 * RT - 1) / (16 * RT), col_tiles = (uint32_t)(p.cols + 16 * NT - 1) / (16 * NT);
     const uint32_t tiles = row_tiles * col_tiles * (uint32_t)p.base_slices, per = (tiles + 7) / 8, tile = (wg & 7) * per + (wg >> 3);
     if ((wg >> 3) >= per || tile >= tiles) return;
     const int row0 = (int)(tile % row_tiles) * 16 * RT, col0 = (int)(tile / row_tiles % col_tiles) * 16 * NT, slice = (int)(tile / row_tiles / col_tiles);
@@ -237,11 +237,12 @@ __global__ __launch_bounds__(64 * kWaves) void adapters_few_kernel(const Adapter
 // y[m][n] = base[m][n] + sum_r inner[m][r] * b[g][n][r] + bias[n].  A thread has a column of R rows, and reads its row of b again only where the next row has
 // another adapter.  Bound by memory: b of the adapters that the rows have, and the product, which is still in the caches.
 template <int ES, int R>
-__global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p, int col_blocks)
+__global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p, uint32_t begin, uint32_t col_blocks)
 {
     constexpr int E = 16 / ES, PIECE = 64;                 // of the rank at a time
     __shared__ float inner[R][PIECE];
-    const int t = threadIdx.x, row0 = (int)(blockIdx.x / (unsigned)col_blocks) * R, col = (int)(blockIdx.x % (unsigned)col_blocks) * 256 + t, width = p.inner_bytes / 4;
+    const uint32_t wg = begin + blockIdx.x;
+    const int t = threadIdx.x, row0 = (int)(wg / col_blocks) * R, col = (int)(wg % col_blocks) * 256 + t, width = p.inner_bytes / 4;
     int ids[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -315,14 +316,23 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(const AdapterParams p,
     }
 }
 
+// f(begin, how many) of as many launches as n workgroups of 256 threads take: one has fewer than 2^32 threads.  (Whole eights, for the XCDs.)
+template <typename F>
+hipError_t in_launches(int64_t n, F f)
+{
+    static_assert(64 * kWaves == 256, "threads of a workgroup");
+    constexpr int64_t most = (1 << 24) - 8;
+    if (n > 0xffffffffll) return hipErrorInvalidConfiguration;
+    for (int64_t begin = 0; begin < n; begin += most) f((uint32_t)begin, dim3((unsigned)std::min(n - begin, most)));
+    return hipGetLastError();
+}
+
 template <typename T, int NT>
 hipError_t down(AdapterParams p, hipStream_t st)
 {
     p.col_tiles = (p.rank + 16 * NT - 1) / (16 * NT);
     const int64_t n = (int64_t)p.tiles * p.col_tiles * std::max(p.slices, 1) * p.slots;
-    if (n * 64 * kWaves > 0xffffffffll) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((adapters_down_kernel<T, NT>), dim3((unsigned)n), dim3(64 * kWaves), 0, st, p);
-    return hipGetLastError();
+    return in_launches(n, [&](uint32_t begin, dim3 grid) { hipLaunchKernelGGL((adapters_down_kernel<T, NT>), grid, dim3(64 * kWaves), 0, st, p, begin); });
 }
 
 template <typename T, int RT, int NT>
@@ -332,9 +342,7 @@ hipError_t few(AdapterParams p, hipStream_t st)
     const int64_t downs = ((int64_t)p.tiles * p.col_tiles * p.slices * p.slots + 7) / 8 * 8;
     const int64_t tiles = ((int64_t)p.rows + 16 * RT - 1) / (16 * RT) * ((p.cols + 16 * NT - 1) / (16 * NT)) * p.base_slices;
     const int64_t n = downs + (tiles + 7) / 8 * 8;
-    if (n * 64 * kWaves > 0xffffffffll) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((adapters_few_kernel<T, RT, NT>), dim3((unsigned)n), dim3(64 * kWaves), 0, st, p, (uint32_t)downs);
-    return hipGetLastError();
+    return in_launches(n, [&](uint32_t begin, dim3 grid) { hipLaunchKernelGGL((adapters_few_kernel<T, RT, NT>), grid, dim3(64 * kWaves), 0, st, p, begin, (uint32_t)downs); });
 }
 
 template <typename T>
@@ -348,9 +356,7 @@ template <int ES, int R>
 hipError_t up(const AdapterParams &p, hipStream_t st)
 {
     const int64_t cols = ((int64_t)p.cols + 255) / 256, n = ((int64_t)p.rows + R - 1) / R * cols;
-    if (n * 256 > 0xffffffffll) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((adapters_up_kernel<ES, R>), dim3((unsigned)n), dim3(256), 0, st, p, (int)cols);
-    return hipGetLastError();
+    return in_launches(n, [&](uint32_t begin, dim3 grid) { hipLaunchKernelGGL((adapters_up_kernel<ES, R>), grid, dim3(256), 0, st, p, begin, (uint32_t)cols); });
 }
 
 }  // namespace

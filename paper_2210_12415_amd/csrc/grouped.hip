@@ -423,15 +423,11 @@ extern "C" alt_status_t alt_gemm_adapters(alt_handle_t h, const alt_adapters_des
         p.inner = ws;
         p.up = (const char *)b;
     }
-    hipError_t e;
-    if (q.few) {
-        e = adapters_few(l.in_dtype, q, st);
-    } else {
-        ALT_CHECK_HIP(h, adapters_down(l.in_dtype, q, st));
+    hipError_t e = q.few ? adapters_few(l.in_dtype, q, st) : adapters_down(l.in_dtype, q, st);
+    if (e == hipSuccess && !q.few) {
         char *more = ws + c.inner + (c.base + 15) / 16 * 16;
         s = run(h, "alt_gemm_adapters", l.in_dtype, kForward, p, more, (size_t)((char *)workspace + ws_bytes - more), st);
         if (s != ALT_OK) return s;
-        e = hipSuccess;
     }
     if (e == hipSuccess && q.beside) e = adapters_up(l.in_dtype, q, st);
     if (e == hipErrorInvalidConfiguration) return fail(h, ALT_UNSUPPORTED, "alt_gemm_adapters: more workgroups than a launch holds");

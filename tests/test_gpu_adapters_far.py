@@ -1,10 +1,10 @@
-"""Products with low-rank adapters where values are at an end: infinities in an adapter."""
+"""Products with low-rank adapters where values or extents are at an end: infinities in an adapter, and more rows than one launch has workgroups for."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2210_12415_amd as alt
-from rows_util import f64, matrix, normal, ws
+from rows_util import EPS, HALF, f64, matrix, normal, ws
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,31 @@ def test_infinities_in_an_adapter_are_the_definitions(h, M, N, K, G, r, dtype, o
         assert (at[np.isinf(want)] == want[np.isinf(want)]).all(), g
         seen |= {(g, v) for v, is_ in (("inf", np.isinf(want).any()), ("nan", np.isnan(want).any())) if is_}
     assert {(0, "inf"), (0, "nan"), (1, "nan"), (2, "inf")} <= seen and not any(g in (-1, 3) for g, _ in seen)
+
+
+@pytest.mark.parametrize("M,N,K,G,r", [((1 << 23) + 5, 8, 8, 3, 512), ((1 << 26) + 7, 8, 8, 32, 64)])
+def test_more_rows_than_a_launch_has_workgroups(h, M, N, K, G, r):
+    """The inner sums of rank 512 have 32 workgroups for 16 rows, a last pass one for four rows: 2^24 workgroups of 256 threads are more threads than one launch has."""
+    torch.manual_seed(1)
+    x = torch.randn(M, K, device="cuda").bfloat16()
+    w, a, b = torch.randn(N, K, device="cuda").bfloat16(), torch.randn(G, r, K, device="cuda").bfloat16(), torch.randn(G, N, r, device="cuda").bfloat16()
+    ids = torch.randint(-1, G, (M,), dtype=torch.int32, device="cuda")
+    d = alt.adapters_desc(M, N, K, G, r, out_dtype=alt.F32)
+    y = torch.full((M, N), float("nan"), device="cuda")
+    need = h.gemm_adapters_workspace_size(d)
+    h.gemm_adapters(d, x, w, ids, a, b, y, workspace=torch.empty(need, dtype=torch.uint8, device="cuda"), ws_bytes=need)
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(y).all())
+    step = M // 64
+    for lo in list(range(0, M - 600, step)) + [M - 600]:                     # 600 rows of each 64th, and the last
+        at = slice(lo, lo + 600)
+        xs, of = f64(x[at]), ids[at].cpu().numpy()
+        want, size = xs @ f64(w).T, K * EPS * (np.abs(xs) @ np.abs(f64(w)).T)
+        for g in range(G):
+            m = np.flatnonzero(of == g)
+            A, B = f64(a[g]), f64(b[g])
+            inner, about = xs[m] @ A.T, np.abs(xs[m]) @ np.abs(A).T
+            want[m] += inner @ B.T
+            size[m] += ((K + 1) * EPS * about + (2.0 ** -16 + EPS) * np.abs(inner)) @ np.abs(B).T + (2 * r + 3) * EPS * (np.abs(inner) @ np.abs(B).T)
+        tol = 1.01 * size + 4 * EPS * np.abs(want) + HALF[alt.F32]
+        assert (np.abs(f64(y[at]) - want) <= tol).all(), lo
