@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "../../include/alt.h"
+#include "once.h"
 
 namespace alt {
 
@@ -110,6 +111,14 @@ struct alt_context {
 };
 
 namespace alt {
+
+// Lets `kern` have up to `bytes` of LDS on the current device; `once` is the kernel's own.
+inline hipError_t allow_lds(OncePerDevice &once, const void *kern, int bytes = 160 * 1024)
+{
+    int device = 0;
+    const hipError_t e = hipGetDevice(&device);
+    return e != hipSuccess ? e : once(device, [&] { return hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+}
 
 alt_status_t fail(alt_handle_t h, alt_status_t s, const char *fmt, ...);
 

@@ -1023,12 +1023,9 @@ template <int BM, int BN, int WGM, int WGN, int KW, int NS, int BK, int KR, int 
 hipError_t dconv_launch_kr(const DconvParams &p, size_t lds, hipStream_t st)
 {
     auto kern = dconv_kernel<BM, BN, WGM, WGN, KW, NS, BK, KR, NCC>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static OncePerDevice lds_once;
+    const hipError_t e = allow_lds(lds_once, (const void *)kern);
+    if (e != hipSuccess) return e;
     const int tiles = p.tiles_m * p.tiles_n;
     const unsigned grid = (unsigned)(tiles * p.splitk);
     hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * WGM * WGN * KW), lds, st, p);

@@ -537,12 +537,9 @@ template <int BM, int BN, int WGM, int WGN, int KW, int KR>
 hipError_t dplanar_launch_kr(const DconvParams &p, size_t lds, hipStream_t st)
 {
     auto kern = dplanar_kernel<BM, BN, WGM, WGN, KW, KR>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static OncePerDevice lds_once;
+    const hipError_t e = allow_lds(lds_once, (const void *)kern);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(64 * WGM * WGN * KW), lds, st, p);
     return hipGetLastError();
 }

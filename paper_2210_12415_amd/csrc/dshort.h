@@ -122,12 +122,9 @@ template <int TN, int KS>
 hipError_t dshort_launch_ks(const DconvParams &p, size_t lds, hipStream_t st)
 {
     auto kern = dshort_kernel<TN, KS>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static OncePerDevice lds_once;
+    const hipError_t e = allow_lds(lds_once, (const void *)kern);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n * p.batch)), dim3(256), lds, st, p);
     return hipGetLastError();
 }

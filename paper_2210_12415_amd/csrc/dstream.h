@@ -523,12 +523,9 @@ hipError_t dstream_launch(const DconvParams &p, size_t lds, hipStream_t st)
             if (p.w_dense) return dstream_launch<BM, BN, WGM, WGN, KW, NS, BK, BT, kTapsDense, T>(p, lds, st);
         }
         auto kern = dstream_kernel<BM, BN, WGM, WGN, KW, NS, BK, BT, TAPS, T>;
-        static bool attr_set = false;
-        if (!attr_set) {
-            hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-            if (e != hipSuccess) return e;
-            attr_set = true;
-        }
+        static OncePerDevice lds_once;
+        const hipError_t e = allow_lds(lds_once, (const void *)kern);
+        if (e != hipSuccess) return e;
         const int tiles = p.tiles_m * p.tiles_n;
         const unsigned grid = (unsigned)(tiles * p.splitk);
         hipLaunchKernelGGL(kern, dim3(grid, (unsigned)p.batch), dim3(64 * WGM * WGN * KW), lds, st, p);

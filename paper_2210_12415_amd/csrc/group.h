@@ -67,12 +67,9 @@ __global__ __launch_bounds__(F::kThreads, F::kWaves) void group_kernel(const Gro
 template <typename F>
 hipError_t group_launch(const GroupParams &g, unsigned workgroups, size_t lds, hipStream_t st)
 {
-    static bool attr_set = false;
-    if (!attr_set) {
-        hipError_t e = hipFuncSetAttribute((const void *)group_kernel<F>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static OncePerDevice lds_once;
+    const hipError_t e = allow_lds(lds_once, (const void *)group_kernel<F>);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(group_kernel<F>, dim3(workgroups), dim3(F::kThreads), lds, st, g);
     return hipGetLastError();
 }

@@ -1793,12 +1793,9 @@ hipError_t grouped_tiles(GroupedParams p, hipStream_t st)
     hipError_t e = grp_grid<K::kForm, K::kBM, K::kBN>(p, K::THREADS, &grid);
     if (e != hipSuccess || !grid) return e;
     auto kern = grouped_kernel<K>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static OncePerDevice lds_once;
+    e = allow_lds(lds_once, (const void *)kern);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3(grid), dim3(K::THREADS), K::kLds, st, p);
     return hipGetLastError();
 }
@@ -1810,12 +1807,9 @@ hipError_t grouped_large(GroupedParams p, hipStream_t st)
     p.d_panel = make_fastdiv((uint32_t)(kPanel * p.tiles_n));
     if (grp_row_tiles(p, 256) * p.tiles_n * 4 > 0x7fffffff) return hipErrorInvalidConfiguration;
     auto kern = grouped_large_kernel<T, FORM>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != hipSuccess) return e;
-        attr_set = true;
-    }
+    static OncePerDevice lds_once;
+    const hipError_t e = allow_lds(lds_once, (const void *)kern);
+    if (e != hipSuccess) return e;
     constexpr int lds = GrpLarge<T, FORM>::kLds;
     hipLaunchKernelGGL(kern, dim3((p.places + 7) / 8 * 8), dim3(kLargeThreads), lds, st, p);
     return hipGetLastError();

@@ -683,11 +683,10 @@ hipError_t igemm_launch(const IgemmParams &p, dim3 grid, hipStream_t st)
     using TR = ElemTraits<T>;
     constexpr size_t lds = (size_t)2 * (BM + BN) * (BK + TR::EPV) * TR::SIZE + kKTab * sizeof(KEntry);
     auto kern = igemm_kernel<T, BM, BN, BK, WGM, WGN, AMODE, BMODE, PF>;
-    static bool attr_set = false;
-    if (!attr_set && lds > 48 * 1024) {
-        hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    static OncePerDevice lds_once;
+    if (lds > 48 * 1024) {
+        const hipError_t e = allow_lds(lds_once, (const void *)kern, (int)lds);
         if (e != hipSuccess) return e;
-        attr_set = true;
     }
     hipLaunchKernelGGL(kern, grid, dim3(kIgemmThreads), lds, st, p);
     return hipGetLastError();

@@ -270,11 +270,10 @@ hipError_t igemm_dma_launch(const IgemmParams &p, dim3 grid, hipStream_t st)
     constexpr size_t lds = igemm_dma_lds_bytes<T, BM, BN, BK, NS>();
     static_assert(lds <= 160 * 1024, "LDS per workgroup");
     auto kern = igemm_dma_kernel<T, BM, BN, BK, WGM, WGN, NS>;
-    static bool attr_set = false;
-    if (!attr_set && lds > 48 * 1024) {
-        hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    static OncePerDevice lds_once;
+    if (lds > 48 * 1024) {
+        const hipError_t e = allow_lds(lds_once, (const void *)kern, (int)lds);
         if (e != hipSuccess) return e;
-        attr_set = true;
     }
     hipLaunchKernelGGL(kern, grid, dim3(NT), lds, st, p);
     return hipGetLastError();

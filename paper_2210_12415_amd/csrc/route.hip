@@ -7,8 +7,6 @@
 // wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 23.2 us, 20 without groups, 18
 // without biases, and of them 8 for the ranks' two launches.  One launch chooses and ranks the choices inside each
 // workgroup's tokens; where there is one workgroup that is all, else the ranks are moved by what the workgroups before have of each expert.
-#include <atomic>
-
 #include "common.h"
 #include "rows.h"
 
@@ -919,20 +917,16 @@ bool counts_each(int64_t chunks, int num) { return chunks * num <= kCountsEach; 
 int64_t chunks_of(const alt_route_desc_t &d) { return (d.tokens + kRouteThreads / shape_of(d).l - 1) / (kRouteThreads / shape_of(d).l); }
 
 template <int ES>
-hipError_t route_run(const alt_route_desc_t &d, const RouteParams &p, int device, hipStream_t st)
+hipError_t route_run(const alt_route_desc_t &d, const RouteParams &p, hipStream_t st)
 {
     hipError_t e = hipSuccess;
     by_shape(d, [&](auto l, auto v) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
         const size_t lds = route_lds(L, V, p.num, p.bias || p.top_groups < p.groups);
         if (lds > 64 * 1024) {
-            static std::atomic<uint64_t> set{0};           // a bit for each device
-            const uint64_t bit = 1ull << (device & 63);
-            if (device >= 64 || !(set.load() & bit)) {
-                e = hipFuncSetAttribute((const void *)route_kernel<ES, L, V>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 256);
-                if (e != hipSuccess) return;
-                set |= bit;
-            }
+            static OncePerDevice lds_once;
+            e = allow_lds(lds_once, (const void *)route_kernel<ES, L, V>, 160 * 1024 - 256);
+            if (e != hipSuccess) return;
         }
         hipLaunchKernelGGL((route_kernel<ES, L, V>), dim3((unsigned)p.chunks), dim3(kRouteThreads), lds, st, p);
         if ((e = hipGetLastError()) != hipSuccess || p.chunks == 1) return;
@@ -1024,7 +1018,7 @@ extern "C" alt_status_t alt_route(alt_handle_t h, const alt_route_desc_t *desc, 
         ALT_CHECK_HIP(h, hipGetLastError());
         return ALT_OK;
     }
-    ALT_CHECK_HIP(h, d.dtype == ALT_F32 ? route_run<4>(d, p, h->device, st) : route_run<2>(d, p, h->device, st));
+    ALT_CHECK_HIP(h, d.dtype == ALT_F32 ? route_run<4>(d, p, st) : route_run<2>(d, p, st));
     return ALT_OK;
 }
 
