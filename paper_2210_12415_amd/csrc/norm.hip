@@ -47,7 +47,7 @@ struct Part {
         for (int i = 0; i < K; ++i)
             if (i * TPR + t < chunks) {
                 const char *at = row + (int64_t)(i * TPR + t) * (E * ES) - shift;
-                __builtin_memcpy(&c[i], __builtin_assume_aligned(at, 4), E * ES);
+                __builtin_memcpy(&c[i], __builtin_assume_aligned(at, SHIFT ? 4 : ES), E * ES);
                 if constexpr (SHIFT) {
                     if (shift) more[i] = *(const uint32_t *)(at + 16);
                 }
