@@ -620,7 +620,7 @@ typedef struct {
  *   experts[token][top_k]  the top_k experts of largest choice, in that order, ties by the lower index (of groups, too).  Choices are compared as if
  *           computed in 64 bits;
  *   weights[token][top_k]  score * scale, with `renormalize` divided by the sum of the token's chosen scores before, however small they
- *           are (a sum that is zero in 64 bits counts as one).
+ *           are (sigmoids that are zero in 64 bits stay zeros).
  * A logit of -inf (or a choice that is -inf or NaN) takes its expert out, a group without experts too; what a token lacks of top_k experts is expert -1
  * with weight 0, so a padded row of logits may be all -inf.  A row with a NaN (softmax: or +inf) has no experts and weights NaN.
  * The order of the experts, as alt_gemm_grouped takes it: offsets[e] (groups + 1 = experts + 1 of them) is the first row of expert e, its rows
