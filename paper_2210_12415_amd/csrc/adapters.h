@@ -3,7 +3,7 @@
 // Every row's inner sums, inner[m][r] = scale[g] * sum_k x[m,k] a[g,r,k], come first.  Then there are two ways:
 //   fused   the product's tiles take the adapters' part into their sums (grp_adapt in grouped.h)
 //   beside  the product goes to the workspace in fp32, and a last pass adds each row's part to it, column by column: where there are few rows, whose tiles
-//           would wait for the loads of one adapter after another (32 rows of 32 requests, 4096 x 4096, rank 16: 29 us fused, 16 beside)
+//           would wait for the loads of one adapter after another (32 rows, each with an adapter of its own, 4096 x 4096, rank 16: 53 us fused, 17 beside)
 #pragma once
 
 #include "grouped.h"

@@ -369,11 +369,12 @@ void adapters_plan(int dtype, const GroupedParams &product, AdapterParams &p)
     const int64_t rt = p.rows <= 16 ? 1 : 2, row_tiles = (p.rows + 16 * rt - 1) / (16 * rt);
     p.few_cols = rt == 2 && row_tiles * ((p.cols + 31) / 32) >= p.places ? 2 : 1;
     const int64_t tiles = row_tiles * ((p.cols + 16 * p.few_cols - 1) / (16 * p.few_cols));
-    // Times in us.  The last pass runs at 5 TB/s behind its launch; the fused tiles wait 0.7 for each adapter of 32 rows, and most of those that there can be
-    // are taken to be.  The product of few rows takes its tiles' loads from the caches at 13 TB/s (fp32, whose matrix instructions take longer, at 7); others
-    // come after the launch of the inner sums.  bf16, rank 16, either way: 128 x 4096 x 4096 29 of few rows and 36 otherwise, 256 x 4096 x 4096 44 and 37, 256 x
-    // 1024 x 4096 18 and 33, 200 x 8192 x 2048 41 and 30, 64 x 8192 x 8192 56 and 62 (the one of these that is taken on the slower side); fp32 60 x 4096 x 4096
-    // 42 and 101.
+    // Times in us.  The last pass runs at 5 TB/s behind its launch.  The fused tiles wait for one adapter of 32 rows after another: 2048 x 4096 x 4096 92 with
+    // one adapter, 120 with 8 and 196 with 32 in turn (beside 127, 145 and 166), 1.7 to 2 for each and each round; requests of many rows, which have one or two of
+    // them there, wait far less, and 0.5 for each that there can be stands between the two.  The product of few rows takes its tiles' loads from the caches at 13
+    // TB/s (fp32, whose matrix instructions take longer, at 7); others come after the launch of the inner sums.  bf16, rank 16, 32 adapters in turn: 128 x 4096 x
+    // 4096 30 of few rows and 37 otherwise, 256 x 4096 x 4096 43 and 40, 256 x 1024 x 4096 20 and 39; taken on the slower side are 64 x 8192 x 8192 (57 and 61) and
+    // 200 x 8192 x 2048 (few rows 40, beside 38, fused, as it goes, 48).  fp32 60 x 4096 x 4096 39 and 65.
     const double rounds = std::ceil(grp_tiles<kForward>(product, 128, 128) / places), wait = 0.5 * std::min(p.adapters, 32) * rounds;
     const double last = 3 + (double)p.rows * p.cols * (8 + p.rank * es) / 5e6, loads = (double)tiles * 16 * (rt + p.few_cols) * p.K * es;
     GrpTime t;

@@ -4,8 +4,8 @@
 //   a place for every (token, choice) in the order of expert, token, choice: offsets and rows
 //
 // There is little to read: 16384 x 256 fp32 logits are 3 us of memory.  The time goes into launches and into the selection, about 100 instructions of a
-// wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 23.2 us, 20 without groups, 18
-// without biases, and of them 8 for the ranks' two launches.  One launch chooses and ranks the choices inside each
+// wave for each choice of its four rows, so lanes hold many experts and few lanes a row: with eight choices, biases and groups 23.4 us, 20.5 without groups,
+// 16.3 without biases, and of them 7 for the ranks' two launches.  One launch chooses and ranks the choices inside each
 // workgroup's tokens; where there is one workgroup that is all, else the ranks are moved by what the workgroups before have of each expert.
 #include "common.h"
 #include "rows.h"

@@ -96,7 +96,7 @@ __device__ __forceinline__ w4_t chunk16_of(const float (&v)[16 / ELSZ])
 }
 
 // A store of 16 bytes, at any alignment of whole elements, that the caches give up first.  Lanes side by side have to store side by side: with gaps
-// between them lines go out in parts (rows of 8192 tokens to two places each, 4096 bf16, 31 us for 40; fp32 in pieces of 32 bytes a lane 120 for 83).
+// between them lines go out in parts (rows of 8192 tokens to two places each, 4096 bf16, 40 us with gaps and 31 without).
 __device__ __forceinline__ void put_streaming(char *p, const w4_t &c)
 {
     typedef uint32_t any4_t __attribute__((ext_vector_type(4), aligned(2)));
