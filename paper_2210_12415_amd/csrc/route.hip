@@ -189,7 +189,7 @@ __device__ __forceinline__ void better_of(F v, F &one, F &two)
 template <typename F, int L, int V, typename W, typename B>
 __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, F *worth, W worth_at, B best_two, F &apart)
 {
-    const F none = -INFINITY;
+    const F none = -INFINITY, lowest = sizeof(F) == 4 ? (F)-__FLT_MAX__ : (F)-__DBL_MAX__;
     const int each = (int)p.each.d;
     const bool lanes = each % V == 0;
     const int per = lanes ? each / V * 2 : each;           // numbers of a group
@@ -210,7 +210,8 @@ __device__ __forceinline__ uint32_t kept_experts(const RouteParams &p, int sub, 
     for (int g = sub; g < p.groups; g += L) {
         one = two = none;
         for (int i = g * per; i < (g + 1) * per; ++i) better_of(worth[at(i)], one, two);
-        worth[at(g * per)] = p.group_best == 2 && two > none ? one + two : one;        // (these numbers are this lane's alone)
+        // (a sum below the lowest number is not that of a group without experts; these numbers are this lane's alone)
+        worth[at(g * per)] = p.group_best == 2 && two > none ? larger(one + two, lowest) : one;
     }
     wave_sync();
     uint32_t mine = 0;

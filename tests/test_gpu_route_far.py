@@ -1,5 +1,5 @@
 """Routing where values leave the range of 32 bits, against the definition in 64: renormalized sigmoid weights of logits far below zero, and their gradients;
-biases of infinity by groups.
+biases of infinity and of the lowest value by groups.
 
 Shares of the chosen scores are quotients of exponentials: each is off by (|x| + 2) * 2^-24 of itself, x the difference of two logits, which is itself rounded, the sum
 of up to 32 of them by 32 * 2^-24 more, and a handful of single roundings."""
@@ -125,3 +125,44 @@ def test_biases_of_infinity_by_groups(h, E, groups, top_groups, k, best, score):
     key = np.where(np.repeat(place >= top_groups, each, axis=1), -INF, key)
     order = np.argsort(-key, axis=1, kind="stable")[:, :k]
     equal(experts, np.where(np.take_along_axis(key, order, 1) == -INF, -1, order), "experts")
+
+
+def groups_and_experts(l, bias, groups, top_groups, best, k, softmax):
+    """The experts of each token, choices and worths in 64 bits."""
+    full, (T, E) = f64(l), l.shape
+    with np.errstate(invalid="ignore"):
+        e = np.exp(full - np.where(np.isfinite(full.max(1)), full.max(1), 0)[:, None])
+    s = e / np.maximum(e.sum(1, keepdims=True), 1e-300) if softmax else 1 / (1 + np.exp(-full))
+    key = np.where(full == -INF, -INF, s + f64(bias))
+    two = -np.sort(-key.reshape(T, groups, E // groups), axis=2)[:, :, :best]
+    worth = np.where(two[:, :, 0] == -INF, -INF, np.where(two == -INF, 0, two).sum(2))
+    place = np.argsort(np.argsort(-worth, axis=1, kind="stable"), axis=1, kind="stable")
+    key = np.where(np.repeat(place >= top_groups, E // groups, axis=1), -INF, key)
+    order = np.argsort(-key, axis=1, kind="stable")[:, :k]
+    return np.where(np.take_along_axis(key, order, 1) == -INF, -1, order)
+
+
+@pytest.mark.parametrize("score", [alt.SCORE_SOFTMAX, alt.SCORE_SIGMOID])
+@pytest.mark.parametrize("best", [1, 2])
+@pytest.mark.parametrize("E,groups,top_groups,k", [(64, 8, 4, 20), (256, 8, 4, 16), (60, 12, 5, 9), (512, 16, 5, 32), (1024, 8, 3, 24), (416, 8, 6, 21)])
+def test_biases_of_the_lowest_value_by_groups(h, E, groups, top_groups, k, best, score):
+    """Experts that a bias of the type's lowest value puts last are still before those that a logit of -inf takes out; so are groups of them, whose worth of two is beyond
+    that type."""
+    T, each = 120, E // groups
+    l = normal(E + 1, T, E)
+    for t in range(T):                                     # but for two, all groups are out for some tokens
+        l[t, each * (t % 4 + 2):] = -INF
+        if t % 5 == 0:
+            l[t, :each] = -INF
+    low = torch.finfo(torch.float32).min
+    for value in (low, 0.9 * low, -low, -0.9 * low):
+        bias = normal(7, E, std=0.1)
+        bias[each:2 * each] = value
+        bias[-each:] = value
+        bias[2 * each:2 * each + 2] = value * 0.75
+        if groups > 6:
+            bias[3 * each:4 * each], bias[4 * each:5 * each] = 0.8 * value, 0.95 * value         # (sums of two that only 64 bits tell apart)
+        for logits, add in ((l, bias), (l.flip(1), bias.flip(0))):           # (what is left at either end)
+            m = matrix(logits, torch.float32)
+            experts = run(h, m, alt.route_desc(T, E, k, score=score, groups=groups, top_groups=top_groups, group_best=best), add.contiguous().cuda())[0]
+            equal(experts, groups_and_experts(m, add, groups, top_groups, best, k, score == alt.SCORE_SOFTMAX), "experts")
